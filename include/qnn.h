@@ -326,6 +326,81 @@ qnn_status qnn_qdwconv2d_asym(const uint8_t *x, int N, int H, int W, int C, int3
                               const int32_t *mult, const int32_t *shift, int32_t z_out, int32_t act_min, int32_t act_max,
                               uint8_t *y, void *stream);
 
+/* ---------------------------------------------------------------- quantized language models
+ *
+ * The same quantizers where the activations stay 16-bit floats: weights in 4 bits with one scale per GROUP of a
+ * row's weights (Sec. 2.6 with a finer granularity than the channel), and the keys and values that attention keeps of past
+ * tokens in 8 bits with one scale per block of tokens and head.  `type` is the element type of activations: */
+#define QNN_BF16 0
+#define QNN_F16 1
+
+/* y[m][n] = bias[n] + sum_k x[m][k] * (c[n][k] - z[k / group][n]) * s[k / group][n]
+ * The weights enter exactly (code minus zero-point is a whole number of at most 5 bits, the scale multiplies the group's sum in
+ * binary32); sums are binary32, y is rounded once.
+ * x: DEVICE, M x K of `type`, row pitch ldx >= K elements.  codes: DEVICE uint8 [N][K/2], nibbles as in qnn_qgemm
+ * (two's complement, element 2j in the low one), K even.  scales: DEVICE [ceil(K / group)][N] of `type`.
+ * zeros: DEVICE int8 [ceil(K / group)][N], or NULL for symmetric weights.  bias: DEVICE [N] of `type` or NULL.
+ * group: a multiple of 32 (one scale per row: any such number >= K).  y: DEVICE, M x N of `type`, row pitch ldy >= N (written).
+ * M == 0 is a no-op.  workspace: DEVICE scratch, 16-byte aligned, of at least qnn_w4_matmul_workspace_bytes bytes (NULL where that
+ * is 0), else QNN_EINVAL. */
+qnn_status qnn_w4_matmul(const void *x, int64_t ldx, const uint8_t *codes, const void *scales, const int8_t *zeros,
+                         const void *bias, int64_t M, int64_t N, int64_t K, int64_t group, int type, void *y, int64_t ldy,
+                         void *workspace, size_t workspace_bytes, void *stream);
+size_t qnn_w4_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t group);
+
+/* A cache of keys and values in 8 bits.  A page holds `block` consecutive tokens of one request for all heads; the page of a
+ * request's tokens j * block ... is table[request][j].  A value is code * scale, codes within [-127, 127] and
+ * one scale per page and head.  Values lie transposed: consecutive tokens of a channel are what the product
+ * with the probabilities reads at once.  All four arrays DEVICE, contiguous, 16-byte aligned.
+ * dim: 64, 96, 128, 192 or 256.  block: a multiple of 32 up to 256. */
+typedef struct qnn_kv_cache {
+    int8_t *k_codes; /* [pages][heads][block][dim] */
+    float *k_scales; /* [pages][heads] */
+    int8_t *v_codes; /* [pages][heads][dim][block] */
+    float *v_scales; /* [pages][heads] */
+    int64_t pages;
+    int32_t heads, dim, block;
+} qnn_kv_cache;
+
+/* Appends new tokens.  Request r (0 <= r < requests) has start[r] tokens in the cache; its new ones are the rows
+ * cu[r] ... cu[r + 1] - 1 of k and v and become its tokens start[r] ... .  For each page that they touch, and each head:
+ *   s_old = the page's scale if it holds earlier tokens of the request, else 0;  a = max|x| over the FINITE new values
+ *   s = max(s_old, a / 127);  if s > s_old, the codes held are replaced by round(code * (s_old / s))
+ *   new codes: clamp(round(x / s), -127, 127), NaN like 0;  s == 0 gives codes 0
+ * in binary32, round() with ties away from zero.
+ * k, v: DEVICE [tokens][heads][dim] of `type`; element (t, h, d) at t * token_pitch + h * head_pitch + d (elements).
+ * cu: DEVICE int32 [requests + 1], not decreasing, cu[0] == 0, cu[requests] <= tokens.  start: DEVICE int32 [requests].
+ * table: DEVICE int32 [requests][table_width].  A page must not be reached by two requests of one call.  Entries outside
+ * [0, pages) and tokens past table_width * block are left out. */
+qnn_status qnn_kv_append(const qnn_kv_cache *cache, const void *k, int64_t k_token_pitch, int64_t k_head_pitch, const void *v,
+                         int64_t v_token_pitch, int64_t v_head_pitch, int type, const int32_t *cu, const int32_t *start,
+                         const int32_t *table, int64_t table_width, int64_t requests, int64_t tokens, void *stream);
+
+/* Reads tokens back: row cu[r] + i of k and v = code * scale of token first[r] + i of request r, rounded to `type`.
+ * k, v: DEVICE [tokens][heads][dim] contiguous (written: a token without a page gives 0, rows that no request has stay as they
+ * are).  cu, first, table as above. */
+qnn_status qnn_kv_gather(const qnn_kv_cache *cache, const int32_t *cu, const int32_t *first, const int32_t *table,
+                         int64_t table_width, int64_t requests, int64_t tokens, int type, void *k, void *v, void *stream);
+
+/* Attention of query heads over the cache.  Request r has lengths[r] tokens in the cache, its queries (rows cu[r] ... of q,
+ * n of them) belong to the last n of those.  Query i stands at p = lengths[r] - n + i and sees tokens t with 0 <= t <= p and,
+ * for window > 0, t > p - window.  q_heads is a multiple of cache->heads; head e reads the cache's head e / (q_heads / heads).
+ *   out = sum_t softmax_t(scale * q . k_t) v_t;  a query that sees nothing gives 0
+ *   lse = log sum_t exp(scale * q . k_t) (natural; -inf where nothing is seen), for joining results over parts of a context
+ * Sums, maxima and products are binary32; codes enter the matrix units exactly, as binary16; q is scaled by a power of two per
+ * row to fit binary16, the probabilities (scaled to at most 2^14) are rounded to binary16.
+ * q, out: DEVICE [tokens][q_heads][dim] of `type`, element (t, e, d) of q at t * q_token_pitch + e * q_head_pitch + d; out
+ * contiguous (rows of requests are written).  lse: DEVICE float [tokens][q_heads] or NULL.
+ * max_queries: the largest number of queries of a request (more are computed too, slower); max_queries <= 0: tokens.
+ * Page numbers outside [0, pages) count as tokens that nothing sees.
+ * workspace: DEVICE, 16-byte aligned, of at least qnn_kv_attention_workspace_bytes bytes for the same sizes, else QNN_EINVAL. */
+qnn_status qnn_kv_attention(const qnn_kv_cache *cache, const void *q, int64_t q_token_pitch, int64_t q_head_pitch,
+                            int32_t q_heads, int type, const int32_t *cu, const int32_t *lengths, const int32_t *table,
+                            int64_t table_width, int64_t requests, int64_t tokens, float scale, int64_t window,
+                            int64_t max_queries, void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+size_t qnn_kv_attention_workspace_bytes(const qnn_kv_cache *cache, int32_t q_heads, int64_t table_width, int64_t requests,
+                                        int64_t tokens, int64_t window, int64_t max_queries);
+
 /* Calibration of the machine for the benchmark (not part of the inference path).
  * qnn_calibrate_mfma: `workgroups` workgroups of 8 waves each issue iters x 4 independent
  *   v_mfma_i32_32x32x32_i8 from registers only (random_operands != 0: a different pseudo-random
@@ -372,6 +447,16 @@ qnn_status qnn_quantize_weights(const float *w, size_t channels, size_t per_chan
 
 /* Pack n (even) int8 values in [-8,7] two per byte, element 2j in the low nibble.  HOST pointers. */
 qnn_status qnn_pack_int4(const int8_t *v, size_t n, uint8_t *packed);
+
+/* Group-wise weight quantizer for qnn_w4_matmul (Sec. 2.1, 2.2 with one quantizer per `group` consecutive weights of a row):
+ * symmetric (zeros == NULL): s = max|w| / 7 rounded to `type`, codes clamp(round(w / s), -7, 7); else the range widened to
+ * contain 0, s = (max - min) / 15 rounded to `type`, zero = clamp(round(-min / s), 0, 15) - 8, codes
+ * clamp(round(w / s) + zero, -8, 7), so that w ~= (code - zero) * s.  A range of nothing but zeros, or one whose s
+ * rounds to 0, gives s = 1.  Ties away from zero.
+ * w: HOST fp32 [rows][cols], finite, cols even.  codes: HOST uint8 [rows][cols/2]; scales: HOST, 16-bit patterns of `type`
+ * [ceil(cols / group)][rows]; zeros: HOST int8 of the same shape, or NULL. */
+qnn_status qnn_quantize_weights_grouped(const float *w, size_t rows, size_t cols, size_t group, int type, uint8_t *codes,
+                                        uint16_t *scales, int8_t *zeros);
 
 #ifdef __cplusplus
 }

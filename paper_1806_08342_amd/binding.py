@@ -26,6 +26,8 @@ EXPORTS = [
     "qnn_quantize_dynamic", "qnn_simquant", "qnn_simquant_backward", "qnn_choose_qparams", "qnn_quantize_multiplier", "qnn_act_range",
     "qnn_qadd_params", "qnn_quantize_weights", "qnn_pack_int4", "qnn_qgemm_workspace_bytes", "qnn_qconv2d_workspace_bytes",
     "qnn_tuning_set", "qnn_calibrate_mfma", "qnn_calibrate_copy", "qnn_qgemm_noalloc", "qnn_quantize_u16", "qnn_dequantize_u16", "qnn_calibrate_rescale",
+    "qnn_w4_matmul", "qnn_w4_matmul_workspace_bytes", "qnn_kv_append", "qnn_kv_gather", "qnn_kv_attention", "qnn_kv_attention_workspace_bytes",
+    "qnn_quantize_weights_grouped",
 ]
 
 
@@ -91,6 +93,11 @@ def load_library():
         "qnn_qadd_params": [f64, f64, f64] + [C.POINTER(i32)] * 7,
         "qnn_quantize_weights": [vp, sz, sz, ci, ci, vp, vp],
         "qnn_pack_int4": [vp, sz, vp],
+        "qnn_quantize_weights_grouped": [vp, sz, sz, sz, ci, vp, vp, vp],
+        "qnn_w4_matmul": [vp, i64, vp, vp, vp, vp, i64, i64, i64, i64, ci, vp, i64, vp, sz, vp],
+        "qnn_kv_append": [vp, vp, i64, i64, vp, i64, i64, ci, vp, vp, vp, i64, i64, i64, vp],
+        "qnn_kv_gather": [vp, vp, vp, vp, i64, i64, i64, ci, vp, vp, vp],
+        "qnn_kv_attention": [vp, vp, i64, i64, i32, ci, vp, vp, vp, i64, i64, i64, f32, i64, i64, vp, vp, vp, sz, vp],
     }
     for name, args in sigs.items():
         fn = getattr(lib, name)
@@ -100,6 +107,10 @@ def load_library():
     lib.qnn_qgemm_workspace_bytes.argtypes = [i64, i64, i64, ci, ci]
     lib.qnn_qconv2d_workspace_bytes.restype = sz
     lib.qnn_qconv2d_workspace_bytes.argtypes = [ci] * 13
+    lib.qnn_w4_matmul_workspace_bytes.restype = sz
+    lib.qnn_w4_matmul_workspace_bytes.argtypes = [i64] * 4
+    lib.qnn_kv_attention_workspace_bytes.restype = sz
+    lib.qnn_kv_attention_workspace_bytes.argtypes = [vp, i32, i64, i64, i64, i64, i64]
     _lib = lib
     return lib
 
@@ -441,3 +452,73 @@ def qdwconv2d(x, z_x, w, stride, pad, mult, shift, z_out, act_min, act_max, bias
 
 def qadd(a, z_a, b, z_b, params, z_out, act_min, act_max, out=None):
     return (_nat or _native()).qadd(a, z_a, b, z_b, params, z_out, act_min, act_max, out)
+
+
+# ------------------------------------------------------------------------------- quantized language models
+
+BF16, F16 = 0, 1
+
+
+def _half_code(dtype):
+    torch = _torch()
+    if dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError(f"expected torch.bfloat16 or torch.float16, got {dtype}")
+    return BF16 if dtype == torch.bfloat16 else F16
+
+
+def quantize_weights_grouped(w, group=128, dtype=None, asymmetric=False):
+    """fp32 [N,K] (numpy, finite, K even) -> what `w4_matmul` takes, on the host: codes uint8 [N,K/2], scales
+    [ceil(K/group),N] of `dtype` (torch.bfloat16 unless given), zeros int8 of the same shape or None (symmetric)."""
+    torch = _torch()
+    dtype = dtype or torch.bfloat16
+    w = np.ascontiguousarray(w, dtype=np.float32)
+    if w.ndim != 2:
+        raise ValueError(f"expected weights [N, K], got shape {w.shape}")
+    n, k = w.shape
+    groups = -(-k // group) if group > 0 else 0
+    codes = np.empty((n, k // 2), np.uint8)
+    scales = np.empty((groups, n), np.uint16)
+    zeros = np.empty((groups, n), np.int8) if asymmetric else None
+    _check("qnn_quantize_weights_grouped", load_library().qnn_quantize_weights_grouped(
+        w.ctypes.data, n, k, max(group, 0), _half_code(dtype), codes.ctypes.data, scales.ctypes.data, zeros.ctypes.data if asymmetric else None))
+    as_half = torch.from_numpy(scales.view(np.int16)).view(dtype)
+    return torch.from_numpy(codes), as_half, torch.from_numpy(zeros) if asymmetric else None
+
+
+def w4_matmul(x, codes, scales, group, zeros=None, bias=None, out=None, workspace=None):
+    """x [M,K] (bfloat16 or float16, rows may be spaced apart) times 4-bit weights [N,K] with one scale per `group` weights of
+    a row: y[m,n] = bias[n] + sum_k x[m,k] * (c[n,k] - zeros[k//group,n]) * scales[k//group,n].  codes: uint8 [N,K/2]
+    (as `pack_int4` packs rows); scales: [ceil(K/group),N] of x's type; zeros: int8 of that shape or None; group: a multiple of
+    32.  Returns [M,N] of x's type."""
+    return (_nat or _native()).w4_matmul(x, codes, scales, group, zeros, bias, out, workspace)
+
+
+def new_kv_cache(pages, heads, dim, block=64, device="cuda:0"):
+    """A cache of keys and values in 8 bits with one scale per page (`block` tokens of a request) and head:
+    (k_codes int8 [pages,heads,block,dim], k_scales float32 [pages,heads], v_codes int8 [pages,heads,dim,block], v_scales)."""
+    torch = _torch()
+    return (torch.zeros(pages, heads, block, dim, dtype=torch.int8, device=device), torch.zeros(pages, heads, device=device),
+            torch.zeros(pages, heads, dim, block, dtype=torch.int8, device=device), torch.zeros(pages, heads, device=device))
+
+
+def kv_append(cache, k, v, cu, start, table):
+    """Append rows cu[r]:cu[r+1] of k and v ([T,heads,dim], bfloat16 or float16, views with a contiguous last dimension will do)
+    to request r, which holds start[r] tokens.  cu int32 [R+1], start int32 [R], table int32 [R,W]: page of its tokens
+    j*block and up.  Where a block's range grows, the codes it holds are rescaled."""
+    (_nat or _native()).kv_append(cache, k, v, cu, start, table)
+
+
+def kv_gather(cache, cu, first, table, tokens, dtype):
+    """The cached tokens first[r] + i as rows cu[r] + i of (k, v), each [tokens,heads,dim] of `dtype`."""
+    return (_nat or _native()).kv_gather(cache, cu, first, table, tokens, _half_code(dtype))
+
+
+def kv_attention(cache, q, cu, lengths, table, scale=None, window=0, max_queries=None, with_lse=False, out=None, workspace=None):
+    """Attention of q [T,q_heads,dim] over the cache: rows cu[r]:cu[r+1] are the queries of request r's last tokens (of
+    lengths[r] in the cache), each sees the tokens up to its own, the last `window` of them if window > 0.  q_heads is a multiple
+    of the cache's heads.  scale: 1/sqrt(dim) unless given.  max_queries: the largest number of queries of a request (T unless
+    given).  Returns [T,q_heads,dim] of q's type, with_lse: and the logarithm of each row's sum, float32 [T,q_heads].  A query
+    that sees nothing gives 0 (and -inf)."""
+    if scale is None:
+        scale = q.shape[-1] ** -0.5
+    return (_nat or _native()).kv_attention(cache, q, cu, lengths, table, scale, window, max_queries or 0, with_lse, out, workspace)

@@ -109,6 +109,8 @@ const char *type_name(at::ScalarType t)
     case at::kChar: return "a contiguous device tensor of torch.int8";
     case at::kInt: return "a contiguous device tensor of torch.int32";
     case at::kFloat: return "a contiguous device tensor of torch.float32";
+    case at::kBFloat16: return "a contiguous device tensor of torch.bfloat16";
+    case at::kHalf: return "a contiguous device tensor of torch.float16";
     default: return "a contiguous device tensor of torch.uint16";
     }
 }
@@ -666,6 +668,191 @@ PyObject *f_qdwconv2d_asym(Args a) // x, z_x, w, z_w, stride, pad, mult, shift, 
     return y.release();
 }
 
+// ------------------------------------------------------------------------------- quantized language models
+
+// pointer, and the pitches of all but the last dimension, of a device tensor of 16-bit floats whose last dimension is contiguous
+struct Halves {
+    const at::Tensor &t;
+    void *p;
+    int type;
+};
+Halves halves(PyObject *o, const char *name, int64_t dims)
+{
+    const at::Tensor &t = tensor(o, name);
+    const bool kind = t.scalar_type() == at::kBFloat16 || t.scalar_type() == at::kHalf;
+    if (!t.is_cuda() || !kind || t.dim() != dims || !(t.numel() == 0 || t.size(dims - 1) == 1 || t.stride(dims - 1) == 1))
+        type_error(name, dims == 2 ? "a 2-D device tensor of torch.bfloat16 or torch.float16 with contiguous rows"
+                                   : "a 3-D device tensor of torch.bfloat16 or torch.float16 whose last dimension is contiguous");
+    return {t, t.data_ptr(), t.scalar_type() == at::kBFloat16 ? QNN_BF16 : QNN_F16};
+}
+bool bad_type(int type) { return type != QNN_BF16 && type != QNN_F16; }
+PyObject *pair_of(PyObject *x, PyObject *y) // takes both
+{
+    PyObject *const p = x && y ? PyTuple_Pack(2, x, y) : nullptr;
+    Py_XDECREF(x);
+    Py_XDECREF(y);
+    if (!p) throw PythonErrorSet{};
+    return p;
+}
+at::ScalarType half_type(int type) { return type == QNN_BF16 ? at::kBFloat16 : at::kHalf; }
+void same_type(const Halves &x, int type, const char *name)
+{
+    if (x.type != type) type_error(name, "a device tensor of the activations' type");
+}
+void want_shape(const at::Tensor &t, const char *name, at::IntArrayRef want)
+{
+    if (t.sizes() != want) shape_error(name, t.sizes(), want);
+}
+void same_device(const at::Tensor &t, const at::Tensor &like, const char *name)
+{
+    if (t.device() != like.device()) type_error(name, "a tensor on the device of the others");
+}
+const void *param(PyObject *o, at::ScalarType type, const char *name, at::IntArrayRef want, const at::Tensor &like)
+{
+    const at::Tensor &t = tensor(o, name);
+    if (!t.is_cuda() || t.scalar_type() != type || !t.is_contiguous()) type_error(name, type_name(type));
+    want_shape(t, name, want);
+    same_device(t, like, name);
+    return t.data_ptr();
+}
+
+PyObject *f_w4_matmul(Args a) // x, codes, scales, group, zeros, bias, out, workspace
+{
+    const Halves x = halves(a[0], "x", 2);
+    const int64_t M = x.t.size(0), K = x.t.size(1);
+    const at::Tensor &codes = tensor(a[1], "codes");
+    if (codes.dim() != 2) type_error("codes", "a 2-D device tensor of torch.uint8");
+    const int64_t N = codes.size(0), group = integer(a[3]);
+    const auto *pc = static_cast<const uint8_t *>(param(a[1], at::kByte, "codes", {N, K / 2}, x.t));
+    if (group <= 0) {
+        PyErr_SetString(PyExc_ValueError, "group must be positive");
+        throw PythonErrorSet{};
+    }
+    const int64_t groups = (K + group - 1) / group;
+    const void *ps = param(a[2], half_type(x.type), "scales", {groups, N}, x.t);
+    const auto *pz = a[4] == Py_None ? nullptr : static_cast<const int8_t *>(param(a[4], at::kChar, "zeros", {groups, N}, x.t));
+    const void *pb = a[5] == Py_None ? nullptr : param(a[5], half_type(x.type), "bias", {N}, x.t);
+    Out y = output(a[6], {M, N}, half_type(x.type), x.t);
+    const Halves out{y.t, y.t.data_ptr(), x.type};
+    if (y.given) {
+        same_type(halves(a[6], "out", 2), x.type, "out");
+        same_device(y.t, x.t, "out");
+    }
+    const int64_t ldx = M > 1 ? x.t.stride(0) : K, ldy = M > 1 ? y.t.stride(0) : N;
+    if (ldx < K) type_error("x", "rows that do not overlap");
+    if (ldy < N) type_error("out", "rows that do not overlap");
+    const Workspace ws = workspace(a[7], x.t, true, [&] { return qnn_w4_matmul_workspace_bytes(M, N, K, group); });
+    call("qnn_w4_matmul", [&](void *s) {
+        return qnn_w4_matmul(x.p, ldx, pc, ps, pz, pb, M, N, K, group, x.type, out.p, ldy, ws.p, ws.bytes, s);
+    });
+    return y.release();
+}
+
+// the four tensors of a cache: (k_codes, k_scales, v_codes, v_scales)
+qnn_kv_cache kv_cache(PyObject *o, const at::Tensor &like)
+{
+    if (!PySequence_Check(o) || PySequence_Size(o) != 4) {
+        PyErr_Clear();
+        type_error("cache", "(k_codes, k_scales, v_codes, v_scales)");
+    }
+    struct Item {
+        PyObject *o;
+        ~Item() { Py_XDECREF(o); }
+    } items[4] = {{PySequence_GetItem(o, 0)}, {PySequence_GetItem(o, 1)}, {PySequence_GetItem(o, 2)}, {PySequence_GetItem(o, 3)}};
+    for (const Item &i : items)
+        if (!i.o) throw PythonErrorSet{};
+    const at::Tensor &k = tensor(items[0].o, "k_codes");
+    if (k.dim() != 4) type_error("k_codes", "a 4-D device tensor [pages, heads, block, dim] of torch.int8");
+    const int64_t pages = k.size(0), heads = k.size(1), block = k.size(2), dim = k.size(3);
+    if (heads > INT32_MAX || block > INT32_MAX || dim > INT32_MAX) type_error("k_codes", "sizes within 32 bits");
+    qnn_kv_cache c;
+    c.k_codes = static_cast<int8_t *>(const_cast<void *>(param(items[0].o, at::kChar, "k_codes", {pages, heads, block, dim}, like)));
+    c.k_scales = static_cast<float *>(const_cast<void *>(param(items[1].o, at::kFloat, "k_scales", {pages, heads}, like)));
+    c.v_codes = static_cast<int8_t *>(const_cast<void *>(param(items[2].o, at::kChar, "v_codes", {pages, heads, dim, block}, like)));
+    c.v_scales = static_cast<float *>(const_cast<void *>(param(items[3].o, at::kFloat, "v_scales", {pages, heads}, like)));
+    c.pages = pages, c.heads = (int32_t)heads, c.dim = (int32_t)dim, c.block = (int32_t)block;
+    return c;
+}
+
+// per-request arrays: offsets [requests + 1], one number each, pages [requests, width]
+struct Requests {
+    const int32_t *cu, *each, *table;
+    int64_t width, requests;
+};
+Requests requests(PyObject *cu, PyObject *each, const char *each_name, PyObject *table, const at::Tensor &like)
+{
+    const at::Tensor &t = tensor(table, "table");
+    if (t.dim() != 2) type_error("table", "a 2-D device tensor [requests, pages] of torch.int32");
+    const int64_t n = t.size(0), width = t.size(1);
+    return {static_cast<const int32_t *>(param(cu, at::kInt, "cu", {n + 1}, like)), static_cast<const int32_t *>(param(each, at::kInt, each_name, {n}, like)),
+            static_cast<const int32_t *>(param(table, at::kInt, "table", {n, width}, like)), width, n};
+}
+
+PyObject *f_kv_append(Args a) // cache, k, v, cu, start, table
+{
+    const Halves k = halves(a[1], "k", 3), v = halves(a[2], "v", 3);
+    const qnn_kv_cache c = kv_cache(a[0], k.t);
+    const int64_t T = k.t.size(0);
+    want_shape(k.t, "k", {T, c.heads, c.dim});
+    want_shape(v.t, "v", {T, c.heads, c.dim});
+    same_type(v, k.type, "v");
+    same_device(v.t, k.t, "v");
+    const Requests r = requests(a[3], a[4], "start", a[5], k.t);
+    call("qnn_kv_append", [&](void *s) {
+        return qnn_kv_append(&c, k.p, k.t.stride(0), k.t.stride(1), v.p, v.t.stride(0), v.t.stride(1), k.type, r.cu, r.each, r.table, r.width, r.requests, T, s);
+    });
+    Py_RETURN_NONE;
+}
+
+PyObject *f_kv_gather(Args a) // cache, cu, first, table, tokens, type
+{
+    const at::Tensor &table = tensor(a[3], "table");
+    const qnn_kv_cache c = kv_cache(a[0], table);
+    const Requests r = requests(a[1], a[2], "first", a[3], table);
+    const int64_t T = integer(a[4]);
+    const int type = i32(a[5]);
+    if (T < 0 || T > INT32_MAX / 2 || bad_type(type)) {
+        PyErr_SetString(PyExc_ValueError, "tokens must lie in [0, 2^30), the type must be torch.bfloat16 or torch.float16");
+        throw PythonErrorSet{};
+    }
+    at::Tensor k = fresh({T, c.heads, c.dim}, half_type(type), table), v = fresh({T, c.heads, c.dim}, half_type(type), table);
+    void *const pk = k.data_ptr(), *const pv = v.data_ptr();
+    call("qnn_kv_gather", [&](void *s) { return qnn_kv_gather(&c, r.cu, r.each, r.table, r.width, r.requests, T, type, pk, pv, s); });
+    return pair_of(THPVariable_Wrap(std::move(k)), THPVariable_Wrap(std::move(v)));
+}
+
+PyObject *f_kv_attention(Args a) // cache, q, cu, lengths, table, scale, window, max_queries, with_lse, out, workspace
+{
+    const Halves q = halves(a[1], "q", 3);
+    const qnn_kv_cache c = kv_cache(a[0], q.t);
+    const int64_t T = q.t.size(0), heads = q.t.size(1), window = integer(a[6]), most = integer(a[7]);
+    want_shape(q.t, "q", {T, heads, c.dim});
+    if (heads > INT32_MAX) type_error("q", "sizes within 32 bits");
+    const Requests r = requests(a[2], a[3], "lengths", a[4], q.t);
+    const double scale = PyFloat_AsDouble(a[5]);
+    if (scale == -1.0 && PyErr_Occurred()) throw PythonErrorSet{};
+    const int with_lse = PyObject_IsTrue(a[8]);
+    if (with_lse < 0) throw PythonErrorSet{};
+    Out o = output(a[9], {T, heads, c.dim}, half_type(q.type), q.t);
+    if (o.given) {
+        same_type(halves(a[9], "out", 3), q.type, "out");
+        same_device(o.t, q.t, "out");
+        if (!o.t.is_contiguous()) type_error("out", "a contiguous tensor");
+    }
+    void *const po = o.t.data_ptr();
+    at::Tensor lse;
+    if (with_lse) lse = fresh({T, heads}, at::kFloat, q.t);
+    float *const pl = with_lse ? static_cast<float *>(lse.data_ptr()) : nullptr;
+    const Workspace ws = workspace(a[10], q.t, true, [&] {
+        return qnn_kv_attention_workspace_bytes(&c, (int32_t)heads, r.width, r.requests, T, window, most);
+    });
+    call("qnn_kv_attention", [&](void *s) {
+        return qnn_kv_attention(&c, q.p, q.t.stride(0), q.t.stride(1), (int32_t)heads, q.type, r.cu, r.each, r.table, r.width, r.requests, T, (float)scale,
+                                window, most, po, pl, ws.p, ws.bytes, s);
+    });
+    return with_lse ? pair_of(o.release(), THPVariable_Wrap(std::move(lse))) : o.release();
+}
+
 PyObject *f_set_check(Args a)
 {
     Py_INCREF(a[0]);
@@ -699,6 +886,10 @@ PyMethodDef kMethods[] = {
     QNN_ENTRY("qconv2d_asym", f_qconv2d_asym, 15),
     QNN_ENTRY("qdwconv2d", f_qdwconv2d, 12),
     QNN_ENTRY("qdwconv2d_asym", f_qdwconv2d_asym, 13),
+    QNN_ENTRY("w4_matmul", f_w4_matmul, 8),
+    QNN_ENTRY("kv_append", f_kv_append, 6),
+    QNN_ENTRY("kv_gather", f_kv_gather, 6),
+    QNN_ENTRY("kv_attention", f_kv_attention, 11),
     {nullptr, nullptr, 0, nullptr},
 };
 

@@ -184,4 +184,60 @@ qnn_status qnn_pack_int4(const int8_t *v, size_t n, uint8_t *packed)
     return QNN_OK;
 }
 
+// a 16-bit float's pattern of a positive finite value (to nearest even), and its value again
+static uint16_t half_pattern(float v, int type)
+{
+    if (type == QNN_F16) {
+        const _Float16 h = static_cast<_Float16>(v);
+        uint16_t b;
+        std::memcpy(&b, &h, 2);
+        return b;
+    }
+    uint32_t u;
+    std::memcpy(&u, &v, 4);
+    return static_cast<uint16_t>((u + 0x7fffu + (u >> 16 & 1u)) >> 16);
+}
+static float half_value(uint16_t b, int type)
+{
+    if (type == QNN_F16) {
+        _Float16 h;
+        std::memcpy(&h, &b, 2);
+        return static_cast<float>(h);
+    }
+    const uint32_t u = static_cast<uint32_t>(b) << 16;
+    float v;
+    std::memcpy(&v, &u, 4);
+    return v;
+}
+
+qnn_status qnn_quantize_weights_grouped(const float *w, size_t rows, size_t cols, size_t group, int type, uint8_t *codes, uint16_t *scales,
+                                        int8_t *zeros)
+{
+    if (!w || !codes || !scales || rows == 0 || cols == 0 || cols % 2 != 0 || group == 0 || group % 32 != 0) return QNN_EINVAL;
+    if (type != QNN_BF16 && type != QNN_F16) return QNN_EINVAL;
+    for (size_t i = 0; i < rows * cols; ++i)
+        if (!std::isfinite(w[i])) return QNN_EINVAL;
+    std::memset(codes, 0, rows * (cols / 2));
+    for (size_t n = 0; n < rows; ++n)
+        for (size_t k0 = 0, g = 0; k0 < cols; k0 += group, ++g) {
+            const float *const row = w + n * cols;
+            const size_t k1 = k0 + group < cols ? k0 + group : cols;
+            double lo = 0.0, hi = 0.0;
+            for (size_t k = k0; k < k1; ++k) lo = std::fmin(lo, row[k]), hi = std::fmax(hi, row[k]);
+            const double range = zeros ? (hi - lo) / 15.0 : std::fmax(-lo, hi) / 7.0;
+            uint16_t pattern = half_pattern(static_cast<float>(range), type);
+            if (!std::isfinite(half_value(pattern, type))) return QNN_EINVAL; // beyond the range of the scales' type
+            if (half_value(pattern, type) == 0.0f) pattern = half_pattern(1.0f, type);
+            const double step = half_value(pattern, type);
+            const double zero = zeros ? std::fmin(std::fmax(qnn::nearest_away(-lo / step), 0.0), 15.0) - 8.0 : 0.0;
+            scales[g * rows + n] = pattern;
+            if (zeros) zeros[g * rows + n] = static_cast<int8_t>(zero);
+            for (size_t k = k0; k < k1; ++k) {
+                const double c = std::fmin(std::fmax(qnn::nearest_away(row[k] / step) + zero, zeros ? -8.0 : -7.0), 7.0);
+                codes[(n * cols + k) / 2] |= static_cast<uint8_t>((static_cast<uint8_t>(static_cast<int8_t>(c)) & 0x0F) << (k % 2 * 4));
+            }
+        }
+    return QNN_OK;
+}
+
 } // extern "C"

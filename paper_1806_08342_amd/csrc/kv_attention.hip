@@ -1,0 +1,426 @@
+// Attention of query heads over a paged cache of 8-bit codes (qnn_kv_attention).
+//
+//   o = sum_t softmax_t(scale * ks[t] * q . ck[t]) * vs[t] * cv[t],  ks, vs: one scale per page and head
+//
+// One pass over the tokens with a running maximum m and sum l; a page's key scale multiplies its scores, its value scale the
+// product of its probabilities with its codes, so that the codes themselves go through the matrix units, in binary16, where
+// they are exact.
+//
+// The products are formed transposed, S^T = K q^T and O^T = V^T p^T on 16x16x32 tiles: a lane's column is one query row
+// throughout, the maximum over tokens is a maximum over the lane's registers and four lanes, and which token a row
+// of S^T stands for is free to choose.  It is chosen so that the four rows that a lane gets of each tile are tokens that lie one
+// after the other in its part of the value product: the probabilities go from the first product into the second in the lane
+// that holds them, without LDS or shuffles.  Keys and values come straight from memory into registers: each wave
+// reads tokens of its own, so nothing would be shared through LDS.
+#include "kv_attention.h"
+#include "tuning.h"
+
+namespace qnn {
+
+// One unit of U tokens per wave and step; four waves take units in turn.  NT tiles of 16 query rows (row = query * group + head of
+// the group) share the cache's codes.
+template <class T, int D, int U, int NT> __global__ void __launch_bounds__(256) attend_few_kernel(const AttendArgs a)
+{
+    constexpr int J = D / 64, TAIL = D % 64 != 0; // key pieces of 64 channels (16 bytes a lane), and one of 32
+    constexpr int S = U / 16, VW = U / 16;        // score tiles; dwords of a value row that a lane takes
+    constexpr int VT = D / 16;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+    const int h = blockIdx.y;
+    const int chunk = blockIdx.x % a.chunks, rb = blockIdx.x / a.chunks % a.row_blocks, r = blockIdx.x / a.chunks / a.row_blocks;
+    const Request rq = request_of<U>(a, r);
+    const int chunks = chunks_of(a, rq);
+    if (chunk >= chunks) return;
+    const int rows = rq.n * a.group;
+    const int64_t t0 = rq.low + (int64_t)chunk * a.chunk_tokens;
+    const int block = a.cache.block, heads = a.cache.heads;
+
+    __shared__ float s_m[4][16 * NT], s_l[4][16 * NT];
+    __shared__ __attribute__((aligned(16))) float s_o[2][16 * NT][D + 4];
+
+    for (int rt = rb * 16 * NT; rt < rows; rt += a.row_blocks * 16 * NT) {
+        // queries: this lane's row of each tile, the channels that its key bytes have
+        h16x8 qf[NT][J * 2 + TAIL];
+        float factor[NT];
+        int64_t pos[NT], row_id[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int row = rt + nt * 16 + c, qi = min(row, rows - 1) / a.group, e = min(row, rows - 1) % a.group;
+            pos[nt] = row < rows ? rq.length - rq.n + qi : -1; // a row beyond the last sees nothing
+            row_id[nt] = (rq.row0 + qi) * a.q_heads + h * a.group + e;
+            const uint16_t *q = a.q + (rq.row0 + qi) * a.q_token_pitch + (int64_t)(h * a.group + e) * a.q_head_pitch;
+            w32x4 raw[J * 2 + TAIL];
+#pragma unroll
+            for (int j = 0; j < J * 2 + TAIL; ++j)
+                raw[j] = load_any<w32x4>(q + (j < 2 * J ? 64 * (j >> 1) + 16 * g + 8 * (j & 1) : 64 * J + 8 * g));
+            float v[8 * (J * 2 + TAIL)], peak = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8 * (J * 2 + TAIL); ++i) {
+                v[i] = T::widen((uint16_t)(raw[i >> 3][i >> 1 & 3] >> (i & 1) * 16));
+                peak = fmaxf(peak, fabsf(v[i]));
+            }
+            const int ex = std::is_same_v<T, F16> ? 0 : row_exponent(max_over_groups(peak));
+            const float down = ldexpf(1.0f, -ex);
+            factor[nt] = a.scale * ldexpf(1.0f, ex);
+#pragma unroll
+            for (int j = 0; j < J * 2 + TAIL; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) qf[nt][j][i] = (_Float16)(v[j * 8 + i] * down);
+        }
+        // tokens beyond what the last row of this block sees are left out
+        const int last_row = min(rt + 16 * NT, rows) - 1;
+        const int64_t t1 = min(chunk + 1 < chunks ? min(rq.high, t0 + a.chunk_tokens) : rq.high, rq.length - rq.n + last_row / a.group + 1);
+        const int64_t first_pos = rq.length - rq.n + rt / a.group, last_pos = rq.length - rq.n + last_row / a.group;
+        const int units = t1 > t0 ? (int)((t1 - t0 + U - 1) / U) : 0;
+        const int mine = (units - wave + 3) / 4; // units wave, wave + 4, ...
+
+        f32x4 o[NT][VT];
+        float m[NT], l[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            m[nt] = kNothing, l[nt] = 0.0f;
+#pragma unroll
+            for (int v = 0; v < VT; ++v) o[nt][v] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+
+        // lane i holds page, place in the page and scales of the i-th of 64 units
+        int32_t u_page = 0, u_at = 0;
+        float u_ks = 0.0f, u_vs = 0.0f;
+        auto look_up = [&](int from) {
+            const int64_t t = t0 + (int64_t)(wave + 4 * (from + lane)) * U;
+            u_page = -1, u_at = 0, u_ks = 0.0f, u_vs = 0.0f;
+            if (from + lane < mine) {
+                const int32_t p = a.table[(int64_t)r * a.table_width + t / block];
+                u_at = (int32_t)(t % block);
+                if ((uint32_t)p < (uint64_t)a.cache.pages) {
+                    u_page = p;
+                    u_ks = a.cache.k_scales[(int64_t)p * heads + h], u_vs = a.cache.v_scales[(int64_t)p * heads + h];
+                }
+            }
+        };
+        w32x4 kr[S][J];
+        w32x2 kt[S];
+        uint32_t vr[VT][VW];
+        // (a unit without a page reads page 0 and is masked)
+        auto load_keys = [&](int k) {
+            const int p = max(__builtin_amdgcn_readlane(u_page, k & 63), 0), at = __builtin_amdgcn_readlane(u_at, k & 63);
+            const int8_t *base = a.cache.k_codes + (((int64_t)p * heads + h) * block + at) * D;
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                const int8_t *row = base + ((c >> 2) * (U / 4) + s * 4 + (c & 3)) * D;
+#pragma unroll
+                for (int j = 0; j < J; ++j) kr[s][j] = *reinterpret_cast<const w32x4 *>(row + 64 * j + 16 * g);
+                if (TAIL) kt[s] = *reinterpret_cast<const w32x2 *>(row + 64 * J + 8 * g);
+            }
+        };
+        auto load_values = [&](int k) {
+            const int p = max(__builtin_amdgcn_readlane(u_page, k & 63), 0), at = __builtin_amdgcn_readlane(u_at, k & 63);
+            const int8_t *base = a.cache.v_codes + ((int64_t)p * heads + h) * block * D + at + g * (U / 4);
+#pragma unroll
+            for (int v = 0; v < VT; ++v) {
+                const int8_t *row = base + (int64_t)(v * 16 + c) * block;
+                if constexpr (VW == 4) {
+                    const w32x4 w = *reinterpret_cast<const w32x4 *>(row);
+                    vr[v][0] = w[0], vr[v][1] = w[1], vr[v][2] = w[2], vr[v][3] = w[3];
+                } else {
+                    const w32x2 w = *reinterpret_cast<const w32x2 *>(row);
+                    vr[v][0] = w[0], vr[v][1] = w[1];
+                }
+            }
+        };
+
+        if (mine > 0) {
+            look_up(0);
+            load_keys(0);
+            load_values(0);
+        }
+        for (int k = 0; k < mine; ++k) {
+            const int64_t t = t0 + (int64_t)(wave + 4 * k) * U;
+            const bool missing = __builtin_amdgcn_readlane(u_page, k & 63) < 0;
+            const float ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, u_ks), k & 63));
+            const float vs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, u_vs), k & 63));
+            f32x4 s[NT][S];
+#pragma unroll
+            for (int i = 0; i < S; ++i) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) s[nt][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const h16x8 kf = codes_to_halves8(kr[i][j][2 * half], kr[i][j][2 * half + 1]);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+                            s[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[nt][2 * j + half], s[nt][i], 0, 0, 0);
+                    }
+                if constexpr (TAIL) {
+                    const h16x8 kf = codes_to_halves8(kt[i][0], kt[i][1]);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) s[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[nt][2 * J], s[nt][i], 0, 0, 0);
+                }
+            }
+            const bool more = k + 1 < mine, refill = ((k + 1) & 63) == 0;
+            if (more && !refill) load_keys(k + 1);
+
+            // probabilities, and what the accumulators are rescaled with where a maximum grew
+            const bool masked = missing || t + U - 1 > first_pos || (a.window > 0 && t <= last_pos - a.window);
+            h16x8 p[NT][U / 32];
+            float shrink[NT];
+            bool grew = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const float f = factor[nt] * ks;
+                float top = kNothing;
+#pragma unroll
+                for (int i = 0; i < S; ++i) s[nt][i] *= f;
+                if (masked) {
+                    // tokens of this lane that its row sees: base + (from, to]
+                    const int64_t base = t + g * (U / 4);
+                    const int to = missing ? -1 : (int)min(pos[nt] - base, (int64_t)U);
+                    const int from = a.window > 0 ? (int)min(max(pos[nt] - a.window - base, (int64_t)-1), (int64_t)U) : -1;
+#pragma unroll
+                    for (int i = 0; i < S; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[nt][i][e] = (i * 4 + e <= to && i * 4 + e > from) ? s[nt][i][e] : -INFINITY;
+                }
+#pragma unroll
+                for (int i = 0; i < S; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) top = fmaxf(top, s[nt][i][e]);
+                const float now = fmaxf(m[nt], max_over_groups(top));
+                shrink[nt] = exp2_fast(m[nt] - now);
+                grew |= now > m[nt];
+                m[nt] = now;
+                float sum = 0.0f;
+#pragma unroll
+                for (int i = 0; i < S; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float x = exp2_fast(s[nt][i][e] - (now - kHead));
+                        sum += x;
+                        p[nt][i >> 1][(i & 1) * 4 + e] = (_Float16)x;
+                    }
+                l[nt] = l[nt] * shrink[nt] + sum;
+            }
+            if (__any(grew)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int v = 0; v < VT; ++v) o[nt][v] *= shrink[nt];
+            }
+#pragma unroll
+            for (int v = 0; v < VT; ++v)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int half = 0; half < U / 32; ++half)
+                        x = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_halves8(vr[v][2 * half], vr[v][2 * half + 1]), p[nt][half], x, 0, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[nt][v][e] = fmaf(vs, x[e], o[nt][v][e]);
+                }
+            if (more) {
+                if (refill) {
+                    look_up(k + 1);
+                    load_keys(k + 1);
+                }
+                load_values(k + 1);
+            }
+        }
+
+        // the four waves' parts, joined: two of them, then the other two, in a fixed order
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            l[nt] = sum_over_groups(l[nt]);
+            if (g == 0) s_m[wave][nt * 16 + c] = m[nt], s_l[wave][nt * 16 + c] = l[nt];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            float top = s_m[0][nt * 16 + c], sum = 0.0f;
+#pragma unroll
+            for (int w = 1; w < 4; ++w) top = fmaxf(top, s_m[w][nt * 16 + c]);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) sum += s_l[w][nt * 16 + c] * exp2_fast(s_m[w][nt * 16 + c] - top);
+            const float by = exp2_fast(m[nt] - top);
+            m[nt] = top, l[nt] = sum;
+#pragma unroll
+            for (int v = 0; v < VT; ++v) o[nt][v] *= by;
+        }
+#pragma unroll
+        for (int half = 2; half >= 1; half >>= 1) {
+            if (wave >= half && wave < 2 * half)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int v = 0; v < VT; ++v) *reinterpret_cast<f32x4 *>(&s_o[wave - half][nt * 16 + c][v * 16 + g * 4]) = o[nt][v];
+            __syncthreads();
+            if (wave < half)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int v = 0; v < VT; ++v) o[nt][v] += *reinterpret_cast<const f32x4 *>(&s_o[wave][nt * 16 + c][v * 16 + g * 4]);
+            __syncthreads();
+        }
+        if (wave == 0)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                if (rt + nt * 16 + c >= rows) continue;
+                if (chunks == 1) {
+                    const float inv = l[nt] != 0.0f ? 1.0f / l[nt] : 0.0f;
+                    uint16_t *out = a.out + row_id[nt] * D;
+#pragma unroll
+                    for (int v = 0; v < VT; ++v) {
+                        const f32x4 x = o[nt][v] * inv;
+                        *reinterpret_cast<w32x2 *>(out + v * 16 + g * 4) = w32x2{narrow2<T>(x[0], x[1]), narrow2<T>(x[2], x[3])};
+                    }
+                    if (a.lse && g == 0) a.lse[row_id[nt]] = l[nt] != 0.0f ? (m[nt] - kHead + log2f(l[nt])) * 0.69314718056f : -INFINITY;
+                } else {
+                    const int64_t part = row_id[nt] * a.chunks + chunk;
+#pragma unroll
+                    for (int v = 0; v < VT; ++v) *reinterpret_cast<f32x4 *>(a.part_o + part * D + v * 16 + g * 4) = o[nt][v];
+                    if (g == 0) a.part_ml[2 * part] = m[nt], a.part_ml[2 * part + 1] = l[nt];
+                }
+            }
+    }
+}
+
+// Joins the chunks of a row: one workgroup per row, its four waves take chunks in turn.
+template <class T, int D, int U> __global__ void __launch_bounds__(256) attend_join_kernel(const AttendArgs a, int rows_per_block)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = blockIdx.y;
+    const int sub = blockIdx.x % rows_per_block, r = blockIdx.x / rows_per_block;
+    const Request rq = request_of<U>(a, r);
+    const int chunks = chunks_of(a, rq);
+    if (chunks == 1) return;
+    __shared__ float s_l[4], s_o[4][D];
+    for (int row = sub; row < rq.n * a.group; row += rows_per_block) {
+        const int64_t id = (rq.row0 + row / a.group) * a.q_heads + h * a.group + row % a.group;
+        const float *ml = a.part_ml + id * a.chunks * 2, *po = a.part_o + id * a.chunks * D;
+        float top = kNothing;
+        for (int i = lane; i < chunks; i += 64) top = fmaxf(top, ml[2 * i]);
+#pragma unroll
+        for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
+        float o[(D + 63) / 64] = {}, l = 0.0f;
+#pragma unroll 4
+        for (int i = wave; i < chunks; i += 4) {
+            const float w = exp2_fast(ml[2 * i] - top);
+            l += w * ml[2 * i + 1];
+#pragma unroll
+            for (int d = 0; d < (D + 63) / 64; ++d)
+                if (D % 64 == 0 || d * 64 + lane < D) o[d] = fmaf(w, po[(int64_t)i * D + d * 64 + lane], o[d]);
+        }
+        if (lane == 0) s_l[wave] = l;
+#pragma unroll
+        for (int d = 0; d < (D + 63) / 64; ++d)
+            if (D % 64 == 0 || d * 64 + lane < D) s_o[wave][d * 64 + lane] = o[d];
+        __syncthreads();
+        l = (s_l[0] + s_l[1]) + (s_l[2] + s_l[3]);
+        const int d = threadIdx.x;
+        if (d < D) {
+            const float x = (s_o[0][d] + s_o[1][d]) + (s_o[2][d] + s_o[3][d]);
+            a.out[id * D + d] = T::narrow(l != 0.0f ? x / l : 0.0f);
+        }
+        if (a.lse && threadIdx.x == 0) a.lse[id] = l != 0.0f ? (top - kHead + log2f(l)) * 0.69314718056f : -INFINITY;
+        __syncthreads();
+    }
+}
+
+struct AttendPlan {
+    int tiles, row_blocks, chunks;
+    int64_t chunk_tokens;
+};
+
+static AttendPlan attend_plan(const qnn_kv_cache &cache, int q_heads, int64_t table_width, int64_t requests, int64_t tokens, int64_t window,
+                              int64_t max_queries)
+{
+    AttendPlan p;
+    if (max_queries <= 0 || max_queries > tokens) max_queries = tokens;
+    const int64_t rows = max_queries * (q_heads / cache.heads), unit = 64;
+    const int most = cache.dim <= 128 ? 4 : 2;
+    p.tiles = rows <= 16 ? 1 : rows <= 32 || most == 2 ? 2 : 4;
+    int64_t reach = table_width * cache.block;
+    if (window > 0 && window < reach) reach = reach < window + max_queries - 1 + 2 * unit ? reach : window + max_queries - 1 + 2 * unit;
+    int64_t blocks = (rows + p.tiles * 16 - 1) / (p.tiles * 16);
+    p.row_blocks = (int)(blocks < 4096 ? blocks : 4096);
+    const int64_t groups = requests * cache.heads * p.row_blocks;
+    int64_t want = groups < 2048 ? 2048 / groups : 1;
+    if (want > 128) want = 128;
+    int64_t chunk = (reach + want - 1) / want;
+    chunk = (chunk + 255) / 256 * 256;
+    if (rows > 64) chunk = reach;
+    if (chunk < 256) chunk = 256;
+    p.chunk_tokens = chunk;
+    p.chunks = (int)((reach + chunk - 1) / chunk);
+    return p;
+}
+
+template <class T, int D, int U> static qnn_status run_attend(AttendArgs &a, const AttendPlan &p, int64_t max_queries, hipStream_t s)
+{
+    const dim3 grid((unsigned)((int64_t)a.requests * p.row_blocks * p.chunks), (unsigned)a.cache.heads);
+    if (p.tiles == 1) hipLaunchKernelGGL((attend_few_kernel<T, D, U, 1>), grid, dim3(256), 0, s, a);
+    else if (p.tiles == 2 || D > 128) hipLaunchKernelGGL((attend_few_kernel<T, D, U, 2>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((attend_few_kernel<T, D, U, (D > 128 ? 2 : 4)>), grid, dim3(256), 0, s, a);
+    if (p.chunks > 1) {
+        const int per = (int)(max_queries * a.group < 4096 ? max_queries * a.group : 4096);
+        hipLaunchKernelGGL((attend_join_kernel<T, D, U>), dim3((unsigned)((int64_t)a.requests * per), (unsigned)a.cache.heads), dim3(256), 0, s, a, per);
+    }
+    return launch_status(hipGetLastError());
+}
+
+template <class T, int D> static qnn_status run_attend_unit(AttendArgs &a, const AttendPlan &p, int64_t max_queries, hipStream_t s)
+{
+    return a.cache.block % 64 == 0 ? run_attend<T, D, 64>(a, p, max_queries, s) : run_attend<T, D, 32>(a, p, max_queries, s);
+}
+
+template <class T> static qnn_status run_attend_dim(AttendArgs &a, const AttendPlan &p, int64_t max_queries, hipStream_t s)
+{
+    switch (a.cache.dim) {
+    case 64: return run_attend_unit<T, 64>(a, p, max_queries, s);
+    case 96: return run_attend_unit<T, 96>(a, p, max_queries, s);
+    case 128: return run_attend_unit<T, 128>(a, p, max_queries, s);
+    case 192: return run_attend_unit<T, 192>(a, p, max_queries, s);
+    default: return run_attend_unit<T, 256>(a, p, max_queries, s);
+    }
+}
+
+} // namespace qnn
+
+using namespace qnn;
+
+extern "C" {
+
+static bool bad_attend_sizes(const qnn_kv_cache *cache, int32_t q_heads, int64_t table_width, int64_t requests, int64_t tokens, int64_t window)
+{
+    return bad_cache(cache) || q_heads <= 0 || q_heads % cache->heads != 0 || table_width < 0 || requests < 0 || requests > (1 << 20) || tokens < 0 ||
+           tokens > INT32_MAX || table_width > INT32_MAX / cache->block || window < 0 || tokens * (q_heads / cache->heads) > INT32_MAX;
+}
+
+size_t qnn_kv_attention_workspace_bytes(const qnn_kv_cache *cache, int32_t q_heads, int64_t table_width, int64_t requests, int64_t tokens,
+                                        int64_t window, int64_t max_queries)
+{
+    if (bad_attend_sizes(cache, q_heads, table_width, requests, tokens, window) || requests == 0 || tokens == 0) return 0;
+    const AttendPlan p = attend_plan(*cache, q_heads, table_width, requests, tokens, window, max_queries);
+    return p.chunks > 1 ? (size_t)tokens * q_heads * p.chunks * (cache->dim + 2) * sizeof(float) : 0;
+}
+
+qnn_status qnn_kv_attention(const qnn_kv_cache *cache, const void *q, int64_t q_token_pitch, int64_t q_head_pitch, int32_t q_heads, int type,
+                            const int32_t *cu, const int32_t *lengths, const int32_t *table, int64_t table_width, int64_t requests, int64_t tokens,
+                            float scale, int64_t window, int64_t max_queries, void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (bad_attend_sizes(cache, q_heads, table_width, requests, tokens, window) || bad_half_type(type) || !isfinite(scale)) return QNN_EINVAL;
+    if (requests == 0 || tokens == 0) return QNN_OK;
+    if (!q || !cu || !lengths || !out || (table_width > 0 && !table)) return QNN_EINVAL;
+    if (bad_cache_arrays(cache) || ((uintptr_t)out & 15) != 0) return QNN_EINVAL;
+    const AttendPlan p = attend_plan(*cache, q_heads, table_width, requests, tokens, window, max_queries);
+    const size_t need = qnn_kv_attention_workspace_bytes(cache, q_heads, table_width, requests, tokens, window, max_queries);
+    if (need > 0 && (!workspace || ((uintptr_t)workspace & 15) != 0 || workspace_bytes < need)) return QNN_EINVAL;
+    if (requests * p.row_blocks * p.chunks > INT32_MAX) return QNN_EUNSUPPORTED;
+    if (max_queries <= 0 || max_queries > tokens) max_queries = tokens;
+    AttendArgs a{*cache, static_cast<const uint16_t *>(q), q_token_pitch, q_head_pitch, cu, lengths, table, static_cast<uint16_t *>(out), lse,
+                 static_cast<float *>(workspace), nullptr, table_width, tokens, window, scale * 1.44269504089f, q_heads, q_heads / cache->heads,
+                 (int32_t)requests, (int32_t)p.chunk_tokens, p.chunks, p.row_blocks};
+    if (need > 0) a.part_ml = a.part_o + (size_t)tokens * q_heads * p.chunks * cache->dim;
+    return type == QNN_BF16 ? run_attend_dim<Bf16>(a, p, max_queries, as_stream(stream)) : run_attend_dim<F16>(a, p, max_queries, as_stream(stream));
+}
+
+} // extern "C"
