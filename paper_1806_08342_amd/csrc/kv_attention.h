@@ -26,12 +26,14 @@ struct AttendArgs {
     const int32_t *cu, *lengths, *table;
     uint16_t *out;
     float *lse;
-    float *part_o;  // [tokens * q_heads][chunks][dim]
-    float *part_ml; // [tokens * q_heads][chunks][2]
+    float *part_o;  // [requests][heads][part_rows][chunks][dim]
+    float *part_ml; // [requests][heads][part_rows][chunks][2]
     int64_t table_width, tokens, window;
     float scale; // times log2(e)
     int32_t q_heads, group, requests;
     int32_t chunk_tokens, chunks, row_blocks;
+    int32_t part_rows;            // rows per request and head that there is scratch for
+    int32_t rows_over, rows_upto; // requests with other numbers of rows (queries * group) are another launch's
 };
 
 constexpr float kNothing = -3.0e38f; // running maximum before the first token that is seen
@@ -57,9 +59,12 @@ template <int U> __device__ __forceinline__ Request request_of(const AttendArgs 
 }
 __device__ __forceinline__ int chunks_of(const AttendArgs &a, const Request &q)
 {
+    if (q.n * a.group > a.part_rows) return 1; // (more queries than the host was told: no room for parts)
     // (a request with more queries than the host was told can reach back further under a window: its last chunk is longer)
     return (int)min(max((int64_t)1, (q.high - q.low + a.chunk_tokens - 1) / a.chunk_tokens), (int64_t)a.chunks);
 }
+
+__device__ __forceinline__ int64_t part_row(const AttendArgs &a, int r, int h, int row) { return ((int64_t)r * a.cache.heads + h) * a.part_rows + row; }
 
 // Four codes of a dword to binary16, exactly: with the sign bit flipped a code is c + 128, which behind the byte 0x64 is the
 // binary16 1024 + c + 128.

@@ -13,13 +13,13 @@
 // that holds them, without LDS or shuffles.  Keys and values come straight from memory into registers: each wave
 // reads tokens of its own, so nothing would be shared through LDS.
 #include "kv_attention.h"
-#include "tuning.h"
+#include "kv_prompt.h"
 
 namespace qnn {
 
 // One unit of U tokens per wave and step; four waves take units in turn.  NT tiles of 16 query rows (row = query * group + head of
 // the group) share the cache's codes.
-template <class T, int D, int U, int NT> __global__ void __launch_bounds__(256) attend_few_kernel(const AttendArgs a)
+template <class T, int D, int U, int NT> __global__ void __launch_bounds__(256, D * NT <= 128 ? 2 : 1) attend_few_kernel(const AttendArgs a)
 {
     constexpr int J = D / 64, TAIL = D % 64 != 0; // key pieces of 64 channels (16 bytes a lane), and one of 32
     constexpr int S = U / 16, VW = U / 16;        // score tiles; dwords of a value row that a lane takes
@@ -28,9 +28,10 @@ template <class T, int D, int U, int NT> __global__ void __launch_bounds__(256) 
     const int h = blockIdx.y;
     const int chunk = blockIdx.x % a.chunks, rb = blockIdx.x / a.chunks % a.row_blocks, r = blockIdx.x / a.chunks / a.row_blocks;
     const Request rq = request_of<U>(a, r);
+    const int rows = rq.n * a.group;
+    if (rows <= a.rows_over || rows > a.rows_upto) return;
     const int chunks = chunks_of(a, rq);
     if (chunk >= chunks) return;
-    const int rows = rq.n * a.group;
     const int64_t t0 = rq.low + (int64_t)chunk * a.chunk_tokens;
     const int block = a.cache.block, heads = a.cache.heads;
 
@@ -275,7 +276,7 @@ template <class T, int D, int U, int NT> __global__ void __launch_bounds__(256) 
                     }
                     if (a.lse && g == 0) a.lse[row_id[nt]] = l[nt] != 0.0f ? (m[nt] - kHead + log2f(l[nt])) * 0.69314718056f : -INFINITY;
                 } else {
-                    const int64_t part = row_id[nt] * a.chunks + chunk;
+                    const int64_t part = part_row(a, r, h, rt + nt * 16 + c) * a.chunks + chunk;
 #pragma unroll
                     for (int v = 0; v < VT; ++v) *reinterpret_cast<f32x4 *>(a.part_o + part * D + v * 16 + g * 4) = o[nt][v];
                     if (g == 0) a.part_ml[2 * part] = m[nt], a.part_ml[2 * part + 1] = l[nt];
@@ -290,12 +291,15 @@ template <class T, int D, int U> __global__ void __launch_bounds__(256) attend_j
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = blockIdx.y;
     const int sub = blockIdx.x % rows_per_block, r = blockIdx.x / rows_per_block;
     const Request rq = request_of<U>(a, r);
+    const int rows = rq.n * a.group;
+    if (rows <= a.rows_over || rows > a.rows_upto) return;
     const int chunks = chunks_of(a, rq);
     if (chunks == 1) return;
     __shared__ float s_l[4], s_o[4][D];
-    for (int row = sub; row < rq.n * a.group; row += rows_per_block) {
+    for (int row = sub; row < rows; row += rows_per_block) {
         const int64_t id = (rq.row0 + row / a.group) * a.q_heads + h * a.group + row % a.group;
-        const float *ml = a.part_ml + id * a.chunks * 2, *po = a.part_o + id * a.chunks * D;
+        const int64_t part = part_row(a, r, h, row) * a.chunks;
+        const float *ml = a.part_ml + part * 2, *po = a.part_o + part * D;
         float top = kNothing;
         for (int i = lane; i < chunks; i += 64) top = fmaxf(top, ml[2 * i]);
 #pragma unroll
@@ -325,61 +329,121 @@ template <class T, int D, int U> __global__ void __launch_bounds__(256) attend_j
     }
 }
 
-struct AttendPlan {
-    int tiles, row_blocks, chunks;
-    int64_t chunk_tokens;
+// One launch over a batch: the kernel for few rows, or that for many.
+struct AttendLaunch {
+    bool used = false;
+    int tiles = 1, waves = 8, row_blocks = 1, chunks = 1, part_rows = 0, rows_over = 0, rows_upto = INT32_MAX;
+    int64_t chunk_tokens = 256;
+    size_t part_bytes(int64_t requests, const qnn_kv_cache &c) const
+    {
+        return used && chunks > 1 ? (size_t)requests * c.heads * part_rows * chunks * (c.dim + 2) * sizeof(float) : 0;
+    }
 };
+struct AttendPlan {
+    AttendLaunch few, many;
+};
+
+// the context in chunks, so that there are about `want` workgroups; a chunk is at least `least` tokens
+static void divide_context(AttendLaunch &p, int64_t reach, int64_t groups, int64_t want, int64_t least, int most)
+{
+    int64_t n = groups < want ? want / groups : 1;
+    if (n > most) n = most;
+    int64_t chunk = (reach + n - 1) / n;
+    chunk = (chunk + 255) / 256 * 256;
+    if (chunk < least) chunk = least;
+    p.chunk_tokens = chunk;
+    p.chunks = (int)((reach + chunk - 1) / chunk);
+    if (p.chunks < 1) p.chunks = 1;
+}
+
+constexpr int kFewRows = 64;
 
 static AttendPlan attend_plan(const qnn_kv_cache &cache, int q_heads, int64_t table_width, int64_t requests, int64_t tokens, int64_t window,
                               int64_t max_queries)
 {
     AttendPlan p;
     if (max_queries <= 0 || max_queries > tokens) max_queries = tokens;
-    const int64_t rows = max_queries * (q_heads / cache.heads), unit = 64;
-    const int most = cache.dim <= 128 ? 4 : 2;
-    p.tiles = rows <= 16 ? 1 : rows <= 32 || most == 2 ? 2 : 4;
+    const int64_t rows = max_queries * (q_heads / cache.heads), groups = requests * cache.heads;
     int64_t reach = table_width * cache.block;
-    if (window > 0 && window < reach) reach = reach < window + max_queries - 1 + 2 * unit ? reach : window + max_queries - 1 + 2 * unit;
-    int64_t blocks = (rows + p.tiles * 16 - 1) / (p.tiles * 16);
-    p.row_blocks = (int)(blocks < 4096 ? blocks : 4096);
-    const int64_t groups = requests * cache.heads * p.row_blocks;
-    int64_t want = groups < 2048 ? 2048 / groups : 1;
-    if (want > 128) want = 128;
-    int64_t chunk = (reach + want - 1) / want;
-    chunk = (chunk + 255) / 256 * 256;
-    if (rows > 64) chunk = reach;
-    if (chunk < 256) chunk = 256;
-    p.chunk_tokens = chunk;
-    p.chunks = (int)((reach + chunk - 1) / chunk);
+    if (window > 0 && window < reach && window + max_queries + 127 < reach) reach = window + max_queries + 127;
+    // Requests with few rows among others with many: a prompt's workgroups would walk along a long context for each of them
+    p.few.used = rows <= kFewRows || requests > 1;
+    p.many.used = rows > kFewRows;
+    if (p.few.used) {
+        const int64_t few = rows < kFewRows ? rows : kFewRows;
+        const int most = cache.dim <= 64 ? 4 : cache.dim <= 128 ? 2 : 1; // (more do not fit the registers)
+        p.few.tiles = few <= 16 || most == 1 ? 1 : few <= 32 || most == 2 ? 2 : 4;
+        p.few.row_blocks = (int)((few + p.few.tiles * 16 - 1) / (p.few.tiles * 16));
+        p.few.part_rows = (int)few;
+        if (p.many.used) p.few.rows_upto = kFewRows;
+        divide_context(p.few, reach, groups * p.few.row_blocks, 2048, 256, 128);
+    }
+    if (p.many.used) {
+        if (p.few.used) p.many.rows_over = kFewRows;
+        const int64_t wide = (rows + 255) / 256;
+        p.many.waves = cache.dim > 128 || groups * wide < 256 ? 4 : 8;
+        const int64_t blocks = (rows + 32 * p.many.waves - 1) / (32 * p.many.waves);
+        p.many.row_blocks = (int)(blocks < 4096 ? blocks : 4096);
+        p.many.part_rows = (int)rows;
+        divide_context(p.many, reach, groups * blocks, 512, 1024, 16);
+    }
     return p;
 }
 
-template <class T, int D, int U> static qnn_status run_attend(AttendArgs &a, const AttendPlan &p, int64_t max_queries, hipStream_t s)
+template <class T, int D, int U> static void run_few(const AttendArgs &a, const AttendLaunch &p, hipStream_t s)
 {
+    constexpr int MOST = D <= 64 ? 4 : D <= 128 ? 2 : 1;
     const dim3 grid((unsigned)((int64_t)a.requests * p.row_blocks * p.chunks), (unsigned)a.cache.heads);
     if (p.tiles == 1) hipLaunchKernelGGL((attend_few_kernel<T, D, U, 1>), grid, dim3(256), 0, s, a);
-    else if (p.tiles == 2 || D > 128) hipLaunchKernelGGL((attend_few_kernel<T, D, U, 2>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((attend_few_kernel<T, D, U, (D > 128 ? 2 : 4)>), grid, dim3(256), 0, s, a);
-    if (p.chunks > 1) {
-        const int per = (int)(max_queries * a.group < 4096 ? max_queries * a.group : 4096);
-        hipLaunchKernelGGL((attend_join_kernel<T, D, U>), dim3((unsigned)((int64_t)a.requests * per), (unsigned)a.cache.heads), dim3(256), 0, s, a, per);
+    else if (p.tiles == 2) hipLaunchKernelGGL((attend_few_kernel<T, D, U, (MOST < 2 ? MOST : 2)>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((attend_few_kernel<T, D, U, MOST>), grid, dim3(256), 0, s, a);
+}
+
+template <class T, int D> static void run_many(const AttendArgs &a, const AttendLaunch &p, hipStream_t s)
+{
+    const dim3 grid((unsigned)((int64_t)a.requests * p.row_blocks * p.chunks * a.cache.heads));
+    if (D > 128 || p.waves == 4) hipLaunchKernelGGL((attend_prompt_kernel<T, D, 4, 1>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((attend_prompt_kernel<T, D, (D > 128 ? 4 : 8), 1>), grid, dim3(512), 0, s, a);
+}
+
+template <class T, int D, int U> static void run_join(const AttendArgs &a, hipStream_t s)
+{
+    const int per = a.part_rows < 4096 ? a.part_rows : 4096;
+    hipLaunchKernelGGL((attend_join_kernel<T, D, U>), dim3((unsigned)((int64_t)a.requests * per), (unsigned)a.cache.heads), dim3(256), 0, s, a, per);
+}
+
+template <class T, int D> static qnn_status run_attend(AttendArgs a, const AttendPlan &p, char *workspace, hipStream_t s)
+{
+    const auto with = [&](const AttendLaunch &l) {
+        a.chunk_tokens = (int32_t)l.chunk_tokens, a.chunks = l.chunks, a.row_blocks = l.row_blocks;
+        a.part_rows = l.part_rows, a.rows_over = l.rows_over, a.rows_upto = l.rows_upto;
+        a.part_o = reinterpret_cast<float *>(workspace);
+        a.part_ml = a.part_o + (size_t)a.requests * a.cache.heads * l.part_rows * l.chunks * D;
+        workspace += l.part_bytes(a.requests, a.cache);
+    };
+    if (p.many.used) {
+        with(p.many);
+        run_many<T, D>(a, p.many, s);
+        if (p.many.chunks > 1) run_join<T, D, 64>(a, s);
+    }
+    if (p.few.used) {
+        with(p.few);
+        if (a.cache.block % 64 == 0) run_few<T, D, 64>(a, p.few, s);
+        else run_few<T, D, 32>(a, p.few, s);
+        if (p.few.chunks > 1 && a.cache.block % 64 == 0) run_join<T, D, 64>(a, s);
+        else if (p.few.chunks > 1) run_join<T, D, 32>(a, s);
     }
     return launch_status(hipGetLastError());
 }
 
-template <class T, int D> static qnn_status run_attend_unit(AttendArgs &a, const AttendPlan &p, int64_t max_queries, hipStream_t s)
-{
-    return a.cache.block % 64 == 0 ? run_attend<T, D, 64>(a, p, max_queries, s) : run_attend<T, D, 32>(a, p, max_queries, s);
-}
-
-template <class T> static qnn_status run_attend_dim(AttendArgs &a, const AttendPlan &p, int64_t max_queries, hipStream_t s)
+template <class T> static qnn_status run_attend_dim(const AttendArgs &a, const AttendPlan &p, char *workspace, hipStream_t s)
 {
     switch (a.cache.dim) {
-    case 64: return run_attend_unit<T, 64>(a, p, max_queries, s);
-    case 96: return run_attend_unit<T, 96>(a, p, max_queries, s);
-    case 128: return run_attend_unit<T, 128>(a, p, max_queries, s);
-    case 192: return run_attend_unit<T, 192>(a, p, max_queries, s);
-    default: return run_attend_unit<T, 256>(a, p, max_queries, s);
+    case 64: return run_attend<T, 64>(a, p, workspace, s);
+    case 96: return run_attend<T, 96>(a, p, workspace, s);
+    case 128: return run_attend<T, 128>(a, p, workspace, s);
+    case 192: return run_attend<T, 192>(a, p, workspace, s);
+    default: return run_attend<T, 256>(a, p, workspace, s);
     }
 }
 
@@ -400,7 +464,7 @@ size_t qnn_kv_attention_workspace_bytes(const qnn_kv_cache *cache, int32_t q_hea
 {
     if (bad_attend_sizes(cache, q_heads, table_width, requests, tokens, window) || requests == 0 || tokens == 0) return 0;
     const AttendPlan p = attend_plan(*cache, q_heads, table_width, requests, tokens, window, max_queries);
-    return p.chunks > 1 ? (size_t)tokens * q_heads * p.chunks * (cache->dim + 2) * sizeof(float) : 0;
+    return p.few.part_bytes(requests, *cache) + p.many.part_bytes(requests, *cache);
 }
 
 qnn_status qnn_kv_attention(const qnn_kv_cache *cache, const void *q, int64_t q_token_pitch, int64_t q_head_pitch, int32_t q_heads, int type,
@@ -414,13 +478,15 @@ qnn_status qnn_kv_attention(const qnn_kv_cache *cache, const void *q, int64_t q_
     const AttendPlan p = attend_plan(*cache, q_heads, table_width, requests, tokens, window, max_queries);
     const size_t need = qnn_kv_attention_workspace_bytes(cache, q_heads, table_width, requests, tokens, window, max_queries);
     if (need > 0 && (!workspace || ((uintptr_t)workspace & 15) != 0 || workspace_bytes < need)) return QNN_EINVAL;
-    if (requests * p.row_blocks * p.chunks > INT32_MAX) return QNN_EUNSUPPORTED;
-    if (max_queries <= 0 || max_queries > tokens) max_queries = tokens;
-    AttendArgs a{*cache, static_cast<const uint16_t *>(q), q_token_pitch, q_head_pitch, cu, lengths, table, static_cast<uint16_t *>(out), lse,
-                 static_cast<float *>(workspace), nullptr, table_width, tokens, window, scale * 1.44269504089f, q_heads, q_heads / cache->heads,
-                 (int32_t)requests, (int32_t)p.chunk_tokens, p.chunks, p.row_blocks};
-    if (need > 0) a.part_ml = a.part_o + (size_t)tokens * q_heads * p.chunks * cache->dim;
-    return type == QNN_BF16 ? run_attend_dim<Bf16>(a, p, max_queries, as_stream(stream)) : run_attend_dim<F16>(a, p, max_queries, as_stream(stream));
+    if (requests * p.few.row_blocks * p.few.chunks > INT32_MAX || requests * p.many.row_blocks * p.many.chunks * cache->heads > INT32_MAX)
+        return QNN_EUNSUPPORTED;
+    AttendArgs a{};
+    a.cache = *cache, a.q = static_cast<const uint16_t *>(q), a.q_token_pitch = q_token_pitch, a.q_head_pitch = q_head_pitch;
+    a.cu = cu, a.lengths = lengths, a.table = table, a.out = static_cast<uint16_t *>(out), a.lse = lse;
+    a.table_width = table_width, a.tokens = tokens, a.window = window, a.scale = scale * 1.44269504089f;
+    a.q_heads = q_heads, a.group = q_heads / cache->heads, a.requests = (int32_t)requests;
+    char *const scratch = static_cast<char *>(workspace);
+    return type == QNN_BF16 ? run_attend_dim<Bf16>(a, p, scratch, as_stream(stream)) : run_attend_dim<F16>(a, p, scratch, as_stream(stream));
 }
 
 } // extern "C"

@@ -1,0 +1,299 @@
+// Attention over the cache for requests with many query rows: 32 rows per wave and row tile, keys and values of 64 tokens at a
+// time in LDS, as binary16.
+//
+// 8-bit codes are converted once for all waves of the workgroup, on the way from memory to LDS (two buffers: the codes of the next
+// 64 tokens are in flight while these are worked on).  S^T = K q^T and O^T = V^T p^T on 32x32x16 tiles; as in the kernel for few
+// rows the tokens' order in a tile is chosen so that the probabilities are the second product's operand in the lane that
+// computed them: rows of K in LDS have bits 2 and 3 of the token's number exchanged.
+//
+// The running maximum and the scale that the accumulators stand in follow lazily: they are kept while a row's scores stay below
+// 2^kRoom times the reference and a page's value scale within 2^kRoom of it, so that most units rescale nothing.  A page's
+// value scale is part of the exponent (p * vs / reference), and the sum of p is corrected once per tile.
+#pragma once
+
+#include "kv_attention.h"
+
+namespace qnn {
+
+constexpr float kPromptHead = 6.0f, kRoom = 4.0f; // p * vs / reference stays below 2^(6 + 4 + 4) of binary16's 2^16
+
+__device__ __forceinline__ float other_half(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+    // r[0]: the low half's value in all lanes, r[1]: the high half's
+    return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
+}
+
+template <class T, int D, int WAVES, int RT> __global__ void __launch_bounds__(64 * WAVES) attend_prompt_kernel(const AttendArgs a)
+{
+    constexpr int BR = 32 * RT * WAVES, KS = D / 16, VT = D / 32;
+    constexpr int PIECES = (4 * D + 64 * WAVES - 1) / (64 * WAVES); // 16-byte pieces of 64 tokens' keys (or values) per thread
+    constexpr bool EVEN = 4 * D % (64 * WAVES) == 0;
+    constexpr int KP = D + 8, VP = 64 + 8; // pitches in LDS: 16 bytes more than the row, so that rows start in different banks
+    __shared__ __attribute__((aligned(16))) _Float16 s_k[2][64][KP];
+    __shared__ __attribute__((aligned(16))) _Float16 s_v[2][D][VP];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, hh = lane >> 5;
+    const int heads = a.cache.heads, block = a.cache.block;
+    // heads next to each other: workgroups are dealt to the XCDs in turn, so that one XCD's L2 holds few heads' keys and values
+    const int h = blockIdx.x % heads, rest = blockIdx.x / heads;
+    const int chunk = rest % a.chunks, rb0 = rest / a.chunks % a.row_blocks, r = rest / a.chunks / a.row_blocks;
+    const Request rq = request_of<64>(a, r);
+    const int rows = rq.n * a.group;
+    if (rows <= a.rows_over || rows > a.rows_upto) return;
+    const int chunks = chunks_of(a, rq);
+    if (chunk >= chunks) return;
+    const int blocks = (rows + BR - 1) / BR;
+
+    // the last rows see most tokens: they go first
+    for (int rb = blocks - 1 - rb0; rb >= 0; rb -= a.row_blocks) {
+        const int rt = rb * BR;
+        const int64_t pos0 = rq.length - rq.n; // position of the first query
+        const int last_row = min(rt + BR, rows) - 1;
+        int64_t t0 = rq.low + (int64_t)chunk * a.chunk_tokens;
+        const int64_t t1 = min(chunk + 1 < chunks ? min(rq.high, t0 + a.chunk_tokens) : rq.high, pos0 + last_row / a.group + 1);
+        if (a.window > 0) t0 = max(t0, (pos0 + rt / a.group - a.window + 1) & ~(int64_t)63);
+        const int units = t1 > t0 ? (int)((t1 - t0 + 63) / 64) : 0;
+
+        // this wave's rows
+        h16x8 qf[RT][KS];
+        float factor[RT];
+        int64_t pos[RT], row_id[RT];
+#pragma unroll
+        for (int x = 0; x < RT; ++x) {
+            const int row = rt + (wave * RT + x) * 32 + c, qi = min(row, rows - 1) / a.group, e = min(row, rows - 1) % a.group;
+            pos[x] = row < rows ? pos0 + qi : -1;
+            row_id[x] = (rq.row0 + qi) * a.q_heads + h * a.group + e;
+            const uint16_t *q = a.q + (rq.row0 + qi) * a.q_token_pitch + (int64_t)(h * a.group + e) * a.q_head_pitch + 8 * hh;
+            w32x4 raw[KS];
+            float peak = 0.0f;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) raw[k] = load_any<w32x4>(q + 16 * k);
+            if constexpr (!std::is_same_v<T, F16>)
+#pragma unroll
+                for (int k = 0; k < KS; ++k)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) peak = fmaxf(peak, fabsf(T::widen((uint16_t)(raw[k][i >> 1] >> (i & 1) * 16))));
+            const int ex = std::is_same_v<T, F16> ? 0 : row_exponent(fmaxf(peak, other_half(peak)));
+            const float down = ldexpf(a.scale < 0.0f ? -1.0f : 1.0f, -ex); // (scores grow with the products: the sign goes to q)
+            factor[x] = fabsf(a.scale) * ldexpf(1.0f, ex);
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) qf[x][k][i] = (_Float16)(T::widen((uint16_t)(raw[k][i >> 1] >> (i & 1) * 16)) * down);
+        }
+        const int wave_row = rt + wave * RT * 32;
+        const int64_t wave_first = pos0 + wave_row / a.group, wave_last = pos0 + min(wave_row + 32 * RT - 1, rows - 1) / a.group;
+        const bool idle = wave_row >= rows;
+
+        f32x16 o[RT][VT];
+        float m[RT], l[RT];
+#pragma unroll
+        for (int x = 0; x < RT; ++x) {
+            m[x] = kNothing, l[x] = 0.0f;
+#pragma unroll
+            for (int v = 0; v < VT; ++v)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[x][v][i] = 0.0f;
+        }
+        float reference = 0.0f; // the value scale that o stands in; 0: none yet
+
+        // lane i holds place and scales of the i-th of 64 halves (32 tokens)
+        int32_t u_page = 0, u_at = 0;
+        float u_ks = 0.0f, u_vs = 0.0f;
+        int looked = 0;
+        auto look_up = [&](int unit) {
+            looked = unit;
+            const int64_t t = t0 + (int64_t)unit * 64 + lane * 32;
+            u_page = -1, u_at = 0, u_ks = 0.0f, u_vs = 0.0f;
+            if (t < t1) {
+                const int32_t p = a.table[(int64_t)r * a.table_width + t / block];
+                u_at = (int32_t)(t % block);
+                if ((uint32_t)p < (uint64_t)a.cache.pages) {
+                    u_page = p;
+                    u_ks = a.cache.k_scales[(int64_t)p * heads + h], u_vs = a.cache.v_scales[(int64_t)p * heads + h];
+                }
+            }
+        };
+        w32x4 kr[PIECES], vr[PIECES];
+        auto load = [&](int unit) {
+            const int i = (unit - looked) * 2;
+            const int p[2] = {max(__builtin_amdgcn_readlane(u_page, i), 0), max(__builtin_amdgcn_readlane(u_page, i + 1), 0)};
+            const int at[2] = {__builtin_amdgcn_readlane(u_at, i), __builtin_amdgcn_readlane(u_at, i + 1)};
+            const int8_t *const kb[2] = {a.cache.k_codes + (((int64_t)p[0] * heads + h) * block + at[0]) * D, a.cache.k_codes + (((int64_t)p[1] * heads + h) * block + at[1]) * D};
+            const int8_t *const vb[2] = {a.cache.v_codes + ((int64_t)p[0] * heads + h) * block * D + at[0], a.cache.v_codes + ((int64_t)p[1] * heads + h) * block * D + at[1]};
+#pragma unroll
+            for (int x = 0; x < PIECES; ++x) {
+                const int piece = x * 64 * WAVES + tid;
+                if (!EVEN && piece >= 4 * D) break;
+                const int token = piece / (D / 16), d16 = piece % (D / 16);
+                kr[x] = *reinterpret_cast<const w32x4 *>((token < 32 ? kb[0] : kb[1]) + (token & 31) * D + 16 * d16);
+                const int d = piece >> 2, seg = piece & 3;
+                vr[x] = *reinterpret_cast<const w32x4 *>((seg < 2 ? vb[0] : vb[1]) + (int64_t)d * block + 16 * (seg & 1));
+            }
+        };
+        auto stage = [&](int buf) {
+#pragma unroll
+            for (int x = 0; x < PIECES; ++x) {
+                const int piece = x * 64 * WAVES + tid;
+                if (!EVEN && piece >= 4 * D) break;
+                const int token = piece / (D / 16), d16 = piece % (D / 16);
+                const int row = (token & ~12) | (token & 4) << 1 | (token & 8) >> 1;
+                *reinterpret_cast<h16x8 *>(&s_k[buf][row][16 * d16]) = codes_to_halves8(kr[x][0], kr[x][1]);
+                *reinterpret_cast<h16x8 *>(&s_k[buf][row][16 * d16 + 8]) = codes_to_halves8(kr[x][2], kr[x][3]);
+                const int d = piece >> 2, seg = piece & 3;
+                *reinterpret_cast<h16x8 *>(&s_v[buf][d][16 * seg]) = codes_to_halves8(vr[x][0], vr[x][1]);
+                *reinterpret_cast<h16x8 *>(&s_v[buf][d][16 * seg + 8]) = codes_to_halves8(vr[x][2], vr[x][3]);
+            }
+        };
+
+        __syncthreads(); // the buffers' last readers (of the block of rows before) are done
+        if (units > 0) {
+            look_up(0);
+            load(0);
+            stage(0);
+        }
+        __syncthreads();
+        for (int u = 0; u < units; ++u) {
+            const int buf = u & 1;
+            const int64_t t = t0 + (int64_t)u * 64;
+            float ks[2], vs[2];
+            bool missing[2];
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const int i = (u - looked) * 2 + y;
+                missing[y] = __builtin_amdgcn_readlane(u_page, i) < 0;
+                ks[y] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, u_ks), i));
+                vs[y] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, u_vs), i));
+            }
+            if (u + 1 < units) {
+                if (u + 1 - looked == 32) look_up(u + 1);
+                load(u + 1);
+            }
+            if (!idle && t <= wave_last && !(a.window > 0 && t + 63 <= wave_first - a.window)) {
+                f32x16 s[RT][2];
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+#pragma unroll
+                    for (int x = 0; x < RT; ++x)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[x][y][i] = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < KS; ++k) {
+                        const h16x8 kf = *reinterpret_cast<const h16x8 *>(&s_k[buf][32 * y + c][16 * k + 8 * hh]);
+#pragma unroll
+                        for (int x = 0; x < RT; ++x) s[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[x][k], s[x][y], 0, 0, 0);
+                    }
+                }
+                if (missing[0] || missing[1] || t + 63 > wave_first || (a.window > 0 && t <= wave_last - a.window)) {
+#pragma unroll
+                    for (int x = 0; x < RT; ++x) {
+                        const int64_t base = t + 8 * hh;
+                        const int to = (int)min(pos[x] - base, (int64_t)64);
+                        const int from = a.window > 0 ? (int)min(max(pos[x] - a.window - base, (int64_t)-1), (int64_t)64) : -1;
+#pragma unroll
+                        for (int y = 0; y < 2; ++y)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const int at = 32 * y + 16 * (i >> 3) + (i & 7);
+                                s[x][y][i] = (at <= to && at > from && !missing[y]) ? s[x][y][i] : -INFINITY;
+                            }
+                    }
+                }
+                // references that no longer do
+                float most[RT], fk[RT][2];
+                bool grew = false;
+#pragma unroll
+                for (int x = 0; x < RT; ++x) {
+                    float top[2];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        fk[x][y] = fmaxf(factor[x] * ks[y], 1e-30f); // (not 0: minus infinity stays that)
+                        top[y] = s[x][y][0];
+#pragma unroll
+                        for (int i = 1; i < 16; ++i) top[y] = fmaxf(top[y], s[x][y][i]);
+                        top[y] *= fk[x][y];
+                    }
+                    most[x] = fmaxf(top[0], top[1]);
+                    most[x] = fmaxf(most[x], other_half(most[x]));
+                    grew |= most[x] > m[x] + kRoom;
+                }
+                if (__any(grew)) {
+#pragma unroll
+                    for (int x = 0; x < RT; ++x) {
+                        const float now = fmaxf(m[x], most[x]), by = exp2_fast(m[x] - now);
+                        m[x] = now, l[x] *= by;
+#pragma unroll
+                        for (int v = 0; v < VT; ++v) o[x][v] *= by;
+                    }
+                }
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const bool any = vs[y] > 0.0f; // a page of zeros adds to the sum only
+                    float ratio = any ? vs[y] / reference : 1.0f;
+                    if (any && !(ratio < 16.0f && ratio > 0.0625f)) {
+                        const float by = reference > 0.0f ? reference / vs[y] : 0.0f;
+                        reference = vs[y], ratio = 1.0f;
+#pragma unroll
+                        for (int x = 0; x < RT; ++x)
+#pragma unroll
+                            for (int v = 0; v < VT; ++v) o[x][v] *= by;
+                    }
+                    const float up = __log2f(ratio) + kPromptHead, down = 1.0f / ratio;
+                    h16x8 p[RT][2];
+#pragma unroll
+                    for (int x = 0; x < RT; ++x) {
+                        const float off = up - m[x];
+                        float sum = 0.0f;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const float e = exp2_fast(fmaf(s[x][y][i], fk[x][y], off));
+                            sum += e;
+                            p[x][i >> 3][i & 7] = (_Float16)e;
+                        }
+                        l[x] = fmaf(sum, down, l[x]);
+                        if (!any) p[x][0] = p[x][1] = h16x8{};
+                    }
+#pragma unroll
+                    for (int v = 0; v < VT; ++v)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const h16x8 vf = *reinterpret_cast<const h16x8 *>(&s_v[buf][32 * v + c][32 * y + 16 * k + 8 * hh]);
+#pragma unroll
+                            for (int x = 0; x < RT; ++x) o[x][v] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p[x][k], o[x][v], 0, 0, 0);
+                        }
+                }
+            }
+            if (u + 1 < units) stage(buf ^ 1);
+            __syncthreads();
+        }
+
+#pragma unroll
+        for (int x = 0; x < RT; ++x) {
+            l[x] += other_half(l[x]);
+            if (wave_row + x * 32 + c >= rows) continue;
+            if (chunks == 1) {
+                const float inv = l[x] != 0.0f ? reference / l[x] : 0.0f;
+                uint16_t *out = a.out + row_id[x] * D + 4 * hh;
+#pragma unroll
+                for (int v = 0; v < VT; ++v)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4)
+                        *reinterpret_cast<w32x2 *>(out + 32 * v + 2 * i) = w32x2{narrow2<T>(o[x][v][i] * inv, o[x][v][i + 1] * inv), narrow2<T>(o[x][v][i + 2] * inv, o[x][v][i + 3] * inv)};
+                if (a.lse && hh == 0) a.lse[row_id[x]] = l[x] != 0.0f ? (m[x] - kPromptHead + log2f(l[x])) * 0.69314718056f : -INFINITY;
+            } else {
+                const int64_t part = part_row(a, r, h, rt + (wave * RT + x) * 32 + c) * a.chunks + chunk;
+#pragma unroll
+                for (int v = 0; v < VT; ++v)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4)
+                        *reinterpret_cast<f32x4 *>(a.part_o + part * D + 32 * v + 2 * i + 4 * hh) =
+                            f32x4{o[x][v][i] * reference, o[x][v][i + 1] * reference, o[x][v][i + 2] * reference, o[x][v][i + 3] * reference};
+                // (the join takes maxima with the head room of the kernel for few rows)
+                if (hh == 0) a.part_ml[2 * part] = m[x] + (kHead - kPromptHead), a.part_ml[2 * part + 1] = l[x];
+            }
+        }
+    }
+}
+
+} // namespace qnn
