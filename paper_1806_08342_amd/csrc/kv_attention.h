@@ -83,14 +83,6 @@ __device__ __forceinline__ h16x8 codes_to_halves8(uint32_t w0, uint32_t w1)
     return h16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// 2^-e for the largest |q| of a row, so that q * 2^-e is at most 1: binary16 then holds what bfloat16 holds, but for elements
-// below 2^-17 of the row's largest, which keep fewer bits.  (2^e stays finite: at most 2^120.)
-__device__ __forceinline__ int row_exponent(float peak)
-{
-    const int e = (int)(__builtin_bit_cast(uint32_t, peak) >> 23 & 255u) - 126;
-    return peak > 0.0f ? min(max(e, -100), 120) : 0;
-}
-
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 } // namespace qnn

@@ -5,56 +5,9 @@
 // A nibble u = 8 + c becomes a 16-bit float by setting the bits of a power of two above it: 128 + u in bfloat16, 1024 + u in
 // binary16 (from which the 1024 is then taken off; bfloat16 has no packed subtraction, so there the 128 stays and joins the
 // 8 + z of the group's term).  No weight is rounded.  The group's sum of x comes from one more matrix product with ones.
-#include "halves.h"
+#include "w4.h"
 
 namespace qnn {
-
-struct W4Args {
-    const uint16_t *x;
-    const uint8_t *codes;
-    const uint16_t *scales;
-    const int8_t *zeros;
-    const uint16_t *bias;
-    uint16_t *y;
-    int64_t ldx, ldy;
-    int32_t M, N, K, group;
-};
-
-// eight nibbles of a dword as 16-bit floats in the order 0 4 1 5 2 6 3 7: pairs (i, i + 4)
-template <class T> struct Nibbles;
-template <> struct Nibbles<Bf16> {
-    static constexpr float kOffset = 128.0f + 8.0f;
-    static __device__ __forceinline__ uint32_t two(uint32_t w) { return (w & 0x000f000fu) | 0x43004300u; }
-    static __device__ __forceinline__ f32x4 mfma(w32x4 a, w32x4 b, f32x4 c)
-    {
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b16x8, a), __builtin_bit_cast(b16x8, b), c, 0, 0, 0);
-    }
-    static constexpr uint32_t kOnes = 0x3f803f80u;
-};
-template <> struct Nibbles<F16> {
-    static constexpr float kOffset = 8.0f;
-    static __device__ __forceinline__ uint32_t two(uint32_t w)
-    {
-        const h16x2 off = {(_Float16)1024.0f, (_Float16)1024.0f};
-        return __builtin_bit_cast(uint32_t, __builtin_bit_cast(h16x2, (w & 0x000f000fu) | 0x64006400u) - off);
-    }
-    static __device__ __forceinline__ f32x4 mfma(w32x4 a, w32x4 b, f32x4 c)
-    {
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h16x8, a), __builtin_bit_cast(h16x8, b), c, 0, 0, 0);
-    }
-    static constexpr uint32_t kOnes = 0x3c003c00u;
-};
-template <class T> __device__ __forceinline__ w32x4 expand_nibbles(uint32_t w)
-{
-    w ^= 0x88888888u;
-    return w32x4{Nibbles<T>::two(w), Nibbles<T>::two(w >> 4), Nibbles<T>::two(w >> 8), Nibbles<T>::two(w >> 12)};
-}
-// eight consecutive 16-bit elements in the same order
-__device__ __forceinline__ w32x4 pair_order(w32x4 v)
-{
-    return w32x4{__builtin_amdgcn_perm(v[2], v[0], 0x05040100u), __builtin_amdgcn_perm(v[2], v[0], 0x07060302u),
-                 __builtin_amdgcn_perm(v[3], v[1], 0x05040100u), __builtin_amdgcn_perm(v[3], v[1], 0x07060302u)};
-}
 
 // dword j of lane group g <-> dword g of lane group j
 __device__ __forceinline__ w32x4 transpose_groups(w32x4 a)
@@ -68,67 +21,75 @@ __device__ __forceinline__ w32x4 transpose_groups(w32x4 a)
 
 // One wave takes 16 * NT rows of the weights and 16 * MT rows of x; the waves of a workgroup share K in turns of 128 and join
 // their sums in LDS.  The product is formed transposed (weights are the left operand): a lane has one row of x and four
-// consecutive outputs.  A lane loads 16 bytes of a row of codes, 32 weights; after exchange among the four lanes of a
-// row, dword j of each holds weights of the j-th 32 of the 128, so that every product of 32 lies within one group.
+// consecutive outputs.  A lane loads 16 bytes of a row of codes, 32 weights.
+// After an exchange of dwords among the four lanes of a row, dword j of each holds weights of the j-th 32 of the 128, so that every
+// product of 32 lies within one group, and x is read in pieces of 64 consecutive bytes.
 // GS: groups in 128 weights as far as the sums are concerned (1: groups of whole 128s, 2: 64, 4: any multiple of 32).
-template <class T, int MT, int NT, int WAVES, int GS> __global__ void __launch_bounds__(64 * WAVES) w4_rows_kernel(const W4Args a)
+// TINY: fewer than four scales in all.
+// The codes of a wave's next 128 are in flight while it works on these; x comes from the L2, which all workgroups read it from.  The loop has no branches (rows
+// beyond the ends are the last one again, and dropped at the end); a last part of K below 128 follows it.
+template <class T, int MT, int NT, int WAVES, int GS, bool ZEROS, bool TINY> __global__ void __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : 2) w4_rows_kernel(const W4Args a)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
     const int n0 = blockIdx.x * 16 * NT, m0 = blockIdx.y * 16 * MT;
-    const int steps = (a.K + 127) / 128;
-    const int row_bytes = a.K / 2;
+    const int whole = a.K / 128, row_bytes = a.K / 2;
+    const uint32_t bits = kept(Nibbles<T>::kBits);
     f32x4 acc[MT][NT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    const uint8_t *w_row[NT];
+    const uint8_t *const w_base = a.codes + (int64_t)n0 * row_bytes;
+    uint32_t w_row[NT]; // (at most 16 * NT rows of 2^23 bytes)
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) w_row[nt] = a.codes + (int64_t)min(n0 + nt * 16 + c, a.N - 1) * row_bytes;
+    for (int nt = 0; nt < NT; ++nt) w_row[nt] = (uint32_t)(min(n0 + nt * 16 + c, a.N - 1) - n0) * row_bytes;
     const uint16_t *x_row[MT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) x_row[mt] = a.x + (int64_t)min(m0 + mt * 16 + c, a.M - 1) * a.ldx;
+    const uint32_t params = (uint32_t)a.groups * a.N; // scales, zero-points: less than 2^30
 
-    for (int step = wave; step < steps; step += WAVES) {
-        const int k0 = step * 128;
-        const bool whole = k0 + 128 <= a.K;
-        w32x4 w[NT], x[MT][4];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const int at = k0 / 2 + 16 * g;
-            if (whole || at + 16 <= row_bytes) w[nt] = load_any<w32x4>(w_row[nt] + at);
-            else {
-                w[nt] = w32x4{0u, 0u, 0u, 0u};
-                for (int b = 0; b < row_bytes - at; ++b) w[nt][b >> 2] |= (uint32_t)w_row[nt][at + b] << (b & 3) * 8;
-            }
-        }
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int at = k0 + 32 * j + 8 * g;
-                x[mt][j] = w32x4{0u, 0u, 0u, 0u};
-                if (m0 + mt * 16 + c < a.M) {
-                    if (whole || at + 8 <= a.K) x[mt][j] = load_any<w32x4>(x_row[mt] + at);
-                    else
-                        for (int b = 0; b < a.K - at; ++b) x[mt][j][b >> 1] |= (uint32_t)x_row[mt][at + b] << (b & 1) * 16;
-                }
-            }
-        float s[NT][GS][4], z[NT][GS][4];
+    // scales as they were loaded: four from (group, n) on or, where that is beyond the array, its last four, which have to be moved
+    // down by `drop` when they are used
+    struct Step {
+        w32x4 w[NT];
+        uint64_t s[NT][GS];
+        uint32_t z[NT][GS], drop[NT][GS];
+    };
+    auto load_scales = [&](Step &f, int step) {
 #pragma unroll
         for (int q = 0; q < GS; ++q) {
-            const int group = min((k0 + q * (128 / GS)), a.K - 1) / a.group;
+            const uint32_t group = (uint32_t)group_of(a, min(step * 128 + q * (128 / GS), a.K - 1)) * a.N;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int nt = 0; nt < NT; ++nt) {
+                const uint32_t want = group + min(n0 + nt * 16 + 4 * g, a.N - 1);
+                f.z[nt][q] = 0, f.drop[nt][q] = 0;
+                if (TINY) {
+                    f.s[nt][q] = 0;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int n = min(n0 + nt * 16 + 4 * g + e, a.N - 1);
-                    s[nt][q][e] = T::widen(a.scales[(int64_t)group * a.N + n]);
-                    z[nt][q][e] = Nibbles<T>::kOffset + (a.zeros ? (float)a.zeros[(int64_t)group * a.N + n] : 0.0f);
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t at = min(want + e, params - 1);
+                        f.s[nt][q] |= (uint64_t)a.scales[at] << 16 * e;
+                        if (ZEROS) f.z[nt][q] |= (uint32_t)(uint8_t)a.zeros[at] << 8 * e;
+                    }
+                } else {
+                    const uint32_t at = min(want, params - 4);
+                    f.drop[nt][q] = want - at;
+                    f.s[nt][q] = load_any<uint64_t>(a.scales + at);
+                    if (ZEROS) f.z[nt][q] = load_any<uint32_t>(a.zeros + at);
                 }
+            }
         }
+    };
+    auto load = [&](Step &f, int step) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) w[nt] = transpose_groups(w[nt]);
+        for (int nt = 0; nt < NT; ++nt) f.w[nt] = load_any<w32x4>(w_base + (w_row[nt] + (uint32_t)(64 * step + 16 * g)));
+        load_scales(f, step);
+    };
+    auto row_at = [&](int step, int j) { return step * 128 + 32 * j + 8 * g; };
+    auto compute = [&](const Step &f, const w32x4 (&x)[MT][4]) {
+        w32x4 w[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) w[nt] = transpose_groups(f.w[nt]);
 #pragma unroll
         for (int q = 0; q < GS; ++q) {
             f32x4 part[MT][NT], sums[MT];
@@ -140,25 +101,72 @@ template <class T, int MT, int NT, int WAVES, int GS> __global__ void __launch_b
             }
 #pragma unroll
             for (int j = q * (4 / GS); j < (q + 1) * (4 / GS); ++j) {
-                w32x4 wide[NT];
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) wide[nt] = expand_nibbles<T>(w[nt][j]);
+                w32x4 xp[MT];
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) {
-                    const w32x4 xp = pair_order(x[mt][j]);
+                    xp[mt] = pair_order(x[mt][j]);
                     const w32x4 ones = {Nibbles<T>::kOnes, Nibbles<T>::kOnes, Nibbles<T>::kOnes, Nibbles<T>::kOnes};
-                    sums[mt] = Nibbles<T>::mfma(ones, xp, sums[mt]);
+                    sums[mt] = Nibbles<T>::mfma(ones, xp[mt], sums[mt]);
+                }
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) part[mt][nt] = Nibbles<T>::mfma(wide[nt], xp, part[mt][nt]);
+                for (int nt = 0; nt < NT; ++nt) {
+                    const w32x4 wide = expand_nibbles<T>(w[nt][j], bits);
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) part[mt][nt] = Nibbles<T>::mfma(wide, xp[mt], part[mt][nt]);
                 }
             }
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+            for (int nt = 0; nt < NT; ++nt) {
+                const u16x4 s4 = __builtin_bit_cast(u16x4, f.s[nt][q] >> (TINY ? 0 : 16 * f.drop[nt][q]));
+                const uint32_t z4 = f.z[nt][q] >> (TINY ? 0 : 8 * f.drop[nt][q]);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                for (int e = 0; e < 4; ++e) {
+                    const float s = T::widen(s4[e]);
+                    const float z = Nibbles<T>::kOffset + (ZEROS ? (float)(int8_t)(z4 >> 8 * e) : 0.0f);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[mt][nt][e] = fmaf(s[nt][q][e], fmaf(-z[nt][q][e], sums[mt][e], part[mt][nt][e]), acc[mt][nt][e]);
+                    for (int mt = 0; mt < MT; ++mt) acc[mt][nt][e] = fmaf(s, fmaf(-z, sums[mt][e], part[mt][nt][e]), acc[mt][nt][e]);
+                }
+            }
         }
+    };
+    w32x4 x[MT][4];
+    auto load_rows = [&](int step) {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[mt][j] = load_any<w32x4>(x_row[mt] + row_at(step, j));
+    };
+    Step f[2];
+    // Each workgroup begins at another place of K: rows lie a power of two apart more often than not, and workgroups that
+    // read the same columns of all rows at one time would keep to a part of the memory's channels.
+    const int mine = (whole - wave + WAVES - 1) / WAVES;
+    if (mine > 0) {
+        int at = (int)(blockIdx.x % (uint32_t)mine);
+        const auto next = [&] { at = at + 1 < mine ? at + 1 : 0; };
+        load(f[0], wave + WAVES * at);
+        for (int i = 0; i < mine / 2; ++i) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                load_rows(wave + WAVES * at);
+                next();
+                load(f[1 - half], wave + WAVES * at); // (after the last: once again, unused)
+                compute(f[half], x);
+            }
+        }
+        if (mine & 1) {
+            load_rows(wave + WAVES * at);
+            compute(f[0], x);
+        }
+    }
+    if (a.K % 128 != 0 && wave == whole % WAVES) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) f[0].w[nt] = load_end(w_base + w_row[nt], row_bytes, 64 * whole + 16 * g);
+        load_scales(f[0], whole);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[mt][j] = load_end(reinterpret_cast<const uint8_t *>(x_row[mt]), 2 * a.K, 2 * row_at(whole, j));
+        compute(f[0], x);
     }
 
     // outputs [row of x][n], the waves' sums added in their order
@@ -179,16 +187,25 @@ template <class T, int MT, int NT, int WAVES, int GS> __global__ void __launch_b
     }
 }
 
+template <class T, int MT, int NT, int WAVES, int GS, bool TINY = false> static void launch_rows(const W4Args &a, hipStream_t s)
+{
+    const dim3 grid((unsigned)((a.N + 16 * NT - 1) / (16 * NT)), (unsigned)((a.M + 16 * MT - 1) / (16 * MT)));
+    if (a.zeros) hipLaunchKernelGGL((w4_rows_kernel<T, MT, NT, WAVES, GS, true, TINY>), grid, dim3(64 * WAVES), 0, s, a);
+    else hipLaunchKernelGGL((w4_rows_kernel<T, MT, NT, WAVES, GS, false, TINY>), grid, dim3(64 * WAVES), 0, s, a);
+}
+
 template <class T, int GS> static void launch_w4(const W4Args &a, hipStream_t s)
 {
-    if (a.M <= 16) {
-        const dim3 grid((unsigned)((a.N + 15) / 16), 1u);
-        hipLaunchKernelGGL((w4_rows_kernel<T, 1, 1, 4, GS>), grid, dim3(256), 0, s, a);
-    } else {
-        const dim3 grid((unsigned)((a.N + 31) / 32), (unsigned)((a.M + 31) / 32));
-        hipLaunchKernelGGL((w4_rows_kernel<T, 2, 2, 4, GS>), grid, dim3(256), 0, s, a);
-    }
+    if ((int64_t)a.groups * a.N < 4) launch_rows<T, 1, 1, 4, GS, true>(a, s); // (no four scales to load at once)
+    else if (a.M <= 16) {
+        if (a.N > 16384) launch_rows<T, 1, 2, 8, GS>(a, s);
+        else launch_rows<T, 1, 1, 16, GS>(a, s);
+    } else if (a.M <= 32) launch_rows<T, 2, 4, 8, GS>(a, s);
+    else launch_rows<T, 4, 2, 8, GS>(a, s);
 }
+
+// From how many rows on the kernel with tiles in LDS is ahead (it takes two launches)
+constexpr int64_t kTileRows = 65;
 
 template <class T> static qnn_status run_w4(const W4Args &a, hipStream_t s)
 {
@@ -206,13 +223,16 @@ extern "C" {
 
 static bool bad_w4_sizes(int64_t M, int64_t N, int64_t K, int64_t group)
 {
-    return M < 0 || N <= 0 || K <= 0 || K % 2 != 0 || group <= 0 || group % 32 != 0 || M > (1 << 20) || N > (1 << 28) || K > (1 << 28);
+    return M < 0 || N <= 0 || K <= 0 || K % 2 != 0 || group <= 0 || group % 32 != 0 || M > (1 << 20) || N > (1 << 28) || K > (1 << 24) || (K + group - 1) / group * N >= (1 << 30);
 }
+
+// (longer rows than the tile kernel's offsets reach stay with the kernel for few)
+static bool tiled(int64_t M, int64_t K) { return M >= kTileRows && K <= (1 << 21); }
 
 size_t qnn_w4_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t group)
 {
-    if (bad_w4_sizes(M, N, K, group)) return 0;
-    return 0;
+    if (bad_w4_sizes(M, N, K, group) || !tiled(M, K)) return 0;
+    return w4_tile_bytes(M, K);
 }
 
 qnn_status qnn_w4_matmul(const void *x, int64_t ldx, const uint8_t *codes, const void *scales, const int8_t *zeros, const void *bias, int64_t M,
@@ -223,8 +243,13 @@ qnn_status qnn_w4_matmul(const void *x, int64_t ldx, const uint8_t *codes, const
     if (!x || !codes || !scales || !y || ldx < K || ldy < N) return QNN_EINVAL;
     const size_t need = qnn_w4_matmul_workspace_bytes(M, N, K, group);
     if (need > 0 && (!workspace || ((uintptr_t)workspace & 15) != 0 || workspace_bytes < need)) return QNN_EINVAL;
-    const W4Args a{static_cast<const uint16_t *>(x), codes, static_cast<const uint16_t *>(scales), zeros, static_cast<const uint16_t *>(bias),
-                   static_cast<uint16_t *>(y), ldx, ldy, (int32_t)M, (int32_t)N, (int32_t)K, (int32_t)(group < K ? group : (K + 127) / 128 * 128)};
+    W4Args a{static_cast<const uint16_t *>(x), codes, static_cast<const uint16_t *>(scales), zeros, static_cast<const uint16_t *>(bias),
+                   static_cast<uint16_t *>(y), ldx, ldy, (int32_t)M, (int32_t)N, (int32_t)K, (int32_t)(group < K ? group : (K + 127) / 128 * 128), (int32_t)((K + group - 1) / group), 0, 0};
+    fast_division((uint32_t)a.group / 32, a.group_magic, a.group_shift);
+    if (tiled(M, K)) {
+        launch_w4_tile(a, type, workspace, as_stream(stream));
+        return launch_status(hipGetLastError());
+    }
     return type == QNN_BF16 ? run_w4<Bf16>(a, as_stream(stream)) : run_w4<F16>(a, as_stream(stream));
 }
 

@@ -1,0 +1,272 @@
+// Products with 4-bit weights for many rows: x tiles through LDS, weights from memory into registers and from there, scaled, into
+// the matrix units as binary16.
+//
+// Weights enter the matrix units as the whole numbers c - z, which binary16 holds exactly.  An accumulator stands in units of the
+// scale of the group that it is at: at the next group it is multiplied by the ratio of the two scales.  That is
+// one set of accumulators and one multiplication per output and group; as x is the left operand here, a lane's outputs are all of
+// one row of weights, and the ratio is one number per lane.
+// x has to fit binary16: a first launch writes it with each row scaled by a power of two to at most 1, which is exact (elements
+// below 2^-17 of their row's largest keep fewer bits), in the order of expand_nibbles, rows padded with zeros to whole 128s.
+#include "buffer_ops.h"
+#include "lds_ring.h"
+#include "w4.h"
+
+namespace qnn {
+
+struct W4Prepared {
+    uint16_t *x;      // binary16 [M][pitch]
+    int32_t *row_exp; // [M]
+    int32_t pitch;
+};
+
+static W4Prepared prepared(void *workspace, int64_t M, int64_t K)
+{
+    const int64_t pitch = (K + 127) / 128 * 128;
+    W4Prepared p;
+    p.x = static_cast<uint16_t *>(workspace);
+    p.row_exp = reinterpret_cast<int32_t *>(p.x + M * pitch);
+    p.pitch = (int32_t)pitch;
+    return p;
+}
+size_t w4_tile_bytes(int64_t M, int64_t K) { return (size_t)M * ((K + 127) / 128 * 128) * 2 + 4 * (size_t)M; }
+
+template <class T> __global__ void __launch_bounds__(256) w4_prepare_kernel(const W4Args a, const W4Prepared p)
+{
+    const int tid = threadIdx.x;
+    const uint16_t *const x = a.x + (int64_t)blockIdx.x * a.ldx;
+    uint16_t *const out = p.x + (int64_t)blockIdx.x * p.pitch;
+    __shared__ float s_peak[4];
+    float peak = 0.0f;
+    for (int k = 8 * tid; k < a.K; k += 8 * 256) {
+        const w32x4 v = load_end(reinterpret_cast<const uint8_t *>(x), 2 * a.K, 2 * k);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) peak = fmaxf(peak, fabsf(T::widen((uint16_t)(v[i >> 1] >> (i & 1) * 16))));
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) peak = fmaxf(peak, __shfl_xor(peak, d));
+    if ((tid & 63) == 0) s_peak[tid >> 6] = peak;
+    __syncthreads();
+    const int e = row_exponent(fmaxf(fmaxf(s_peak[0], s_peak[1]), fmaxf(s_peak[2], s_peak[3])));
+    if (tid == 0) p.row_exp[blockIdx.x] = e;
+    const float down = ldexpf(1.0f, -e);
+    for (int k = 8 * tid; k < p.pitch; k += 8 * 256) {
+        const w32x4 v = load_end(reinterpret_cast<const uint8_t *>(x), 2 * a.K, 2 * k);
+        w32x4 h;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = narrow2<F16>(T::widen((uint16_t)v[i]) * down, T::widen((uint16_t)(v[i] >> 16)) * down);
+        *reinterpret_cast<w32x4 *>(out + k) = pair_order(h);
+    }
+}
+
+// 256 rows of weights (64 per wave) times 32 * MT rows of x, K in steps of 128: x by LDS copies in two buffers, 16-byte pieces of a row exchanged
+// by its number so that reads of 8 rows meet 8 different places; each lane loads 32 bytes of a row of codes, 64 weights, and
+// the next 32 are on their way.
+// GS: groups in 128 weights (1: groups of whole 128s, 2: of 64s, 4: any multiple of 32).  A product of 16 has to lie
+// within a group: the two lanes of a row exchange dwords for GS > 1.
+template <class T, int MT, int GS, bool ZEROS> __global__ void __launch_bounds__(256, 2) w4_tile_kernel(const W4Args a, const W4Prepared p, int m_tiles, int n_tiles)
+{
+    constexpr int BM = 32 * MT;
+    __shared__ __attribute__((aligned(16))) uint8_t s_x[2][BM * 256];
+    // workgroups are dealt to the 8 XCDs in turn: each XCD has weights of its own, for all rows of x
+    const int xcd = blockIdx.x % 8, local = blockIdx.x / 8;
+    const int tn = xcd + 8 * (local / m_tiles), tm = local % m_tiles;
+    if (tn >= n_tiles) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 31, hh = lane >> 5;
+    const int n0 = tn * 256 + wave * 64, m0 = tm * BM;
+    const int row_bytes = a.K / 2, whole = a.K / 128, steps = (a.K + 127) / 128;
+
+    const uint8_t *const x_tile = reinterpret_cast<const uint8_t *>(p.x + (int64_t)m0 * p.pitch);
+    const int x_bytes = min(a.M - m0, BM) * p.pitch * 2; // rows beyond the last read as zeros
+    auto copy_x = [&](int step, int buf) {
+#pragma unroll
+        for (int i = 0; i < 2 * MT; ++i) {
+            const int row = (wave * 2 * MT + i) * 4 + (lane >> 4);
+            const uint32_t piece = (lane & 15) ^ (row & 15);
+            buffer_to_lds16(x_tile, x_bytes, (uint32_t)row * p.pitch * 2 + step * 256 + piece * 16, &s_x[buf][(wave * 2 * MT + i) * 1024]);
+        }
+    };
+
+    const uint8_t *w_row[2];
+    uint32_t n_at[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        n_at[t] = min(n0 + 32 * t + c, a.N - 1);
+        w_row[t] = a.codes + (int64_t)n_at[t] * row_bytes + 32 * hh;
+    }
+    struct Weights {
+        w32x4 w[2][2];
+        uint16_t s[2][GS];
+        int8_t z[2][GS];
+    };
+    auto load_scales = [&](Weights &f, int step) {
+#pragma unroll
+        for (int q = 0; q < GS; ++q) {
+            const uint32_t group = (uint32_t)group_of(a, min(step * 128 + q * (128 / GS), a.K - 1)) * a.N;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                f.s[t][q] = a.scales[group + n_at[t]];
+                f.z[t][q] = ZEROS ? a.zeros[group + n_at[t]] : 0;
+            }
+        }
+    };
+    auto load = [&](Weights &f, int step) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) f.w[t][i] = load_any<w32x4>(w_row[t] + 64 * step + 16 * i);
+        load_scales(f, step);
+    };
+
+    f32x16 acc[2][MT];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[t][mt][i] = 0.0f;
+    float unit[2] = {0.0f, 0.0f};
+    const uint32_t bits = kept(Nibbles<F16>::kBits);
+
+    auto compute = [&](const Weights &f, int buf) {
+        uint32_t w[2][8];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[t][i] = f.w[t][i >> 2][i & 3];
+            // dwords i and i + 4: the low lanes' two, the high lanes' two
+            if constexpr (GS >= 2)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const auto r = __builtin_amdgcn_permlane32_swap(w[t][i], w[t][i + 4], false, false);
+                    w[t][i] = r[0], w[t][i + 4] = r[1];
+                }
+            if constexpr (GS == 4)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if ((i & 2) == 0) {
+                        const auto r = __builtin_amdgcn_permlane32_swap(w[t][i], w[t][i + 2], false, false);
+                        w[t][i] = r[0], w[t][i + 2] = r[1];
+                    }
+        }
+        const uint8_t *const row = &s_x[buf][c * 256];
+        h16x2 off[2];
+        uint32_t mask[2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (i % (8 / GS) == 0) {
+                const int q = i / (8 / GS);
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const float s = T::widen(f.s[t][q]);
+                    // a scale of 0, or 2^-100 of the last one (whose accumulators could overflow in its unit): left out
+                    const bool none = s == 0.0f || fabsf(s) * 0x1p100f < fabsf(unit[t]);
+                    const float ratio = none ? 1.0f : unit[t] / s;
+                    unit[t] = none ? unit[t] : s;
+                    const _Float16 z = (_Float16)(1032.0f + (none ? 0.0f : (float)f.z[t][q]));
+                    off[t] = h16x2{z, z}, mask[t] = none ? 0u : 0x000f000fu;
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) acc[t][mt] *= ratio;
+                }
+            }
+            // the dword's weights are those of 16-byte piece `piece` of x
+            const int piece = GS == 1 ? 8 * hh + i : GS == 2 ? 8 * (i >> 2) + 4 * hh + (i & 3) : 4 * (i >> 1) + 2 * hh + (i & 1);
+            h16x8 xf[MT];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) xf[mt] = *reinterpret_cast<const h16x8 *>(row + mt * 32 * 256 + (piece ^ (c & 15)) * 16);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                w32x4 wide;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) wide[e] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h16x2, (w[t][i] >> 4 * e & mask[t]) ^ bits) - off[t]);
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) acc[t][mt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(xf[mt], __builtin_bit_cast(h16x8, wide), acc[t][mt], 0, 0, 0);
+            }
+        }
+    };
+
+    Weights f[2];
+    copy_x(0, 0);
+    if (whole > 0) load(f[0], 0);
+    const auto next_buffer = [] { // this wave's copies have arrived, all waves are done with the other buffer
+        wait_vmcnt<0>();
+        block_barrier();
+    };
+    int step = 0;
+    for (; step + 2 < whole; step += 2) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            next_buffer();
+            copy_x(step + half + 1, 1 - half);
+            load(f[1 - half], step + half + 1);
+            compute(f[half], half);
+        }
+    }
+    // up to two whole steps are left, and the part of one
+    for (; step < steps; ++step) {
+        next_buffer();
+        if (step + 1 < steps) copy_x(step + 1, (step + 1) & 1);
+        Weights last;
+        if (step + 1 < whole) load(last, step + 1);
+        if (step >= whole) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) f[0].w[t][i] = load_end(w_row[t] - 32 * hh, row_bytes, 64 * step + 32 * hh + 16 * i);
+            load_scales(f[0], step);
+        }
+        compute(f[0], step & 1);
+        if (step + 1 < whole) f[0] = last;
+    }
+
+    // outputs through LDS, rows of 64 per wave, 16-byte pieces exchanged as above
+    block_barrier();
+    uint8_t *const tile = &s_x[0][0] + wave * (BM * 128);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const float b = a.bias ? T::widen(a.bias[n_at[t]]) : 0.0f;
+        const int n = 32 * t + c;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int m = 32 * mt + 8 * (i >> 2) + 4 * hh + (i & 3);
+                const float v = ldexpf(acc[t][mt][i] * unit[t], p.row_exp[min(m0 + m, a.M - 1)]) + b;
+                *reinterpret_cast<uint16_t *>(tile + m * 128 + ((n >> 3) ^ (m & 7)) * 16 + (n & 7) * 2) = T::narrow(v);
+            }
+    }
+    lds_barrier(); // (between waves nothing is exchanged; the compiler keeps the order of writes and reads)
+#pragma unroll
+    for (int i = 0; i < 4 * MT; ++i) {
+        const int m = i * 8 + (lane >> 3), n = n0 + 8 * (lane & 7);
+        if (m0 + m >= a.M || n >= a.N) continue;
+        const w32x4 v = *reinterpret_cast<const w32x4 *>(tile + m * 128 + ((lane & 7) ^ (m & 7)) * 16);
+        uint16_t *const y = a.y + (int64_t)(m0 + m) * a.ldy + n;
+        if (n + 8 <= a.N) store_any(y, v);
+        else
+            for (int e = 0; e < a.N - n; ++e) y[e] = (uint16_t)(v[e >> 1] >> (e & 1) * 16);
+    }
+}
+
+template <class T, int GS, bool ZEROS> static void launch_tiles(const W4Args &a, const W4Prepared &p, hipStream_t s)
+{
+    constexpr int MT = 4;
+    const int m_tiles = (a.M + 32 * MT - 1) / (32 * MT), n_tiles = (a.N + 255) / 256;
+    hipLaunchKernelGGL((w4_tile_kernel<T, MT, GS, ZEROS>), dim3((unsigned)(((n_tiles + 7) / 8) * 8 * m_tiles)), dim3(256), 0, s, a, p, m_tiles, n_tiles);
+}
+
+template <class T> static void run_tiles(const W4Args &a, void *workspace, hipStream_t s)
+{
+    const W4Prepared p = prepared(workspace, a.M, a.K);
+    hipLaunchKernelGGL(w4_prepare_kernel<T>, dim3((unsigned)a.M), dim3(256), 0, s, a, p);
+    if (a.group % 128 == 0) a.zeros ? launch_tiles<T, 1, true>(a, p, s) : launch_tiles<T, 1, false>(a, p, s);
+    else if (a.group % 64 == 0) a.zeros ? launch_tiles<T, 2, true>(a, p, s) : launch_tiles<T, 2, false>(a, p, s);
+    else a.zeros ? launch_tiles<T, 4, true>(a, p, s) : launch_tiles<T, 4, false>(a, p, s);
+}
+
+void launch_w4_tile(const W4Args &a, int type, void *workspace, hipStream_t s)
+{
+    if (type == QNN_BF16) run_tiles<Bf16>(a, workspace, s);
+    else run_tiles<F16>(a, workspace, s);
+}
+
+} // namespace qnn
