@@ -15,7 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libqnn.so")
 NATIVE = os.path.join(HERE, "_native.so")
 # (the ones that take longest first)
-SOURCES = ["igemm_bres.hip", "igemm_bres4.hip", "kv_attention.hip", "w4_matmul.hip", "w4_tile.hip", "igemm_ring_int8_low.hip", "igemm_ring_int4_low.hip", "igemm.hip", "igemm_shortk.hip", "igemm_shortk4.hip",
+SOURCES = ["igemm_bres.hip", "igemm_bres4.hip", "kv_attention.hip", "w4_matmul.hip", "w4_tile.hip", "w4_parts.hip", "igemm_ring_int8_low.hip", "igemm_ring_int4_low.hip", "igemm.hip", "igemm_shortk.hip", "igemm_shortk4.hip",
            "dwconv.hip", "igemm_ring_int8_high.hip", "igemm_ring_int4_high.hip", "igemm_tiles.hip", "igemm_stem.hip", "igemm_smallk.hip", "igemm_tail.hip",
            "igemm_tile64.hip", "elementwise.hip", "igemm_repack.hip", "kv_cache.hip", "host_helpers.hip", "calibrate.hip"]
 FLAGS = [

@@ -88,8 +88,79 @@ __device__ __forceinline__ w32x4 load_end(const uint8_t *row, int bytes, int at)
     return v;
 }
 
-// the kernel for many rows (w4_tile.hip), and the scratch that it takes
-size_t w4_tile_bytes(int64_t M, int64_t K);
-void launch_w4_tile(const W4Args &a, int type, void *workspace, hipStream_t s);
+// Where a lane (of the two of a row) has loaded 32 consecutive bytes, 64 weights, a product of 16 takes a dword of each.  For it to lie
+// within a group of 64 or 32 the two lanes exchange dwords; piece_of: the 16-byte piece of x that goes with dword i then.
+template <int GS> __device__ __forceinline__ void swap_halves(uint32_t (&w)[8])
+{
+    if constexpr (GS >= 2)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const auto r = __builtin_amdgcn_permlane32_swap(w[i], w[i + 4], false, false);
+            w[i] = r[0], w[i + 4] = r[1];
+        }
+    if constexpr (GS == 4)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if ((i & 2) == 0) {
+                const auto r = __builtin_amdgcn_permlane32_swap(w[i], w[i + 2], false, false);
+                w[i] = r[0], w[i + 2] = r[1];
+            }
+}
+template <int GS> __device__ __forceinline__ int piece_of(int i, int hh)
+{
+    return GS == 1 ? 8 * hh + i : GS == 2 ? 8 * (i >> 2) + 4 * hh + (i & 3) : 4 * (i >> 1) + 2 * hh + (i & 1);
+}
+
+// x as the kernels for tens and for many rows take it: binary16, each row scaled by a power of two to at most 1, which is exact
+// (elements below 2^-17 of their row's largest keep fewer bits), in the order of expand_nibbles, rows padded with zeros to
+// whole 128s
+struct W4Prepared {
+    uint16_t *x;      // binary16 [M][pitch]
+    int32_t *row_exp; // [M]
+    int32_t pitch;
+};
+
+inline W4Prepared prepared(void *workspace, int64_t M, int64_t K)
+{
+    const int64_t pitch = (K + 127) / 128 * 128;
+    W4Prepared p;
+    p.x = static_cast<uint16_t *>(workspace);
+    p.row_exp = reinterpret_cast<int32_t *>(p.x + M * pitch);
+    p.pitch = (int32_t)pitch;
+    return p;
+}
+// scratch of the kernels that take x this way
+inline size_t w4_prepared_bytes(int64_t M, int64_t K) { return (size_t)M * ((K + 127) / 128 * 128) * 2 + 4 * (size_t)M; }
+
+void prepare_x(const W4Args &a, int type, const W4Prepared &p, hipStream_t s);
+// tens of rows (w4_parts.hip), many (w4_tile.hip)
+void launch_w4_parts(const W4Args &a, int type, const W4Prepared &p, hipStream_t s);
+void launch_w4_tile(const W4Args &a, int type, const W4Prepared &p, hipStream_t s);
+
+// The scale of the group that accumulators come to: `ratio` brings them into its unit.  A scale of 0, or of 2^-100 of the last one
+// (in whose unit they could overflow), leaves its weights out: all nibbles masked, and an offset that takes off what is left.
+struct GroupUnit {
+    float ratio;
+    h16x2 off;
+    uint32_t mask;
+};
+__device__ __forceinline__ GroupUnit enter_group(float s, int z, float &unit)
+{
+    const bool none = s == 0.0f || fabsf(s) * 0x1p100f < fabsf(unit);
+    GroupUnit g;
+    g.ratio = none ? 1.0f : unit / s;
+    unit = none ? unit : s;
+    const _Float16 o = (_Float16)(1032.0f + (none ? 0.0f : (float)z));
+    g.off = h16x2{o, o}, g.mask = none ? 0u : 0x000f000fu;
+    return g;
+}
+// eight weights c - z of a dword, in binary16
+__device__ __forceinline__ h16x8 whole_weights(uint32_t w, const GroupUnit &g, uint32_t bits)
+{
+    w32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h16x2, (w >> 4 * e & g.mask) ^ bits) - g.off);
+    return __builtin_bit_cast(h16x8, v);
+}
 
 } // namespace qnn

@@ -200,12 +200,8 @@ template <class T, int GS> static void launch_w4(const W4Args &a, hipStream_t s)
     else if (a.M <= 16) {
         if (a.N > 16384) launch_rows<T, 1, 2, 8, GS>(a, s);
         else launch_rows<T, 1, 1, 16, GS>(a, s);
-    } else if (a.M <= 32) launch_rows<T, 2, 4, 8, GS>(a, s);
-    else launch_rows<T, 4, 2, 8, GS>(a, s);
+    } else launch_rows<T, 2, 2, 4, GS>(a, s);
 }
-
-// From how many rows on the kernel with tiles in LDS is ahead (it takes two launches)
-constexpr int64_t kTileRows = 65;
 
 template <class T> static qnn_status run_w4(const W4Args &a, hipStream_t s)
 {
@@ -226,13 +222,14 @@ static bool bad_w4_sizes(int64_t M, int64_t N, int64_t K, int64_t group)
     return M < 0 || N <= 0 || K <= 0 || K % 2 != 0 || group <= 0 || group % 32 != 0 || M > (1 << 20) || N > (1 << 28) || K > (1 << 24) || (K + group - 1) / group * N >= (1 << 30);
 }
 
-// (longer rows than the tile kernel's offsets reach stay with the kernel for few)
-static bool tiled(int64_t M, int64_t K) { return M >= kTileRows && K <= (1 << 21); }
+// From 17 rows on x goes through LDS, prepared by a launch of its own (longer rows than these kernels' offsets reach, and fewer
+// than four scales, stay with the kernel for few rows)
+static bool prepares_x(int64_t M, int64_t K) { return M > 16 && K <= (1 << 21); }
 
 size_t qnn_w4_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t group)
 {
-    if (bad_w4_sizes(M, N, K, group) || !tiled(M, K)) return 0;
-    return w4_tile_bytes(M, K);
+    if (bad_w4_sizes(M, N, K, group) || !prepares_x(M, K)) return 0;
+    return w4_prepared_bytes(M, K);
 }
 
 qnn_status qnn_w4_matmul(const void *x, int64_t ldx, const uint8_t *codes, const void *scales, const int8_t *zeros, const void *bias, int64_t M,
@@ -246,8 +243,12 @@ qnn_status qnn_w4_matmul(const void *x, int64_t ldx, const uint8_t *codes, const
     W4Args a{static_cast<const uint16_t *>(x), codes, static_cast<const uint16_t *>(scales), zeros, static_cast<const uint16_t *>(bias),
                    static_cast<uint16_t *>(y), ldx, ldy, (int32_t)M, (int32_t)N, (int32_t)K, (int32_t)(group < K ? group : (K + 127) / 128 * 128), (int32_t)((K + group - 1) / group), 0, 0};
     fast_division((uint32_t)a.group / 32, a.group_magic, a.group_shift);
-    if (tiled(M, K)) {
-        launch_w4_tile(a, type, workspace, as_stream(stream));
+    if (prepares_x(M, K)) {
+        const W4Prepared p = prepared(workspace, M, K);
+        prepare_x(a, type, p, as_stream(stream));
+        // tiles of 128 x 256 where there are enough of them for the chip
+        if ((M + 127) / 128 * ((N + 255) / 256) >= 160) launch_w4_tile(a, type, p, as_stream(stream));
+        else launch_w4_parts(a, type, p, as_stream(stream));
         return launch_status(hipGetLastError());
     }
     return type == QNN_BF16 ? run_w4<Bf16>(a, as_stream(stream)) : run_w4<F16>(a, as_stream(stream));

@@ -13,23 +13,6 @@
 
 namespace qnn {
 
-struct W4Prepared {
-    uint16_t *x;      // binary16 [M][pitch]
-    int32_t *row_exp; // [M]
-    int32_t pitch;
-};
-
-static W4Prepared prepared(void *workspace, int64_t M, int64_t K)
-{
-    const int64_t pitch = (K + 127) / 128 * 128;
-    W4Prepared p;
-    p.x = static_cast<uint16_t *>(workspace);
-    p.row_exp = reinterpret_cast<int32_t *>(p.x + M * pitch);
-    p.pitch = (int32_t)pitch;
-    return p;
-}
-size_t w4_tile_bytes(int64_t M, int64_t K) { return (size_t)M * ((K + 127) / 128 * 128) * 2 + 4 * (size_t)M; }
-
 template <class T> __global__ void __launch_bounds__(256) w4_prepare_kernel(const W4Args a, const W4Prepared p)
 {
     const int tid = threadIdx.x;
@@ -133,53 +116,30 @@ template <class T, int MT, int GS, bool ZEROS> __global__ void __launch_bounds__
         for (int t = 0; t < 2; ++t) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[t][i] = f.w[t][i >> 2][i & 3];
-            // dwords i and i + 4: the low lanes' two, the high lanes' two
-            if constexpr (GS >= 2)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const auto r = __builtin_amdgcn_permlane32_swap(w[t][i], w[t][i + 4], false, false);
-                    w[t][i] = r[0], w[t][i + 4] = r[1];
-                }
-            if constexpr (GS == 4)
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if ((i & 2) == 0) {
-                        const auto r = __builtin_amdgcn_permlane32_swap(w[t][i], w[t][i + 2], false, false);
-                        w[t][i] = r[0], w[t][i + 2] = r[1];
-                    }
+            swap_halves<GS>(w[t]);
         }
         const uint8_t *const row = &s_x[buf][c * 256];
-        h16x2 off[2];
-        uint32_t mask[2];
+        GroupUnit unit_of[2];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (i % (8 / GS) == 0) {
                 const int q = i / (8 / GS);
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    const float s = T::widen(f.s[t][q]);
-                    // a scale of 0, or 2^-100 of the last one (whose accumulators could overflow in its unit): left out
-                    const bool none = s == 0.0f || fabsf(s) * 0x1p100f < fabsf(unit[t]);
-                    const float ratio = none ? 1.0f : unit[t] / s;
-                    unit[t] = none ? unit[t] : s;
-                    const _Float16 z = (_Float16)(1032.0f + (none ? 0.0f : (float)f.z[t][q]));
-                    off[t] = h16x2{z, z}, mask[t] = none ? 0u : 0x000f000fu;
+                    unit_of[t] = enter_group(T::widen(f.s[t][q]), f.z[t][q], unit[t]);
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) acc[t][mt] *= ratio;
+                    for (int mt = 0; mt < MT; ++mt) acc[t][mt] *= unit_of[t].ratio;
                 }
             }
-            // the dword's weights are those of 16-byte piece `piece` of x
-            const int piece = GS == 1 ? 8 * hh + i : GS == 2 ? 8 * (i >> 2) + 4 * hh + (i & 3) : 4 * (i >> 1) + 2 * hh + (i & 1);
+            const int piece = piece_of<GS>(i, hh);
             h16x8 xf[MT];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) xf[mt] = *reinterpret_cast<const h16x8 *>(row + mt * 32 * 256 + (piece ^ (c & 15)) * 16);
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                w32x4 wide;
+                const h16x8 wide = whole_weights(w[t][i], unit_of[t], bits);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) wide[e] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h16x2, (w[t][i] >> 4 * e & mask[t]) ^ bits) - off[t]);
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) acc[t][mt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(xf[mt], __builtin_bit_cast(h16x8, wide), acc[t][mt], 0, 0, 0);
+                for (int mt = 0; mt < MT; ++mt) acc[t][mt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(xf[mt], wide, acc[t][mt], 0, 0, 0);
             }
         }
     };
@@ -254,19 +214,23 @@ template <class T, int GS, bool ZEROS> static void launch_tiles(const W4Args &a,
     hipLaunchKernelGGL((w4_tile_kernel<T, MT, GS, ZEROS>), dim3((unsigned)(((n_tiles + 7) / 8) * 8 * m_tiles)), dim3(256), 0, s, a, p, m_tiles, n_tiles);
 }
 
-template <class T> static void run_tiles(const W4Args &a, void *workspace, hipStream_t s)
+template <class T> static void run_tiles(const W4Args &a, const W4Prepared &p, hipStream_t s)
 {
-    const W4Prepared p = prepared(workspace, a.M, a.K);
-    hipLaunchKernelGGL(w4_prepare_kernel<T>, dim3((unsigned)a.M), dim3(256), 0, s, a, p);
     if (a.group % 128 == 0) a.zeros ? launch_tiles<T, 1, true>(a, p, s) : launch_tiles<T, 1, false>(a, p, s);
     else if (a.group % 64 == 0) a.zeros ? launch_tiles<T, 2, true>(a, p, s) : launch_tiles<T, 2, false>(a, p, s);
     else a.zeros ? launch_tiles<T, 4, true>(a, p, s) : launch_tiles<T, 4, false>(a, p, s);
 }
 
-void launch_w4_tile(const W4Args &a, int type, void *workspace, hipStream_t s)
+void prepare_x(const W4Args &a, int type, const W4Prepared &p, hipStream_t s)
 {
-    if (type == QNN_BF16) run_tiles<Bf16>(a, workspace, s);
-    else run_tiles<F16>(a, workspace, s);
+    if (type == QNN_BF16) hipLaunchKernelGGL(w4_prepare_kernel<Bf16>, dim3((unsigned)a.M), dim3(256), 0, s, a, p);
+    else hipLaunchKernelGGL(w4_prepare_kernel<F16>, dim3((unsigned)a.M), dim3(256), 0, s, a, p);
+}
+
+void launch_w4_tile(const W4Args &a, int type, const W4Prepared &p, hipStream_t s)
+{
+    if (type == QNN_BF16) run_tiles<Bf16>(a, p, s);
+    else run_tiles<F16>(a, p, s);
 }
 
 } // namespace qnn
