@@ -16,6 +16,7 @@ using b16x8 = __bf16 __attribute__((ext_vector_type(8)));
 using u16x4 = uint16_t __attribute__((ext_vector_type(4)));
 using w32x2 = uint32_t __attribute__((ext_vector_type(2)));
 using w32x4 = uint32_t __attribute__((ext_vector_type(4)));
+using w32x4_at4 = w32x4 __attribute__((aligned(4)));
 
 // the element types of activations: QNN_BF16 and QNN_F16 of the C interface
 struct Bf16 {

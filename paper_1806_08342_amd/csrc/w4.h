@@ -15,6 +15,7 @@ struct W4Args {
     int64_t ldx, ldy;
     int32_t M, N, K, group, groups;
     uint32_t group_magic, group_shift; // of the division by 32-weight units of a group
+    int32_t skewed;                    // rows of codes do not all begin at a multiple of 4 bytes
 };
 
 __device__ __forceinline__ int group_of(const W4Args &a, int k)
@@ -88,6 +89,47 @@ __device__ __forceinline__ w32x4 load_end(const uint8_t *row, int bytes, int at)
     return v;
 }
 
+// Consecutive dwords of a row of codes.  Where the row does not begin at a multiple of 4 bytes, loads from there take about
+// twice as long (1 x 4100 x 4096 8.3 us, 4104 6.1): the dwords that hold them are loaded instead, one more of them,
+// and shifted into place when they are used.  Every dword that is read holds a byte of the row.
+template <int DWORDS> struct Codes {
+    uint32_t w[DWORDS + 1];
+    // row: where the lane's part of its row begins
+    __device__ __forceinline__ void load(const uint8_t *row, int skewed)
+    {
+        const uint32_t skew = (uint32_t)(uintptr_t)row & 3u;
+        row -= skew;
+#pragma unroll
+        for (int i = 0; i < DWORDS; i += 4) {
+            const w32x4 v = *reinterpret_cast<const w32x4_at4 *>(row + 4 * i);
+            w[i] = v[0], w[i + 1] = v[1], w[i + 2] = v[2], w[i + 3] = v[3];
+        }
+        if (skewed) w[DWORDS] = *reinterpret_cast<const uint32_t *>(row + 4 * DWORDS - (skew == 0 ? 4 : 0));
+    }
+    // (row: any address with the same last two bits)
+    __device__ __forceinline__ void place(const uint8_t *row, int skewed)
+    {
+        if (!skewed) return;
+#pragma unroll
+        for (int i = 0; i < DWORDS; ++i) w[i] = __builtin_amdgcn_alignbyte(w[i + 1], w[i], (uint32_t)(uintptr_t)row);
+    }
+    // where the row ends within them; at: of the lane's part, from the row's beginning
+    __device__ __forceinline__ void load_tail(const uint8_t *row, int bytes, int at, int skewed)
+    {
+#pragma unroll
+        for (int i = 0; i < DWORDS; i += 4) {
+            const w32x4 v = load_end(row, bytes, at + 4 * i);
+            w[i] = v[0], w[i + 1] = v[1], w[i + 2] = v[2], w[i + 3] = v[3];
+        }
+        w[DWORDS] = 0;
+        if (!skewed) return;
+        // as `place` expects them
+        const uint32_t skew = (uint32_t)(uintptr_t)(row + at) & 3u;
+#pragma unroll
+        for (int i = DWORDS; i >= 0; --i) w[i] = (uint32_t)(((uint64_t)w[i] << 32 | (i ? w[i - 1] : 0u)) << 8 * skew >> 32);
+    }
+};
+
 // Where a lane (of the two of a row) has loaded 32 consecutive bytes, 64 weights, a product of 16 takes a dword of each.  For it to lie
 // within a group of 64 or 32 the two lanes exchange dwords; piece_of: the 16-byte piece of x that goes with dword i then.
 template <int GS> __device__ __forceinline__ void swap_halves(uint32_t (&w)[8])
@@ -134,6 +176,7 @@ inline size_t w4_prepared_bytes(int64_t M, int64_t K) { return (size_t)M * ((K +
 
 void prepare_x(const W4Args &a, int type, const W4Prepared &p, hipStream_t s);
 // tens of rows (w4_parts.hip), many (w4_tile.hip)
+float w4_parts_us(int64_t M, int64_t N, int64_t K); // estimated time
 void launch_w4_parts(const W4Args &a, int type, const W4Prepared &p, hipStream_t s);
 void launch_w4_tile(const W4Args &a, int type, const W4Prepared &p, hipStream_t s);
 

@@ -27,7 +27,7 @@ __device__ __forceinline__ w32x4 transpose_groups(w32x4 a)
 // GS: groups in 128 weights as far as the sums are concerned (1: groups of whole 128s, 2: 64, 4: any multiple of 32).
 // TINY: fewer than four scales in all.
 // The codes of a wave's next 128 are in flight while it works on these; x comes from the L2, which all workgroups read it from.  The loop has no branches (rows
-// beyond the ends are the last one again, and dropped at the end); a last part of K below 128 follows it.
+// beyond the ends are the last one again, and dropped at the end); a last part of K below 128 goes before it.
 template <class T, int MT, int NT, int WAVES, int GS, bool ZEROS, bool TINY> __global__ void __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : 2) w4_rows_kernel(const W4Args a)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
@@ -51,7 +51,7 @@ template <class T, int MT, int NT, int WAVES, int GS, bool ZEROS, bool TINY> __g
     // scales as they were loaded: four from (group, n) on or, where that is beyond the array, its last four, which have to be moved
     // down by `drop` when they are used
     struct Step {
-        w32x4 w[NT];
+        Codes<4> w[NT];
         uint64_t s[NT][GS];
         uint32_t z[NT][GS], drop[NT][GS];
     };
@@ -82,14 +82,17 @@ template <class T, int MT, int NT, int WAVES, int GS, bool ZEROS, bool TINY> __g
     };
     auto load = [&](Step &f, int step) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) f.w[nt] = load_any<w32x4>(w_base + (w_row[nt] + (uint32_t)(64 * step + 16 * g)));
+        for (int nt = 0; nt < NT; ++nt) f.w[nt].load(w_base + (w_row[nt] + (uint32_t)(64 * step + 16 * g)), a.skewed);
         load_scales(f, step);
     };
     auto row_at = [&](int step, int j) { return step * 128 + 32 * j + 8 * g; };
-    auto compute = [&](const Step &f, const w32x4 (&x)[MT][4]) {
+    auto compute = [&](Step &f, const w32x4 (&x)[MT][4]) {
         w32x4 w[NT];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) w[nt] = transpose_groups(f.w[nt]);
+        for (int nt = 0; nt < NT; ++nt) {
+            f.w[nt].place(w_base + w_row[nt], a.skewed);
+            w[nt] = transpose_groups(w32x4{f.w[nt].w[0], f.w[nt].w[1], f.w[nt].w[2], f.w[nt].w[3]});
+        }
 #pragma unroll
         for (int q = 0; q < GS; ++q) {
             f32x4 part[MT][NT], sums[MT];
@@ -140,10 +143,20 @@ template <class T, int MT, int NT, int WAVES, int GS, bool ZEROS, bool TINY> __g
     // Each workgroup begins at another place of K: rows lie a power of two apart more often than not, and workgroups that
     // read the same columns of all rows at one time would keep to a part of the memory's channels.
     const int mine = (whole - wave + WAVES - 1) / WAVES;
+    int at = mine > 0 ? (int)(blockIdx.x % (uint32_t)mine) : 0;
+    if (mine > 0) load(f[0], wave + WAVES * at);
+    if (a.K % 128 != 0 && wave == whole % WAVES) { // the last, shorter part, while the first whole one is on its way
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) f[1].w[nt].load_tail(w_base + w_row[nt], row_bytes, 64 * whole + 16 * g, a.skewed);
+        load_scales(f[1], whole);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[mt][j] = load_end(reinterpret_cast<const uint8_t *>(x_row[mt]), 2 * a.K, 2 * row_at(whole, j));
+        compute(f[1], x);
+    }
     if (mine > 0) {
-        int at = (int)(blockIdx.x % (uint32_t)mine);
         const auto next = [&] { at = at + 1 < mine ? at + 1 : 0; };
-        load(f[0], wave + WAVES * at);
         for (int i = 0; i < mine / 2; ++i) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
@@ -157,16 +170,6 @@ template <class T, int MT, int NT, int WAVES, int GS, bool ZEROS, bool TINY> __g
             load_rows(wave + WAVES * at);
             compute(f[0], x);
         }
-    }
-    if (a.K % 128 != 0 && wave == whole % WAVES) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) f[0].w[nt] = load_end(w_base + w_row[nt], row_bytes, 64 * whole + 16 * g);
-        load_scales(f[0], whole);
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[mt][j] = load_end(reinterpret_cast<const uint8_t *>(x_row[mt]), 2 * a.K, 2 * row_at(whole, j));
-        compute(f[0], x);
     }
 
     // outputs [row of x][n], the waves' sums added in their order
@@ -194,13 +197,17 @@ template <class T, int MT, int NT, int WAVES, int GS, bool TINY = false> static 
     else hipLaunchKernelGGL((w4_rows_kernel<T, MT, NT, WAVES, GS, false, TINY>), grid, dim3(64 * WAVES), 0, s, a);
 }
 
+// tiles of 16 rows of weights per wave
+static int few_tiles(int64_t N) { return N > 16384 ? 2 : 1; }
+
 template <class T, int GS> static void launch_w4(const W4Args &a, hipStream_t s)
 {
+    const int64_t columns = ((int64_t)a.N + 15) / 16;
     if ((int64_t)a.groups * a.N < 4) launch_rows<T, 1, 1, 4, GS, true>(a, s); // (no four scales to load at once)
-    else if (a.M <= 16) {
-        if (a.N > 16384) launch_rows<T, 1, 2, 8, GS>(a, s);
-        else launch_rows<T, 1, 1, 16, GS>(a, s);
-    } else launch_rows<T, 2, 2, 4, GS>(a, s);
+    else if (few_tiles(a.N) == 2) launch_rows<T, 1, 2, 8, GS>(a, s);
+    // a workgroup of 16 waves has a CU to itself
+    else if (columns > 256) launch_rows<T, 1, 1, 8, GS>(a, s);
+    else launch_rows<T, 1, 1, 16, GS>(a, s);
 }
 
 template <class T> static qnn_status run_w4(const W4Args &a, hipStream_t s)
@@ -222,13 +229,28 @@ static bool bad_w4_sizes(int64_t M, int64_t N, int64_t K, int64_t group)
     return M < 0 || N <= 0 || K <= 0 || K % 2 != 0 || group <= 0 || group % 32 != 0 || M > (1 << 20) || N > (1 << 28) || K > (1 << 24) || (K + group - 1) / group * N >= (1 << 30);
 }
 
-// From 17 rows on x goes through LDS, prepared by a launch of its own (longer rows than these kernels' offsets reach, and fewer
-// than four scales, stay with the kernel for few rows)
-static bool prepares_x(int64_t M, int64_t K) { return M > 16 && K <= (1 << 21); }
+// Which kernel, by what each is estimated to take (us):
+// few rows: weights at 4 TB/s and x, read again for every 16 or 32 rows of weights, at 9 TB/s from the L2 (measured / estimated at
+// 16 rows: 4096 x 4096 7.8 / 8.3, 12288 x 4096 19.5 / 20, 28672 x 8192 51 / 58);
+// tens: see w4_parts.hip;  many: 2 us for a round of tiles and 128 of K (200 rows x 28672 x 8192 132 / 133, 1000: 444 / 453).
+enum class W4Kernel { Few, Tens, Many };
+static W4Kernel w4_kernel(int64_t M, int64_t N, int64_t K)
+{
+    // (longer rows than the other kernels' offsets reach stay with that for few)
+    if (K > (1 << 21)) return W4Kernel::Few;
+    const float tens = w4_parts_us(M, N, K);
+    if (M <= 16) {
+        const float weights = (float)N * (float)K * 0.5e-6f;
+        return 2.5f + weights * (0.25f + (float)M / (float)(36 * few_tiles(N))) <= tens ? W4Kernel::Few : W4Kernel::Tens;
+    }
+    const int64_t tiles = (M + 127) / 128 * ((N + 255) / 256);
+    const float rounds = tiles <= 256 ? 1.0f : (float)tiles / 256.0f;
+    return 5.0f + rounds * (float)((K + 127) / 128) * 2.0f < tens ? W4Kernel::Many : W4Kernel::Tens;
+}
 
 size_t qnn_w4_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t group)
 {
-    if (bad_w4_sizes(M, N, K, group) || !prepares_x(M, K)) return 0;
+    if (bad_w4_sizes(M, N, K, group) || M == 0 || w4_kernel(M, N, K) == W4Kernel::Few) return 0;
     return w4_prepared_bytes(M, K);
 }
 
@@ -241,13 +263,12 @@ qnn_status qnn_w4_matmul(const void *x, int64_t ldx, const uint8_t *codes, const
     const size_t need = qnn_w4_matmul_workspace_bytes(M, N, K, group);
     if (need > 0 && (!workspace || ((uintptr_t)workspace & 15) != 0 || workspace_bytes < need)) return QNN_EINVAL;
     W4Args a{static_cast<const uint16_t *>(x), codes, static_cast<const uint16_t *>(scales), zeros, static_cast<const uint16_t *>(bias),
-                   static_cast<uint16_t *>(y), ldx, ldy, (int32_t)M, (int32_t)N, (int32_t)K, (int32_t)(group < K ? group : (K + 127) / 128 * 128), (int32_t)((K + group - 1) / group), 0, 0};
+                   static_cast<uint16_t *>(y), ldx, ldy, (int32_t)M, (int32_t)N, (int32_t)K, (int32_t)(group < K ? group : (K + 127) / 128 * 128), (int32_t)((K + group - 1) / group), 0, 0, (((uintptr_t)codes | (uintptr_t)(K / 2)) & 3) != 0};
     fast_division((uint32_t)a.group / 32, a.group_magic, a.group_shift);
-    if (prepares_x(M, K)) {
+    if (const W4Kernel kernel = w4_kernel(M, N, K); kernel != W4Kernel::Few) {
         const W4Prepared p = prepared(workspace, M, K);
         prepare_x(a, type, p, as_stream(stream));
-        // tiles of 128 x 256 where there are enough of them for the chip
-        if ((M + 127) / 128 * ((N + 255) / 256) >= 160) launch_w4_tile(a, type, p, as_stream(stream));
+        if (kernel == W4Kernel::Many) launch_w4_tile(a, type, p, as_stream(stream));
         else launch_w4_parts(a, type, p, as_stream(stream));
         return launch_status(hipGetLastError());
     }

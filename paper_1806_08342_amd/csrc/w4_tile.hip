@@ -13,32 +13,43 @@
 
 namespace qnn {
 
-template <class T> __global__ void __launch_bounds__(256) w4_prepare_kernel(const W4Args a, const W4Prepared p)
+// One row per workgroup; rows of up to 16384 stay in registers between the two passes over them.
+template <class T> __global__ void __launch_bounds__(1024) w4_prepare_kernel(const W4Args a, const W4Prepared p)
 {
     const int tid = threadIdx.x;
-    const uint16_t *const x = a.x + (int64_t)blockIdx.x * a.ldx;
+    const uint8_t *const x = reinterpret_cast<const uint8_t *>(a.x + (int64_t)blockIdx.x * a.ldx);
     uint16_t *const out = p.x + (int64_t)blockIdx.x * p.pitch;
-    __shared__ float s_peak[4];
+    __shared__ float s_peak[16];
+    w32x4 first[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) first[i] = load_end(x, 2 * a.K, 16 * (tid + 1024 * i));
     float peak = 0.0f;
-    for (int k = 8 * tid; k < a.K; k += 8 * 256) {
-        const w32x4 v = load_end(reinterpret_cast<const uint8_t *>(x), 2 * a.K, 2 * k);
+    const auto look = [&](const w32x4 &v) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) peak = fmaxf(peak, fabsf(T::widen((uint16_t)(v[i >> 1] >> (i & 1) * 16))));
-    }
+    };
+    look(first[0]), look(first[1]);
+    for (int k = 8 * (tid + 2048); k < a.K; k += 8 * 1024) look(load_end(x, 2 * a.K, 2 * k));
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) peak = fmaxf(peak, __shfl_xor(peak, d));
     if ((tid & 63) == 0) s_peak[tid >> 6] = peak;
     __syncthreads();
-    const int e = row_exponent(fmaxf(fmaxf(s_peak[0], s_peak[1]), fmaxf(s_peak[2], s_peak[3])));
+    peak = s_peak[tid & 15];
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) peak = fmaxf(peak, __shfl_xor(peak, d));
+    const int e = row_exponent(peak);
     if (tid == 0) p.row_exp[blockIdx.x] = e;
     const float down = ldexpf(1.0f, -e);
-    for (int k = 8 * tid; k < p.pitch; k += 8 * 256) {
-        const w32x4 v = load_end(reinterpret_cast<const uint8_t *>(x), 2 * a.K, 2 * k);
+    const auto write = [&](const w32x4 &v, int k) {
         w32x4 h;
 #pragma unroll
         for (int i = 0; i < 4; ++i) h[i] = narrow2<F16>(T::widen((uint16_t)v[i]) * down, T::widen((uint16_t)(v[i] >> 16)) * down);
         *reinterpret_cast<w32x4 *>(out + k) = pair_order(h);
-    }
+    };
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (8 * (tid + 1024 * i) < p.pitch) write(first[i], 8 * (tid + 1024 * i));
+    for (int k = 8 * (tid + 2048); k < p.pitch; k += 8 * 1024) write(load_end(x, 2 * a.K, 2 * k), k);
 }
 
 // 256 rows of weights (64 per wave) times 32 * MT rows of x, K in steps of 128: x by LDS copies in two buffers, 16-byte pieces of a row exchanged
@@ -77,7 +88,7 @@ template <class T, int MT, int GS, bool ZEROS> __global__ void __launch_bounds__
         w_row[t] = a.codes + (int64_t)n_at[t] * row_bytes + 32 * hh;
     }
     struct Weights {
-        w32x4 w[2][2];
+        Codes<8> w[2];
         uint16_t s[2][GS];
         int8_t z[2][GS];
     };
@@ -94,9 +105,7 @@ template <class T, int MT, int GS, bool ZEROS> __global__ void __launch_bounds__
     };
     auto load = [&](Weights &f, int step) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) f.w[t][i] = load_any<w32x4>(w_row[t] + 64 * step + 16 * i);
+        for (int t = 0; t < 2; ++t) f.w[t].load(w_row[t] + 64 * step, a.skewed);
         load_scales(f, step);
     };
 
@@ -110,12 +119,13 @@ template <class T, int MT, int GS, bool ZEROS> __global__ void __launch_bounds__
     float unit[2] = {0.0f, 0.0f};
     const uint32_t bits = kept(Nibbles<F16>::kBits);
 
-    auto compute = [&](const Weights &f, int buf) {
+    auto compute = [&](Weights &f, int buf) {
         uint32_t w[2][8];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
+            f.w[t].place(w_row[t], a.skewed);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[t][i] = f.w[t][i >> 2][i & 3];
+            for (int i = 0; i < 8; ++i) w[t][i] = f.w[t].w[i];
             swap_halves<GS>(w[t]);
         }
         const uint8_t *const row = &s_x[buf][c * 256];
@@ -169,9 +179,7 @@ template <class T, int MT, int GS, bool ZEROS> __global__ void __launch_bounds__
         if (step + 1 < whole) load(last, step + 1);
         if (step >= whole) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) f[0].w[t][i] = load_end(w_row[t] - 32 * hh, row_bytes, 64 * step + 32 * hh + 16 * i);
+            for (int t = 0; t < 2; ++t) f[0].w[t].load_tail(w_row[t] - 32 * hh, row_bytes, 64 * step + 32 * hh, a.skewed);
             load_scales(f[0], step);
         }
         compute(f[0], step & 1);
@@ -223,8 +231,8 @@ template <class T> static void run_tiles(const W4Args &a, const W4Prepared &p, h
 
 void prepare_x(const W4Args &a, int type, const W4Prepared &p, hipStream_t s)
 {
-    if (type == QNN_BF16) hipLaunchKernelGGL(w4_prepare_kernel<Bf16>, dim3((unsigned)a.M), dim3(256), 0, s, a, p);
-    else hipLaunchKernelGGL(w4_prepare_kernel<F16>, dim3((unsigned)a.M), dim3(256), 0, s, a, p);
+    if (type == QNN_BF16) hipLaunchKernelGGL(w4_prepare_kernel<Bf16>, dim3((unsigned)a.M), dim3(1024), 0, s, a, p);
+    else hipLaunchKernelGGL(w4_prepare_kernel<F16>, dim3((unsigned)a.M), dim3(1024), 0, s, a, p);
 }
 
 void launch_w4_tile(const W4Args &a, int type, const W4Prepared &p, hipStream_t s)
