@@ -52,73 +52,203 @@ __device__ __forceinline__ Piece piece_of_item(const CacheArgs &a, int64_t item)
     return p;
 }
 
-// round(x / scale) of a finite or NaN quotient, as a code
-__device__ __forceinline__ int code_of(float x)
+// x / by, correctly rounded: two steps of r = x - q * by, q + r / by with the reciprocal (exact residuals; the first makes q one of
+// the two neighbours, the second the nearest).  `plain`: by is too small for that.
+__device__ __forceinline__ float quotient(float x, float by, float reciprocal, bool plain)
 {
-    const float r = roundf(x); // ties away from zero
-    return (int)fminf(fmaxf(r, -127.0f), 127.0f); // (NaN: the first comparison gives -127)
+    if (plain) return __fdiv_rn(x, by);
+    float q = x * reciprocal;
+    q = fmaf(fmaf(-q, by, x), reciprocal, q);
+    return fmaf(fmaf(-q, by, x), reciprocal, q);
 }
-
-// One page and head of keys (blockIdx.y even) or values.
-template <class T> __global__ void __launch_bounds__(256) append_kernel(const CacheArgs a)
+// round() with ties away from zero, as a code: 0.5 less its last bit added, then cut off.  NaN gives 0.
+__device__ __forceinline__ int code_of(float q)
 {
-    const int h = blockIdx.y >> 1, tid = threadIdx.x;
-    const bool is_v = blockIdx.y & 1;
-    const Piece p = piece_of_item(a, blockIdx.x);
-    if (p.hi <= p.lo || p.page < 0) return;
-    const int block = a.cache.block, D = a.cache.dim;
-    const int64_t token = is_v ? a.v_token : a.k_token;
-    const uint16_t *x = (is_v ? a.v : a.k) + p.row * token + (int64_t)h * (is_v ? a.v_head : a.k_head);
-    const int64_t slot = p.page * a.cache.heads + h;
-    int8_t *codes = (is_v ? a.cache.v_codes : a.cache.k_codes) + slot * block * D;
-    float *scale = (is_v ? a.cache.v_scales : a.cache.k_scales) + slot;
-    const int count = (p.hi - p.lo) * D;
-
-    float peak = 0.0f;
-    for (int i = tid; i < count; i += 256) {
-        const float v = fabsf(T::widen(x[(int64_t)(i / D) * token + i % D]));
-        peak = v < INFINITY ? fmaxf(peak, v) : peak;
-    }
-    __shared__ float s_peak[4];
+    const float c = __builtin_amdgcn_fmed3f(q, -127.0f, 127.0f); // (infinities: the ends)
+    return (int)(c + copysignf(0.49999997f, c));
+}
+__device__ __forceinline__ uint32_t four_codes(int a, int b, int c, int d)
+{
+    const uint32_t lo = __builtin_amdgcn_perm((uint32_t)b, (uint32_t)a, 0x0c0c0400u), hi = __builtin_amdgcn_perm((uint32_t)d, (uint32_t)c, 0x04000c0cu);
+    return lo | hi;
+}
+// the codes of a dword in another scale
+__device__ __forceinline__ uint32_t rescaled(uint32_t w, float ratio)
+{
+    int c[4];
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) peak = fmaxf(peak, __shfl_xor(peak, d));
-    if ((tid & 63) == 0) s_peak[tid >> 6] = peak;
-    __syncthreads();
-    peak = fmaxf(fmaxf(s_peak[0], s_peak[1]), fmaxf(s_peak[2], s_peak[3]));
-    const float before = p.lo > 0 ? *scale : 0.0f;
-    const float after = fmaxf(before, __fdiv_rn(peak, 127.0f)), by = after > 0.0f ? after : 1.0f;
-    __syncthreads(); // the scale is read by all before one writes it
-    if (tid == 0) *scale = after;
-    if (after > before && p.lo > 0) { // what is held, in the new scale
-        const float ratio = __fdiv_rn(before, by);
-        for (int i = tid; i < p.lo * D; i += 256) {
-            int8_t *c = is_v ? codes + (i / p.lo) * block + i % p.lo : codes + i;
-            *c = (int8_t)code_of((float)*c * ratio);
-        }
-    }
-    for (int i = tid; i < count; i += 256) {
-        const int t = i / D, d = i % D;
-        const float v = T::widen(x[(int64_t)t * token + d]);
-        const int c = v == v ? code_of(__fdiv_rn(v, by)) : 0;
-        codes[is_v ? d * block + p.lo + t : (p.lo + t) * D + d] = (int8_t)c;
-    }
+    for (int i = 0; i < 4; ++i) c[i] = code_of((float)(int8_t)(w >> 8 * i) * ratio);
+    return four_codes(c[0], c[1], c[2], c[3]);
 }
 
-template <class T> __global__ void __launch_bounds__(256) gather_kernel(const CacheArgs a)
+// Each wave takes keys or values of one head in one page, by itself: blockIdx.y * 4 + wave counts heads and, in its lowest bit, values.
+// Elements are loaded 8 at a time and stay in registers between the largest and the codes where they fit (64 x 128 do).
+// Keys: piece i is row i / (D / 8), channels 8 * (i % (D / 8)).  Values, which are stored with consecutive tokens of a channel
+// together: unit i is 4 tokens (aligned in the page) by 8 channels, turned in registers.
+constexpr int kHeld = 16; // pieces of 8 per lane
+
+template <class T, int D> __global__ void __launch_bounds__(256) append_kernel(const CacheArgs a)
 {
-    const int h = blockIdx.y >> 1, tid = threadIdx.x;
-    const bool is_v = blockIdx.y & 1;
+    constexpr int DG = D / 8;
+    const int lane = threadIdx.x & 63, hk = blockIdx.y * 4 + (threadIdx.x >> 6), h = hk >> 1;
+    const bool is_v = hk & 1;
+    if (h >= a.cache.heads) return;
     const Piece p = piece_of_item(a, blockIdx.x);
     if (p.hi <= p.lo) return;
-    const int block = a.cache.block, D = a.cache.dim, heads = a.cache.heads;
-    uint16_t *out = (is_v ? a.v_out : a.k_out) + (p.row * heads + h) * D;
-    const int64_t slot = p.page * heads + h;
-    const float scale = p.page < 0 ? 0.0f : (is_v ? a.cache.v_scales : a.cache.k_scales)[slot];
-    const int8_t *codes = (is_v ? a.cache.v_codes : a.cache.k_codes) + slot * block * D;
-    for (int i = tid; i < (p.hi - p.lo) * D; i += 256) {
-        const int t = i / D, d = i % D;
-        const float v = p.page < 0 ? 0.0f : (float)codes[is_v ? d * block + p.lo + t : (p.lo + t) * D + d] * scale;
-        out[(int64_t)t * heads * D + d] = T::narrow(v);
+    const int block = a.cache.block;
+    const int64_t token = is_v ? a.v_token : a.k_token;
+    const uint16_t *const x = (is_v ? a.v : a.k) + p.row * token + (int64_t)h * (is_v ? a.v_head : a.k_head);
+    const int groups0 = p.lo >> 2, groups = ((p.hi + 3) >> 2) - groups0; // of 4 tokens
+    const int n = is_v ? groups * DG * 4 : (p.hi - p.lo) * DG, batches = (n + 64 * kHeld - 1) / (64 * kHeld);
+
+    w32x4 held[kHeld];
+    // piece k of a lane's 16 in a batch: keys by 64, values four of one unit after the other
+    const auto load = [&](int batch) {
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) {
+            const int i = is_v ? (batch * (kHeld / 4) + k / 4) * 64 + lane : (batch * kHeld + k) * 64 + lane;
+            const int t = is_v ? (groups0 + i % groups) * 4 + k % 4 - p.lo : i / DG, d = is_v ? i / groups : i % DG;
+            held[k] = w32x4{0u, 0u, 0u, 0u};
+            if (is_v ? d < DG && t >= 0 && t < p.hi - p.lo : i < n) held[k] = load_any<w32x4>(x + t * token + d * 8);
+        }
+    };
+    float peak = 0.0f;
+    for (int batch = 0; batch < batches; ++batch) {
+        load(batch);
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float v = fabsf(T::widen((uint16_t)(held[k][e >> 1] >> (e & 1) * 16)));
+                peak = v < INFINITY ? fmaxf(peak, v) : peak;
+            }
+    }
+    if (p.page < 0) return;
+    const int64_t slot = p.page * a.cache.heads + h;
+    int8_t *const codes = (is_v ? a.cache.v_codes : a.cache.k_codes) + slot * block * D;
+    float *const scale = (is_v ? a.cache.v_scales : a.cache.k_scales) + slot;
+    const float before = p.lo > 0 ? *scale : 0.0f;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) peak = fmaxf(peak, __shfl_xor(peak, d));
+    const float after = fmaxf(before, __fdiv_rn(peak, 127.0f)), by = after > 0.0f ? after : 1.0f;
+    if (lane == 0) *scale = after;
+    if (after > before && p.lo > 0) { // what is held, in the new scale
+        const float ratio = __fdiv_rn(before, by);
+        if (!is_v) {
+            uint32_t *const w = reinterpret_cast<uint32_t *>(codes);
+            for (int i = lane; i < p.lo * (D / 4); i += 64) w[i] = rescaled(w[i], ratio);
+        } else {
+            for (int i = lane; i < groups0 * D; i += 64) {
+                uint32_t *const w = reinterpret_cast<uint32_t *>(codes + (i / groups0) * block) + i % groups0;
+                *w = rescaled(*w, ratio);
+            }
+            const int rest = p.lo & 3; // of a group that new tokens share
+            for (int i = lane; i < rest * D; i += 64) {
+                int8_t *const c = codes + (i / rest) * block + 4 * groups0 + i % rest;
+                *c = (int8_t)code_of((float)*c * ratio);
+            }
+        }
+    }
+    const float reciprocal = __fdiv_rn(1.0f, by);
+    const bool plain = !(by > 0x1p-100f && by < 0x1p100f);
+    for (int batch = 0; batch < batches; ++batch) {
+        if (batches > 1) load(batch);
+#pragma unroll
+        for (int k = 0; k < kHeld; k += 4) {
+            int c[4][8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float v = T::widen((uint16_t)(held[k + j][e >> 1] >> (e & 1) * 16));
+                    c[j][e] = v == v ? code_of(quotient(v, by, reciprocal, plain)) : 0;
+                }
+            if (!is_v) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int i = (batch * kHeld + k + j) * 64 + lane;
+                    if (i < n)
+                        *reinterpret_cast<w32x2 *>(codes + (int64_t)p.lo * D + i * 8) =
+                            w32x2{four_codes(c[j][0], c[j][1], c[j][2], c[j][3]), four_codes(c[j][4], c[j][5], c[j][6], c[j][7])};
+                }
+            } else {
+                const int i = (batch * (kHeld / 4) + k / 4) * 64 + lane, t = (groups0 + i % groups) * 4, d = i / groups;
+                if (d >= DG) continue;
+                int8_t *const to = codes + d * 8 * block + t;
+                if (t >= p.lo && t + 4 <= p.hi) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) *reinterpret_cast<uint32_t *>(to + e * block) = four_codes(c[0][e], c[1][e], c[2][e], c[3][e]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (t + j >= p.lo && t + j < p.hi)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) to[e * block + j] = (int8_t)c[j][e];
+                }
+            }
+        }
+    }
+}
+
+template <class T, int D> __global__ void __launch_bounds__(256) gather_kernel(const CacheArgs a)
+{
+    constexpr int DG = D / 8;
+    const int lane = threadIdx.x & 63, hk = blockIdx.y * 4 + (threadIdx.x >> 6), h = hk >> 1;
+    const bool is_v = hk & 1;
+    const int heads = a.cache.heads;
+    if (h >= heads) return;
+    const Piece p = piece_of_item(a, blockIdx.x);
+    if (p.hi <= p.lo) return;
+    const int block = a.cache.block;
+    uint16_t *const out = (is_v ? a.v_out : a.k_out) + (p.row * heads + h) * D;
+    const bool none = p.page < 0; // zeros
+    const int64_t slot = (none ? 0 : p.page) * heads + h;
+    const float scale = none ? 0.0f : (is_v ? a.cache.v_scales : a.cache.k_scales)[slot];
+    const int8_t *const codes = (is_v ? a.cache.v_codes : a.cache.k_codes) + slot * block * D;
+    const auto value = [&](uint32_t w, int i) { return none ? 0.0f : (float)(int8_t)(w >> 8 * i) * scale; };
+    if (!is_v) {
+        const int n = (p.hi - p.lo) * DG;
+#pragma unroll 4
+        for (int i = lane; i < n; i += 64) {
+            const w32x2 c = none ? w32x2{0u, 0u} : *reinterpret_cast<const w32x2 *>(codes + (int64_t)p.lo * D + i * 8);
+            w32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = narrow2<T>(value(c[e >> 1], 2 * (e & 1)), value(c[e >> 1], 2 * (e & 1) + 1));
+            *reinterpret_cast<w32x4 *>(out + (int64_t)(i / DG) * heads * D + i % DG * 8) = v;
+        }
+    } else {
+        const int groups0 = p.lo >> 2, groups = ((p.hi + 3) >> 2) - groups0;
+#pragma unroll 2
+        for (int i = lane; i < groups * DG; i += 64) {
+            const int t = (groups0 + i % groups) * 4, d = i / groups;
+            uint32_t c[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) c[e] = none ? 0u : *reinterpret_cast<const uint32_t *>(codes + (d * 8 + e) * block + t);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (t + j < p.lo || t + j >= p.hi) continue;
+                w32x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = narrow2<T>(value(c[2 * e], j), value(c[2 * e + 1], j));
+                *reinterpret_cast<w32x4 *>(out + (int64_t)(t + j - p.lo) * heads * D + d * 8) = v;
+            }
+        }
+    }
+}
+
+template <class T, bool GATHER> static void launch_pieces(const CacheArgs &a, hipStream_t s)
+{
+    const dim3 grid((unsigned)(a.tokens / a.cache.block + 2 * (int64_t)a.requests), (unsigned)((2 * a.cache.heads + 3) / 4));
+    const auto with = [&](auto dim) {
+        if constexpr (GATHER) hipLaunchKernelGGL((gather_kernel<T, dim>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((append_kernel<T, dim>), grid, dim3(256), 0, s, a);
+    };
+    switch (a.cache.dim) {
+    case 64: with(std::integral_constant<int, 64>{}); break;
+    case 96: with(std::integral_constant<int, 96>{}); break;
+    case 128: with(std::integral_constant<int, 128>{}); break;
+    case 192: with(std::integral_constant<int, 192>{}); break;
+    default: with(std::integral_constant<int, 256>{}); break;
     }
 }
 
@@ -127,11 +257,6 @@ static bool bad_cache_call(const qnn_kv_cache *cache, int64_t table_width, int64
     return bad_cache(cache) || bad_half_type(type) || table_width < 0 || table_width > INT32_MAX / cache->block || requests < 0 || requests > (1 << 20) ||
            tokens < 0 || tokens > INT32_MAX / 2;
 }
-static dim3 piece_grid(const CacheArgs &a)
-{
-    return dim3((unsigned)(a.tokens / a.cache.block + 2 * (int64_t)a.requests), 2u * (unsigned)a.cache.heads);
-}
-
 } // namespace qnn
 
 using namespace qnn;
@@ -147,8 +272,8 @@ qnn_status qnn_kv_append(const qnn_kv_cache *cache, const void *k, int64_t k_tok
     if (!k || !v || !cu || !start || (table_width > 0 && !table) || bad_cache_arrays(cache)) return QNN_EINVAL;
     const CacheArgs a{*cache, static_cast<const uint16_t *>(k), static_cast<const uint16_t *>(v), k_token_pitch, k_head_pitch, v_token_pitch,
                       v_head_pitch, nullptr, nullptr, cu, start, table, table_width, tokens, (int32_t)requests};
-    if (type == QNN_BF16) hipLaunchKernelGGL(append_kernel<Bf16>, piece_grid(a), dim3(256), 0, as_stream(stream), a);
-    else hipLaunchKernelGGL(append_kernel<F16>, piece_grid(a), dim3(256), 0, as_stream(stream), a);
+    if (type == QNN_BF16) launch_pieces<Bf16, false>(a, as_stream(stream));
+    else launch_pieces<F16, false>(a, as_stream(stream));
     return launch_status(hipGetLastError());
 }
 
@@ -160,8 +285,8 @@ qnn_status qnn_kv_gather(const qnn_kv_cache *cache, const int32_t *cu, const int
     if (!k || !v || !cu || !first || (table_width > 0 && !table) || bad_cache_arrays(cache)) return QNN_EINVAL;
     const CacheArgs a{*cache, nullptr, nullptr, 0, 0, 0, 0, static_cast<uint16_t *>(k), static_cast<uint16_t *>(v), cu, first, table, table_width,
                       tokens, (int32_t)requests};
-    if (type == QNN_BF16) hipLaunchKernelGGL(gather_kernel<Bf16>, piece_grid(a), dim3(256), 0, as_stream(stream), a);
-    else hipLaunchKernelGGL(gather_kernel<F16>, piece_grid(a), dim3(256), 0, as_stream(stream), a);
+    if (type == QNN_BF16) launch_pieces<Bf16, true>(a, as_stream(stream));
+    else launch_pieces<F16, true>(a, as_stream(stream));
     return launch_status(hipGetLastError());
 }
 

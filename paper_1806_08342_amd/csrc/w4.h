@@ -158,7 +158,7 @@ template <int GS> __device__ __forceinline__ int piece_of(int i, int hh)
 // whole 128s
 struct W4Prepared {
     uint16_t *x;      // binary16 [M][pitch]
-    int32_t *row_exp; // [M]
+    int32_t *row_exp; // [M], with room for whole tiles
     int32_t pitch;
 };
 
@@ -172,7 +172,7 @@ inline W4Prepared prepared(void *workspace, int64_t M, int64_t K)
     return p;
 }
 // scratch of the kernels that take x this way
-inline size_t w4_prepared_bytes(int64_t M, int64_t K) { return (size_t)M * ((K + 127) / 128 * 128) * 2 + 4 * (size_t)M; }
+inline size_t w4_prepared_bytes(int64_t M, int64_t K) { return (size_t)M * ((K + 127) / 128 * 128) * 2 + 4 * (size_t)((M + 127) / 128 * 128); }
 
 void prepare_x(const W4Args &a, int type, const W4Prepared &p, hipStream_t s);
 // tens of rows (w4_parts.hip), many (w4_tile.hip)

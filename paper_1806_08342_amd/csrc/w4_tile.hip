@@ -189,19 +189,24 @@ template <class T, int MT, int GS, bool ZEROS> __global__ void __launch_bounds__
     // outputs through LDS, rows of 64 per wave, 16-byte pieces exchanged as above
     block_barrier();
     uint8_t *const tile = &s_x[0][0] + wave * (BM * 128);
+    float bias[2];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        const float b = a.bias ? T::widen(a.bias[n_at[t]]) : 0.0f;
-        const int n = 32 * t + c;
+    for (int t = 0; t < 2; ++t) bias[t] = a.bias ? T::widen(a.bias[n_at[t]]) : 0.0f;
+    using i32x4 = int32_t __attribute__((ext_vector_type(4)));
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int m = 32 * mt + 8 * (i >> 2) + 4 * hh + (i & 3);
-                const float v = ldexpf(acc[t][mt][i] * unit[t], p.row_exp[min(m0 + m, a.M - 1)]) + b;
-                *reinterpret_cast<uint16_t *>(tile + m * 128 + ((n >> 3) ^ (m & 7)) * 16 + (n & 7) * 2) = T::narrow(v);
-            }
-    }
+        for (int i = 0; i < 16; i += 4) {
+            const int m = 32 * mt + 2 * i + 4 * hh;
+            const i32x4 exp = *reinterpret_cast<const i32x4 *>(p.row_exp + m0 + m);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float v = ldexpf(acc[t][mt][i + e] * unit[t], exp[e]) + bias[t];
+                    *reinterpret_cast<uint16_t *>(tile + (m + e) * 128 + ((4 * t + (c >> 3)) ^ ((m + e) & 7)) * 16 + (c & 7) * 2) = T::narrow(v);
+                }
+        }
     lds_barrier(); // (between waves nothing is exchanged; the compiler keeps the order of writes and reads)
 #pragma unroll
     for (int i = 0; i < 4 * MT; ++i) {
