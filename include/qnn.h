@@ -377,8 +377,8 @@ qnn_status qnn_kv_append(const qnn_kv_cache *cache, const void *k, int64_t k_tok
                          const int32_t *table, int64_t table_width, int64_t requests, int64_t tokens, void *stream);
 
 /* Reads tokens back: row cu[r] + i of k and v = code * scale of token first[r] + i of request r, rounded to `type`.
- * k, v: DEVICE [tokens][heads][dim] contiguous (written: a token without a page gives 0, rows that no request has stay as they
- * are).  cu, first, table as above. */
+ * k, v: DEVICE [tokens][heads][dim] contiguous, 16-byte aligned (written: a token without a page gives 0, rows that no request
+ * has stay as they are).  cu, first, table as above. */
 qnn_status qnn_kv_gather(const qnn_kv_cache *cache, const int32_t *cu, const int32_t *first, const int32_t *table,
                          int64_t table_width, int64_t requests, int64_t tokens, int type, void *k, void *v, void *stream);
 

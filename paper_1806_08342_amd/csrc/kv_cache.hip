@@ -103,9 +103,11 @@ template <class T, int D> __global__ void __launch_bounds__(256) append_kernel(c
 
     w32x4 held[kHeld];
     // piece k of a lane's 16 in a batch: keys by 64, values four of one unit after the other
+    const auto past = [&](int batch, int k) { return is_v ? (batch * (kHeld / 4) + k / 4) * 64 >= groups * DG : (batch * kHeld + k) * 64 >= n; };
     const auto load = [&](int batch) {
 #pragma unroll
         for (int k = 0; k < kHeld; ++k) {
+            if (past(batch, k)) break;
             const int i = is_v ? (batch * (kHeld / 4) + k / 4) * 64 + lane : (batch * kHeld + k) * 64 + lane;
             const int t = is_v ? (groups0 + i % groups) * 4 + k % 4 - p.lo : i / DG, d = is_v ? i / groups : i % DG;
             held[k] = w32x4{0u, 0u, 0u, 0u};
@@ -116,12 +118,14 @@ template <class T, int D> __global__ void __launch_bounds__(256) append_kernel(c
     for (int batch = 0; batch < batches; ++batch) {
         load(batch);
 #pragma unroll
-        for (int k = 0; k < kHeld; ++k)
+        for (int k = 0; k < kHeld; ++k) {
+            if (past(batch, k)) break;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float v = fabsf(T::widen((uint16_t)(held[k][e >> 1] >> (e & 1) * 16)));
                 peak = v < INFINITY ? fmaxf(peak, v) : peak;
             }
+        }
     }
     if (p.page < 0) return;
     const int64_t slot = p.page * a.cache.heads + h;
@@ -155,17 +159,21 @@ template <class T, int D> __global__ void __launch_bounds__(256) append_kernel(c
         if (batches > 1) load(batch);
 #pragma unroll
         for (int k = 0; k < kHeld; k += 4) {
+            if (past(batch, k)) break;
             int c[4][8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < 4; ++j) {
+                if (!is_v && past(batch, k + j)) break;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float v = T::widen((uint16_t)(held[k + j][e >> 1] >> (e & 1) * 16));
                     c[j][e] = v == v ? code_of(quotient(v, by, reciprocal, plain)) : 0;
                 }
+            }
             if (!is_v) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
+                    if (past(batch, k + j)) break;
                     const int i = (batch * kHeld + k + j) * 64 + lane;
                     if (i < n)
                         *reinterpret_cast<w32x2 *>(codes + (int64_t)p.lo * D + i * 8) =
@@ -190,13 +198,13 @@ template <class T, int D> __global__ void __launch_bounds__(256) append_kernel(c
     }
 }
 
+// Each workgroup: keys or values (blockIdx.y odd) of one head in one page; 8 codes, or 4 tokens by 8 channels, per lane and step.
 template <class T, int D> __global__ void __launch_bounds__(256) gather_kernel(const CacheArgs a)
 {
     constexpr int DG = D / 8;
-    const int lane = threadIdx.x & 63, hk = blockIdx.y * 4 + (threadIdx.x >> 6), h = hk >> 1;
-    const bool is_v = hk & 1;
+    const int tid = threadIdx.x, h = blockIdx.y >> 1;
+    const bool is_v = blockIdx.y & 1;
     const int heads = a.cache.heads;
-    if (h >= heads) return;
     const Piece p = piece_of_item(a, blockIdx.x);
     if (p.hi <= p.lo) return;
     const int block = a.cache.block;
@@ -209,7 +217,7 @@ template <class T, int D> __global__ void __launch_bounds__(256) gather_kernel(c
     if (!is_v) {
         const int n = (p.hi - p.lo) * DG;
 #pragma unroll 4
-        for (int i = lane; i < n; i += 64) {
+        for (int i = tid; i < n; i += 256) {
             const w32x2 c = none ? w32x2{0u, 0u} : *reinterpret_cast<const w32x2 *>(codes + (int64_t)p.lo * D + i * 8);
             w32x4 v;
 #pragma unroll
@@ -218,8 +226,7 @@ template <class T, int D> __global__ void __launch_bounds__(256) gather_kernel(c
         }
     } else {
         const int groups0 = p.lo >> 2, groups = ((p.hi + 3) >> 2) - groups0;
-#pragma unroll 2
-        for (int i = lane; i < groups * DG; i += 64) {
+        for (int i = tid; i < groups * DG; i += 256) {
             const int t = (groups0 + i % groups) * 4, d = i / groups;
             uint32_t c[8];
 #pragma unroll
@@ -238,7 +245,7 @@ template <class T, int D> __global__ void __launch_bounds__(256) gather_kernel(c
 
 template <class T, bool GATHER> static void launch_pieces(const CacheArgs &a, hipStream_t s)
 {
-    const dim3 grid((unsigned)(a.tokens / a.cache.block + 2 * (int64_t)a.requests), (unsigned)((2 * a.cache.heads + 3) / 4));
+    const dim3 grid((unsigned)(a.tokens / a.cache.block + 2 * (int64_t)a.requests), (unsigned)(GATHER ? 2 * a.cache.heads : (2 * a.cache.heads + 3) / 4));
     const auto with = [&](auto dim) {
         if constexpr (GATHER) hipLaunchKernelGGL((gather_kernel<T, dim>), grid, dim3(256), 0, s, a);
         else hipLaunchKernelGGL((append_kernel<T, dim>), grid, dim3(256), 0, s, a);
@@ -282,7 +289,7 @@ qnn_status qnn_kv_gather(const qnn_kv_cache *cache, const int32_t *cu, const int
 {
     if (bad_cache_call(cache, table_width, requests, tokens, type)) return QNN_EINVAL;
     if (requests == 0 || tokens == 0) return QNN_OK;
-    if (!k || !v || !cu || !first || (table_width > 0 && !table) || bad_cache_arrays(cache)) return QNN_EINVAL;
+    if (!k || !v || !cu || !first || (table_width > 0 && !table) || bad_cache_arrays(cache) || (((uintptr_t)k | (uintptr_t)v) & 15) != 0) return QNN_EINVAL;
     const CacheArgs a{*cache, nullptr, nullptr, 0, 0, 0, 0, static_cast<uint16_t *>(k), static_cast<uint16_t *>(v), cu, first, table, table_width,
                       tokens, (int32_t)requests};
     if (type == QNN_BF16) launch_pieces<Bf16, true>(a, as_stream(stream));
