@@ -49,9 +49,11 @@ struct Request {
 template <int U> __device__ __forceinline__ Request request_of(const AttendArgs &a, int r)
 {
     Request q;
-    const int64_t c0 = min(max((int64_t)a.cu[r], (int64_t)0), a.tokens), c1 = min(max((int64_t)a.cu[r + 1], c0), a.tokens);
+    // (the same in all lanes: kept in scalar registers)
+    const int32_t cu0 = __builtin_amdgcn_readfirstlane(a.cu[r]), cu1 = __builtin_amdgcn_readfirstlane(a.cu[r + 1]);
+    const int64_t c0 = min(max((int64_t)cu0, (int64_t)0), a.tokens), c1 = min(max((int64_t)cu1, c0), a.tokens);
     q.row0 = c0, q.n = (int32_t)(c1 - c0);
-    q.length = min(max((int64_t)a.lengths[r], (int64_t)0), a.table_width * a.cache.block);
+    q.length = min(max((int64_t)__builtin_amdgcn_readfirstlane(a.lengths[r]), (int64_t)0), a.table_width * a.cache.block);
     int64_t low = a.window > 0 ? q.length - q.n + 1 - a.window : 0;
     low = max(low, (int64_t)0) / U * U;
     q.low = min(low, q.length / U * U), q.high = a.cache.pages > 0 ? q.length : q.low;

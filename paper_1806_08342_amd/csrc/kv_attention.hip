@@ -24,7 +24,7 @@ template <class T, int D, int U, int NT> __global__ void __launch_bounds__(256, 
     constexpr int J = D / 64, TAIL = D % 64 != 0; // key pieces of 64 channels (16 bytes a lane), and one of 32
     constexpr int S = U / 16, VW = U / 16;        // score tiles; dwords of a value row that a lane takes
     constexpr int VT = D / 16;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
     const int h = blockIdx.y;
     const int chunk = blockIdx.x % a.chunks, rb = blockIdx.x / a.chunks % a.row_blocks, r = blockIdx.x / a.chunks / a.row_blocks;
     const Request rq = request_of<U>(a, r);
@@ -285,18 +285,20 @@ template <class T, int D, int U, int NT> __global__ void __launch_bounds__(256, 
     }
 }
 
-// Joins the chunks of a row: one workgroup per row, its four waves take chunks in turn.
-template <class T, int D, int U> __global__ void __launch_bounds__(256) attend_join_kernel(const AttendArgs a, int rows_per_block)
+// Joins the chunks of a row.  SHARED: one workgroup per row, whose four waves take chunks in turn (few rows of many chunks); else a
+// wave per row.
+template <class T, int D, int U, bool SHARED> __global__ void __launch_bounds__(256) attend_join_kernel(const AttendArgs a, int rows_at_once)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = blockIdx.y;
-    const int sub = blockIdx.x % rows_per_block, r = blockIdx.x / rows_per_block;
+    const int groups = SHARED ? rows_at_once : (rows_at_once + 3) / 4; // workgroups per request
+    const int sub = SHARED ? blockIdx.x % groups : (blockIdx.x % groups) * 4 + wave, r = blockIdx.x / groups;
     const Request rq = request_of<U>(a, r);
     const int rows = rq.n * a.group;
     if (rows <= a.rows_over || rows > a.rows_upto) return;
     const int chunks = chunks_of(a, rq);
     if (chunks == 1) return;
-    __shared__ float s_l[4], s_o[4][D];
-    for (int row = sub; row < rows; row += rows_per_block) {
+    __shared__ float s_l[4], s_o[4][SHARED ? D : 1];
+    for (int row = sub; row < rows; row += SHARED ? groups : 4 * groups) {
         const int64_t id = (rq.row0 + row / a.group) * a.q_heads + h * a.group + row % a.group;
         const int64_t part = part_row(a, r, h, row) * a.chunks;
         const float *ml = a.part_ml + part * 2, *po = a.part_o + part * D;
@@ -306,26 +308,33 @@ template <class T, int D, int U> __global__ void __launch_bounds__(256) attend_j
         for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
         float o[(D + 63) / 64] = {}, l = 0.0f;
 #pragma unroll 4
-        for (int i = wave; i < chunks; i += 4) {
+        for (int i = SHARED ? wave : 0; i < chunks; i += SHARED ? 4 : 1) {
             const float w = exp2_fast(ml[2 * i] - top);
             l += w * ml[2 * i + 1];
 #pragma unroll
             for (int d = 0; d < (D + 63) / 64; ++d)
                 if (D % 64 == 0 || d * 64 + lane < D) o[d] = fmaf(w, po[(int64_t)i * D + d * 64 + lane], o[d]);
         }
-        if (lane == 0) s_l[wave] = l;
+        if (SHARED) {
+            if (lane == 0) s_l[wave] = l;
 #pragma unroll
-        for (int d = 0; d < (D + 63) / 64; ++d)
-            if (D % 64 == 0 || d * 64 + lane < D) s_o[wave][d * 64 + lane] = o[d];
-        __syncthreads();
-        l = (s_l[0] + s_l[1]) + (s_l[2] + s_l[3]);
-        const int d = threadIdx.x;
-        if (d < D) {
-            const float x = (s_o[0][d] + s_o[1][d]) + (s_o[2][d] + s_o[3][d]);
-            a.out[id * D + d] = T::narrow(l != 0.0f ? x / l : 0.0f);
+            for (int d = 0; d < (D + 63) / 64; ++d)
+                if (D % 64 == 0 || d * 64 + lane < D) s_o[wave][d * 64 + lane] = o[d];
+            __syncthreads();
+            l = (s_l[0] + s_l[1]) + (s_l[2] + s_l[3]);
+            const int d = threadIdx.x;
+            if (d < D) {
+                const float x = (s_o[0][d] + s_o[1][d]) + (s_o[2][d] + s_o[3][d]);
+                a.out[id * D + d] = T::narrow(l != 0.0f ? x / l : 0.0f);
+            }
+        } else {
+            const float inv = l != 0.0f ? 1.0f / l : 0.0f;
+#pragma unroll
+            for (int d = 0; d < (D + 63) / 64; ++d)
+                if (D % 64 == 0 || d * 64 + lane < D) a.out[id * D + d * 64 + lane] = T::narrow(o[d] * inv);
         }
-        if (a.lse && threadIdx.x == 0) a.lse[id] = l != 0.0f ? (top - kHead + log2f(l)) * 0.69314718056f : -INFINITY;
-        __syncthreads();
+        if (a.lse && (SHARED ? threadIdx.x == 0 : lane == 0)) a.lse[id] = l != 0.0f ? (top - kHead + log2f(l)) * 0.69314718056f : -INFINITY;
+        if (SHARED) __syncthreads();
     }
 }
 
@@ -343,16 +352,22 @@ struct AttendPlan {
     AttendLaunch few, many;
 };
 
-// the context in chunks, so that there are about `want` workgroups; a chunk is at least `least` tokens
-static void divide_context(AttendLaunch &p, int64_t reach, int64_t groups, int64_t want, int64_t least, int most)
+// Into how many chunks the context is divided: 1, 2, 4 ... 128, whichever is estimated to take least.  A workgroup takes 4 us to
+// begin and to join its waves, and for each turn of its four waves 1 us per 4000 bytes of a wave's unit where a CU has one workgroup,
+// per 3000 where it has two (what 4 contexts of 131072 tokens took in 8 and 16 chunks: 272 and 185 us); joining chunks is another
+// launch, 5 us.  32 contexts up to 8000 took 64 us undivided, 65, 70 and 75 in 2, 4 and 8; 48 windows of 1024 16 undivided, 20 in 2.
+static void divide_context(AttendLaunch &p, int64_t reach, int64_t groups, int64_t unit, int64_t unit_bytes, int per_cu)
 {
-    int64_t n = groups < want ? want / groups : 1;
-    if (n > most) n = most;
-    int64_t chunk = (reach + n - 1) / n;
-    chunk = (chunk + 255) / 256 * 256;
-    if (chunk < least) chunk = least;
-    p.chunk_tokens = chunk;
-    p.chunks = (int)((reach + chunk - 1) / chunk);
+    const int64_t turn = 4 * unit, turns = (reach + turn - 1) / turn;
+    double best = 0.0;
+    for (int64_t n = 1; n <= 128 && n <= (turns > 1 ? turns : 1); n *= 2) {
+        const int64_t workgroups = groups * n, rounds = (workgroups + 256 * per_cu - 1) / (256 * per_cu);
+        const double turn_us = (double)unit_bytes / (workgroups > 256 && per_cu > 1 ? 3000.0 : 4000.0);
+        const double us = (double)rounds * (4.0 + (double)((turns + n - 1) / n) * turn_us) + (n > 1 ? 5.0 + 0.05 * (double)n : 0.0);
+        if (n == 1 || us < best) best = us, p.chunk_tokens = (turns + n - 1) / n * turn;
+    }
+    if (p.chunk_tokens < turn) p.chunk_tokens = turn;
+    p.chunks = (int)((reach + p.chunk_tokens - 1) / p.chunk_tokens);
     if (p.chunks < 1) p.chunks = 1;
 }
 
@@ -376,7 +391,8 @@ static AttendPlan attend_plan(const qnn_kv_cache &cache, int q_heads, int64_t ta
         p.few.row_blocks = (int)((few + p.few.tiles * 16 - 1) / (p.few.tiles * 16));
         p.few.part_rows = (int)few;
         if (p.many.used) p.few.rows_upto = kFewRows;
-        divide_context(p.few, reach, groups * p.few.row_blocks, 2048, 256, 128);
+        const int64_t unit = cache.block % 64 == 0 ? 64 : 32;
+        divide_context(p.few, reach, groups * p.few.row_blocks, unit, unit * cache.dim * 2, p.few.tiles * cache.dim <= 128 ? 2 : 1);
     }
     if (p.many.used) {
         if (p.few.used) p.many.rows_over = kFewRows;
@@ -385,7 +401,13 @@ static AttendPlan attend_plan(const qnn_kv_cache &cache, int q_heads, int64_t ta
         const int64_t blocks = (rows + 32 * p.many.waves - 1) / (32 * p.many.waves);
         p.many.row_blocks = (int)(blocks < 4096 ? blocks : 4096);
         p.many.part_rows = (int)rows;
-        divide_context(p.many, reach, groups * blocks, 512, 1024, 16);
+        // (prompts fill the chip by themselves; a few hundred rows over a long context are divided into at most 16)
+        int64_t n = groups * blocks < 512 ? 512 / (groups * blocks) : 1;
+        if (n > 16) n = 16;
+        const int64_t chunk = ((reach + n - 1) / n + 255) / 256 * 256;
+        p.many.chunk_tokens = chunk < 1024 ? 1024 : chunk;
+        p.many.chunks = (int)((reach + p.many.chunk_tokens - 1) / p.many.chunk_tokens);
+        if (p.many.chunks < 1) p.many.chunks = 1;
     }
     return p;
 }
@@ -409,7 +431,12 @@ template <class T, int D> static void run_many(const AttendArgs &a, const Attend
 template <class T, int D, int U> static void run_join(const AttendArgs &a, hipStream_t s)
 {
     const int per = a.part_rows < 4096 ? a.part_rows : 4096;
-    hipLaunchKernelGGL((attend_join_kernel<T, D, U>), dim3((unsigned)((int64_t)a.requests * per), (unsigned)a.cache.heads), dim3(256), 0, s, a, per);
+    const unsigned heads = (unsigned)a.cache.heads;
+    // waves enough for the chip (or few chunks): one per row
+    if ((int64_t)a.requests * per * heads >= 2048 || a.chunks <= 8)
+        hipLaunchKernelGGL((attend_join_kernel<T, D, U, false>), dim3((unsigned)((int64_t)a.requests * ((per + 3) / 4)), heads), dim3(256), 0, s, a, per);
+    else
+        hipLaunchKernelGGL((attend_join_kernel<T, D, U, true>), dim3((unsigned)((int64_t)a.requests * per), heads), dim3(256), 0, s, a, per);
 }
 
 template <class T, int D> static qnn_status run_attend(AttendArgs a, const AttendPlan &p, char *workspace, hipStream_t s)

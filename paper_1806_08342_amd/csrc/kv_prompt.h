@@ -8,7 +8,8 @@
 //
 // The running maximum and the scale that the accumulators stand in follow lazily: they are kept while a row's scores stay below
 // 2^kRoom times the reference and a page's value scale within 2^kRoom of it, so that most units rescale nothing.  A page's
-// value scale is part of the exponent (p * vs / reference), and the sum of p is corrected once per tile.
+// value scale is part of the exponent (p * vs / reference), and the sum of p is corrected once per tile; for a tile whose value
+// scale is below 2^-20 of its unit's other tile's, or zero, the sum is formed separately.
 #pragma once
 
 #include "kv_attention.h"
@@ -24,7 +25,7 @@ __device__ __forceinline__ float other_half(float v)
     return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
 }
 
-template <class T, int D, int WAVES, int RT> __global__ void __launch_bounds__(64 * WAVES) attend_prompt_kernel(const AttendArgs a)
+template <class T, int D, int WAVES, int RT> __global__ void __launch_bounds__(64 * WAVES, D <= 128 ? 2 : 1) attend_prompt_kernel(const AttendArgs a)
 {
     constexpr int BR = 32 * RT * WAVES, KS = D / 16, VT = D / 32;
     constexpr int PIECES = (4 * D + 64 * WAVES - 1) / (64 * WAVES); // 16-byte pieces of 64 tokens' keys (or values) per thread
@@ -33,7 +34,7 @@ template <class T, int D, int WAVES, int RT> __global__ void __launch_bounds__(6
     __shared__ __attribute__((aligned(16))) _Float16 s_k[2][64][KP];
     __shared__ __attribute__((aligned(16))) _Float16 s_v[2][D][VP];
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, hh = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, hh = lane >> 5;
     const int heads = a.cache.heads, block = a.cache.block;
     // heads next to each other: workgroups are dealt to the XCDs in turn, so that one XCD's L2 holds few heads' keys and values
     const int h = blockIdx.x % heads, rest = blockIdx.x / heads;
@@ -186,6 +187,7 @@ template <class T, int D, int WAVES, int RT> __global__ void __launch_bounds__(6
                     }
                 }
                 if (missing[0] || missing[1] || t + 63 > wave_first || (a.window > 0 && t <= wave_last - a.window)) {
+                    asm volatile(""); // (a branch: few units are cut)
 #pragma unroll
                     for (int x = 0; x < RT; ++x) {
                         const int64_t base = t + 8 * hh;
@@ -218,51 +220,49 @@ template <class T, int D, int WAVES, int RT> __global__ void __launch_bounds__(6
                     most[x] = fmaxf(most[x], other_half(most[x]));
                     grew |= most[x] > m[x] + kRoom;
                 }
-                if (__any(grew)) {
+                const float vmost = fmaxf(vs[0], vs[1]);
+                const bool change = vmost > 0.0f && !(vmost < 16.0f * reference && vmost > 0.0625f * reference);
+                if (__any(grew) || change) {
+                    const float to_new = change ? (reference > 0.0f ? reference / vmost : 0.0f) : 1.0f;
+                    reference = change ? vmost : reference;
 #pragma unroll
                     for (int x = 0; x < RT; ++x) {
-                        const float now = fmaxf(m[x], most[x]), by = exp2_fast(m[x] - now);
-                        m[x] = now, l[x] *= by;
+                        const float now = fmaxf(m[x], most[x]), shrink = exp2_fast(m[x] - now), by = shrink * to_new;
+                        m[x] = now, l[x] *= shrink;
 #pragma unroll
                         for (int v = 0; v < VT; ++v) o[x][v] *= by;
                     }
                 }
+                h16x8 p[RT][4];
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    const bool any = vs[y] > 0.0f; // a page of zeros adds to the sum only
-                    float ratio = any ? vs[y] / reference : 1.0f;
-                    if (any && !(ratio < 16.0f && ratio > 0.0625f)) {
-                        const float by = reference > 0.0f ? reference / vs[y] : 0.0f;
-                        reference = vs[y], ratio = 1.0f;
-#pragma unroll
-                        for (int x = 0; x < RT; ++x)
-#pragma unroll
-                            for (int v = 0; v < VT; ++v) o[x][v] *= by;
-                    }
-                    const float up = __log2f(ratio) + kPromptHead, down = 1.0f / ratio;
-                    h16x8 p[RT][2];
+                    const float ratio = vmost > 0.0f ? vs[y] * __builtin_amdgcn_rcpf(reference) : 0.0f;
+                    const bool small = !(ratio > 0x1p-20f);
+                    const float up = __log2f(ratio) + kPromptHead, down = small ? 0.0f : __builtin_amdgcn_rcpf(ratio); // (takes out what `up` has brought in)
 #pragma unroll
                     for (int x = 0; x < RT; ++x) {
+                        if (small)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) l[x] += exp2_fast(fmaf(s[x][y][i], fk[x][y], kPromptHead - m[x]));
                         const float off = up - m[x];
                         float sum = 0.0f;
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             const float e = exp2_fast(fmaf(s[x][y][i], fk[x][y], off));
                             sum += e;
-                            p[x][i >> 3][i & 7] = (_Float16)e;
+                            p[x][2 * y + (i >> 3)][i & 7] = (_Float16)e;
                         }
                         l[x] = fmaf(sum, down, l[x]);
-                        if (!any) p[x][0] = p[x][1] = h16x8{};
                     }
-#pragma unroll
-                    for (int v = 0; v < VT; ++v)
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const h16x8 vf = *reinterpret_cast<const h16x8 *>(&s_v[buf][32 * v + c][32 * y + 16 * k + 8 * hh]);
-#pragma unroll
-                            for (int x = 0; x < RT; ++x) o[x][v] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p[x][k], o[x][v], 0, 0, 0);
-                        }
                 }
+#pragma unroll
+                for (int v = 0; v < VT; ++v)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const h16x8 vf = *reinterpret_cast<const h16x8 *>(&s_v[buf][32 * v + c][16 * k + 8 * hh]);
+#pragma unroll
+                        for (int x = 0; x < RT; ++x) o[x][v] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p[x][k], o[x][v], 0, 0, 0);
+                    }
             }
             if (u + 1 < units) stage(buf ^ 1);
             __syncthreads();
