@@ -14,6 +14,7 @@
 // reads tokens of its own, so nothing would be shared through LDS.
 #include "kv_attention.h"
 #include "kv_prompt.h"
+#include "kv_prompt_wide.h"
 
 namespace qnn {
 
@@ -424,8 +425,9 @@ template <class T, int D, int U> static void run_few(const AttendArgs &a, const 
 template <class T, int D> static void run_many(const AttendArgs &a, const AttendLaunch &p, hipStream_t s)
 {
     const dim3 grid((unsigned)((int64_t)a.requests * p.row_blocks * p.chunks * a.cache.heads));
-    if (D > 128 || p.waves == 4) hipLaunchKernelGGL((attend_prompt_kernel<T, D, 4, 1>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((attend_prompt_kernel<T, D, (D > 128 ? 4 : 8), 1>), grid, dim3(512), 0, s, a);
+    if constexpr (D > 128) hipLaunchKernelGGL((attend_wide_kernel<T, D>), grid, dim3(512), 0, s, a);
+    else if (p.waves == 4) hipLaunchKernelGGL((attend_prompt_kernel<T, D, 4, 1>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((attend_prompt_kernel<T, D, 8, 1>), grid, dim3(512), 0, s, a);
 }
 
 template <class T, int D, int U> static void run_join(const AttendArgs &a, hipStream_t s)

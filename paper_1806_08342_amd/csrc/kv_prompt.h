@@ -38,7 +38,8 @@ template <class T, int D, int WAVES, int RT> __global__ void __launch_bounds__(6
     const int heads = a.cache.heads, block = a.cache.block;
     // heads next to each other: workgroups are dealt to the XCDs in turn, so that one XCD's L2 holds few heads' keys and values
     const int h = blockIdx.x % heads, rest = blockIdx.x / heads;
-    const int chunk = rest % a.chunks, rb0 = rest / a.chunks % a.row_blocks, r = rest / a.chunks / a.row_blocks;
+    // (the last rows of all requests, which see most tokens, go first)
+    const int chunk = rest % a.chunks, r = rest / a.chunks % a.requests, rb0 = rest / a.chunks / a.requests;
     const Request rq = request_of<64>(a, r);
     const int rows = rq.n * a.group;
     if (rows <= a.rows_over || rows > a.rows_upto) return;
@@ -174,18 +175,17 @@ template <class T, int D, int WAVES, int RT> __global__ void __launch_bounds__(6
             if (!idle && t <= wave_last && !(a.window > 0 && t + 63 <= wave_first - a.window)) {
                 f32x16 s[RT][2];
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {
+                for (int x = 0; x < RT; ++x)
 #pragma unroll
-                    for (int x = 0; x < RT; ++x)
+                    for (int i = 0; i < 16; ++i) s[x][0][i] = s[x][1][i] = 0.0f;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[x][y][i] = 0.0f;
+                for (int k = 0; k < KS; ++k)
 #pragma unroll
-                    for (int k = 0; k < KS; ++k) {
+                    for (int y = 0; y < 2; ++y) {
                         const h16x8 kf = *reinterpret_cast<const h16x8 *>(&s_k[buf][32 * y + c][16 * k + 8 * hh]);
 #pragma unroll
                         for (int x = 0; x < RT; ++x) s[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[x][k], s[x][y], 0, 0, 0);
                     }
-                }
                 if (missing[0] || missing[1] || t + 63 > wave_first || (a.window > 0 && t <= wave_last - a.window)) {
                     asm volatile(""); // (a branch: few units are cut)
 #pragma unroll
@@ -256,9 +256,9 @@ template <class T, int D, int WAVES, int RT> __global__ void __launch_bounds__(6
                     }
                 }
 #pragma unroll
-                for (int v = 0; v < VT; ++v)
+                for (int k = 0; k < 4; ++k)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
+                    for (int v = 0; v < VT; ++v) {
                         const h16x8 vf = *reinterpret_cast<const h16x8 *>(&s_v[buf][32 * v + c][16 * k + 8 * hh]);
 #pragma unroll
                         for (int x = 0; x < RT; ++x) o[x][v] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p[x][k], o[x][v], 0, 0, 0);
