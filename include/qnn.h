@@ -336,7 +336,9 @@ qnn_status qnn_qdwconv2d_asym(const uint8_t *x, int N, int H, int W, int C, int3
 
 /* y[m][n] = bias[n] + sum_k x[m][k] * (c[n][k] - z[k / group][n]) * s[k / group][n]
  * The weights enter exactly (code minus zero-point is a whole number of at most 5 bits, the scale multiplies the group's sum in
- * binary32); sums are binary32, y is rounded once.
+ * binary32); sums are binary32, y is rounded once.  From about 17 rows on x enters as binary16, each row scaled by a power of two to at
+ * most 1, which is exact but for elements below 2^-17 of their row's largest (bfloat16; 2^-14 for binary16), which keep fewer bits; and a group whose scale is
+ * less than 2^-100 of the one before it in its row counts as 0.  An infinite or NaN x gives infinities or NaN in its row.
  * x: DEVICE, M x K of `type`, row pitch ldx >= K elements.  codes: DEVICE uint8 [N][K/2], nibbles as in qnn_qgemm
  * (two's complement, element 2j in the low one), K even.  scales: DEVICE [ceil(K / group)][N] of `type`.
  * zeros: DEVICE int8 [ceil(K / group)][N], or NULL for symmetric weights.  bias: DEVICE [N] of `type` or NULL.
@@ -347,6 +349,10 @@ qnn_status qnn_w4_matmul(const void *x, int64_t ldx, const uint8_t *codes, const
                          const void *bias, int64_t M, int64_t N, int64_t K, int64_t group, int type, void *y, int64_t ldy,
                          void *workspace, size_t workspace_bytes, void *stream);
 size_t qnn_w4_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t group);
+
+/* Name of the kernel that qnn_w4_matmul selects: "few", "tens" or "many", rows of x by rows of weights of a workgroup's or wave's tile, and
+ * "/" the parts that K is in.  For logging and profiling.  HOST string owned by the library; "" for sizes that are refused. */
+const char *qnn_w4_matmul_plan(int64_t M, int64_t N, int64_t K, int64_t group);
 
 /* A cache of keys and values in 8 bits.  A page holds `block` consecutive tokens of one request for all heads; the page of a
  * request's tokens j * block ... is table[request][j].  A value is code * scale, codes within [-127, 127] and

@@ -26,7 +26,7 @@ EXPORTS = [
     "qnn_quantize_dynamic", "qnn_simquant", "qnn_simquant_backward", "qnn_choose_qparams", "qnn_quantize_multiplier", "qnn_act_range",
     "qnn_qadd_params", "qnn_quantize_weights", "qnn_pack_int4", "qnn_qgemm_workspace_bytes", "qnn_qconv2d_workspace_bytes",
     "qnn_tuning_set", "qnn_calibrate_mfma", "qnn_calibrate_copy", "qnn_qgemm_noalloc", "qnn_quantize_u16", "qnn_dequantize_u16", "qnn_calibrate_rescale",
-    "qnn_w4_matmul", "qnn_w4_matmul_workspace_bytes", "qnn_kv_append", "qnn_kv_gather", "qnn_kv_attention", "qnn_kv_attention_workspace_bytes",
+    "qnn_w4_matmul", "qnn_w4_matmul_workspace_bytes", "qnn_w4_matmul_plan", "qnn_kv_append", "qnn_kv_gather", "qnn_kv_attention", "qnn_kv_attention_workspace_bytes",
     "qnn_quantize_weights_grouped",
 ]
 
@@ -107,6 +107,8 @@ def load_library():
     lib.qnn_qgemm_workspace_bytes.argtypes = [i64, i64, i64, ci, ci]
     lib.qnn_qconv2d_workspace_bytes.restype = sz
     lib.qnn_qconv2d_workspace_bytes.argtypes = [ci] * 13
+    lib.qnn_w4_matmul_plan.restype = C.c_char_p
+    lib.qnn_w4_matmul_plan.argtypes = [i64] * 4
     lib.qnn_w4_matmul_workspace_bytes.restype = sz
     lib.qnn_w4_matmul_workspace_bytes.argtypes = [i64] * 4
     lib.qnn_kv_attention_workspace_bytes.restype = sz
@@ -491,6 +493,11 @@ def w4_matmul(x, codes, scales, group, zeros=None, bias=None, out=None, workspac
     (as `pack_int4` packs rows); scales: [ceil(K/group),N] of x's type; zeros: int8 of that shape or None; group: a multiple of
     32.  Returns [M,N] of x's type."""
     return (_nat or _native()).w4_matmul(x, codes, scales, group, zeros, bias, out, workspace)
+
+
+def w4_matmul_plan(M, N, K, group=128):
+    """Name of the kernel that `w4_matmul` runs for these sizes."""
+    return load_library().qnn_w4_matmul_plan(M, N, K, group).decode()
 
 
 def new_kv_cache(pages, heads, dim, block=64, device="cuda:0"):

@@ -177,6 +177,7 @@ inline size_t w4_prepared_bytes(int64_t M, int64_t K) { return (size_t)M * ((K +
 void prepare_x(const W4Args &a, int type, const W4Prepared &p, hipStream_t s);
 // tens of rows (w4_parts.hip), many (w4_tile.hip)
 float w4_parts_us(int64_t M, int64_t N, int64_t K); // estimated time
+const char *w4_parts_name(int64_t M, int64_t N, int64_t K);
 void launch_w4_parts(const W4Args &a, int type, const W4Prepared &p, hipStream_t s);
 void launch_w4_tile(const W4Args &a, int type, const W4Prepared &p, hipStream_t s);
 

@@ -200,14 +200,18 @@ template <class T, int MT, int NT, int WAVES, int GS, bool TINY = false> static 
 // tiles of 16 rows of weights per wave
 static int few_tiles(int64_t N) { return N > 16384 ? 2 : 1; }
 
+// waves along K: fewer than four scales in all (no four to load at once); two tiles per wave; as a workgroup of 16 waves has a CU to
+// itself, 16 only where there are no more workgroups than CUs (1 x 12288 x 4096 13.1 us with 16, 9.9 with 8)
+static int few_form(int64_t N, int64_t groups) { return groups * N < 4 ? 0 : few_tiles(N) == 2 ? 1 : (N + 15) / 16 > 256 ? 2 : 3; }
+
 template <class T, int GS> static void launch_w4(const W4Args &a, hipStream_t s)
 {
-    const int64_t columns = ((int64_t)a.N + 15) / 16;
-    if ((int64_t)a.groups * a.N < 4) launch_rows<T, 1, 1, 4, GS, true>(a, s); // (no four scales to load at once)
-    else if (few_tiles(a.N) == 2) launch_rows<T, 1, 2, 8, GS>(a, s);
-    // a workgroup of 16 waves has a CU to itself
-    else if (columns > 256) launch_rows<T, 1, 1, 8, GS>(a, s);
-    else launch_rows<T, 1, 1, 16, GS>(a, s);
+    switch (few_form(a.N, a.groups)) {
+    case 0: launch_rows<T, 1, 1, 4, GS, true>(a, s); break;
+    case 1: launch_rows<T, 1, 2, 8, GS>(a, s); break;
+    case 2: launch_rows<T, 1, 1, 8, GS>(a, s); break;
+    default: launch_rows<T, 1, 1, 16, GS>(a, s); break;
+    }
 }
 
 template <class T> static qnn_status run_w4(const W4Args &a, hipStream_t s)
@@ -252,6 +256,19 @@ size_t qnn_w4_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t gr
 {
     if (bad_w4_sizes(M, N, K, group) || M == 0 || w4_kernel(M, N, K) == W4Kernel::Few) return 0;
     return w4_prepared_bytes(M, K);
+}
+
+const char *qnn_w4_matmul_plan(int64_t M, int64_t N, int64_t K, int64_t group)
+{
+    if (bad_w4_sizes(M, N, K, group) || M == 0) return "";
+    switch (w4_kernel(M, N, K)) {
+    case W4Kernel::Few: {
+        static const char *const names[] = {"few16x16/4", "few16x32/8", "few16x16/8", "few16x16/16"};
+        return names[few_form(N, (K + group - 1) / group)];
+    }
+    case W4Kernel::Tens: return w4_parts_name(M, N, K);
+    default: return "many128x256";
+    }
 }
 
 qnn_status qnn_w4_matmul(const void *x, int64_t ldx, const uint8_t *codes, const void *scales, const int8_t *zeros, const void *bias, int64_t M,

@@ -164,8 +164,10 @@ template <class T, int MT, int NW, int PARTS, int RING> static void launch_group
 struct PartsForm {
     int mt, nw, parts;
     float turn_us;
+    const char *name; // rows of x, x rows of weights, / parts of K
 };
-constexpr PartsForm kForms[] = {{1, 4, 4, 2.0f}, {1, 2, 4, 1.2f}, {1, 1, 8, 1.55f}, {2, 4, 4, 2.4f}, {2, 4, 2, 1.3f}, {2, 2, 4, 1.75f}};
+constexpr PartsForm kForms[] = {{1, 4, 4, 2.0f, "tens32x128/4"}, {1, 2, 4, 1.2f, "tens32x64/4"},   {1, 1, 8, 1.55f, "tens32x32/8"},
+                                {2, 4, 4, 2.4f, "tens64x128/4"}, {2, 4, 2, 1.3f, "tens64x128/2"}, {2, 2, 4, 1.75f, "tens64x64/4"}};
 
 static float form_us(const PartsForm &f, int64_t M, int64_t N, int64_t K)
 {
@@ -179,6 +181,7 @@ static int best_form(int64_t M, int64_t N, int64_t K)
         if (form_us(kForms[i], M, N, K) < form_us(kForms[best], M, N, K)) best = i;
     return best;
 }
+const char *w4_parts_name(int64_t M, int64_t N, int64_t K) { return kForms[best_form(M, N, K)].name; }
 float w4_parts_us(int64_t M, int64_t N, int64_t K) { return form_us(kForms[best_form(M, N, K)], M, N, K); }
 
 template <class T> static void run_parts(const W4Args &a, const W4Prepared &p, hipStream_t s)

@@ -15,8 +15,10 @@ def check(cache, q, cu, lengths, table, what="", **kw):
     kw.pop("max_queries", None)
     want, want_lse, spread = attend(cache, q, cu.cpu(), lengths.cpu(), table.cpu(), **kw)
     # one rounding of the result; each probability rounded to binary16 (2^-11); scores of size up to 100 in binary32 and the
-    # exponential and the sum give another 2^-14 of what is averaged; channels that average to little: 2^-30
-    assert_close(out, want, 1.01 * half_ulp(q.dtype) * want.abs() + (2.0 ** -11 + 2.0 ** -13) * spread + 2.0 ** -30, what)
+    # exponential and the sum give another 2^-14 of what is averaged; channels that average to little: 2^-30; binary16's last step
+    # is 2^-24
+    last = 2.0 ** -25 if q.dtype == torch.float16 else 0.0
+    assert_close(out, want, 1.01 * half_ulp(q.dtype) * want.abs() + (2.0 ** -11 + 2.0 ** -13) * spread + 2.0 ** -30 + last, what)
     rows = int(cu[-1])
     seen = torch.isfinite(want_lse[:rows])
     assert torch.equal(torch.isfinite(lse[:rows].cpu()), seen) and (lse[:rows].cpu()[~seen] == -math.inf).all()
@@ -204,3 +206,46 @@ def test_refusals():
     long = case([(9000, 1)], 1, 64, 64, torch.bfloat16, 0, q_heads=1)
     with pytest.raises(qnn.QnnError, match="QNN_EINVAL"):
         f(*long, max_queries=1, workspace=torch.empty(16, dtype=torch.uint8, device=DEV))  # too little scratch
+
+
+@pytest.mark.parametrize("dim", [64, 96, 128])
+def test_many_prompts_at_once(dim):
+    # rows enough for workgroups of eight waves; requests with few rows among them go to the other kernel
+    requests = [(70 + i % 13, 70 + i % 13) if i % 7 else (90 + i, 1 + i % 3) for i in range(36)] + [(0, 0), (500, 20)]
+    check(*case(requests, 8, dim, 64, torch.bfloat16, dim, q_heads=32), dim, max_queries=82)
+
+
+@pytest.mark.parametrize("dim,group", [(64, 8), (128, 4), (256, 3)])
+def test_hundreds_of_rows_over_a_long_context(dim, group):
+    # one context is divided over workgroups and joined, with the kernels for many rows too
+    args = case([(9001, 40), (700, 33), (3000, 1)], 1, dim, 64, torch.bfloat16, 7, q_heads=group)
+    check(*args, (dim, group), max_queries=40)
+    check(*args, (dim, group, "window"), max_queries=40, window=3000)
+
+
+@pytest.mark.parametrize("block", [32, 64])
+@pytest.mark.parametrize("dim", [64, 256])
+def test_value_scales_far_apart_and_zero(dim, block):
+    # accumulators stand in units of a page's value scale: rows that see small pages only stay exact, pages of zeros count in the sum
+    for requests, most in (([(300, 300), (200, 150)], 300), ([(300, 1), (200, 3)], 3)):
+        cache, q, cu, lengths, table = case(requests, 2, dim, block, torch.float16, block, q_heads=4)
+        for r in range(2):
+            for j, by in enumerate((1e-4, 1.0, 300.0, 0.0, 1e-3, 1.0, 1e-2)):
+                if j < table.shape[1] and table[r, j] >= 0:
+                    cache[3][int(table[r, j])] *= by
+        check(cache, q, cu, lengths, table, (dim, block, most), max_queries=most)
+        cache[1][:] = 0.0  # all scores equal
+        check(cache, q, cu, lengths, table, (dim, block, most, "keys"), max_queries=most)
+
+
+def test_negative_scale_factor_and_large_scores():
+    for requests, most in (([(300, 300)], 300), ([(300, 2)], 2)):
+        args = case(requests, 1, 64, 64, torch.bfloat16, 4, q_heads=2)
+        check(*args, most, max_queries=most, scale=-0.2)
+        args[0][1].mul_(20.0)  # scores of hundreds: the running maximum moves on and on
+        out = qnn.kv_attention(*args, max_queries=most)
+        want, _, spread = attend(args[0], args[1], *(t.cpu() for t in args[2:]))
+        # scores of size 400 in binary32: an error of 400 * 2^-22 in the exponent is one of 1e-4 of what is averaged.  Where one
+        # token takes nearly all, the others' probabilities are below binary16's normal numbers: 2^-25 of the 2^2 that 1 is at least
+        # held as, for each of 300 values of at most 127 * 0.025
+        assert_close(out, want, 1.01 * 2.0 ** -8 * want.abs() + (2.0 ** -11 + 4e-4) * spread + 300 * 127 * 0.025 * 2.0 ** -27, "large")

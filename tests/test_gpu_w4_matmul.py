@@ -98,3 +98,71 @@ def test_refusals():
             bad()
     with pytest.raises(qnn.QnnError, match="QNN_EINVAL"):
         f(x, codes, torch.cat([scales, scales]), 16)  # a group is a multiple of 32
+
+
+# every kernel and form of one, at sizes that divide nothing
+FORMS = {"few16x16/4": (3, 3, 30), "few16x32/8": (5, 17001, 330), "few16x16/8": (9, 4103, 514), "few16x16/16": (15, 1000, 1030), "tens32x64/4": (17, 1001, 386),
+         "tens32x32/8": (65, 301, 1034), "tens32x128/4": (17, 17003, 770), "tens64x128/4": (33, 17001, 770), "tens64x128/2": (70, 9001, 514), "tens64x64/4": (40, 8203, 514),
+         "many128x256": (201, 17003, 770)}
+
+
+@pytest.mark.parametrize("group,zeros,dtype", [(128, False, torch.bfloat16), (64, True, torch.float16), (32, True, torch.bfloat16), (96, False, torch.float16)])
+@pytest.mark.parametrize("form", FORMS)
+def test_every_form(form, group, zeros, dtype):
+    M, N, K = FORMS[form]
+    assert qnn.w4_matmul_plan(M, N, K, 128) == form and (form == "few16x16/4" or qnn.w4_matmul_plan(M, N, K, group) == form)
+    if form == "few16x16/4" and group < 64:
+        group = 32
+    x, codes, scales, z, b = make(M, N, K, group, dtype, zeros, True)
+    check(qnn.w4_matmul(x, codes, scales, group, z, b), x, codes, scales, group, z, b, form)
+
+
+@pytest.mark.parametrize("M", [2, 30, 300])
+@pytest.mark.parametrize("skip", [1, 2, 3])
+def test_rows_of_codes_at_any_byte(M, skip):
+    # rows of 65 bytes, the first of them `skip` bytes after a multiple of 4; guarded on both sides
+    N, K = 260, 130
+    x, codes, scales, z, _ = make(M, N, K, 32, torch.bfloat16, True, False)
+    flat = torch.full((skip + codes.numel() + 8,), 0x77, dtype=torch.uint8, device=DEV)
+    moved = flat[skip:skip + codes.numel()].view(N, K // 2)
+    moved.copy_(codes)
+    assert torch.equal(qnn.w4_matmul(x, moved, scales, 32, z), qnn.w4_matmul(x, codes, scales, 32, z))
+
+
+@pytest.mark.parametrize("M", [4, 20, 50, 300])
+def test_scales_far_apart_zero_and_negative(M):
+    N, K, group = 300, 640, 64
+    x, codes, scales, z, _ = make(M, N, K, group, torch.bfloat16, True, False)
+    scales[0] *= 2.0 ** 30
+    scales[3] *= 2.0 ** -30
+    scales[4] = 0.0
+    scales[5, ::2] = 0.0
+    scales[0, 1::3] = 0.0
+    scales[6] *= -1.0
+    scales[9, 5] = 0.0
+    check(qnn.w4_matmul(x, codes, scales, group, z), x, codes, scales, group, z, None, "apart")
+    scales[:] = 0.0
+    assert (qnn.w4_matmul(x, codes, scales, group, z) == 0).all()
+
+
+@pytest.mark.parametrize("M", [3, 20, 300])
+def test_sizes_of_rows_do_not_matter(M):
+    # rows scaled by powers of two scale their results, up to the ends of the type's range
+    x, codes, scales, z, _ = make(M, 260, 384, 128, torch.bfloat16, True, False)
+    want = qnn.w4_matmul(x, codes, scales, 128, z)
+    by = torch.tensor([2.0 ** (i % 9 * 20 - 80) for i in range(M)], device=DEV)[:, None].to(torch.bfloat16)
+    got = qnn.w4_matmul(x * by, codes, scales, 128, z)
+    assert torch.equal(got, want * by)
+    x[1, 7] = float("nan")
+    y = qnn.w4_matmul(x, codes, scales, 128, z)
+    assert torch.isnan(y[1]).all() and torch.isfinite(y[0]).all() and torch.isfinite(y[2:]).all()
+
+
+def test_long_rows():
+    K = (1 << 21) + 258  # beyond the offsets of the kernels for many rows of x
+    g = torch.Generator().manual_seed(0)
+    x = torch.randn(18, K, generator=g).to(torch.bfloat16).to(DEV)
+    codes = torch.randint(0, 256, (5, K // 2), generator=g).to(torch.uint8).to(DEV)
+    scales = torch.full((-(-K // 1024), 5), 0.01, dtype=torch.bfloat16, device=DEV)
+    assert qnn.w4_matmul_plan(18, 5, K, 1024).startswith("few")
+    check(qnn.w4_matmul(x, codes, scales, 1024), x, codes, scales, 1024, None, None, "long")
