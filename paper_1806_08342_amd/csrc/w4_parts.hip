@@ -11,14 +11,14 @@
 namespace qnn {
 
 // A workgroup: 32 * NW rows of weights, 32 * MT rows of x; part `part` of K takes 128s part, part + PARTS, ...: a turn is one of them.
-// Requests are made RING - 1 turns ahead, the same number in each turn (past the end the last one again), so that waiting for all
-// but the younger turns' is waiting for the copies of the one that begins.  GS: groups in 128 weights (1: of whole 128s, 2: of 64s,
+// Requests are made RING - 1 turns ahead, copies first, at least REQUESTS in each turn (past the end the last one again), so that
+// waiting for all but so many for each younger turn is waiting for the copies of the one that begins.  GS: groups in 128 weights (1: of whole 128s, 2: of 64s,
 // 4: any multiple of 32).
 template <class T, int MT, int NW, int PARTS, int RING, int GS, bool ZEROS> __global__ void __launch_bounds__(64 * NW * PARTS, NW * PARTS == 16 ? 4 : 2) w4_parts_kernel(const W4Args a, const W4Prepared p)
 {
     constexpr int ROWS = 32 * MT, BN = 32 * NW, COPIES = 8 * MT / NW; // copies of 1 KB per wave and turn
     constexpr int X_BYTES = RING * PARTS * ROWS * 256, SUM_BYTES = PARTS * ROWS * (BN + 4) * 4;
-    constexpr int REQUESTS = COPIES + 2 + GS * (ZEROS ? 2 : 1), AHEAD = RING - 1;
+    constexpr int REQUESTS = COPIES + 2, AHEAD = RING - 1; // a turn's copies and codes (scales, or codes that the compiler moves, make it more: the wait is longer then, not shorter)
     __shared__ __attribute__((aligned(16))) uint8_t s_mem[X_BYTES > SUM_BYTES ? X_BYTES : SUM_BYTES];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, hh = lane >> 5;
     const int part = wave / NW, nw = wave % NW;
