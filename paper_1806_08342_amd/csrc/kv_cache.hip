@@ -14,39 +14,39 @@ struct CacheArgs {
 };
 
 // Workgroup `item` works on the item-th page that the call touches.  A request whose rows begin at cu and that has n of them
-// touches at most n / block + 2 pages (rounded down), so that pages item_base(r) ... item_base(r + 1) - 1 are its own; the
-// request is found by bisection with 64 lanes at a time.
-__device__ __forceinline__ int64_t first_row(const CacheArgs &a, int r) { return min(max((int64_t)a.cu[r], (int64_t)0), a.tokens); }
-__device__ __forceinline__ int64_t item_base(const CacheArgs &a, int r) { return first_row(a, r) / a.cache.block + 2 * (int64_t)r; }
-__device__ __forceinline__ int request_of_item(const CacheArgs &a, int64_t item)
-{
-    const int lane = threadIdx.x & 63;
-    int low = 0, n = a.requests; // in [low, low + n)
-    while (n > 1) {
-        const int step = (n + 63) / 64, r = low + lane * step;
-        const uint64_t reached = __ballot(lane * step < n && item_base(a, r) <= item);
-        const int k = max(__popcll(reached) - 1, 0);
-        low += k * step, n = min(step, n - k * step);
-    }
-    return low;
-}
+// touches at most n / block + 2 pages (rounded down), so that pages first / block + 2 r ... of request r are its own; the
+// request is found by bisection with 64 lanes at a time, whose last step also brings what is needed of it.  (Rows are below 2^30, tokens below 2^31:
+// 32 bits without a sign hold their sums, and their divisions take a fraction of 64 bits' time.)
+__device__ __forceinline__ uint32_t row_of(const CacheArgs &a, int r) { return (uint32_t)min(max(a.cu[r], 0), (int)a.tokens); }
 
 struct Piece {
     int64_t row;  // of k and v: the first new token's
     int64_t page; // -1: none
     int lo, hi;   // tokens of the page that are new, [lo, hi)
 };
-__device__ __forceinline__ Piece piece_of_item(const CacheArgs &a, int64_t item)
+__device__ __forceinline__ Piece piece_of_item(const CacheArgs &a, uint32_t item)
 {
-    const int r = request_of_item(a, item);
-    const int64_t c0 = first_row(a, r), n = max(first_row(a, r + 1) - c0, (int64_t)0), at = max(a.start[r], 0);
-    const int block = a.cache.block;
-    const int64_t j = at / block + (item - item_base(a, r)); // page of the request
-    const int64_t t0 = max(at, j * block), t1 = min(at + n, (j + 1) * block);
-    Piece p{c0 + (t0 - at), -1, (int)(t0 - j * block), (int)(t1 - j * block)};
+    const int lane = threadIdx.x & 63;
+    const uint32_t block = a.cache.block;
+    int low = 0, n = a.requests; // in [low, low + n)
+    while (n > 64) {
+        const int step = (n + 63) / 64, r = low + min(lane * step, n - 1);
+        const uint64_t reached = __ballot(lane * step < n && row_of(a, r) / block + 2u * r <= item);
+        const int k = max(__popcll(reached) - 1, 0);
+        low += k * step, n = min(step, n - k * step);
+    }
+    const int mine = low + min(lane, n - 1);
+    const uint32_t from = row_of(a, mine), upto = row_of(a, mine + 1), held = max(a.start[mine], 0);
+    const uint32_t base = from / block + 2u * mine;
+    const int k = max(__popcll(__ballot(lane < n && base <= item)) - 1, 0);
+    const auto of = [&](uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, k); };
+    const uint32_t c0 = of(from), c1 = of(upto), at = of(held);
+    const uint32_t j = at / block + (item - of(base)); // page of the request
+    const uint32_t t0 = max(at, j * block), t1 = min(at + (max(c1, c0) - c0), (j + 1) * block);
+    Piece p{(int64_t)c0 + (t0 - at), -1, (int)(t0 - j * block), (int)(t1 - j * block)};
     if (t1 <= t0) p.hi = p.lo;
     else if (j < a.table_width) {
-        const int32_t page = a.table[(int64_t)r * a.table_width + j];
+        const int32_t page = a.table[(int64_t)(low + k) * a.table_width + j];
         if ((uint32_t)page < (uint64_t)a.cache.pages) p.page = page;
     }
     return p;
@@ -101,6 +101,12 @@ template <class T, int D> __global__ void __launch_bounds__(256) append_kernel(c
     const int groups0 = p.lo >> 2, groups = ((p.hi + 3) >> 2) - groups0; // of 4 tokens
     const int n = is_v ? groups * DG * 4 : (p.hi - p.lo) * DG, batches = (n + 64 * kHeld - 1) / (64 * kHeld);
 
+    if (p.page < 0) return;
+    const int64_t slot = p.page * a.cache.heads + h;
+    int8_t *const codes = (is_v ? a.cache.v_codes : a.cache.k_codes) + slot * block * D;
+    float *const scale = (is_v ? a.cache.v_scales : a.cache.k_scales) + slot;
+    const float before = p.lo > 0 ? *scale : 0.0f; // (on its way with the elements)
+
     w32x4 held[kHeld];
     // piece k of a lane's 16 in a batch: keys by 64, values four of one unit after the other
     const auto past = [&](int batch, int k) { return is_v ? (batch * (kHeld / 4) + k / 4) * 64 >= groups * DG : (batch * kHeld + k) * 64 >= n; };
@@ -127,11 +133,6 @@ template <class T, int D> __global__ void __launch_bounds__(256) append_kernel(c
             }
         }
     }
-    if (p.page < 0) return;
-    const int64_t slot = p.page * a.cache.heads + h;
-    int8_t *const codes = (is_v ? a.cache.v_codes : a.cache.k_codes) + slot * block * D;
-    float *const scale = (is_v ? a.cache.v_scales : a.cache.k_scales) + slot;
-    const float before = p.lo > 0 ? *scale : 0.0f;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) peak = fmaxf(peak, __shfl_xor(peak, d));
     const float after = fmaxf(before, __fdiv_rn(peak, 127.0f)), by = after > 0.0f ? after : 1.0f;
