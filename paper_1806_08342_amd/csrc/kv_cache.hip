@@ -3,6 +3,8 @@
 
 namespace qnn {
 
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
 struct CacheArgs {
     qnn_kv_cache cache;
     const uint16_t *k, *v;
@@ -52,20 +54,21 @@ __device__ __forceinline__ Piece piece_of_item(const CacheArgs &a, uint32_t item
     return p;
 }
 
-// x / by, correctly rounded: two steps of r = x - q * by, q + r / by with the reciprocal (exact residuals; the first makes q one of
-// the two neighbours, the second the nearest).  `plain`: by is too small for that.
-__device__ __forceinline__ float quotient(float x, float by, float reciprocal, bool plain)
-{
-    if (plain) return __fdiv_rn(x, by);
-    float q = x * reciprocal;
-    q = fmaf(fmaf(-q, by, x), reciprocal, q);
-    return fmaf(fmaf(-q, by, x), reciprocal, q);
-}
-// round() with ties away from zero, as a code: 0.5 less its last bit added, then cut off.  NaN gives 0.
+// round() with ties away from zero, as a code: 0.5 less its last bit added, then cut off.
+__device__ __forceinline__ int rounded(float q) { return (int)(q + copysignf(0.49999997f, q)); }
 __device__ __forceinline__ int code_of(float q)
 {
-    const float c = __builtin_amdgcn_fmed3f(q, -127.0f, 127.0f); // (infinities: the ends)
-    return (int)(c + copysignf(0.49999997f, c));
+    return rounded(__builtin_amdgcn_fmed3f(q, -127.0f, 127.0f)); // (infinities: the ends)
+}
+// The code of x at scale s is that of x / s rounded to binary32 once, which x * hi + x * lo (rounded once, but for a product that is
+// 2^-24 of it) is within 3 * 2^-48 of before its rounding, where hi = 1 / s rounded and lo what it lacks.  The two codes differ only if the midpoint
+// below some k + 1/2 lies between, and that close to x / s: with s = B * 2^.., 2^23 <= B < 2^24, and x of 11 bits at
+// most, B would have to be within 6 of a multiple of 2^17 and not the multiple.  Scales within 8, and those whose reciprocals come near the
+// ends of binary32's range, are divided by.
+__device__ __forceinline__ bool divide_by(float s)
+{
+    const uint32_t b = __builtin_bit_cast(uint32_t, s);
+    return !(s > 0x1p-60f && s < 0x1p60f) || (((b + 8) & 0x1ffffu) <= 16 && (b & 0x1ffffu) != 0);
 }
 __device__ __forceinline__ uint32_t four_codes(int a, int b, int c, int d)
 {
@@ -120,21 +123,30 @@ template <class T, int D> __global__ void __launch_bounds__(256) append_kernel(c
             if (is_v ? d < DG && t >= 0 && t < p.hi - p.lo : i < n) held[k] = load_any<w32x4>(x + t * token + d * 8);
         }
     };
-    float peak = 0.0f;
+    u16x2 peaks = {0, 0}; // of the absolute values' patterns, which are in the values' order
     for (int batch = 0; batch < batches; ++batch) {
         load(batch);
 #pragma unroll
         for (int k = 0; k < kHeld; ++k) {
             if (past(batch, k)) break;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float v = fabsf(T::widen((uint16_t)(held[k][e >> 1] >> (e & 1) * 16)));
-                peak = v < INFINITY ? fmaxf(peak, v) : peak;
-            }
+            for (int e = 0; e < 4; ++e) peaks = __builtin_elementwise_max(peaks, __builtin_bit_cast(u16x2, held[k][e] & 0x7fff7fffu));
         }
     }
+    uint32_t pattern = max(peaks[0], peaks[1]);
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) peak = fmaxf(peak, __shfl_xor(peak, d));
+    for (int d = 1; d < 64; d *= 2) pattern = max(pattern, (uint32_t)__shfl_xor((int)pattern, d));
+    float peak = T::widen((uint16_t)pattern);
+    const bool infinite = !(peak < INFINITY); // or NaN
+    if (infinite) { // (rare: once more, by element)
+        peak = 0.0f;
+        for (int i = lane; i < (p.hi - p.lo) * D; i += 64) {
+            const float v = fabsf(T::widen(x[(i / D) * token + i % D]));
+            peak = v < INFINITY ? fmaxf(peak, v) : peak;
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) peak = fmaxf(peak, __shfl_xor(peak, d));
+    }
     const float after = fmaxf(before, __fdiv_rn(peak, 127.0f)), by = after > 0.0f ? after : 1.0f;
     if (lane == 0) *scale = after;
     if (after > before && p.lo > 0) { // what is held, in the new scale
@@ -154,8 +166,15 @@ template <class T, int D> __global__ void __launch_bounds__(256) append_kernel(c
             }
         }
     }
-    const float reciprocal = __fdiv_rn(1.0f, by);
-    const bool plain = !(by > 0x1p-100f && by < 0x1p100f);
+    if (infinite || divide_by(by)) {
+        for (int i = lane; i < (p.hi - p.lo) * D; i += 64) {
+            const int t = i / D, d = i % D;
+            const float v = T::widen(x[t * token + d]);
+            codes[is_v ? d * block + p.lo + t : (p.lo + t) * D + d] = (int8_t)(v == v ? code_of(__fdiv_rn(v, by)) : 0);
+        }
+        return;
+    }
+    const float hi = __fdiv_rn(1.0f, by), lo = hi * fmaf(-by, hi, 1.0f);
     for (int batch = 0; batch < batches; ++batch) {
         if (batches > 1) load(batch);
 #pragma unroll
@@ -168,7 +187,7 @@ template <class T, int D> __global__ void __launch_bounds__(256) append_kernel(c
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float v = T::widen((uint16_t)(held[k + j][e >> 1] >> (e & 1) * 16));
-                    c[j][e] = v == v ? code_of(quotient(v, by, reciprocal, plain)) : 0;
+                    c[j][e] = rounded(fmaf(v, hi, v * lo)); // (no value is over 127 steps of its own page's scale)
                 }
             }
             if (!is_v) {

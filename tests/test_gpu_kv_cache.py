@@ -45,6 +45,35 @@ def test_values_that_are_no_numbers_and_pages_of_zeros():
     check(cache, k, v, cu, start, table, "no numbers")
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("held, new", [(0, 64), (63, 1), (40, 20)])
+def test_infinities_beside_ordinary_values(held, new, dtype):
+    cache, k, v, cu, start, table = fresh([(held, new)], 2, 128, 64, dtype)
+    for x in (k, v):
+        x[0, 0, 3], x[0, 0, 77], x[new - 1, 1, 64] = float("inf"), float("-inf"), float("nan")
+        x[new - 1, 1, 127] = float("inf")
+    check(cache, k, v, cu, start, table, "infinite")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_quotients_at_the_ends_of_codes(dtype):
+    # each page's scale is (its largest element) / 127: all values of the type up to it, for largest elements whose scales lie on,
+    # beside and away from multiples of 2^17 of their last place, and ones far from 1
+    tops = [127.0, 63.5, 1.0, 1.9921875, 129.0, 100.0, 3.0, 0.3, 2.0 ** -14] + ([1e-37, 1e30, 3e38] if dtype is torch.bfloat16 else [65504.0])
+    n, dim, block = len(tops), 128, 64
+    kinds = torch.float64
+    top = torch.tensor(tops, dtype=kinds).to(dtype).to(kinds)
+    steps = (torch.arange(block * dim, dtype=kinds).reshape(block, dim) + 0.5) / (block * dim)
+    x = top[:, None, None] * steps[None]  # within a code's half of every multiple
+    half = (torch.arange(256 * 32, dtype=torch.int64).reshape(block, dim) % 255 - 127).to(kinds) + 0.5
+    y = (top[:, None, None] / 127 * half).clamp(-top[:, None, None], top[:, None, None])  # at the ends of codes, rounded to the type
+    y[:, 0, 0] = top
+    x[:, 0, 0] = -top
+    cache, _, _, cu, start, table = fresh([(0, block)] * n, 1, dim, block, dtype)
+    rows = lambda a: a.reshape(n * block, 1, dim).to(dtype).to(DEV)  # noqa: E731
+    check(cache, rows(x), rows(y), cu, start, table, "ends")
+
+
 def test_strided_views_missing_pages_and_positions_past_the_table():
     cache, k, v, cu, start, table = fresh([(40, 30), (0, 130)], 2, 64, 64, torch.float16)
     rows = torch.full((k.shape[0], 7, 2, 80), float("nan"), dtype=k.dtype, device=DEV)
