@@ -84,16 +84,15 @@ __device__ __forceinline__ uint32_t rescaled(uint32_t w, float ratio)
     return four_codes(c[0], c[1], c[2], c[3]);
 }
 
-// Each wave takes keys or values of one head in one page, by itself: blockIdx.y * 4 + wave counts heads and, in its lowest bit, values.
-// Elements are loaded 8 at a time and stay in registers between the largest and the codes where they fit (64 x 128 do).
+// WAVES waves take keys or values of one head in one page; blockIdx.y (times four and the wave's number if WAVES is 1) counts heads and, in its
+// lowest bit, values.  Elements are loaded 8 at a time and stay in registers between the largest and the codes where they fit (64 x 128 in four
+// waves do).
 // Keys: piece i is row i / (D / 8), channels 8 * (i % (D / 8)).  Values, which are stored with consecutive tokens of a channel
 // together: unit i is 4 tokens (aligned in the page) by 8 channels, turned in registers.
-constexpr int kHeld = 16; // pieces of 8 per lane
-
-template <class T, int D> __global__ void __launch_bounds__(256) append_kernel(const CacheArgs a)
+template <class T, int D, int WAVES> __global__ void __launch_bounds__(256) append_kernel(const CacheArgs a)
 {
-    constexpr int DG = D / 8;
-    const int lane = threadIdx.x & 63, hk = blockIdx.y * 4 + (threadIdx.x >> 6), h = hk >> 1;
+    constexpr int DG = D / 8, LANES = 64 * WAVES, HELD = 4; // HELD: pieces of 8 per lane
+    const int lane = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x, hk = WAVES == 1 ? blockIdx.y * 4 + (threadIdx.x >> 6) : blockIdx.y, h = hk >> 1;
     const bool is_v = hk & 1;
     if (h >= a.cache.heads) return;
     const Piece p = piece_of_item(a, blockIdx.x);
@@ -102,7 +101,7 @@ template <class T, int D> __global__ void __launch_bounds__(256) append_kernel(c
     const int64_t token = is_v ? a.v_token : a.k_token;
     const uint16_t *const x = (is_v ? a.v : a.k) + p.row * token + (int64_t)h * (is_v ? a.v_head : a.k_head);
     const int groups0 = p.lo >> 2, groups = ((p.hi + 3) >> 2) - groups0; // of 4 tokens
-    const int n = is_v ? groups * DG * 4 : (p.hi - p.lo) * DG, batches = (n + 64 * kHeld - 1) / (64 * kHeld);
+    const int n = is_v ? groups * DG * 4 : (p.hi - p.lo) * DG, batches = (n + LANES * HELD - 1) / (LANES * HELD);
 
     if (p.page < 0) return;
     const int64_t slot = p.page * a.cache.heads + h;
@@ -110,14 +109,14 @@ template <class T, int D> __global__ void __launch_bounds__(256) append_kernel(c
     float *const scale = (is_v ? a.cache.v_scales : a.cache.k_scales) + slot;
     const float before = p.lo > 0 ? *scale : 0.0f; // (on its way with the elements)
 
-    w32x4 held[kHeld];
+    w32x4 held[HELD];
     // piece k of a lane's 16 in a batch: keys by 64, values four of one unit after the other
-    const auto past = [&](int batch, int k) { return is_v ? (batch * (kHeld / 4) + k / 4) * 64 >= groups * DG : (batch * kHeld + k) * 64 >= n; };
+    const auto past = [&](int batch, int k) { return is_v ? batch * LANES >= groups * DG : (batch * HELD + k) * LANES >= n; };
     const auto load = [&](int batch) {
 #pragma unroll
-        for (int k = 0; k < kHeld; ++k) {
+        for (int k = 0; k < HELD; ++k) {
             if (past(batch, k)) break;
-            const int i = is_v ? (batch * (kHeld / 4) + k / 4) * 64 + lane : (batch * kHeld + k) * 64 + lane;
+            const int i = is_v ? batch * LANES + lane : (batch * HELD + k) * LANES + lane;
             const int t = is_v ? (groups0 + i % groups) * 4 + k % 4 - p.lo : i / DG, d = is_v ? i / groups : i % DG;
             held[k] = w32x4{0u, 0u, 0u, 0u};
             if (is_v ? d < DG && t >= 0 && t < p.hi - p.lo : i < n) held[k] = load_any<w32x4>(x + t * token + d * 8);
@@ -127,7 +126,7 @@ template <class T, int D> __global__ void __launch_bounds__(256) append_kernel(c
     for (int batch = 0; batch < batches; ++batch) {
         load(batch);
 #pragma unroll
-        for (int k = 0; k < kHeld; ++k) {
+        for (int k = 0; k < HELD; ++k) {
             if (past(batch, k)) break;
 #pragma unroll
             for (int e = 0; e < 4; ++e) peaks = __builtin_elementwise_max(peaks, __builtin_bit_cast(u16x2, held[k][e] & 0x7fff7fffu));
@@ -136,16 +135,30 @@ template <class T, int D> __global__ void __launch_bounds__(256) append_kernel(c
     uint32_t pattern = max(peaks[0], peaks[1]);
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) pattern = max(pattern, (uint32_t)__shfl_xor((int)pattern, d));
+    __shared__ uint32_t s_most[WAVES];
+    if constexpr (WAVES > 1) {
+        if ((lane & 63) == 0) s_most[lane >> 6] = pattern;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) pattern = max(pattern, s_most[w]);
+    }
     float peak = T::widen((uint16_t)pattern);
     const bool infinite = !(peak < INFINITY); // or NaN
     if (infinite) { // (rare: once more, by element)
         peak = 0.0f;
-        for (int i = lane; i < (p.hi - p.lo) * D; i += 64) {
+        for (int i = lane; i < (p.hi - p.lo) * D; i += LANES) {
             const float v = fabsf(T::widen(x[(i / D) * token + i % D]));
             peak = v < INFINITY ? fmaxf(peak, v) : peak;
         }
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) peak = fmaxf(peak, __shfl_xor(peak, d));
+        if constexpr (WAVES > 1) {
+            __syncthreads(); // (the patterns are read)
+            if ((lane & 63) == 0) s_most[lane >> 6] = __builtin_bit_cast(uint32_t, peak);
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) peak = fmaxf(peak, __builtin_bit_cast(float, s_most[w]));
+        }
     }
     const float after = fmaxf(before, __fdiv_rn(peak, 127.0f)), by = after > 0.0f ? after : 1.0f;
     if (lane == 0) *scale = after;
@@ -153,21 +166,21 @@ template <class T, int D> __global__ void __launch_bounds__(256) append_kernel(c
         const float ratio = __fdiv_rn(before, by);
         if (!is_v) {
             uint32_t *const w = reinterpret_cast<uint32_t *>(codes);
-            for (int i = lane; i < p.lo * (D / 4); i += 64) w[i] = rescaled(w[i], ratio);
+            for (int i = lane; i < p.lo * (D / 4); i += LANES) w[i] = rescaled(w[i], ratio);
         } else {
-            for (int i = lane; i < groups0 * D; i += 64) {
+            for (int i = lane; i < groups0 * D; i += LANES) {
                 uint32_t *const w = reinterpret_cast<uint32_t *>(codes + (i / groups0) * block) + i % groups0;
                 *w = rescaled(*w, ratio);
             }
             const int rest = p.lo & 3; // of a group that new tokens share
-            for (int i = lane; i < rest * D; i += 64) {
+            for (int i = lane; i < rest * D; i += LANES) {
                 int8_t *const c = codes + (i / rest) * block + 4 * groups0 + i % rest;
                 *c = (int8_t)code_of((float)*c * ratio);
             }
         }
     }
     if (infinite || divide_by(by)) {
-        for (int i = lane; i < (p.hi - p.lo) * D; i += 64) {
+        for (int i = lane; i < (p.hi - p.lo) * D; i += LANES) {
             const int t = i / D, d = i % D;
             const float v = T::widen(x[t * token + d]);
             codes[is_v ? d * block + p.lo + t : (p.lo + t) * D + d] = (int8_t)(v == v ? code_of(__fdiv_rn(v, by)) : 0);
@@ -177,43 +190,33 @@ template <class T, int D> __global__ void __launch_bounds__(256) append_kernel(c
     const float hi = __fdiv_rn(1.0f, by), lo = hi * fmaf(-by, hi, 1.0f);
     for (int batch = 0; batch < batches; ++batch) {
         if (batches > 1) load(batch);
+        int c[HELD][8];
 #pragma unroll
-        for (int k = 0; k < kHeld; k += 4) {
+        for (int k = 0; k < HELD; ++k) {
             if (past(batch, k)) break;
-            int c[4][8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (!is_v && past(batch, k + j)) break;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float v = T::widen((uint16_t)(held[k + j][e >> 1] >> (e & 1) * 16));
-                    c[j][e] = rounded(fmaf(v, hi, v * lo)); // (no value is over 127 steps of its own page's scale)
-                }
+            for (int e = 0; e < 8; ++e) {
+                const float v = T::widen((uint16_t)(held[k][e >> 1] >> (e & 1) * 16));
+                c[k][e] = rounded(fmaf(v, hi, v * lo)); // (no value is over 127 steps of its own page's scale)
             }
-            if (!is_v) {
+            const int i = (batch * HELD + k) * LANES + lane;
+            if (!is_v && i < n)
+                *reinterpret_cast<w32x2 *>(codes + (int64_t)p.lo * D + i * 8) =
+                    w32x2{four_codes(c[k][0], c[k][1], c[k][2], c[k][3]), four_codes(c[k][4], c[k][5], c[k][6], c[k][7])};
+        }
+        if (!is_v) continue;
+        const int i = batch * LANES + lane, t = (groups0 + i % groups) * 4, d = i / groups;
+        if (d >= DG) continue;
+        int8_t *const to = codes + d * 8 * block + t;
+        if (t >= p.lo && t + 4 <= p.hi) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (past(batch, k + j)) break;
-                    const int i = (batch * kHeld + k + j) * 64 + lane;
-                    if (i < n)
-                        *reinterpret_cast<w32x2 *>(codes + (int64_t)p.lo * D + i * 8) =
-                            w32x2{four_codes(c[j][0], c[j][1], c[j][2], c[j][3]), four_codes(c[j][4], c[j][5], c[j][6], c[j][7])};
-                }
-            } else {
-                const int i = (batch * (kHeld / 4) + k / 4) * 64 + lane, t = (groups0 + i % groups) * 4, d = i / groups;
-                if (d >= DG) continue;
-                int8_t *const to = codes + d * 8 * block + t;
-                if (t >= p.lo && t + 4 <= p.hi) {
+            for (int e = 0; e < 8; ++e) *reinterpret_cast<uint32_t *>(to + e * block) = four_codes(c[0][e], c[1][e], c[2][e], c[3][e]);
+        } else {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) *reinterpret_cast<uint32_t *>(to + e * block) = four_codes(c[0][e], c[1][e], c[2][e], c[3][e]);
-                } else {
+            for (int j = 0; j < 4; ++j)
+                if (t + j >= p.lo && t + j < p.hi)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (t + j >= p.lo && t + j < p.hi)
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) to[e * block + j] = (int8_t)c[j][e];
-                }
-            }
+                    for (int e = 0; e < 8; ++e) to[e * block + j] = (int8_t)c[j][e];
         }
     }
 }
@@ -265,10 +268,13 @@ template <class T, int D> __global__ void __launch_bounds__(256) gather_kernel(c
 
 template <class T, bool GATHER> static void launch_pieces(const CacheArgs &a, hipStream_t s)
 {
-    const dim3 grid((unsigned)(a.tokens / a.cache.block + 2 * (int64_t)a.requests), (unsigned)(GATHER ? 2 * a.cache.heads : (2 * a.cache.heads + 3) / 4));
+    // from 8 new tokens per request on average a page's part is four waves' work
+    const bool alone = a.tokens < 8 * (int64_t)a.requests;
+    const dim3 grid((unsigned)(a.tokens / a.cache.block + 2 * (int64_t)a.requests), (unsigned)(GATHER || !alone ? 2 * a.cache.heads : (2 * a.cache.heads + 3) / 4));
     const auto with = [&](auto dim) {
         if constexpr (GATHER) hipLaunchKernelGGL((gather_kernel<T, dim>), grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((append_kernel<T, dim>), grid, dim3(256), 0, s, a);
+        else if (alone) hipLaunchKernelGGL((append_kernel<T, dim, 1>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((append_kernel<T, dim, 4>), grid, dim3(256), 0, s, a);
     };
     switch (a.cache.dim) {
     case 64: with(std::integral_constant<int, 64>{}); break;

@@ -29,7 +29,8 @@ def check(cache, k, v, cu, start, table, what):
 @pytest.mark.parametrize("requests,heads,dim,block", [
     ([(0, 1)], 1, 64, 32), ([(5, 1), (63, 1), (64, 1), (0, 0), (127, 1)], 2, 128, 64), ([(0, 300), (17, 100), (64, 64), (0, 0), (31, 33), (1, 0)], 3, 96, 64),
     ([(30, 5), (32, 31), (0, 32), (100, 1)], 2, 192, 32), ([(0, 129), (127, 2), (200, 57)], 1, 256, 128), ([(10, 200), (0, 700)], 2, 64, 256),
-    ([(7, 90)], 2, 128, 96), ([(i * 7 % 50, i % 4) for i in range(150)], 1, 64, 32)])
+    ([(7, 90)], 2, 128, 96), ([(i * 7 % 50, i % 4) for i in range(150)], 1, 64, 32),
+    ([(i, 1) for i in range(70)] + [(3, 300), (250, 90)], 3, 96, 256)])
 def test_append_bit_for_bit(requests, heads, dim, block, dtype):
     # small, like and large against what the pages hold: scales stay, or grow and the codes held are rescaled
     for scale in (0.01, 0.6, 5.0):
