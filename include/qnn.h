@@ -343,7 +343,8 @@ qnn_status qnn_qdwconv2d_asym(const uint8_t *x, int N, int H, int W, int C, int3
  * (two's complement, element 2j in the low one), K even.  scales: DEVICE [ceil(K / group)][N] of `type`.
  * zeros: DEVICE int8 [ceil(K / group)][N], or NULL for symmetric weights.  bias: DEVICE [N] of `type` or NULL.
  * group: a multiple of 32 (one scale per row: any such number >= K).  y: DEVICE, M x N of `type`, row pitch ldy >= N (written).
- * M == 0 is a no-op.  workspace: DEVICE scratch, 16-byte aligned, of at least qnn_w4_matmul_workspace_bytes bytes (NULL where that
+ * M up to 2^20 (0 is a no-op), N up to 2^28, K up to 2^24, and fewer than 2^30 scales.
+ * workspace: DEVICE scratch, 16-byte aligned, of at least qnn_w4_matmul_workspace_bytes bytes (NULL where that
  * is 0), else QNN_EINVAL. */
 qnn_status qnn_w4_matmul(const void *x, int64_t ldx, const uint8_t *codes, const void *scales, const int8_t *zeros,
                          const void *bias, int64_t M, int64_t N, int64_t K, int64_t group, int type, void *y, int64_t ldy,
@@ -358,7 +359,8 @@ const char *qnn_w4_matmul_plan(int64_t M, int64_t N, int64_t K, int64_t group);
  * request's tokens j * block ... is table[request][j].  A value is code * scale, codes within [-127, 127] and
  * one scale per page and head.  Values lie transposed: consecutive tokens of a channel are what the product
  * with the probabilities reads at once.  All four arrays DEVICE, contiguous, 16-byte aligned.
- * dim: 64, 96, 128, 192 or 256.  block: a multiple of 32 up to 256. */
+ * dim: 64, 96, 128, 192 or 256.  block: a multiple of 32 up to 256.  Scales have to be finite and not negative (a cache of zeros is a
+ * right beginning; codes and scales of places that hold no token are not used). */
 typedef struct qnn_kv_cache {
     int8_t *k_codes; /* [pages][heads][block][dim] */
     float *k_scales; /* [pages][heads] */
@@ -376,7 +378,7 @@ typedef struct qnn_kv_cache {
  * in binary32, round() with ties away from zero.
  * k, v: DEVICE [tokens][heads][dim] of `type`; element (t, h, d) at t * token_pitch + h * head_pitch + d (elements).
  * cu: DEVICE int32 [requests + 1], not decreasing, cu[0] == 0, cu[requests] <= tokens.  start: DEVICE int32 [requests].
- * table: DEVICE int32 [requests][table_width].  A page must not be reached by two requests of one call.  Entries outside
+ * table: DEVICE int32 [requests][table_width]; requests up to 2^20, tokens below 2^30, table_width * block below 2^31.  A page must not be reached by two requests of one call.  Entries outside
  * [0, pages) and tokens past table_width * block are left out. */
 qnn_status qnn_kv_append(const qnn_kv_cache *cache, const void *k, int64_t k_token_pitch, int64_t k_head_pitch, const void *v,
                          int64_t v_token_pitch, int64_t v_head_pitch, int type, const int32_t *cu, const int32_t *start,
@@ -398,7 +400,7 @@ qnn_status qnn_kv_gather(const qnn_kv_cache *cache, const int32_t *cu, const int
  * q, out: DEVICE [tokens][q_heads][dim] of `type`, element (t, e, d) of q at t * q_token_pitch + e * q_head_pitch + d; out
  * contiguous (rows of requests are written).  lse: DEVICE float [tokens][q_heads] or NULL.
  * max_queries: the largest number of queries of a request (more are computed too, slower); max_queries <= 0: tokens.
- * Page numbers outside [0, pages) count as tokens that nothing sees.
+ * Page numbers outside [0, pages) count as tokens that nothing sees.  tokens * q_heads / heads below 2^31, the rest as above.
  * workspace: DEVICE, 16-byte aligned, of at least qnn_kv_attention_workspace_bytes bytes for the same sizes, else QNN_EINVAL. */
 qnn_status qnn_kv_attention(const qnn_kv_cache *cache, const void *q, int64_t q_token_pitch, int64_t q_head_pitch,
                             int32_t q_heads, int type, const int32_t *cu, const int32_t *lengths, const int32_t *table,

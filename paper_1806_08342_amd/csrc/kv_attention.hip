@@ -12,6 +12,9 @@
 // after the other in its part of the value product: the probabilities go from the first product into the second in the lane
 // that holds them, without LDS or shuffles.  Keys and values come straight from memory into registers: each wave
 // reads tokens of its own, so nothing would be shared through LDS.
+//
+// Bound by reading codes: 4 contexts of 131072 tokens, 40 query heads of 128 over 8: 185 us, 5.8 TB/s; 32 up to 8000, 64 heads over 8: 65 us, where
+// the longest contexts end last; one of 777: 9.5 us, two launches (7 and 2.5) and a chain of loads.
 #include "kv_attention.h"
 #include "kv_prompt.h"
 #include "kv_prompt_wide.h"
@@ -372,6 +375,25 @@ static void divide_context(AttendLaunch &p, int64_t reach, int64_t groups, int64
     if (p.chunks < 1) p.chunks = 1;
 }
 
+// The same for requests with many rows, into at most 16.  A workgroup takes 4 us to begin and, for each 64 tokens, 2.5 us for heads up to 128,
+// 3.8 for 192 and 5 for 256; the chip has 256 of 8 waves at a time, twice as many of 4; of a prompt's tokens a row sees half; parts are written
+// and read at 6 TB/s, the latter in a launch of 5 us.  (Two prompts up to 1616, 8 query heads of 192: 86 us undivided, 84 in two chunks; five of 387, 2 of
+// 128: 21 and 20.)
+static void divide_prompts(AttendLaunch &p, int64_t reach, int64_t groups, int64_t blocks, int64_t rows, int dim, bool half)
+{
+    const int64_t units = (reach + 63) / 64;
+    const double unit_us = dim > 128 ? dim / 51.0 : 2.5, share = (dim > 128 || p.waves == 8 ? 1.0 : 0.5) * (double)(groups * blocks) / 256.0;
+    double best = 0.0;
+    for (int64_t n = 1; n <= 16 && n <= (units > 1 ? units : 1); n *= 2) {
+        const double one = 4.0 + (double)((units + n - 1) / n) * unit_us, all = share * ((double)units * (half ? 0.5 : 1.0) * unit_us + 4.0 * (double)n);
+        const double us = (one > all ? one : all) + (n > 1 ? 5.0 + (double)(rows * groups * dim * n) * 8.0 / 6.0e6 : 0.0);
+        if (n == 1 || us < best) best = us, p.chunk_tokens = (units + n - 1) / n * 64;
+    }
+    if (p.chunk_tokens < 64) p.chunk_tokens = 64;
+    p.chunks = (int)((reach + p.chunk_tokens - 1) / p.chunk_tokens);
+    if (p.chunks < 1) p.chunks = 1;
+}
+
 constexpr int kFewRows = 64;
 
 static AttendPlan attend_plan(const qnn_kv_cache &cache, int q_heads, int64_t table_width, int64_t requests, int64_t tokens, int64_t window,
@@ -402,13 +424,7 @@ static AttendPlan attend_plan(const qnn_kv_cache &cache, int q_heads, int64_t ta
         const int64_t blocks = (rows + 32 * p.many.waves - 1) / (32 * p.many.waves);
         p.many.row_blocks = (int)(blocks < 4096 ? blocks : 4096);
         p.many.part_rows = (int)rows;
-        // (prompts fill the chip by themselves; a few hundred rows over a long context are divided into at most 16)
-        int64_t n = groups * blocks < 512 ? 512 / (groups * blocks) : 1;
-        if (n > 16) n = 16;
-        const int64_t chunk = ((reach + n - 1) / n + 255) / 256 * 256;
-        p.many.chunk_tokens = chunk < 1024 ? 1024 : chunk;
-        p.many.chunks = (int)((reach + p.many.chunk_tokens - 1) / p.many.chunk_tokens);
-        if (p.many.chunks < 1) p.many.chunks = 1;
+        divide_prompts(p.many, reach, groups, blocks, rows, cache.dim, max_queries * 2 > reach);
     }
     return p;
 }
@@ -426,8 +442,8 @@ template <class T, int D> static void run_many(const AttendArgs &a, const Attend
 {
     const dim3 grid((unsigned)((int64_t)a.requests * p.row_blocks * p.chunks * a.cache.heads));
     if constexpr (D > 128) hipLaunchKernelGGL((attend_wide_kernel<T, D>), grid, dim3(512), 0, s, a);
-    else if (p.waves == 4) hipLaunchKernelGGL((attend_prompt_kernel<T, D, 4, 1>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((attend_prompt_kernel<T, D, 8, 1>), grid, dim3(512), 0, s, a);
+    else if (p.waves == 4) hipLaunchKernelGGL((attend_prompt_kernel<T, D, 4>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((attend_prompt_kernel<T, D, 8>), grid, dim3(512), 0, s, a);
 }
 
 template <class T, int D, int U> static void run_join(const AttendArgs &a, hipStream_t s)

@@ -1,5 +1,5 @@
-// Attention over the cache for requests with many query rows: 32 rows per wave and row tile, keys and values of 64 tokens at a
-// time in LDS, as binary16.
+// Attention over the cache for requests with many query rows: 32 rows per wave, keys and values of 64 tokens at a time in LDS, as
+// binary16.
 //
 // 8-bit codes are converted once for all waves of the workgroup, on the way from memory to LDS (two buffers: the codes of the next
 // 64 tokens are in flight while these are worked on).  S^T = K q^T and O^T = V^T p^T on 32x32x16 tiles; as in the kernel for few
@@ -10,6 +10,12 @@
 // 2^kRoom times the reference and a page's value scale within 2^kRoom of it, so that most units rescale nothing.  A page's
 // value scale is part of the exponent (p * vs / reference), and the sum of p is corrected once per tile; for a tile whose value
 // scale is below 2^-20 of its unit's other tile's, or zero, the sum is formed separately.
+//
+// Bound by the two things that a wave does in turn: products (4 D flops per row and token, at 31 % of the matrix units' cycles) and the
+// softmax between them (an exponential, four more operations and half a conversion per score, 49 % of the vector unit's); two waves on
+// a SIMD seldom overlap them, as all wait at one barrier for 64 tokens.  8192 tokens, 32 query heads of 128 over 8: 650 us, 840
+// TFLOP/s of the half that the mask leaves.  Forms that interleave a unit's products with the next one's softmax in a
+// wave, or let the waves of a SIMD alternate, lost more to registers and scalar work than they gained.
 #pragma once
 
 #include "kv_attention.h"
@@ -25,9 +31,9 @@ __device__ __forceinline__ float other_half(float v)
     return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
 }
 
-template <class T, int D, int WAVES, int RT> __global__ void __launch_bounds__(64 * WAVES, D <= 128 ? 2 : 1) attend_prompt_kernel(const AttendArgs a)
+template <class T, int D, int WAVES> __global__ void __launch_bounds__(64 * WAVES, D <= 128 ? 2 : 1) attend_prompt_kernel(const AttendArgs a)
 {
-    constexpr int BR = 32 * RT * WAVES, KS = D / 16, VT = D / 32;
+    constexpr int BR = 32 * WAVES, KS = D / 16, VT = D / 32;
     constexpr int PIECES = (4 * D + 64 * WAVES - 1) / (64 * WAVES); // 16-byte pieces of 64 tokens' keys (or values) per thread
     constexpr bool EVEN = 4 * D % (64 * WAVES) == 0;
     constexpr int KP = D + 8, VP = 64 + 8; // pitches in LDS: 16 bytes more than the row, so that rows start in different banks
@@ -38,7 +44,7 @@ template <class T, int D, int WAVES, int RT> __global__ void __launch_bounds__(6
     const int heads = a.cache.heads, block = a.cache.block;
     // heads next to each other: workgroups are dealt to the XCDs in turn, so that one XCD's L2 holds few heads' keys and values
     const int h = blockIdx.x % heads, rest = blockIdx.x / heads;
-    // (the last rows of all requests, which see most tokens, go first)
+    // the last rows of all requests, which see most tokens, go first
     const int chunk = rest % a.chunks, r = rest / a.chunks % a.requests, rb0 = rest / a.chunks / a.requests;
     const Request rq = request_of<64>(a, r);
     const int rows = rq.n * a.group;
@@ -47,7 +53,6 @@ template <class T, int D, int WAVES, int RT> __global__ void __launch_bounds__(6
     if (chunk >= chunks) return;
     const int blocks = (rows + BR - 1) / BR;
 
-    // the last rows see most tokens: they go first
     for (int rb = blocks - 1 - rb0; rb >= 0; rb -= a.row_blocks) {
         const int rt = rb * BR;
         const int64_t pos0 = rq.length - rq.n; // position of the first query
@@ -58,14 +63,13 @@ template <class T, int D, int WAVES, int RT> __global__ void __launch_bounds__(6
         const int units = t1 > t0 ? (int)((t1 - t0 + 63) / 64) : 0;
 
         // this wave's rows
-        h16x8 qf[RT][KS];
-        float factor[RT];
-        int64_t pos[RT], row_id[RT];
-#pragma unroll
-        for (int x = 0; x < RT; ++x) {
-            const int row = rt + (wave * RT + x) * 32 + c, qi = min(row, rows - 1) / a.group, e = min(row, rows - 1) % a.group;
-            pos[x] = row < rows ? pos0 + qi : -1;
-            row_id[x] = (rq.row0 + qi) * a.q_heads + h * a.group + e;
+        h16x8 qf[KS];
+        float factor;
+        int64_t pos, row_id;
+        {
+            const int row = rt + wave * 32 + c, qi = min(row, rows - 1) / a.group, e = min(row, rows - 1) % a.group;
+            pos = row < rows ? pos0 + qi : -1;
+            row_id = (rq.row0 + qi) * a.q_heads + h * a.group + e;
             const uint16_t *q = a.q + (rq.row0 + qi) * a.q_token_pitch + (int64_t)(h * a.group + e) * a.q_head_pitch + 8 * hh;
             w32x4 raw[KS];
             float peak = 0.0f;
@@ -78,26 +82,22 @@ template <class T, int D, int WAVES, int RT> __global__ void __launch_bounds__(6
                     for (int i = 0; i < 8; ++i) peak = fmaxf(peak, fabsf(T::widen((uint16_t)(raw[k][i >> 1] >> (i & 1) * 16))));
             const int ex = std::is_same_v<T, F16> ? 0 : row_exponent(fmaxf(peak, other_half(peak)));
             const float down = ldexpf(a.scale < 0.0f ? -1.0f : 1.0f, -ex); // (scores grow with the products: the sign goes to q)
-            factor[x] = fabsf(a.scale) * ldexpf(1.0f, ex);
+            factor = fabsf(a.scale) * ldexpf(1.0f, ex);
 #pragma unroll
             for (int k = 0; k < KS; ++k)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) qf[x][k][i] = (_Float16)(T::widen((uint16_t)(raw[k][i >> 1] >> (i & 1) * 16)) * down);
+                for (int i = 0; i < 8; ++i) qf[k][i] = (_Float16)(T::widen((uint16_t)(raw[k][i >> 1] >> (i & 1) * 16)) * down);
         }
-        const int wave_row = rt + wave * RT * 32;
-        const int64_t wave_first = pos0 + wave_row / a.group, wave_last = pos0 + min(wave_row + 32 * RT - 1, rows - 1) / a.group;
+        const int wave_row = rt + wave * 32;
+        const int64_t wave_first = pos0 + wave_row / a.group, wave_last = pos0 + min(wave_row + 31, rows - 1) / a.group;
         const bool idle = wave_row >= rows;
 
-        f32x16 o[RT][VT];
-        float m[RT], l[RT];
+        f32x16 o[VT];
+        float m = kNothing, l = 0.0f;
 #pragma unroll
-        for (int x = 0; x < RT; ++x) {
-            m[x] = kNothing, l[x] = 0.0f;
+        for (int v = 0; v < VT; ++v)
 #pragma unroll
-            for (int v = 0; v < VT; ++v)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[x][v][i] = 0.0f;
-        }
+            for (int i = 0; i < 16; ++i) o[v][i] = 0.0f;
         float reference = 0.0f; // the value scale that o stands in; 0: none yet
 
         // lane i holds place and scales of the i-th of 64 halves (32 tokens)
@@ -173,125 +173,106 @@ template <class T, int D, int WAVES, int RT> __global__ void __launch_bounds__(6
                 load(u + 1);
             }
             if (!idle && t <= wave_last && !(a.window > 0 && t + 63 <= wave_first - a.window)) {
-                f32x16 s[RT][2];
+                f32x16 s[2];
 #pragma unroll
-                for (int x = 0; x < RT; ++x)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[x][0][i] = s[x][1][i] = 0.0f;
+                    for (int i = 0; i < 16; ++i) s[0][i] = s[1][i] = 0.0f;
 #pragma unroll
                 for (int k = 0; k < KS; ++k)
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
                         const h16x8 kf = *reinterpret_cast<const h16x8 *>(&s_k[buf][32 * y + c][16 * k + 8 * hh]);
-#pragma unroll
-                        for (int x = 0; x < RT; ++x) s[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[x][k], s[x][y], 0, 0, 0);
+                        s[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[k], s[y], 0, 0, 0);
                     }
                 if (missing[0] || missing[1] || t + 63 > wave_first || (a.window > 0 && t <= wave_last - a.window)) {
                     asm volatile(""); // (a branch: few units are cut)
+                    const int64_t base = t + 8 * hh;
+                    const int to = (int)min(pos - base, (int64_t)64);
+                    const int from = a.window > 0 ? (int)min(max(pos - a.window - base, (int64_t)-1), (int64_t)64) : -1;
 #pragma unroll
-                    for (int x = 0; x < RT; ++x) {
-                        const int64_t base = t + 8 * hh;
-                        const int to = (int)min(pos[x] - base, (int64_t)64);
-                        const int from = a.window > 0 ? (int)min(max(pos[x] - a.window - base, (int64_t)-1), (int64_t)64) : -1;
+                    for (int y = 0; y < 2; ++y)
 #pragma unroll
-                        for (int y = 0; y < 2; ++y)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                const int at = 32 * y + 16 * (i >> 3) + (i & 7);
-                                s[x][y][i] = (at <= to && at > from && !missing[y]) ? s[x][y][i] : -INFINITY;
-                            }
-                    }
+                        for (int i = 0; i < 16; ++i) {
+                            const int at = 32 * y + 16 * (i >> 3) + (i & 7);
+                            s[y][i] = (at <= to && at > from && !missing[y]) ? s[y][i] : -INFINITY;
+                        }
                 }
                 // references that no longer do
-                float most[RT], fk[RT][2];
+                float most, fk[2];
                 bool grew = false;
+                float top[2];
 #pragma unroll
-                for (int x = 0; x < RT; ++x) {
-                    float top[2];
+                for (int y = 0; y < 2; ++y) {
+                    fk[y] = fmaxf(factor * ks[y], 1e-30f); // (not 0: minus infinity stays that)
+                    top[y] = s[y][0];
 #pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        fk[x][y] = fmaxf(factor[x] * ks[y], 1e-30f); // (not 0: minus infinity stays that)
-                        top[y] = s[x][y][0];
-#pragma unroll
-                        for (int i = 1; i < 16; ++i) top[y] = fmaxf(top[y], s[x][y][i]);
-                        top[y] *= fk[x][y];
-                    }
-                    most[x] = fmaxf(top[0], top[1]);
-                    most[x] = fmaxf(most[x], other_half(most[x]));
-                    grew |= most[x] > m[x] + kRoom;
+                    for (int i = 1; i < 16; ++i) top[y] = fmaxf(top[y], s[y][i]);
+                    top[y] *= fk[y];
                 }
+                most = fmaxf(top[0], top[1]);
+                most = fmaxf(most, other_half(most));
+                grew |= most > m + kRoom;
                 const float vmost = fmaxf(vs[0], vs[1]);
                 const bool change = vmost > 0.0f && !(vmost < 16.0f * reference && vmost > 0.0625f * reference);
                 if (__any(grew) || change) {
                     const float to_new = change ? (reference > 0.0f ? reference / vmost : 0.0f) : 1.0f;
                     reference = change ? vmost : reference;
+                    const float now = fmaxf(m, most), shrink = exp2_fast(m - now), by = shrink * to_new;
+                    m = now, l *= shrink;
 #pragma unroll
-                    for (int x = 0; x < RT; ++x) {
-                        const float now = fmaxf(m[x], most[x]), shrink = exp2_fast(m[x] - now), by = shrink * to_new;
-                        m[x] = now, l[x] *= shrink;
-#pragma unroll
-                        for (int v = 0; v < VT; ++v) o[x][v] *= by;
-                    }
+                    for (int v = 0; v < VT; ++v) o[v] *= by;
                 }
-                h16x8 p[RT][4];
+                h16x8 p[4];
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
                     const float ratio = vmost > 0.0f ? vs[y] * __builtin_amdgcn_rcpf(reference) : 0.0f;
                     const bool small = !(ratio > 0x1p-20f);
                     const float up = __log2f(ratio) + kPromptHead, down = small ? 0.0f : __builtin_amdgcn_rcpf(ratio); // (takes out what `up` has brought in)
+                    if (small)
 #pragma unroll
-                    for (int x = 0; x < RT; ++x) {
-                        if (small)
+                        for (int i = 0; i < 16; ++i) l += exp2_fast(fmaf(s[y][i], fk[y], kPromptHead - m));
+                    const float off = up - m;
+                    float sum = 0.0f;
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) l[x] += exp2_fast(fmaf(s[x][y][i], fk[x][y], kPromptHead - m[x]));
-                        const float off = up - m[x];
-                        float sum = 0.0f;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const float e = exp2_fast(fmaf(s[x][y][i], fk[x][y], off));
-                            sum += e;
-                            p[x][2 * y + (i >> 3)][i & 7] = (_Float16)e;
-                        }
-                        l[x] = fmaf(sum, down, l[x]);
+                    for (int i = 0; i < 16; ++i) {
+                        const float e = exp2_fast(fmaf(s[y][i], fk[y], off));
+                        sum += e;
+                        p[2 * y + (i >> 3)][i & 7] = (_Float16)e;
                     }
+                    l = fmaf(sum, down, l);
                 }
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
 #pragma unroll
                     for (int v = 0; v < VT; ++v) {
                         const h16x8 vf = *reinterpret_cast<const h16x8 *>(&s_v[buf][32 * v + c][16 * k + 8 * hh]);
-#pragma unroll
-                        for (int x = 0; x < RT; ++x) o[x][v] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p[x][k], o[x][v], 0, 0, 0);
+                        o[v] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p[k], o[v], 0, 0, 0);
                     }
             }
             if (u + 1 < units) stage(buf ^ 1);
             __syncthreads();
         }
 
+        l += other_half(l);
+        if (wave_row + c >= rows) continue;
+        if (chunks == 1) {
+            const float inv = l != 0.0f ? reference / l : 0.0f;
+            uint16_t *out = a.out + row_id * D + 4 * hh;
 #pragma unroll
-        for (int x = 0; x < RT; ++x) {
-            l[x] += other_half(l[x]);
-            if (wave_row + x * 32 + c >= rows) continue;
-            if (chunks == 1) {
-                const float inv = l[x] != 0.0f ? reference / l[x] : 0.0f;
-                uint16_t *out = a.out + row_id[x] * D + 4 * hh;
+            for (int v = 0; v < VT; ++v)
 #pragma unroll
-                for (int v = 0; v < VT; ++v)
+                for (int i = 0; i < 16; i += 4)
+                    *reinterpret_cast<w32x2 *>(out + 32 * v + 2 * i) = w32x2{narrow2<T>(o[v][i] * inv, o[v][i + 1] * inv), narrow2<T>(o[v][i + 2] * inv, o[v][i + 3] * inv)};
+            if (a.lse && hh == 0) a.lse[row_id] = l != 0.0f ? (m - kPromptHead + log2f(l)) * 0.69314718056f : -INFINITY;
+        } else {
+            const int64_t part = part_row(a, r, h, rt + wave * 32 + c) * a.chunks + chunk;
 #pragma unroll
-                    for (int i = 0; i < 16; i += 4)
-                        *reinterpret_cast<w32x2 *>(out + 32 * v + 2 * i) = w32x2{narrow2<T>(o[x][v][i] * inv, o[x][v][i + 1] * inv), narrow2<T>(o[x][v][i + 2] * inv, o[x][v][i + 3] * inv)};
-                if (a.lse && hh == 0) a.lse[row_id[x]] = l[x] != 0.0f ? (m[x] - kPromptHead + log2f(l[x])) * 0.69314718056f : -INFINITY;
-            } else {
-                const int64_t part = part_row(a, r, h, rt + (wave * RT + x) * 32 + c) * a.chunks + chunk;
+            for (int v = 0; v < VT; ++v)
 #pragma unroll
-                for (int v = 0; v < VT; ++v)
-#pragma unroll
-                    for (int i = 0; i < 16; i += 4)
-                        *reinterpret_cast<f32x4 *>(a.part_o + part * D + 32 * v + 2 * i + 4 * hh) =
-                            f32x4{o[x][v][i] * reference, o[x][v][i + 1] * reference, o[x][v][i + 2] * reference, o[x][v][i + 3] * reference};
-                // (the join takes maxima with the head room of the kernel for few rows)
-                if (hh == 0) a.part_ml[2 * part] = m[x] + (kHead - kPromptHead), a.part_ml[2 * part + 1] = l[x];
-            }
+                for (int i = 0; i < 16; i += 4)
+                    *reinterpret_cast<f32x4 *>(a.part_o + part * D + 32 * v + 2 * i + 4 * hh) =
+                        f32x4{o[v][i] * reference, o[v][i + 1] * reference, o[v][i + 2] * reference, o[v][i + 3] * reference};
+            // (the join takes maxima with the head room of the kernel for few rows)
+            if (hh == 0) a.part_ml[2 * part] = m + (kHead - kPromptHead), a.part_ml[2 * part + 1] = l;
         }
     }
 }

@@ -1,6 +1,9 @@
 // The kernel for many query rows, for large heads: accumulators and queries of 32 rows would leave no registers for two waves on
 // a SIMD (heads of 256: 512 registers, most of them copied to and fro between the register file's halves, 5 us for 64 tokens by 128 rows).  Here a
 // wave has 16 rows, on 16x16x32 tiles: twice the reads from LDS for each product, but eight waves.
+// Five prompts up to 2047, 16 query heads of 256 over 4: 194 us (249 with 32 rows per wave), 455 TFLOP/s.  LDS is read in 31 % of the cycles,
+// the vector unit works in 35 and the matrix units in 20, one after the other; the longest block of rows is as
+// long as the others' average on a CU, which costs another fifth.
 #pragma once
 
 #include "kv_prompt.h"
@@ -26,7 +29,7 @@ template <class T, int D> __global__ void __launch_bounds__(512, 2) attend_wide_
     const int heads = a.cache.heads, block = a.cache.block;
     // heads next to each other: workgroups are dealt to the XCDs in turn, so that one XCD's L2 holds few heads' keys and values
     const int h = blockIdx.x % heads, rest = blockIdx.x / heads;
-    // (the last rows of all requests, which see most tokens, go first)
+    // the last rows of all requests, which see most tokens, go first
     const int chunk = rest % a.chunks, r = rest / a.chunks % a.requests, rb0 = rest / a.chunks / a.requests;
     const Request rq = request_of<64>(a, r);
     const int rows = rq.n * a.group;
@@ -35,7 +38,6 @@ template <class T, int D> __global__ void __launch_bounds__(512, 2) attend_wide_
     if (chunk >= chunks) return;
     const int blocks = (rows + BR - 1) / BR;
 
-    // the last rows see most tokens: they go first
     for (int rb = blocks - 1 - rb0; rb >= 0; rb -= a.row_blocks) {
         const int rt = rb * BR;
         const int64_t pos0 = rq.length - rq.n; // position of the first query

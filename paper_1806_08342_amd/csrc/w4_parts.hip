@@ -3,7 +3,8 @@
 // With the kernel for few rows every wave reads all of x for its rows of weights, from the L2: at 24 rows that is more
 // bytes than the weights are (24 x 28672 x 8192: 49 us, as long as the L2 needs for them).  Here the waves of a workgroup are NW times 32 rows of weights
 // by PARTS parts of K: the waves of a part read one copy of x, which comes into LDS by itself, in a ring.  Arithmetic as
-// in the kernel for many rows.
+// in the kernel for many rows.  24 x 28672 x 8192: 33 us, 3.7 TB/s of codes (224 workgroups leave 32 CUs without one, and each reads x, two
+// thirds of the bytes of its codes, from the L2), and 5 us before it for the launch that writes x as binary16.
 #include "buffer_ops.h"
 #include "lds_ring.h"
 #include "w4.h"
