@@ -2,8 +2,9 @@
 // a SIMD (heads of 256: 512 registers, most of them copied to and fro between the register file's halves, 5 us for 64 tokens by 128 rows).  Here a
 // wave has 16 rows, on 16x16x32 tiles: twice the reads from LDS for each product, but eight waves.
 // Five prompts up to 2047, 16 query heads of 256 over 4: 194 us (249 with 32 rows per wave), 455 TFLOP/s.  LDS is read in 31 % of the cycles,
-// the vector unit works in 35 and the matrix units in 20, one after the other; the longest block of rows is as
-// long as the others' average on a CU, which costs another fifth.
+// the vector unit works in 35 and the matrix units in 20; a wave waits half of its time, for LDS, for results of its own
+// and at the barrier, and registers and LDS have no room for more waves.  (Letting the second wave of each SIMD stage tokens before its products
+// and the first after them changed nothing; uneven ends cost a tenth.)
 #pragma once
 
 #include "kv_prompt.h"
