@@ -240,9 +240,11 @@ static bool bad_w4_sizes(int64_t M, int64_t N, int64_t K, int64_t group)
 // Which kernel, by what each is estimated to take (us):
 // few rows: weights at 4 TB/s and x, read again for every 16 or 32 rows of weights, at 9 TB/s from the L2 (measured / estimated at
 // 16 rows: 4096 x 4096 7.8 / 8.3, 12288 x 4096 19.5 / 20, 28672 x 8192 51 / 58);
-// tens: see w4_parts.hip;  many: 2 us for a round of tiles and 128 of K (200 rows x 28672 x 8192 132 / 133, 1000: 444 / 453).
+// tens: see w4_parts.hip;  many: for a round of tiles and 128 of K 2 us with groups of whole 128s (200 rows x 28672 x 8192 132 / 133, 1000: 444 /
+// 453), else, for 64 rows, 1.3 with groups of 64s (1000: 570 / 587; 2000 x 12288 x 4096 271 / 255) and 1.65 with smaller ones (333 / 322).  With these
+// groups the kernel for tens takes 1.35 and 1.75 times as long as with whole 128s (2000 x 12288 x 4096 330 / 315 and 416 / 408).
 enum class W4Kernel { Few, Tens, Many };
-static W4Kernel w4_kernel(int64_t M, int64_t N, int64_t K)
+static W4Kernel w4_kernel(int64_t M, int64_t N, int64_t K, int64_t group)
 {
     // (longer rows than the other kernels' offsets reach stay with that for few)
     if (K > (1 << 21)) return W4Kernel::Few;
@@ -251,27 +253,29 @@ static W4Kernel w4_kernel(int64_t M, int64_t N, int64_t K)
         const float weights = (float)N * (float)K * 0.5e-6f;
         return 2.5f + weights * (0.25f + (float)M / (float)(36 * few_tiles(N))) <= tens ? W4Kernel::Few : W4Kernel::Tens;
     }
-    const int64_t tiles = (M + 127) / 128 * ((N + 255) / 256);
+    const bool whole = group % 128 == 0 || group >= K;
+    const int64_t tiles = (whole ? (M + 127) / 128 : (M + 63) / 64) * ((N + 255) / 256);
     const float rounds = tiles <= 256 ? 1.0f : (float)tiles / 256.0f;
-    return 5.0f + rounds * (float)((K + 127) / 128) * 2.0f < tens ? W4Kernel::Many : W4Kernel::Tens;
+    const float step_us = whole ? 2.0f : group % 64 == 0 ? 1.3f : 1.65f, longer = whole ? 1.0f : group % 64 == 0 ? 1.35f : 1.75f;
+    return rounds * (float)((K + 127) / 128) * step_us < (tens - 5.0f) * longer ? W4Kernel::Many : W4Kernel::Tens; // (and 5 us for either)
 }
 
 size_t qnn_w4_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t group)
 {
-    if (bad_w4_sizes(M, N, K, group) || M == 0 || w4_kernel(M, N, K) == W4Kernel::Few) return 0;
+    if (bad_w4_sizes(M, N, K, group) || M == 0 || w4_kernel(M, N, K, group) == W4Kernel::Few) return 0;
     return w4_prepared_bytes(M, K);
 }
 
 const char *qnn_w4_matmul_plan(int64_t M, int64_t N, int64_t K, int64_t group)
 {
     if (bad_w4_sizes(M, N, K, group) || M == 0) return "";
-    switch (w4_kernel(M, N, K)) {
+    switch (w4_kernel(M, N, K, group)) {
     case W4Kernel::Few: {
         static const char *const names[] = {"few16x16/4", "few16x32/8", "few16x16/8", "few16x16/16"};
         return names[few_form(N, (K + group - 1) / group)];
     }
     case W4Kernel::Tens: return w4_parts_name(M, N, K);
-    default: return "many128x256";
+    default: return group % 128 == 0 || group >= K ? "many128x256" : "many64x256";
     }
 }
 
@@ -286,7 +290,7 @@ qnn_status qnn_w4_matmul(const void *x, int64_t ldx, const uint8_t *codes, const
     W4Args a{static_cast<const uint16_t *>(x), codes, static_cast<const uint16_t *>(scales), zeros, static_cast<const uint16_t *>(bias),
                    static_cast<uint16_t *>(y), ldx, ldy, (int32_t)M, (int32_t)N, (int32_t)K, (int32_t)(group < K ? group : (K + 127) / 128 * 128), (int32_t)((K + group - 1) / group), 0, 0, (((uintptr_t)codes | (uintptr_t)(K / 2)) & 3) != 0};
     fast_division((uint32_t)a.group / 32, a.group_magic, a.group_shift);
-    if (const W4Kernel kernel = w4_kernel(M, N, K); kernel != W4Kernel::Few) {
+    if (const W4Kernel kernel = w4_kernel(M, N, K, group); kernel != W4Kernel::Few) {
         const W4Prepared p = prepared(workspace, M, K);
         prepare_x(a, type, p, as_stream(stream));
         if (kernel == W4Kernel::Many) launch_w4_tile(a, type, p, as_stream(stream));

@@ -110,7 +110,8 @@ FORMS = {"few16x16/4": (3, 3, 30), "few16x32/8": (5, 17001, 330), "few16x16/8": 
 @pytest.mark.parametrize("form", FORMS)
 def test_every_form(form, group, zeros, dtype):
     M, N, K = FORMS[form]
-    assert qnn.w4_matmul_plan(M, N, K, 128) == form and (form == "few16x16/4" or qnn.w4_matmul_plan(M, N, K, group) == form)
+    with_group = "many64x256" if form == "many128x256" and group != 128 else form
+    assert qnn.w4_matmul_plan(M, N, K, 128) == form and (form == "few16x16/4" or qnn.w4_matmul_plan(M, N, K, group) == with_group)
     if form == "few16x16/4" and group < 64:
         group = 32
     x, codes, scales, z, b = make(M, N, K, group, dtype, zeros, True)
