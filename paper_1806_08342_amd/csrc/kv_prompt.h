@@ -11,7 +11,7 @@
 // value scale is part of the exponent (p * vs / reference), and the sum of p is corrected once per tile; for a tile whose value
 // scale is below 2^-20 of its unit's other tile's, or zero, the sum is formed separately.
 //
-// Bound by the two things that a wave does in turn: products (4 D flops per row and token, at 31 % of the matrix units' cycles) and the
+// Bound by the two things that a wave does in turn: products (4 D flops per row and token, at 35 % of the matrix units' cycles) and the
 // softmax between them (an exponential, four more operations and half a conversion per score, 49 % of the vector unit's); two waves on
 // a SIMD seldom overlap them, as all wait at one barrier for 64 tokens.  8192 tokens, 32 query heads of 128 over 8: 650 us, 840
 // TFLOP/s of the half that the mask leaves.  Forms that interleave a unit's products with the next one's softmax in a
