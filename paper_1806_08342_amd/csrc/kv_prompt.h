@@ -13,9 +13,9 @@
 //
 // Bound by the two things that a wave does in turn: products (4 D flops per row and token, at 35 % of the matrix units' cycles) and the
 // softmax between them (an exponential, four more operations and half a conversion per score, 49 % of the vector unit's); two waves on
-// a SIMD seldom overlap them, as all wait at one barrier for 64 tokens.  8192 tokens, 32 query heads of 128 over 8: 650 us, 840
-// TFLOP/s of the half that the mask leaves.  Forms that interleave a unit's products with the next one's softmax in a
-// wave, or let the waves of a SIMD alternate, lost more to registers and scalar work than they gained.
+// a SIMD seldom overlap them (half a unit apart, or with a higher priority for products, they did not either).  8192 tokens, 32 query
+// heads of 128 over 8: 650 us, 840 TFLOP/s of the half that the mask leaves.  Forms that interleave a unit's products with the next
+// one's softmax in a wave, or let the waves of a SIMD alternate, lost more to registers and scalar work than they gained.
 #pragma once
 
 #include "kv_attention.h"
