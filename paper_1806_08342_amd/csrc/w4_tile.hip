@@ -161,9 +161,11 @@ template <class T, int MT, int GS, bool ZEROS> __global__ void __launch_bounds__
     Weights f[2];
     copy_x(0, 0);
     if (whole > 0) load(f[0], 0);
-    const auto next_buffer = [] { // this wave's copies have arrived, all waves are done with the other buffer
+    // This wave's copies have arrived, and all waves have what they read of the other buffer in registers: the compiler moves the last
+    // products of a step, and the waits for their reads, past a barrier that does not wait itself, and copies into that buffer follow it.
+    const auto next_buffer = [] {
         wait_vmcnt<0>();
-        block_barrier();
+        lds_barrier();
     };
     int step = 0;
     for (; step + 2 < whole; step += 2) {
@@ -191,7 +193,7 @@ template <class T, int MT, int GS, bool ZEROS> __global__ void __launch_bounds__
     }
 
     // outputs through LDS, rows of 64 per wave, 16-byte pieces exchanged as above
-    block_barrier();
+    lds_barrier(); // (the buffers' last reads are over)
     uint8_t *const tile = &s_x[0][0] + wave * (BM * 128);
     float bias[2];
 #pragma unroll
