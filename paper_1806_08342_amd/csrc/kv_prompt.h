@@ -6,10 +6,11 @@
 // rows the tokens' order in a tile is chosen so that the probabilities are the second product's operand in the lane that
 // computed them: rows of K in LDS have bits 2 and 3 of the token's number exchanged.
 //
-// The running maximum and the scale that the accumulators stand in follow lazily: they are kept while a row's scores stay below
-// 2^kRoom times the reference and a page's value scale within 2^kRoom of it, so that most units rescale nothing.  A page's
-// value scale is part of the exponent (p * vs / reference), and the sum of p is corrected once per tile; for a tile whose value
-// scale is below 2^-20 of its unit's other tile's, or zero, the sum is formed separately.
+// The running maximum and the unit that the accumulators stand in, a power of two, follow lazily: they are kept while a row's scores stay
+// below 2^kRoom times the reference and pages' value scales within 2^(kRoom - 1) of the unit or so, so that most units of tokens rescale nothing.  A
+// page's value scale is then part of the exponent (p * vs / unit), and the sum of p is corrected once per tile.  Where the scales of
+// the two tiles lie further apart, or further from any unit that the accumulators can stand in, probabilities go without them and each tile's
+// product is added by itself, with its scale in binary32: a page says nothing about rows that see only others.
 //
 // Bound by the two things that a wave does in turn: products (4 D flops per row and token, at 35 % of the matrix units' cycles) and the
 // softmax between them (an exponential, four more operations and half a conversion per score, 49 % of the vector unit's); two waves on
@@ -22,7 +23,25 @@
 
 namespace qnn {
 
-constexpr float kPromptHead = 6.0f, kRoom = 4.0f; // p * vs / reference stays below 2^(6 + 4 + 4) of binary16's 2^16
+constexpr float kPromptHead = 6.0f, kRoom = 4.0f; // p * vs / unit stays below 2^(6 + 4 + 4) of binary16's 2^16
+
+// The unit 2^at of a wave's accumulators (the same in all lanes, from scales that are).  A page's scale is near it from 2^-3 to just under 2^4 of it.
+struct ValueUnit {
+    int at = 0, peak = -127; // peak: the largest scale so far
+    // scales are given as their patterns
+    static __device__ __forceinline__ int exponent(int scale) { return (scale >> 23 & 255) - 127; }
+    __device__ __forceinline__ bool is_near(int scale) const { return (unsigned)(exponent(scale) - at + 3) <= 6u; }
+    // To where the scale is near, as far as accumulators can follow: they are below 2^(10 + 7 + 31) times what the unit lacks of the largest
+    // scale, which is at most 2^79, and in units up to 2^20 rows that see only pages of the smallest scales keep them.  Returns the
+    // exponent of what accumulators are to be multiplied with.
+    __device__ __forceinline__ int move_to(int scale)
+    {
+        const int from = at, e = exponent(scale);
+        peak = max(peak, e);
+        at = min(max(max(e, peak - 60), -60), max(20, peak - 79));
+        return from - at;
+    }
+};
 
 __device__ __forceinline__ float other_half(float v)
 {
@@ -98,7 +117,7 @@ template <class T, int D, int WAVES> __global__ void __launch_bounds__(64 * WAVE
         for (int v = 0; v < VT; ++v)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[v][i] = 0.0f;
-        float reference = 0.0f; // the value scale that o stands in; 0: none yet
+        ValueUnit unit; // that o stands in
 
         // lane i holds place and scales of the i-th of 64 halves (32 tokens)
         int32_t u_page = 0, u_at = 0;
@@ -159,14 +178,15 @@ template <class T, int D, int WAVES> __global__ void __launch_bounds__(64 * WAVE
         for (int u = 0; u < units; ++u) {
             const int buf = u & 1;
             const int64_t t = t0 + (int64_t)u * 64;
-            float ks[2], vs[2];
+            float ks[2];
+            int vs[2]; // value scales' patterns (scalar arithmetic)
             bool missing[2];
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
                 const int i = (u - looked) * 2 + y;
                 missing[y] = __builtin_amdgcn_readlane(u_page, i) < 0;
                 ks[y] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, u_ks), i));
-                vs[y] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, u_vs), i));
+                vs[y] = __builtin_amdgcn_readlane(__builtin_bit_cast(int, u_vs), i);
             }
             if (u + 1 < units) {
                 if (u + 1 - looked == 32) look_up(u + 1);
@@ -174,28 +194,31 @@ template <class T, int D, int WAVES> __global__ void __launch_bounds__(64 * WAVE
             }
             if (!idle && t <= wave_last && !(a.window > 0 && t + 63 <= wave_first - a.window)) {
                 f32x16 s[2];
+                const auto scores = [&] {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[0][i] = s[1][i] = 0.0f;
 #pragma unroll
-                for (int k = 0; k < KS; ++k)
+                    for (int k = 0; k < KS; ++k)
 #pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        const h16x8 kf = *reinterpret_cast<const h16x8 *>(&s_k[buf][32 * y + c][16 * k + 8 * hh]);
-                        s[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[k], s[y], 0, 0, 0);
-                    }
-                if (missing[0] || missing[1] || t + 63 > wave_first || (a.window > 0 && t <= wave_last - a.window)) {
-                    asm volatile(""); // (a branch: few units are cut)
-                    const int64_t base = t + 8 * hh;
-                    const int to = (int)min(pos - base, (int64_t)64);
-                    const int from = a.window > 0 ? (int)min(max(pos - a.window - base, (int64_t)-1), (int64_t)64) : -1;
-#pragma unroll
-                    for (int y = 0; y < 2; ++y)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int at = 32 * y + 16 * (i >> 3) + (i & 7);
-                            s[y][i] = (at <= to && at > from && !missing[y]) ? s[y][i] : -INFINITY;
+                        for (int y = 0; y < 2; ++y) {
+                            const h16x8 kf = *reinterpret_cast<const h16x8 *>(&s_k[buf][32 * y + c][16 * k + 8 * hh]);
+                            s[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[k], s[y], 0, 0, 0);
                         }
-                }
+                    if (missing[0] || missing[1] || t + 63 > wave_first || (a.window > 0 && t <= wave_last - a.window)) {
+                        asm volatile(""); // (a branch: few units are cut)
+                        const int64_t base = t + 8 * hh;
+                        const int to = (int)min(pos - base, (int64_t)64);
+                        const int from = a.window > 0 ? (int)min(max(pos - a.window - base, (int64_t)-1), (int64_t)64) : -1;
+#pragma unroll
+                        for (int y = 0; y < 2; ++y)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const int at = 32 * y + 16 * (i >> 3) + (i & 7);
+                                s[y][i] = (at <= to && at > from && !missing[y]) ? s[y][i] : -INFINITY;
+                            }
+                    }
+                };
+                scores();
                 // references that no longer do
                 float most, fk[2];
                 bool grew = false;
@@ -211,26 +234,18 @@ template <class T, int D, int WAVES> __global__ void __launch_bounds__(64 * WAVE
                 most = fmaxf(top[0], top[1]);
                 most = fmaxf(most, other_half(most));
                 grew |= most > m + kRoom;
-                const float vmost = fmaxf(vs[0], vs[1]);
-                const bool change = vmost > 0.0f && !(vmost < 16.0f * reference && vmost > 0.0625f * reference);
-                if (__any(grew) || change) {
-                    const float to_new = change ? (reference > 0.0f ? reference / vmost : 0.0f) : 1.0f;
-                    reference = change ? vmost : reference;
-                    const float now = fmaxf(m, most), shrink = exp2_fast(m - now), by = shrink * to_new;
+                const int vmost = max(vs[0], vs[1]); // (0 where there is no page)
+                const int up = vmost > 0 && !unit.is_near(vmost) ? unit.move_to(vmost) : 0;
+                if (__any(grew) || up != 0) {
+                    const float now = fmaxf(m, most), shrink = exp2_fast(m - now), by = ldexpf(shrink, up);
                     m = now, l *= shrink;
 #pragma unroll
                     for (int v = 0; v < VT; ++v) o[v] *= by;
                 }
                 h16x8 p[4];
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    const float ratio = vmost > 0.0f ? vs[y] * __builtin_amdgcn_rcpf(reference) : 0.0f;
-                    const bool small = !(ratio > 0x1p-20f);
-                    const float up = __log2f(ratio) + kPromptHead, down = small ? 0.0f : __builtin_amdgcn_rcpf(ratio); // (takes out what `up` has brought in)
-                    if (small)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) l += exp2_fast(fmaf(s[y][i], fk[y], kPromptHead - m));
-                    const float off = up - m;
+                // probabilities of a tile, times 2^add; returns their sum
+                const auto probabilities = [&](int y, float add) {
+                    const float off = add - m;
                     float sum = 0.0f;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
@@ -238,15 +253,41 @@ template <class T, int D, int WAVES> __global__ void __launch_bounds__(64 * WAVE
                         sum += e;
                         p[2 * y + (i >> 3)][i & 7] = (_Float16)e;
                     }
-                    l = fmaf(sum, down, l);
+                    return sum;
+                };
+                const auto value = [&](int v, int k) { return *reinterpret_cast<const h16x8 *>(&s_v[buf][32 * v + c][16 * k + 8 * hh]); };
+                const bool joined = (missing[0] || unit.is_near(vs[0])) && (missing[1] || unit.is_near(vs[1])); // scales are part of p
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const float ratio = joined && !missing[y] ? ldexpf(__builtin_bit_cast(float, vs[y]), -unit.at) : 1.0f;
+                    const float sum = probabilities(y, joined ? __log2f(ratio) + kPromptHead : -INFINITY);
+                    l = fmaf(sum, __builtin_amdgcn_rcpf(ratio), l); // (takes out of the sum what the scale has brought in)
                 }
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
 #pragma unroll
-                    for (int v = 0; v < VT; ++v) {
-                        const h16x8 vf = *reinterpret_cast<const h16x8 *>(&s_v[buf][32 * v + c][16 * k + 8 * hh]);
-                        o[v] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p[k], o[v], 0, 0, 0);
+                    for (int v = 0; v < VT; ++v) o[v] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value(v, k), p[k], o[v], 0, 0, 0);
+                if (!joined) { // nothing so far: each tile's product by itself
+                    asm volatile("" : "+v"(l)::"memory"); // (once more from the keys on: scores kept until here would take registers from every unit)
+                    scores();
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        l += probabilities(y, kPromptHead);
+                        asm volatile("" : "+v"(l)); // (formed here: further down the sum would keep all of them)
+                        const float scale = ldexpf(__builtin_bit_cast(float, vs[y]), -unit.at);
+#pragma unroll
+                        for (int v = 0; v < VT; ++v) {
+                            f32x16 x;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) x[i] = 0.0f;
+#pragma unroll
+                            for (int k = 2 * y; k < 2 * y + 2; ++k) x = __builtin_amdgcn_mfma_f32_32x32x16_f16(value(v, k), p[k], x, 0, 0, 0);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[v][i] = fmaf(scale, x[i], o[v][i]);
+                            __builtin_amdgcn_sched_barrier(0); // (one product's registers at a time)
+                        }
                     }
+                }
             }
             if (u + 1 < units) stage(buf ^ 1);
             __syncthreads();
@@ -255,7 +296,7 @@ template <class T, int D, int WAVES> __global__ void __launch_bounds__(64 * WAVE
         l += other_half(l);
         if (wave_row + c >= rows) continue;
         if (chunks == 1) {
-            const float inv = l != 0.0f ? reference / l : 0.0f;
+            const float inv = l != 0.0f ? ldexpf(1.0f, unit.at) / l : 0.0f;
             uint16_t *out = a.out + row_id * D + 4 * hh;
 #pragma unroll
             for (int v = 0; v < VT; ++v)
@@ -270,7 +311,7 @@ template <class T, int D, int WAVES> __global__ void __launch_bounds__(64 * WAVE
 #pragma unroll
                 for (int i = 0; i < 16; i += 4)
                     *reinterpret_cast<f32x4 *>(a.part_o + part * D + 32 * v + 2 * i + 4 * hh) =
-                        f32x4{o[v][i] * reference, o[v][i + 1] * reference, o[v][i + 2] * reference, o[v][i + 3] * reference};
+                        f32x4{o[v][i], o[v][i + 1], o[v][i + 2], o[v][i + 3]} * ldexpf(1.0f, unit.at);
             // (the join takes maxima with the head room of the kernel for few rows)
             if (hh == 0) a.part_ml[2 * part] = m + (kHead - kPromptHead), a.part_ml[2 * part + 1] = l;
         }

@@ -80,7 +80,7 @@ template <class T, int D> __global__ void __launch_bounds__(512, 2) attend_wide_
         float m = kNothing, l = 0.0f;
 #pragma unroll
         for (int v = 0; v < VT; ++v) o[v] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        float reference = 0.0f; // the value scale that o stands in; 0: none yet
+        ValueUnit unit; // that o stands in
 
         // lane i holds place and scales of the i-th of 64 halves (32 tokens)
         int32_t u_page = 0, u_at = 0;
@@ -142,14 +142,15 @@ template <class T, int D> __global__ void __launch_bounds__(512, 2) attend_wide_
         for (int u = 0; u < units; ++u) {
             const int buf = u & 1;
             const int64_t t = t0 + (int64_t)u * 64;
-            float ks[2], vs[2];
+            float ks[2];
+            int vs[2]; // value scales' patterns (scalar arithmetic)
             bool missing[2];
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
                 const int i = (u - looked) * 2 + y;
                 missing[y] = __builtin_amdgcn_readlane(u_page, i) < 0;
                 ks[y] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, u_ks), i));
-                vs[y] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, u_vs), i));
+                vs[y] = __builtin_amdgcn_readlane(__builtin_bit_cast(int, u_vs), i);
             }
             if (u + 1 < units) {
                 if (u + 1 - looked == 32) look_up(u + 1);
@@ -157,26 +158,29 @@ template <class T, int D> __global__ void __launch_bounds__(512, 2) attend_wide_
             }
             if (!idle && t <= wave_last && !(a.window > 0 && t + 63 <= wave_first - a.window)) {
                 f32x4 s[4]; // (products of different tiles follow each other: one that waits for the last of its own takes twice as long)
+                const auto scores = [&] {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                    for (int i = 0; i < 4; ++i) s[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int k = 0; k < KS; ++k)
+                    for (int k = 0; k < KS; ++k)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        s[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(*reinterpret_cast<const h16x8 *>(&s_k[buf][k_place(16 * i + c, 4 * k + g)]), qf[k], s[i], 0, 0, 0);
-                if (missing[0] || missing[1] || t + 63 > wave_first || (a.window > 0 && t <= wave_last - a.window)) {
-                    asm volatile(""); // (a branch: few units are cut)
-                    const int64_t base = t + 8 * g;
-                    const int to = (int)min(pos - base, (int64_t)64);
-                    const int from = a.window > 0 ? (int)min(max(pos - a.window - base, (int64_t)-1), (int64_t)64) : -1;
+                        for (int i = 0; i < 4; ++i)
+                            s[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(*reinterpret_cast<const h16x8 *>(&s_k[buf][k_place(16 * i + c, 4 * k + g)]), qf[k], s[i], 0, 0, 0);
+                    if (missing[0] || missing[1] || t + 63 > wave_first || (a.window > 0 && t <= wave_last - a.window)) {
+                        asm volatile(""); // (a branch: few units are cut)
+                        const int64_t base = t + 8 * g;
+                        const int to = (int)min(pos - base, (int64_t)64);
+                        const int from = a.window > 0 ? (int)min(max(pos - a.window - base, (int64_t)-1), (int64_t)64) : -1;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
+                        for (int i = 0; i < 4; ++i)
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            const int at = 32 * (i >> 1) + 4 * (i & 1) + x;
-                            s[i][x] = (at <= to && at > from && !missing[i >> 1]) ? s[i][x] : -INFINITY;
-                        }
-                }
+                            for (int x = 0; x < 4; ++x) {
+                                const int at = 32 * (i >> 1) + 4 * (i & 1) + x;
+                                s[i][x] = (at <= to && at > from && !missing[i >> 1]) ? s[i][x] : -INFINITY;
+                            }
+                    }
+                };
+                scores();
                 // references that no longer do
                 float fk[2], most = -INFINITY;
 #pragma unroll
@@ -188,24 +192,18 @@ template <class T, int D> __global__ void __launch_bounds__(512, 2) attend_wide_
                     most = fmaxf(most, top * fk[y]);
                 }
                 most = max_over_groups(most);
-                const float vmost = fmaxf(vs[0], vs[1]);
-                const bool change = vmost > 0.0f && !(vmost < 16.0f * reference && vmost > 0.0625f * reference);
-                if (__any(most > m + kRoom) || change) {
-                    const float now = fmaxf(m, most), shrink = exp2_fast(m - now);
-                    const float by = change ? (reference > 0.0f ? shrink * (reference / vmost) : 0.0f) : shrink;
-                    m = now, l *= shrink, reference = change ? vmost : reference;
+                const int vmost = max(vs[0], vs[1]); // (0 where there is no page)
+                const int up = vmost > 0 && !unit.is_near(vmost) ? unit.move_to(vmost) : 0;
+                if (__any(most > m + kRoom) || up != 0) {
+                    const float now = fmaxf(m, most), shrink = exp2_fast(m - now), by = ldexpf(shrink, up);
+                    m = now, l *= shrink;
 #pragma unroll
                     for (int v = 0; v < VT; ++v) o[v] *= by;
                 }
                 h16x8 p[2];
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    const float ratio = vmost > 0.0f ? vs[y] * __builtin_amdgcn_rcpf(reference) : 0.0f;
-                    const bool small = !(ratio > 0x1p-20f);
-                    const float off = __log2f(ratio) + kPromptHead - m, down = small ? 0.0f : __builtin_amdgcn_rcpf(ratio); // (takes out what off has brought in)
-                    if (small)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) l += exp2_fast(fmaf(s[2 * y + (i >> 2)][i & 3], fk[y], kPromptHead - m));
+                // probabilities of a tile, times 2^add; returns their sum
+                const auto probabilities = [&](int y, float add) {
+                    const float off = add - m;
                     float sum = 0.0f;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
@@ -213,13 +211,37 @@ template <class T, int D> __global__ void __launch_bounds__(512, 2) attend_wide_
                         sum += x;
                         p[y][i] = (_Float16)x;
                     }
-                    l = fmaf(sum, down, l);
+                    return sum;
+                };
+                const auto value = [&](int v, int y) { return *reinterpret_cast<const h16x8 *>(&s_v[buf][v_place(16 * v + c, 4 * y + g)]); };
+                const bool joined = (missing[0] || unit.is_near(vs[0])) && (missing[1] || unit.is_near(vs[1])); // scales are part of p
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const float ratio = joined && !missing[y] ? ldexpf(__builtin_bit_cast(float, vs[y]), -unit.at) : 1.0f;
+                    const float sum = probabilities(y, joined ? __log2f(ratio) + kPromptHead : -INFINITY);
+                    l = fmaf(sum, __builtin_amdgcn_rcpf(ratio), l); // (takes out of the sum what the scale has brought in)
                 }
 #pragma unroll
                 for (int y = 0; y < 2; ++y)
 #pragma unroll
-                    for (int v = 0; v < VT; ++v)
-                        o[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(*reinterpret_cast<const h16x8 *>(&s_v[buf][v_place(16 * v + c, 4 * y + g)]), p[y], o[v], 0, 0, 0);
+                    for (int v = 0; v < VT; ++v) o[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(value(v, y), p[y], o[v], 0, 0, 0);
+                if (!joined) { // nothing so far: each tile's product by itself
+                    asm volatile("" : "+v"(l)::"memory"); // (once more from the keys on: scores kept until here would take registers from every unit)
+                    scores();
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        l += probabilities(y, kPromptHead);
+                        asm volatile("" : "+v"(l)); // (formed here: further down the sum would keep all of them)
+                        const float scale = ldexpf(__builtin_bit_cast(float, vs[y]), -unit.at);
+#pragma unroll
+                        for (int v = 0; v < VT; ++v) {
+                            const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_f16(value(v, y), p[y], f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[v][e] = fmaf(scale, x[e], o[v][e]);
+                            __builtin_amdgcn_sched_barrier(0); // (one product's registers at a time)
+                        }
+                    }
+                }
             }
             if (u + 1 < units) stage(buf ^ 1);
             __syncthreads();
@@ -228,7 +250,7 @@ template <class T, int D> __global__ void __launch_bounds__(512, 2) attend_wide_
         l = sum_over_groups(l);
         if (row >= rows) continue;
         if (chunks == 1) {
-            const float inv = l != 0.0f ? reference / l : 0.0f;
+            const float inv = l != 0.0f ? ldexpf(1.0f, unit.at) / l : 0.0f;
             uint16_t *out = a.out + row_id * D + 4 * g;
 #pragma unroll
             for (int v = 0; v < VT; ++v) {
@@ -239,7 +261,7 @@ template <class T, int D> __global__ void __launch_bounds__(512, 2) attend_wide_
         } else {
             const int64_t part = part_row(a, r, h, row) * a.chunks + chunk;
 #pragma unroll
-            for (int v = 0; v < VT; ++v) *reinterpret_cast<f32x4 *>(a.part_o + part * D + 16 * v + 4 * g) = o[v] * reference;
+            for (int v = 0; v < VT; ++v) *reinterpret_cast<f32x4 *>(a.part_o + part * D + 16 * v + 4 * g) = o[v] * ldexpf(1.0f, unit.at);
             // (the join takes maxima with the head room of the kernel for few rows)
             if (g == 0) a.part_ml[2 * part] = m + (kHead - kPromptHead), a.part_ml[2 * part + 1] = l;
         }

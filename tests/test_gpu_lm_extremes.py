@@ -1,0 +1,54 @@
+"""Operators of quantized language models where numbers lie far apart or at the ends of their types, against the definition in 64 bits."""
+import pytest
+import torch
+
+import paper_1806_08342_amd as qnn
+from lm_reference import DEV, assert_close, attend, case, half_ulp
+
+pytestmark = pytest.mark.gpu
+
+
+def attention_allows(cache, q, want, spread, cu, lengths, table, scale=None, window=0):
+    """What a result may be off: one rounding to the type; each probability rounded to binary16 (2^-11), sums, exponentials and scores of
+    size up to 100 in binary32 (2^-13); probabilities below binary16's normal numbers, which are off by up to 2^-25 where the largest is held as 2^2
+    or more: 2^-27 of the sum of all values that the row sees; the type's last step."""
+    _, count, mean = attend(cache, torch.zeros_like(q), cu, lengths, table, scale, window)  # all probabilities equal
+    everything = mean * torch.exp(count)[..., None]
+    last = 2.0 ** -25 if q.dtype == torch.float16 else 2.0 ** -134
+    return 1.01 * half_ulp(q.dtype) * want.abs() + (2.0 ** -11 + 2.0 ** -13) * spread + 2.0 ** -27 * everything + last
+
+
+def check_attention(cache, q, cu, lengths, table, what, window=0, **kw):
+    out = qnn.kv_attention(cache, q, cu, lengths, table, window=window, **kw)
+    of = [t.cpu() for t in (cu, lengths, table)]
+    want, _, spread = attend(cache, q, *of, window=window)
+    assert_close(out, want, attention_allows(cache, q, want, spread, *of, window=window), what)
+    return out
+
+
+# value scales of a request's pages, in turn
+PAGES = {"tiny after ordinary": (1.0, 1.0, 1e-36, 1e-36, 1.0), "2^-105": (1.0, 2.0 ** -105, 2.0 ** -105, 0.5), "no normal numbers": (2.0 ** -130, 2.0 ** -130, 2.0 ** -128),
+         "ordinary and no normal numbers": (0.02, 2.0 ** -130, 0.03), "small, then large": (1e-8, 1.0, 1e-9, 1.0, 1e-12), "ever smaller": (1.0, 1e-9, 1e-18, 1e-27, 1e-36),
+         "ever larger": (1e-36, 1e-27, 1e-18, 1e-9, 1.0), "large and small": (1e18, 1e-18, 1e-36, 1e18), "zeros between": (0.0, 1.0, 0.0, 1e-20, 0.0)}
+
+
+@pytest.mark.parametrize("dim,block", [(64, 32), (96, 96), (128, 64), (128, 32), (192, 64), (256, 32), (256, 128)])
+@pytest.mark.parametrize("pages", PAGES)
+def test_value_scales_at_any_distance(pages, dim, block):
+    for requests, most in (([(300, 300), (200, 150)], 300), ([(300, 1), (200, 3)], 3)):
+        cache, q, cu, lengths, table = case(requests, 2, dim, block, torch.bfloat16, block, q_heads=4)
+        for r in range(2):
+            for j, page in enumerate(table[r].tolist()):
+                if page >= 0:
+                    cache[3][page] = PAGES[pages][j % len(PAGES[pages])] * torch.tensor([1.0, 0.7], device=DEV)
+        for window in (0, 40):
+            check_attention(cache, q, cu, lengths, table, (pages, dim, block, most, window), window=window, max_queries=most)
+
+
+@pytest.mark.parametrize("dim", [64, 256])
+def test_value_scales_far_apart_in_a_divided_context(dim):
+    cache, q, cu, lengths, table = case([(9001, 40)], 1, dim, 64, torch.bfloat16, 7, q_heads=4)
+    j = torch.arange(table.shape[1], device=DEV)
+    cache[3][table[0].long()] = torch.where(j % 3 == 0, 1e-36, torch.where(j < 100, 1e-3, 1.0))[:, None]
+    check_attention(cache, q, cu, lengths, table, dim, max_queries=40)
+    check_attention(cache, q, cu, lengths, table, (dim, "window"), max_queries=40, window=4000)
