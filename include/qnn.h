@@ -338,7 +338,7 @@ qnn_status qnn_qdwconv2d_asym(const uint8_t *x, int N, int H, int W, int C, int3
  * The weights enter exactly (code minus zero-point is a whole number of at most 5 bits, the scale multiplies the group's sum in
  * binary32); sums are binary32, y is rounded once.  From about 17 rows on x enters as binary16, each row scaled by a power of two to at
  * most 1, which is exact but for elements below 2^-17 of their row's largest (bfloat16; 2^-14 for binary16), which keep fewer bits; and a group whose scale is
- * less than 2^-100 of the one before it in its row counts as 0.  An infinite or NaN x gives infinities or NaN in its row.
+ * less than 2^-80 of the largest before it in its row may count as 0.  An infinite or NaN x gives infinities or NaN in its row.
  * x: DEVICE, M x K of `type`, row pitch ldx >= K elements.  codes: DEVICE uint8 [N][K/2], nibbles as in qnn_qgemm
  * (two's complement, element 2j in the low one), K even.  scales: DEVICE [ceil(K / group)][N] of `type`.
  * zeros: DEVICE int8 [ceil(K / group)][N], or NULL for symmetric weights.  bias: DEVICE [N] of `type` or NULL.

@@ -181,19 +181,25 @@ const char *w4_parts_name(int64_t M, int64_t N, int64_t K);
 void launch_w4_parts(const W4Args &a, int type, const W4Prepared &p, hipStream_t s);
 void launch_w4_tile(const W4Args &a, int type, const W4Prepared &p, hipStream_t s);
 
-// The scale of the group that accumulators come to: `ratio` brings them into its unit.  A scale of 0, or of 2^-100 of the last one
-// (in whose unit they could overflow), leaves its weights out: all nibbles masked, and an offset that takes off what is left.
+// The unit that accumulators stand in, the scale of the group that they are at, and the largest so far.
+struct ScaleUnit {
+    float at = 0.0f, most = 0.0f;
+};
+// The scale of the group that accumulators come to: `ratio` brings them into its unit.  A scale of 0, or less than 2^-80 of the largest before
+// it (in whose unit accumulators could overflow, in however many steps they came there), leaves its weights out: all nibbles masked, and
+// an offset that takes off what is left.
 struct GroupUnit {
     float ratio;
     h16x2 off;
     uint32_t mask;
 };
-__device__ __forceinline__ GroupUnit enter_group(float s, int z, float &unit)
+__device__ __forceinline__ GroupUnit enter_group(float s, int z, ScaleUnit &unit)
 {
-    const bool none = s == 0.0f || fabsf(s) * 0x1p100f < fabsf(unit);
+    const bool none = s == 0.0f || fabsf(s) * 0x1p80f < unit.most;
     GroupUnit g;
-    g.ratio = none ? 1.0f : unit / s;
-    unit = none ? unit : s;
+    g.ratio = none ? 1.0f : unit.at / s;
+    unit.at = none ? unit.at : s;
+    unit.most = fmaxf(unit.most, fabsf(s));
     const _Float16 o = (_Float16)(1032.0f + (none ? 0.0f : (float)z));
     g.off = h16x2{o, o}, g.mask = none ? 0u : 0x000f000fu;
     return g;

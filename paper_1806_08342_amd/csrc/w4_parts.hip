@@ -66,7 +66,7 @@ template <class T, int MT, int NW, int PARTS, int RING, int GS, bool ZEROS> __gl
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[mt][i] = 0.0f;
-    float unit = 0.0f;
+    ScaleUnit unit;
     const uint32_t bits = kept(Nibbles<F16>::kBits);
     auto compute = [&](Weights &f, int slot) {
         f.w.place(w_row, a.skewed);
@@ -133,7 +133,7 @@ template <class T, int MT, int NW, int PARTS, int RING, int GS, bool ZEROS> __gl
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s_sum[(part * ROWS + mt * 32 + 8 * (i >> 2) + 4 * hh + (i & 3)) * (BN + 4) + nw * 32 + c] = acc[mt][i] * unit;
+        for (int i = 0; i < 16; ++i) s_sum[(part * ROWS + mt * 32 + 8 * (i >> 2) + 4 * hh + (i & 3)) * (BN + 4) + nw * 32 + c] = acc[mt][i] * unit.at;
     lds_barrier();
     for (int i = tid; i < ROWS * BN; i += 64 * NW * PARTS) {
         const int m = i / BN, n = blockIdx.x * BN + i % BN;

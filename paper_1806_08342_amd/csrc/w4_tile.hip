@@ -120,7 +120,7 @@ template <class T, int MT, int GS, bool ZEROS> __global__ void __launch_bounds__
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[t][mt][i] = 0.0f;
-    float unit[2] = {0.0f, 0.0f};
+    ScaleUnit unit[2];
     const uint32_t bits = kept(Nibbles<F16>::kBits);
 
     auto compute = [&](Weights &f, int buf) {
@@ -209,7 +209,7 @@ template <class T, int MT, int GS, bool ZEROS> __global__ void __launch_bounds__
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float v = ldexpf(acc[t][mt][i + e] * unit[t], exp[e]) + bias[t];
+                    const float v = ldexpf(acc[t][mt][i + e] * unit[t].at, exp[e]) + bias[t];
                     *reinterpret_cast<uint16_t *>(tile + (m + e) * 128 + ((4 * t + (c >> 3)) ^ ((m + e) & 7)) * 16 + (c & 7) * 2) = T::narrow(v);
                 }
         }

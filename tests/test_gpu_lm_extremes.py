@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_1806_08342_amd as qnn
-from lm_reference import DEV, assert_close, attend, case, half_ulp
+from lm_reference import DEV, assert_close, attend, case, half_ulp, w4
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +52,30 @@ def test_value_scales_far_apart_in_a_divided_context(dim):
     cache[3][table[0].long()] = torch.where(j % 3 == 0, 1e-36, torch.where(j < 100, 1e-3, 1.0))[:, None]
     check_attention(cache, q, cu, lengths, table, dim, max_queries=40)
     check_attention(cache, q, cu, lengths, table, (dim, "window"), max_queries=40, window=4000)
+
+
+# --------------------------------------------------------------------------- products
+
+def weights(N, K, group, dtype, g, scales=None):
+    groups = -(-K // group)
+    codes = torch.randint(0, 256, (N, K // 2), generator=g).to(torch.uint8)
+    z = torch.randint(-8, 8, (groups, N), generator=g).to(torch.int8)
+    if scales is None:
+        scales = 2.0 ** -torch.randint(2, 6, (groups, N), generator=g)
+    return codes.to(DEV), scales.to(dtype).to(DEV), z.to(DEV)
+
+
+@pytest.mark.parametrize("M,N,K,stay", [(4, 300, 6144, 1024), (20, 300, 6144, 1024), (50, 300, 6144, 1024), (201, 17003, 770, 128)])
+def test_scales_that_fall_and_fall(M, N, K, stay):
+    # the unit of accumulators falls in steps that add up to more than binary32's range; each scale is that of `stay` columns, so that
+    # every part of K that a kernel sums by itself meets them all
+    group = 64
+    g = torch.Generator().manual_seed(M)
+    x = torch.randint(-8, 9, (M, K), generator=g).to(torch.bfloat16).to(DEV)
+    for falls in ((0, -70, -126), (0, -40, -79, -126, -130), (100, 30, -40, -110), (0, -60, -120, 0, -60, -120), (-126, -100, 0, -50, -100)):
+        power = torch.tensor([falls[i * group // stay % len(falls)] for i in range(-(-K // group))])
+        codes, scales, z = weights(N, K, group, torch.bfloat16, g, torch.ones(len(power), N) * (2.0 ** power.double())[:, None])
+        want, size = w4(x, codes, scales, group, z)
+        # one rounding; sums in binary32, some ten additions for each 128 columns at worst the same way; what lies 2^80 below the largest scale
+        allowed = 1.01 * 2.0 ** -8 * want.abs() + K / 128 * 10 * 2.0 ** -24 * size + float(scales.max()) * 2.0 ** -60
+        assert_close(qnn.w4_matmul(x, codes, scales, group, z), want, allowed, (M, falls))
