@@ -56,6 +56,12 @@ def test_value_scales_far_apart_in_a_divided_context(dim):
 
 # --------------------------------------------------------------------------- products
 
+# every kernel and form of one, at sizes that divide nothing (rows of x, rows of weights, columns)
+PRODUCTS = {"few16x16/4": (3, 3, 30), "few16x32/8": (5, 17001, 330), "few16x16/8": (9, 4103, 514), "few16x16/16": (15, 1000, 1030), "tens32x64/4": (17, 1001, 386),
+            "tens32x32/8": (65, 301, 1034), "tens32x128/4": (17, 17003, 770), "tens64x128/4": (33, 17001, 770), "tens64x128/2": (70, 9001, 514), "tens64x64/4": (40, 8203, 514),
+            "many": (201, 17003, 770), "many, long": (300, 700, 4098), "few, long": (2, 300, 8194)}
+
+
 def weights(N, K, group, dtype, g, scales=None):
     groups = -(-K // group)
     codes = torch.randint(0, 256, (N, K // 2), generator=g).to(torch.uint8)
@@ -63,6 +69,32 @@ def weights(N, K, group, dtype, g, scales=None):
     if scales is None:
         scales = 2.0 ** -torch.randint(2, 6, (groups, N), generator=g)
     return codes.to(DEV), scales.to(dtype).to(DEV), z.to(DEV)
+
+
+@pytest.mark.parametrize("group,dtype", [(128, torch.bfloat16), (128, torch.float16), (64, torch.float16), (64, torch.bfloat16), (32, torch.bfloat16), (96, torch.float16)])
+@pytest.mark.parametrize("form", PRODUCTS)
+def test_products_of_whole_numbers_are_exact(form, group, dtype):
+    # whole x up to 8, scales 2^-2 ... 2^-5: every sum is a multiple of 2^-5 that binary32 holds (128 * 8 * 151 of a step in the kernel's own
+    # offsets, some 10^4 * 2^5 over a row), so that the result is the definition's, rounded once
+    M, N, K = PRODUCTS[form]
+    g = torch.Generator().manual_seed(M + N + K + group)
+    x = torch.randint(-8, 9, (M, K), generator=g).to(dtype).to(DEV)
+    codes, scales, z = weights(N, K, group, dtype, g)
+    bias = torch.randint(-9, 10, (N,), generator=g).to(dtype).to(DEV)
+    for zeros, b in ((z, bias), (None, None)):
+        want, _ = w4(x, codes, scales, group, zeros, b)
+        assert want.abs().max() < 60000 and torch.equal(qnn.w4_matmul(x, codes, scales, group, zeros, b).cpu(), want.to(dtype)), (form, zeros is None)
+
+
+def test_long_rows_of_whole_numbers_are_exact():
+    # beyond the offsets of the kernels for many rows of x: sums of two million products of up to 8 * 15, some 10^5 of 2^24
+    K = (1 << 21) + 258
+    g = torch.Generator().manual_seed(1)
+    x = torch.randint(-8, 9, (18, K), generator=g).to(torch.bfloat16).to(DEV)
+    codes, scales, z = weights(5, K, 1024, torch.bfloat16, g, torch.full((-(-K // 1024), 5), 0.5))
+    assert qnn.w4_matmul_plan(18, 5, K, 1024).startswith("few")
+    want, _ = w4(x, codes, scales, 1024, z)
+    assert torch.equal(qnn.w4_matmul(x, codes, scales, 1024, z).cpu(), want.to(torch.bfloat16))
 
 
 @pytest.mark.parametrize("M,N,K,stay", [(4, 300, 6144, 1024), (20, 300, 6144, 1024), (50, 300, 6144, 1024), (201, 17003, 770, 128)])
