@@ -335,10 +335,11 @@ qnn_status qnn_qdwconv2d_asym(const uint8_t *x, int N, int H, int W, int C, int3
 #define QNN_F16 1
 
 /* y[m][n] = bias[n] + sum_k x[m][k] * (c[n][k] - z[k / group][n]) * s[k / group][n]
- * The weights enter exactly (code minus zero-point is a whole number of at most 5 bits, the scale multiplies the group's sum in
- * binary32); sums are binary32, y is rounded once.  From about 17 rows on x enters as binary16, each row scaled by a power of two to at
- * most 1, which is exact but for elements below 2^-17 of their row's largest (bfloat16; 2^-14 for binary16), which keep fewer bits; and a group whose scale is
- * less than 2^-80 of the largest before it in its row may count as 0.  An infinite or NaN x gives infinities or NaN in its row.
+ * The weights enter exactly (code minus zero-point is a whole number of at most 9 bits, the scale multiplies the group's sum in
+ * binary32); sums are binary32, y is rounded once.  Where qnn_w4_matmul_plan says "tens" or "many" (from 17 rows on, and with fewer on large
+ * weights: from 4 rows with 28672 x 8192) x enters as binary16, each row scaled by a power of two, which is exact but for bfloat16 elements below
+ * 2^-32 of their row's largest, which keep fewer bits; and a group whose scale is less than 2^-80 of the largest before it in its row
+ * may count as 0.  An infinite or NaN x gives infinities or NaN in its row.
  * x: DEVICE, M x K of `type`, row pitch ldx >= K elements.  codes: DEVICE uint8 [N][K/2], nibbles as in qnn_qgemm
  * (two's complement, element 2j in the low one), K even.  scales: DEVICE [ceil(K / group)][N] of `type`.
  * zeros: DEVICE int8 [ceil(K / group)][N], or NULL for symmetric weights.  bias: DEVICE [N] of `type` or NULL.
@@ -395,8 +396,8 @@ qnn_status qnn_kv_gather(const qnn_kv_cache *cache, const int32_t *cu, const int
  * for window > 0, t > p - window.  q_heads is a multiple of cache->heads; head e reads the cache's head e / (q_heads / heads).
  *   out = sum_t softmax_t(scale * q . k_t) v_t;  a query that sees nothing gives 0
  *   lse = log sum_t exp(scale * q . k_t) (natural; -inf where nothing is seen), for joining results over parts of a context
- * Sums, maxima and products are binary32; codes enter the matrix units exactly, as binary16; q is scaled by a power of two per
- * row to fit binary16, the probabilities (scaled to at most 2^14) are rounded to binary16.
+ * Sums, maxima and products are binary32; codes enter the matrix units exactly, as binary16; q too, scaled by a power of two per row (bfloat16
+ * elements below 2^-32 of their row's largest keep fewer bits); the probabilities (scaled to at most 2^14) are rounded to binary16.
  * q, out: DEVICE [tokens][q_heads][dim] of `type`, element (t, e, d) of q at t * q_token_pitch + e * q_head_pitch + d; out
  * contiguous (rows of requests are written).  lse: DEVICE float [tokens][q_heads] or NULL.
  * max_queries: the largest number of queries of a request (more are computed too, slower); max_queries <= 0: tokens.

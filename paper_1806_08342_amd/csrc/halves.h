@@ -58,12 +58,13 @@ __device__ __forceinline__ float sum_over_groups(float v)
     return v + __shfl_xor(v, 32);
 }
 
-// e for the largest |v| of a row, so that v * 2^-e is at most 1: binary16 then holds what bfloat16 holds, but for elements
-// below 2^-17 of the row's largest, which keep fewer bits.  (2^e stays finite: at most 2^120.)
+// e for the largest |v| of a row, so that v * 2^-e is in the last octave of binary16, from 2^15 on: it then holds what the row holds, but for
+// bfloat16 elements below 2^-32 of the row's largest, which keep fewer bits: 256 times less than what a sum in binary32 loses beside the
+// largest.  (2^e and 2^-e stay normal numbers.)
 __device__ __forceinline__ int row_exponent(float peak)
 {
-    const int e = (int)(__builtin_bit_cast(uint32_t, peak) >> 23 & 255u) - 126;
-    return peak > 0.0f ? min(max(e, -100), 120) : 0;
+    const int e = (int)(__builtin_bit_cast(uint32_t, peak) >> 23 & 255u) - 142;
+    return peak > 0.0f ? max(e, -126) : 0;
 }
 
 inline bool bad_half_type(int type) { return type != QNN_BF16 && type != QNN_F16; }

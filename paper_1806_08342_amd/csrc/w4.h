@@ -153,8 +153,8 @@ template <int GS> __device__ __forceinline__ int piece_of(int i, int hh)
     return GS == 1 ? 8 * hh + i : GS == 2 ? 8 * (i >> 2) + 4 * hh + (i & 3) : 4 * (i >> 1) + 2 * hh + (i & 1);
 }
 
-// x as the kernels for tens and for many rows take it: binary16, each row scaled by a power of two to at most 1, which is exact
-// (elements below 2^-17 of their row's largest keep fewer bits), in the order of expand_nibbles, rows padded with zeros to
+// x as the kernels for tens and for many rows take it: binary16, each row scaled by a power of two, which is exact but for bfloat16
+// elements below 2^-32 of their row's largest (row_exponent), in the order of expand_nibbles, rows padded with zeros to
 // whole 128s
 struct W4Prepared {
     uint16_t *x;      // binary16 [M][pitch]

@@ -5,8 +5,8 @@
 // scale of the group that it is at: at the next group it is multiplied by the ratio of the two scales.  That is
 // one set of accumulators and one multiplication per output and group; as x is the left operand here, a lane's outputs are all of
 // one row of weights, and the ratio is one number per lane.
-// x has to fit binary16: a first launch writes it with each row scaled by a power of two to at most 1, which is exact (elements
-// below 2^-17 of their row's largest keep fewer bits), in the order of expand_nibbles, rows padded with zeros to whole 128s.
+// x has to fit binary16: a first launch writes it with each row scaled by a power of two, which is exact but for bfloat16 elements below
+// 2^-32 of their row's largest, in the order of expand_nibbles, rows padded with zeros to whole 128s.
 //
 // Bound by the matrix units and the clock they leave: 2000 x 12288 x 4096 with zero-points 195-210 us with the first launch (6-12), 1000
 // TFLOP/s; the library's product of the same size with 16-bit weights takes 180.  Tiles of 128 x 256 (64 x 256 with groups that are

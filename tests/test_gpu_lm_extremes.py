@@ -111,3 +111,31 @@ def test_scales_that_fall_and_fall(M, N, K, stay):
         # one rounding; sums in binary32, some ten additions for each 128 columns at worst the same way; what lies 2^80 below the largest scale
         allowed = 1.01 * 2.0 ** -8 * want.abs() + K / 128 * 10 * 2.0 ** -24 * size + float(scales.max()) * 2.0 ** -60
         assert_close(qnn.w4_matmul(x, codes, scales, group, z), want, allowed, (M, falls))
+
+
+@pytest.mark.parametrize("M,N,K", [(20, 300, 642), (33, 8300, 514), (201, 17003, 770)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_one_large_channel_takes_no_bits_of_the_others(M, N, K, dtype):
+    # rows whose largest element meets weights of 0 in every second output: those are sums of the others only, whole numbers, exact
+    large, unit, group = (2.0 ** 30, 1.0, 64) if dtype is torch.bfloat16 else (2.0 ** 15, 2.0 ** -24, 64)
+    g = torch.Generator().manual_seed(N)
+    x = (torch.randint(-8, 9, (M, K), generator=g) * unit).to(dtype).to(DEV)
+    codes, scales, z = weights(N, K, group, dtype, g, 2.0 ** torch.randint(4, 8, (-(-K // group), N), generator=g))
+    x[:, 70] = large * torch.where(torch.arange(M, device=DEV) % 2 == 0, 1.0, -1.0).to(dtype)
+    codes[::2, 35] = (codes[::2, 35] & 0xF0) | (z[1, ::2].to(torch.uint8) & 0x0F)  # column 70 is the low half of byte 35; code = zero-point
+    assert not qnn.w4_matmul_plan(M, N, K, group).startswith("few")
+    want, size = w4(x, codes, scales, group, z)
+    got = qnn.w4_matmul(x, codes, scales, group, z)
+    assert torch.equal(got[:, ::2].cpu(), want[:, ::2].to(dtype))
+    if dtype is torch.bfloat16:
+        assert_close(got[:, 1::2], want[:, 1::2], (1.01 * 2.0 ** -8 * want.abs() + 2.0 ** -22 * size)[:, 1::2], "with the large one")
+
+
+@pytest.mark.parametrize("most", [1, 100])
+def test_one_large_channel_of_a_query_takes_no_bits_of_the_others(most):
+    # keys are 0 in the channel where queries are large
+    for dim in (64, 128, 256):
+        cache, q, cu, lengths, table = case([(100, most), (260, most)], 2, dim, 32, torch.bfloat16, dim, q_heads=4)
+        q[:, :, 5] = 2.0 ** 22
+        cache[0][:, :, :, 5] = 0
+        check_attention(cache, q, cu, lengths, table, (dim, most), max_queries=most)
