@@ -25,11 +25,13 @@ __device__ __forceinline__ int group_of(const W4Args &a, int k)
 }
 
 // Two nibbles of a dword, 16 bits apart, as 16-bit floats: with bit 3 flipped a nibble is u = c + 8 (one v_bitop3 where mask and
-// bits are in registers, see kept()).
+// bits are in registers, see kept()).  bfloat16 reaches to the end of binary32's range: there all stands in units of 2^kUnit, so that
+// 128 products with up to 2^8, and their offset, do not pass it where the result does not.
 template <class T> struct Nibbles;
 template <> struct Nibbles<Bf16> {
     static constexpr float kOffset = 128.0f + 8.0f;
-    static constexpr uint32_t kBits = 0x43084308u, kOnes = 0x3f803f80u;
+    static constexpr int kUnit = 16;
+    static constexpr uint32_t kBits = 0x3b083b08u, kOnes = 0x37803780u; // 2^-9 (with bit 3), 2^-16
     static __device__ __forceinline__ uint32_t two(uint32_t w, uint32_t bits) { return (w & 0x000f000fu) ^ bits; }
     static __device__ __forceinline__ f32x4 mfma(w32x4 a, w32x4 b, f32x4 c)
     {
@@ -38,6 +40,7 @@ template <> struct Nibbles<Bf16> {
 };
 template <> struct Nibbles<F16> {
     static constexpr float kOffset = 8.0f;
+    static constexpr int kUnit = 0;
     static constexpr uint32_t kBits = 0x64086408u, kOnes = 0x3c003c00u;
     static __device__ __forceinline__ uint32_t two(uint32_t w, uint32_t bits)
     {

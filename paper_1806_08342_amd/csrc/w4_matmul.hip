@@ -3,8 +3,8 @@
 //   y[m][n] = bias[n] + sum_g s[g][n] * (sum_{k in g} x[m][k] * (8 + c[n][k]) - (8 + z[g][n]) * sum_{k in g} x[m][k])
 //
 // A nibble u = 8 + c becomes a 16-bit float by setting the bits of a power of two above it: 128 + u in bfloat16, 1024 + u in
-// binary16 (from which the 1024 is then taken off; bfloat16 has no packed subtraction, so there the 128 stays and joins the
-// 8 + z of the group's term).  No weight is rounded.  The group's sum of x comes from one more matrix product with ones.
+// binary16 (from which the 1024 is then taken off; bfloat16 has no packed subtraction, so there the 128 stays, as 2^-9 with all else in units
+// of 2^16, and joins the 8 + z of the group's term).  No weight is rounded.  The group's sum of x comes from one more matrix product with ones.
 //
 // Few rows are bound by reading the codes, small products by the launch and one chain of loads: 1 x 4096 x 4096 4.6 us, 5 x 5001 x 2890 with
 // zero-points 8.6 us (its rows of codes begin at any byte).  With more than about 16 rows x is shared through LDS (w4_parts.hip), with hundreds
@@ -189,6 +189,7 @@ template <class T, int MT, int NT, int WAVES, int GS, bool ZEROS, bool TINY> __g
         float v = s_acc[0][m][n];
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) v += s_acc[w][m][n];
+        if constexpr (Nibbles<T>::kUnit != 0) v = ldexpf(v, Nibbles<T>::kUnit);
         if (a.bias) v += T::widen(a.bias[n0 + n]);
         a.y[(int64_t)(m0 + m) * a.ldy + n0 + n] = T::narrow(v);
     }

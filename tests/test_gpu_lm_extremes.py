@@ -139,3 +139,29 @@ def test_one_large_channel_of_a_query_takes_no_bits_of_the_others(most):
         q[:, :, 5] = 2.0 ** 22
         cache[0][:, :, :, 5] = 0
         check_attention(cache, q, cu, lengths, table, (dim, most), max_queries=most)
+
+
+@pytest.mark.parametrize("M", [1, 3, 16, 40, 300])
+@pytest.mark.parametrize("power", [-110, 118])
+def test_rows_at_the_ends_of_the_type(M, power):
+    # x and results scale by powers of two up to where the results themselves end: sums of up to 384 * 4 * 15 * 0.25 < 2^13 times 2^118 * 2^-4
+    g = torch.Generator().manual_seed(M)
+    x = ((torch.rand(M, 384, generator=g) + 1.0) * 2.0 ** torch.randint(0, 2, (M, 384), generator=g) * (1 - 2 * torch.randint(0, 2, (M, 384), generator=g))).to(torch.bfloat16).to(DEV)
+    codes, scales, z = weights(260, 384, 128, torch.bfloat16, g)
+    want = qnn.w4_matmul(x, codes, scales * 2.0 ** -4, 128, z)
+    got = qnn.w4_matmul(x * 2.0 ** power, codes, scales * 2.0 ** -4, 128, z)
+    assert torch.isfinite(want).all() and torch.equal(got, want * 2.0 ** power)
+    bias = torch.ones(260, dtype=torch.bfloat16, device=DEV)
+    assert torch.equal(qnn.w4_matmul(x * 2.0 ** -110, codes, scales * 2.0 ** -4, 128, z, bias), bias.expand(M, 260))
+
+
+@pytest.mark.parametrize("M", [3, 16])
+def test_large_rows_whose_sums_are_small(M):
+    # few rows: x near the largest number of its type, weights that cancel; the result is far inside the range
+    g = torch.Generator().manual_seed(M)
+    x = torch.randint(-8, 9, (M, 1024), generator=g).to(torch.bfloat16).to(DEV)
+    codes, scales, z = weights(300, 1024, 64, torch.bfloat16, g)
+    want, _ = w4(x, codes, scales, 64, z)
+    assert want.abs().max() < 2.0 ** 12
+    got = qnn.w4_matmul(x * 2.0 ** 124, codes, scales * 2.0 ** -20, 64, z)
+    assert torch.equal(got.cpu().double() * 2.0 ** -104, want.to(torch.bfloat16).double())
