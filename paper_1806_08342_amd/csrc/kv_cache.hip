@@ -190,7 +190,7 @@ template <class T, int D, int WAVES> __global__ void __launch_bounds__(256) appe
         for (int i = lane; i < (p.hi - p.lo) * D; i += LANES) {
             const int t = i / D, d = i % D;
             const float v = T::widen(x[t * token + d]);
-            codes[is_v ? d * block + p.lo + t : (p.lo + t) * D + d] = (int8_t)(v == v ? code_of(__fdiv_rn(v, by)) : 0);
+            codes[is_v ? d * block + p.lo + t : (p.lo + t) * D + d] = (int8_t)(v == v && after > 0.0f ? code_of(__fdiv_rn(v, by)) : 0); // (scale 0: nothing but infinities and zeros)
         }
         return;
     }

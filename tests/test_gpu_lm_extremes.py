@@ -165,3 +165,24 @@ def test_large_rows_whose_sums_are_small(M):
     assert want.abs().max() < 2.0 ** 12
     got = qnn.w4_matmul(x * 2.0 ** 124, codes, scales * 2.0 ** -20, 64, z)
     assert torch.equal(got.cpu().double() * 2.0 ** -104, want.to(torch.bfloat16).double())
+
+
+# --------------------------------------------------------------------------- the cache
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("tokens", [1, 70])
+def test_pages_of_nothing_finite(tokens, dtype):
+    # scale 0 gives codes 0, which later values do not bring back
+    cache, _, cu, lengths, table = case([(tokens + 1, 1)], 2, 64, 32, dtype, 0)
+    endless = torch.full((tokens, 2, 64), float("inf"), dtype=dtype, device=DEV)
+    endless[:, 0, ::2], endless[:, 0, 1::4] = float("-inf"), float("nan")
+    endless[:, 1, :5] = 0.0
+    at = lambda *v: torch.tensor(v, dtype=torch.int32, device=DEV)  # noqa: E731
+    qnn.kv_append(cache, endless, endless, at(0, tokens), at(0), table)
+    for j in range(-(-tokens // 32)):
+        page, held = int(table[0, j]), min(32, tokens - 32 * j)
+        assert not cache[0][page, :, :held].any() and not cache[2][page, :, :, :held].any() and not cache[1][page].any() and not cache[3][page].any()
+    ones = torch.ones(1, 2, 64, dtype=dtype, device=DEV)
+    qnn.kv_append(cache, ones, ones, at(0, 1), at(tokens), table)
+    k, v = qnn.kv_gather(cache, at(0, tokens + 1), at(0), table, tokens + 1, dtype)
+    assert not k[:tokens].any() and not v[:tokens].any() and (k[tokens:] == 1).all() and (v[tokens:] == 1).all()
