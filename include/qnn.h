@@ -401,7 +401,7 @@ qnn_status qnn_kv_gather(const qnn_kv_cache *cache, const int32_t *cu, const int
  * q, out: DEVICE [tokens][q_heads][dim] of `type`, element (t, e, d) of q at t * q_token_pitch + e * q_head_pitch + d; out
  * contiguous (rows of requests are written).  lse: DEVICE float [tokens][q_heads] or NULL.
  * max_queries: the largest number of queries of a request (more are computed too, slower); max_queries <= 0: tokens.
- * Page numbers outside [0, pages) count as tokens that nothing sees.  tokens * q_heads / heads below 2^31, the rest as above.
+ * Page numbers outside [0, pages), and tokens past table_width * block, count as tokens that nothing sees.  tokens * q_heads / heads below 2^31, the rest as above.
  * workspace: DEVICE, 16-byte aligned, of at least qnn_kv_attention_workspace_bytes bytes for the same sizes, else QNN_EINVAL. */
 qnn_status qnn_kv_attention(const qnn_kv_cache *cache, const void *q, int64_t q_token_pitch, int64_t q_head_pitch,
                             int32_t q_heads, int type, const int32_t *cu, const int32_t *lengths, const int32_t *table,

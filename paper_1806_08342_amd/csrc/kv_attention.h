@@ -53,10 +53,11 @@ template <int U> __device__ __forceinline__ Request request_of(const AttendArgs 
     const int32_t cu0 = __builtin_amdgcn_readfirstlane(a.cu[r]), cu1 = __builtin_amdgcn_readfirstlane(a.cu[r + 1]);
     const int64_t c0 = min(max((int64_t)cu0, (int64_t)0), a.tokens), c1 = min(max((int64_t)cu1, c0), a.tokens);
     q.row0 = c0, q.n = (int32_t)(c1 - c0);
-    q.length = min(max((int64_t)__builtin_amdgcn_readfirstlane(a.lengths[r]), (int64_t)0), a.table_width * a.cache.block);
+    q.length = max(__builtin_amdgcn_readfirstlane(a.lengths[r]), 0);
+    const int64_t held = min(q.length, a.table_width * a.cache.block); // (queries stand at the end of all tokens, the table's or not)
     int64_t low = a.window > 0 ? q.length - q.n + 1 - a.window : 0;
     low = max(low, (int64_t)0) / U * U;
-    q.low = min(low, q.length / U * U), q.high = a.cache.pages > 0 ? q.length : q.low;
+    q.low = min(low, held / U * U), q.high = a.cache.pages > 0 ? held : q.low;
     return q;
 }
 __device__ __forceinline__ int chunks_of(const AttendArgs &a, const Request &q)

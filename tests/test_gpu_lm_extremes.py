@@ -186,3 +186,21 @@ def test_pages_of_nothing_finite(tokens, dtype):
     qnn.kv_append(cache, ones, ones, at(0, 1), at(tokens), table)
     k, v = qnn.kv_gather(cache, at(0, tokens + 1), at(0), table, tokens + 1, dtype)
     assert not k[:tokens].any() and not v[:tokens].any() and (k[tokens:] == 1).all() and (v[tokens:] == 1).all()
+
+
+# --------------------------------------------------------------------------- lengths
+
+@pytest.mark.parametrize("window", [0, 25, 64, 100])
+@pytest.mark.parametrize("dim,block", [(64, 32), (128, 96), (256, 64)])
+def test_tokens_past_the_table_are_not_seen(dim, block, window):
+    # queries stand where the length says, as if the table went on without pages
+    for n, most in ((1, 1), (5, 5), (150, 150)):
+        cache, q, cu, lengths, table = case([(6 * block, n), (4 * block, n), (6 * block, n)], 2, dim, block, torch.bfloat16, n, q_heads=6)
+        short = table[:, :4].contiguous()
+        lengths[2] += 20
+        more = torch.cat([short, torch.full((3, 4), -1, dtype=torch.int32, device=DEV)], 1)
+        out, lse = qnn.kv_attention(cache, q, cu, lengths, short, window=window, max_queries=most, with_lse=True)
+        of = [t.cpu() for t in (cu, lengths, more)]
+        want, want_lse, spread = attend(cache, q, *of, window=window)
+        assert_close(out, want, attention_allows(cache, q, want, spread, *of, window=window).nan_to_num(2.0 ** -30), (dim, block, window, n))
+        assert torch.equal(torch.isfinite(lse).cpu(), torch.isfinite(want_lse))
