@@ -344,7 +344,7 @@ qnn_status qnn_qdwconv2d_asym(const uint8_t *x, int N, int H, int W, int C, int3
  * (two's complement, element 2j in the low one), K even.  scales: DEVICE [ceil(K / group)][N] of `type`.
  * zeros: DEVICE int8 [ceil(K / group)][N], or NULL for symmetric weights.  bias: DEVICE [N] of `type` or NULL.
  * group: a multiple of 32 (one scale per row: any such number >= K).  y: DEVICE, M x N of `type`, row pitch ldy >= N (written).
- * M up to 2^20 (0 is a no-op), N up to 2^28, K up to 2^24, and fewer than 2^30 scales.
+ * M up to 2^20 (0 is a no-op), N up to 2^28 - 32, K up to 2^24, and fewer than 2^30 scales.
  * workspace: DEVICE scratch, 16-byte aligned, of at least qnn_w4_matmul_workspace_bytes bytes (NULL where that
  * is 0), else QNN_EINVAL. */
 qnn_status qnn_w4_matmul(const void *x, int64_t ldx, const uint8_t *codes, const void *scales, const int8_t *zeros,
@@ -379,7 +379,7 @@ typedef struct qnn_kv_cache {
  * in binary32, round() with ties away from zero.
  * k, v: DEVICE [tokens][heads][dim] of `type`; element (t, h, d) at t * token_pitch + h * head_pitch + d (elements).
  * cu: DEVICE int32 [requests + 1], not decreasing, cu[0] == 0, cu[requests] <= tokens.  start: DEVICE int32 [requests].
- * table: DEVICE int32 [requests][table_width]; requests up to 2^20, tokens below 2^30, table_width * block below 2^31.  A page must not be reached by two requests of one call.  Entries outside
+ * table: DEVICE int32 [requests][table_width]; requests up to 2^20, tokens below 2^30 and tokens / block + 2 * requests below 2^24, table_width * block below 2^31.  A page must not be reached by two requests of one call.  Entries outside
  * [0, pages) and tokens past table_width * block are left out. */
 qnn_status qnn_kv_append(const qnn_kv_cache *cache, const void *k, int64_t k_token_pitch, int64_t k_head_pitch, const void *v,
                          int64_t v_token_pitch, int64_t v_head_pitch, int type, const int32_t *cu, const int32_t *start,
@@ -400,7 +400,9 @@ qnn_status qnn_kv_gather(const qnn_kv_cache *cache, const int32_t *cu, const int
  * elements below 2^-32 of their row's largest keep fewer bits); the probabilities (scaled to at most 2^14) are rounded to binary16.
  * q, out: DEVICE [tokens][q_heads][dim] of `type`, element (t, e, d) of q at t * q_token_pitch + e * q_head_pitch + d; out
  * contiguous (rows of requests are written).  lse: DEVICE float [tokens][q_heads] or NULL.
- * max_queries: the largest number of queries of a request (more are computed too, slower); max_queries <= 0: tokens.
+ * max_queries: the largest number of queries of a request (more are computed too, slower); max_queries <= 0: tokens (a batch of
+ * single tokens then takes the launches of a prompt as long as the batch).  More than 2^23 requests times heads with max_queries * q_heads / heads over
+ * 64 are QNN_EUNSUPPORTED.
  * Page numbers outside [0, pages), and tokens past table_width * block, count as tokens that nothing sees.  tokens * q_heads / heads below 2^31, the rest as above.
  * workspace: DEVICE, 16-byte aligned, of at least qnn_kv_attention_workspace_bytes bytes for the same sizes, else QNN_EINVAL. */
 qnn_status qnn_kv_attention(const qnn_kv_cache *cache, const void *q, int64_t q_token_pitch, int64_t q_head_pitch,

@@ -395,6 +395,8 @@ static void divide_prompts(AttendLaunch &p, int64_t reach, int64_t groups, int64
 }
 
 constexpr int kFewRows = 64;
+// A launch has fewer than 2^32 threads along x (workgroups beyond them are left out without an error); workgroups loop over blocks of rows where there are more.
+constexpr int64_t kMostGroups512 = (1 << 23) - 1, kMostGroups256 = (1 << 24) - 1;
 
 static AttendPlan attend_plan(const qnn_kv_cache &cache, int q_heads, int64_t table_width, int64_t requests, int64_t tokens, int64_t window,
                               int64_t max_queries)
@@ -416,15 +418,18 @@ static AttendPlan attend_plan(const qnn_kv_cache &cache, int q_heads, int64_t ta
         if (p.many.used) p.few.rows_upto = kFewRows;
         const int64_t unit = cache.block % 64 == 0 ? 64 : 32;
         divide_context(p.few, reach, groups * p.few.row_blocks, unit, unit * cache.dim * 2, p.few.tiles * cache.dim <= 128 ? 2 : 1);
+        if (requests * p.few.row_blocks * p.few.chunks > kMostGroups256) p.few.chunks = 1; // (2^20 requests of 4 blocks are within it)
     }
     if (p.many.used) {
         if (p.few.used) p.many.rows_over = kFewRows;
         const int64_t wide = (rows + 255) / 256;
         p.many.waves = cache.dim > 128 || groups * wide < 256 ? 4 : 8;
         const int64_t blocks = (rows + 32 * p.many.waves - 1) / (32 * p.many.waves);
-        p.many.row_blocks = (int)(blocks < 4096 ? blocks : 4096);
         p.many.part_rows = (int)rows;
         divide_prompts(p.many, reach, groups, blocks, rows, cache.dim, max_queries * 2 > reach);
+        int64_t at_once = blocks < 4096 ? blocks : 4096;
+        if (groups * p.many.chunks * at_once > kMostGroups512) at_once = kMostGroups512 / (groups * p.many.chunks);
+        p.many.row_blocks = (int)(at_once > 1 ? at_once : 1);
     }
     return p;
 }
@@ -448,13 +453,14 @@ template <class T, int D> static void run_many(const AttendArgs &a, const Attend
 
 template <class T, int D, int U> static void run_join(const AttendArgs &a, hipStream_t s)
 {
-    const int per = a.part_rows < 4096 ? a.part_rows : 4096;
+    int64_t per = a.part_rows < 4096 ? a.part_rows : 4096;
+    if (a.requests * ((per + 3) / 4) > kMostGroups256) per = kMostGroups256 / a.requests * 4; // (at most 2^20 requests)
     const unsigned heads = (unsigned)a.cache.heads;
     // waves enough for the chip (or few chunks): one per row
-    if ((int64_t)a.requests * per * heads >= 2048 || a.chunks <= 8)
-        hipLaunchKernelGGL((attend_join_kernel<T, D, U, false>), dim3((unsigned)((int64_t)a.requests * ((per + 3) / 4)), heads), dim3(256), 0, s, a, per);
+    if (a.requests * per * heads >= 2048 || a.chunks <= 8)
+        hipLaunchKernelGGL((attend_join_kernel<T, D, U, false>), dim3((unsigned)(a.requests * ((per + 3) / 4)), heads), dim3(256), 0, s, a, (int)per);
     else
-        hipLaunchKernelGGL((attend_join_kernel<T, D, U, true>), dim3((unsigned)((int64_t)a.requests * per), heads), dim3(256), 0, s, a, per);
+        hipLaunchKernelGGL((attend_join_kernel<T, D, U, true>), dim3((unsigned)(a.requests * per), heads), dim3(256), 0, s, a, (int)per);
 }
 
 template <class T, int D> static qnn_status run_attend(AttendArgs a, const AttendPlan &p, char *workspace, hipStream_t s)
@@ -523,8 +529,7 @@ qnn_status qnn_kv_attention(const qnn_kv_cache *cache, const void *q, int64_t q_
     const AttendPlan p = attend_plan(*cache, q_heads, table_width, requests, tokens, window, max_queries);
     const size_t need = qnn_kv_attention_workspace_bytes(cache, q_heads, table_width, requests, tokens, window, max_queries);
     if (need > 0 && (!workspace || ((uintptr_t)workspace & 15) != 0 || workspace_bytes < need)) return QNN_EINVAL;
-    if (requests * p.few.row_blocks * p.few.chunks > INT32_MAX || requests * p.many.row_blocks * p.many.chunks * cache->heads > INT32_MAX)
-        return QNN_EUNSUPPORTED;
+    if (requests * p.many.row_blocks * p.many.chunks * cache->heads > kMostGroups512) return QNN_EUNSUPPORTED;
     AttendArgs a{};
     a.cache = *cache, a.q = static_cast<const uint16_t *>(q), a.q_token_pitch = q_token_pitch, a.q_head_pitch = q_head_pitch;
     a.cu = cu, a.lengths = lengths, a.table = table, a.out = static_cast<uint16_t *>(out), a.lse = lse;

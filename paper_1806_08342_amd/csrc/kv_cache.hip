@@ -295,7 +295,7 @@ template <class T, bool GATHER> static void launch_pieces(const CacheArgs &a, hi
 static bool bad_cache_call(const qnn_kv_cache *cache, int64_t table_width, int64_t requests, int64_t tokens, int type)
 {
     return bad_cache(cache) || bad_half_type(type) || table_width < 0 || table_width > INT32_MAX / cache->block || requests < 0 || requests > (1 << 20) ||
-           tokens < 0 || tokens > INT32_MAX / 2;
+           tokens < 0 || tokens > INT32_MAX / 2 || tokens / cache->block + 2 * requests >= (1 << 24); // (a launch has fewer than 2^32 threads along x)
 }
 } // namespace qnn
 

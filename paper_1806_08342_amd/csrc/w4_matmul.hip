@@ -233,9 +233,10 @@ using namespace qnn;
 
 extern "C" {
 
+// (N: a launch has fewer than 2^32 threads along x, 16 for each row of weights)
 static bool bad_w4_sizes(int64_t M, int64_t N, int64_t K, int64_t group)
 {
-    return M < 0 || N <= 0 || K <= 0 || K % 2 != 0 || group <= 0 || group % 32 != 0 || M > (1 << 20) || N > (1 << 28) || K > (1 << 24) || (K + group - 1) / group * N >= (1 << 30);
+    return M < 0 || N <= 0 || K <= 0 || K % 2 != 0 || group <= 0 || group % 32 != 0 || M > (1 << 20) || N > (1 << 28) - 32 || K > (1 << 24) || (K + group - 1) / group * N >= (1 << 30);
 }
 
 // Which kernel, by what each is estimated to take (us):

@@ -204,3 +204,19 @@ def test_tokens_past_the_table_are_not_seen(dim, block, window):
         want, want_lse, spread = attend(cache, q, *of, window=window)
         assert_close(out, want, attention_allows(cache, q, want, spread, *of, window=window).nan_to_num(2.0 ** -30), (dim, block, window, n))
         assert torch.equal(torch.isfinite(lse).cpu(), torch.isfinite(want_lse))
+
+
+def test_thousands_of_requests_whose_longest_is_not_told():
+    # every request might have all queries: workgroups for all of their rows would be more than a launch takes
+    n, heads, group = 20000, 8, 8
+    cache, q, cu, lengths, table = case([(1 + i % 3, 1) for i in range(40)] + [(2000, 2000)], heads, 64, 32, torch.bfloat16, 0, q_heads=heads * group)
+    rows = torch.arange(n, device=DEV) % 40  # the 40 requests of one query again and again
+    told = qnn.kv_attention(cache, q, cu, lengths, table, max_queries=2000)
+    many = qnn.kv_attention(cache, q[rows].contiguous(), torch.arange(n + 1, dtype=torch.int32, device=DEV), lengths[rows].contiguous(), table[rows].contiguous())
+    assert torch.equal(many, told[rows])
+    # and a last one with many, whose workgroups come last
+    cu = torch.cat([torch.arange(n, dtype=torch.int32, device=DEV), torch.tensor([n + 1999], dtype=torch.int32, device=DEV)])
+    at = torch.cat([rows[:-1], torch.tensor([40], device=DEV)])
+    q = torch.cat([q[rows[:-1]], q[-2000:]])
+    many = qnn.kv_attention(cache, q, cu, lengths[at].contiguous(), table[at].contiguous())
+    assert torch.equal(many[:n - 1], told[rows[:-1]]) and torch.equal(many[n - 1:], told[-2000:])
