@@ -491,7 +491,7 @@ def w4_matmul(x, codes, scales, group, zeros=None, bias=None, out=None, workspac
     """x [M,K] (bfloat16 or float16, rows may be spaced apart) times 4-bit weights [N,K] with one scale per `group` weights of
     a row: y[m,n] = bias[n] + sum_k x[m,k] * (c[n,k] - zeros[k//group,n]) * scales[k//group,n].  codes: uint8 [N,K/2]
     (as `pack_int4` packs rows); scales: [ceil(K/group),N] of x's type; zeros: int8 of that shape or None; group: a multiple of
-    32.  Returns [M,N] of x's type."""
+    32.  Returns [M,N] of x's type.  For inference: tensors that require grad are refused while gradients are recorded."""
     return (_nat or _native()).w4_matmul(x, codes, scales, group, zeros, bias, out, workspace)
 
 
@@ -511,12 +511,14 @@ def new_kv_cache(pages, heads, dim, block=64, device="cuda:0"):
 def kv_append(cache, k, v, cu, start, table):
     """Append rows cu[r]:cu[r+1] of k and v ([T,heads,dim], bfloat16 or float16, views with a contiguous last dimension will do)
     to request r, which holds start[r] tokens.  cu int32 [R+1], start int32 [R], table int32 [R,W]: page of its tokens
-    j*block and up.  Where a block's range grows, the codes it holds are rescaled."""
+    j*block and up.  Where a block's range grows, the codes it holds are rescaled.  Tensors that require grad are refused while
+    gradients are recorded."""
     (_nat or _native()).kv_append(cache, k, v, cu, start, table)
 
 
 def kv_gather(cache, cu, first, table, tokens, dtype):
-    """The cached tokens first[r] + i as rows cu[r] + i of (k, v), each [tokens,heads,dim] of `dtype`."""
+    """The cached tokens first[r] + i as rows cu[r] + i of (k, v), each [tokens,heads,dim] of `dtype`.  Rows from cu[-1] on are
+    uninitialised; a token without a page gives 0."""
     return (_nat or _native()).kv_gather(cache, cu, first, table, tokens, _half_code(dtype))
 
 
@@ -525,7 +527,8 @@ def kv_attention(cache, q, cu, lengths, table, scale=None, window=0, max_queries
     lengths[r] in the cache), each sees the tokens up to its own, the last `window` of them if window > 0.  q_heads is a multiple
     of the cache's heads.  scale: 1/sqrt(dim) unless given.  max_queries: the largest number of queries of a request (T unless
     given).  Returns [T,q_heads,dim] of q's type, with_lse: and the logarithm of each row's sum, float32 [T,q_heads].  A query
-    that sees nothing gives 0 (and -inf)."""
+    that sees nothing gives 0 (and -inf); rows that no request has stay as they are (uninitialised without `out`).  For inference:
+    tensors that require grad are refused while gradients are recorded."""
     if scale is None:
         scale = q.shape[-1] ** -0.5
     return (_nat or _native()).kv_attention(cache, q, cu, lengths, table, scale, window, max_queries or 0, with_lse, out, workspace)

@@ -18,6 +18,7 @@
 #include <c10/util/Exception.h>
 #include <c10/util/SmallVector.h>
 #include <torch/csrc/Exceptions.h>
+#include <ATen/core/grad_mode.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/qnn.h"
@@ -676,9 +677,17 @@ struct Halves {
     void *p;
     int type;
 };
+// These operators have no backward pass: what a caller would differentiate is refused, where a result cut off from it would go unnoticed.
+void no_grad(const at::Tensor &t, const char *name)
+{
+    if (!t.requires_grad() || !at::GradMode::is_enabled()) return;
+    PyErr_Format(PyExc_RuntimeError, "%s requires grad, and this operator has no backward pass: call it under torch.no_grad(), or with a detached tensor", name);
+    throw PythonErrorSet{};
+}
 Halves halves(PyObject *o, const char *name, int64_t dims)
 {
     const at::Tensor &t = tensor(o, name);
+    no_grad(t, name);
     const bool kind = t.scalar_type() == at::kBFloat16 || t.scalar_type() == at::kHalf;
     if (!t.is_cuda() || !kind || t.dim() != dims || !(t.numel() == 0 || t.size(dims - 1) == 1 || t.stride(dims - 1) == 1))
         type_error(name, dims == 2 ? "a 2-D device tensor of torch.bfloat16 or torch.float16 with contiguous rows"
@@ -710,6 +719,7 @@ void same_device(const at::Tensor &t, const at::Tensor &like, const char *name)
 const void *param(PyObject *o, at::ScalarType type, const char *name, at::IntArrayRef want, const at::Tensor &like)
 {
     const at::Tensor &t = tensor(o, name);
+    no_grad(t, name);
     if (!t.is_cuda() || t.scalar_type() != type || !t.is_contiguous()) type_error(name, type_name(type));
     want_shape(t, name, want);
     same_device(t, like, name);

@@ -220,3 +220,25 @@ def test_thousands_of_requests_whose_longest_is_not_told():
     q = torch.cat([q[rows[:-1]], q[-2000:]])
     many = qnn.kv_attention(cache, q, cu, lengths[at].contiguous(), table[at].contiguous())
     assert torch.equal(many[:n - 1], told[rows[:-1]]) and torch.equal(many[n - 1:], told[-2000:])
+
+
+# --------------------------------------------------------------------------- gradients
+
+def test_no_result_is_cut_off_from_what_requires_grad():
+    g = torch.Generator().manual_seed(0)
+    x = torch.randn(4, 64, generator=g).to(torch.bfloat16).to(DEV)
+    codes, scales, z = weights(20, 64, 32, torch.bfloat16, g)
+    bias = torch.zeros(20, dtype=torch.bfloat16, device=DEV)
+    cache, q, cu, lengths, table = case([(70, 2)], 2, 64, 32, torch.bfloat16, 0, q_heads=4)
+    kv = torch.zeros(2, 2, 64, dtype=torch.bfloat16, device=DEV)
+    calls = [(lambda: qnn.w4_matmul(x, codes, scales, 32, z, bias), (x, scales, bias)), (lambda: qnn.kv_attention(cache, q, cu, lengths, table), (q, cache[1], cache[3])),
+             (lambda: qnn.kv_append(cache, kv, kv, cu, lengths - 2, table), (kv,))]
+    for call, tensors in calls:
+        call()
+        for t in tensors:
+            t.requires_grad_(True)
+            with pytest.raises(RuntimeError, match="no backward pass"):
+                call()
+            with torch.no_grad():
+                call()
+            t.requires_grad_(False)
