@@ -40,6 +40,7 @@ template <class T, int D, int U, int NT> __global__ void __launch_bounds__(256, 
     const int block = a.cache.block, heads = a.cache.heads;
 
     __shared__ float s_m[4][16 * NT], s_l[4][16 * NT];
+    __shared__ int s_large[4];
     __shared__ __attribute__((aligned(16))) float s_o[2][16 * NT][D + 4];
 
     for (int rt = rb * 16 * NT; rt < rows; rt += a.row_blocks * 16 * NT) {
@@ -133,11 +134,19 @@ template <class T, int D, int U, int NT> __global__ void __launch_bounds__(256, 
             }
         };
 
+        bool large = false; // o stands in units of 2^kLargeUnit
+        for (int from = 64; from < mine; from += 64) {
+            look_up(from);
+            large |= (bool)__any(u_vs > kLargeScale);
+        }
         if (mine > 0) {
             look_up(0);
             load_keys(0);
             load_values(0);
+            large |= (bool)__any(u_vs > kLargeScale);
         }
+        const float in_unit = ldexpf(1.0f, large ? -kLargeUnit : 0);
+        u_vs *= in_unit;
         for (int k = 0; k < mine; ++k) {
             const int64_t t = t0 + (int64_t)(wave + 4 * k) * U;
             const bool missing = __builtin_amdgcn_readlane(u_page, k & 63) < 0;
@@ -226,6 +235,7 @@ template <class T, int D, int U, int NT> __global__ void __launch_bounds__(256, 
             if (more) {
                 if (refill) {
                     look_up(k + 1);
+                    u_vs *= in_unit;
                     load_keys(k + 1);
                 }
                 load_values(k + 1);
@@ -238,7 +248,10 @@ template <class T, int D, int U, int NT> __global__ void __launch_bounds__(256, 
             l[nt] = sum_over_groups(l[nt]);
             if (g == 0) s_m[wave][nt * 16 + c] = m[nt], s_l[wave][nt * 16 + c] = l[nt];
         }
+        if (lane == 0) s_large[wave] = large;
         __syncthreads();
+        const bool any_large = s_large[0] | s_large[1] | s_large[2] | s_large[3];
+        const float unit = ldexpf(1.0f, any_large && !large ? -kLargeUnit : 0), back = ldexpf(1.0f, any_large ? kLargeUnit : 0);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             float top = s_m[0][nt * 16 + c], sum = 0.0f;
@@ -246,7 +259,7 @@ template <class T, int D, int U, int NT> __global__ void __launch_bounds__(256, 
             for (int w = 1; w < 4; ++w) top = fmaxf(top, s_m[w][nt * 16 + c]);
 #pragma unroll
             for (int w = 0; w < 4; ++w) sum += s_l[w][nt * 16 + c] * exp2_fast(s_m[w][nt * 16 + c] - top);
-            const float by = exp2_fast(m[nt] - top);
+            const float by = exp2_fast(m[nt] - top) * unit;
             m[nt] = top, l[nt] = sum;
 #pragma unroll
             for (int v = 0; v < VT; ++v) o[nt][v] *= by;
@@ -275,7 +288,7 @@ template <class T, int D, int U, int NT> __global__ void __launch_bounds__(256, 
                     uint16_t *out = a.out + row_id[nt] * D;
 #pragma unroll
                     for (int v = 0; v < VT; ++v) {
-                        const f32x4 x = o[nt][v] * inv;
+                        const f32x4 x = o[nt][v] * inv * back;
                         *reinterpret_cast<w32x2 *>(out + v * 16 + g * 4) = w32x2{narrow2<T>(x[0], x[1]), narrow2<T>(x[2], x[3])};
                     }
                     if (a.lse && g == 0) a.lse[row_id[nt]] = l[nt] != 0.0f ? (m[nt] - kHead + log2f(l[nt])) * 0.69314718056f : -INFINITY;
@@ -283,7 +296,7 @@ template <class T, int D, int U, int NT> __global__ void __launch_bounds__(256, 
                     const int64_t part = part_row(a, r, h, rt + nt * 16 + c) * a.chunks + chunk;
 #pragma unroll
                     for (int v = 0; v < VT; ++v) *reinterpret_cast<f32x4 *>(a.part_o + part * D + v * 16 + g * 4) = o[nt][v];
-                    if (g == 0) a.part_ml[2 * part] = m[nt], a.part_ml[2 * part + 1] = l[nt];
+                    if (g == 0) a.part_ml[2 * part] = m[nt], a.part_ml[2 * part + 1] = any_large ? -l[nt] : l[nt];
                 }
             }
     }
@@ -307,14 +320,19 @@ template <class T, int D, int U, bool SHARED> __global__ void __launch_bounds__(
         const int64_t part = part_row(a, r, h, row) * a.chunks;
         const float *ml = a.part_ml + part * 2, *po = a.part_o + part * D;
         float top = kNothing;
-        for (int i = lane; i < chunks; i += 64) top = fmaxf(top, ml[2 * i]);
+        bool large = false;
+        for (int i = lane; i < chunks; i += 64) top = fmaxf(top, ml[2 * i]), large |= ml[2 * i + 1] < 0.0f;
 #pragma unroll
         for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
+        large = __any(large);
+        const float ordinary = ldexpf(1.0f, large ? -kLargeUnit : 0), back = ldexpf(1.0f, large ? kLargeUnit : 0);
         float o[(D + 63) / 64] = {}, l = 0.0f;
 #pragma unroll 4
         for (int i = SHARED ? wave : 0; i < chunks; i += SHARED ? 4 : 1) {
-            const float w = exp2_fast(ml[2 * i] - top);
-            l += w * ml[2 * i + 1];
+            const float part_l = ml[2 * i + 1];
+            float w = exp2_fast(ml[2 * i] - top);
+            l += w * fabsf(part_l);
+            w *= part_l < 0.0f ? 1.0f : ordinary;
 #pragma unroll
             for (int d = 0; d < (D + 63) / 64; ++d)
                 if (D % 64 == 0 || d * 64 + lane < D) o[d] = fmaf(w, po[(int64_t)i * D + d * 64 + lane], o[d]);
@@ -329,13 +347,13 @@ template <class T, int D, int U, bool SHARED> __global__ void __launch_bounds__(
             const int d = threadIdx.x;
             if (d < D) {
                 const float x = (s_o[0][d] + s_o[1][d]) + (s_o[2][d] + s_o[3][d]);
-                a.out[id * D + d] = T::narrow(l != 0.0f ? x / l : 0.0f);
+                a.out[id * D + d] = T::narrow(l != 0.0f ? x / l * back : 0.0f);
             }
         } else {
             const float inv = l != 0.0f ? 1.0f / l : 0.0f;
 #pragma unroll
             for (int d = 0; d < (D + 63) / 64; ++d)
-                if (D % 64 == 0 || d * 64 + lane < D) a.out[id * D + d * 64 + lane] = T::narrow(o[d] * inv);
+                if (D % 64 == 0 || d * 64 + lane < D) a.out[id * D + d * 64 + lane] = T::narrow(o[d] * inv * back);
         }
         if (a.lse && (SHARED ? threadIdx.x == 0 : lane == 0)) a.lse[id] = l != 0.0f ? (top - kHead + log2f(l)) * 0.69314718056f : -INFINITY;
         if (SHARED) __syncthreads();

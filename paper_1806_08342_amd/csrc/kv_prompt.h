@@ -305,15 +305,17 @@ template <class T, int D, int WAVES> __global__ void __launch_bounds__(64 * WAVE
                     *reinterpret_cast<w32x2 *>(out + 32 * v + 2 * i) = w32x2{narrow2<T>(o[v][i] * inv, o[v][i + 1] * inv), narrow2<T>(o[v][i + 2] * inv, o[v][i + 3] * inv)};
             if (a.lse && hh == 0) a.lse[row_id] = l != 0.0f ? (m - kPromptHead + log2f(l)) * 0.69314718056f : -INFINITY;
         } else {
+            const bool large = unit.peak >= ValueUnit::exponent(__builtin_bit_cast(int, kLargeScale));
+            const float own = ldexpf(1.0f, unit.at - (large ? kLargeUnit : 0));
             const int64_t part = part_row(a, r, h, rt + wave * 32 + c) * a.chunks + chunk;
 #pragma unroll
             for (int v = 0; v < VT; ++v)
 #pragma unroll
                 for (int i = 0; i < 16; i += 4)
                     *reinterpret_cast<f32x4 *>(a.part_o + part * D + 32 * v + 2 * i + 4 * hh) =
-                        f32x4{o[v][i], o[v][i + 1], o[v][i + 2], o[v][i + 3]} * ldexpf(1.0f, unit.at);
+                        f32x4{o[v][i], o[v][i + 1], o[v][i + 2], o[v][i + 3]} * own;
             // (the join takes maxima with the head room of the kernel for few rows)
-            if (hh == 0) a.part_ml[2 * part] = m + (kHead - kPromptHead), a.part_ml[2 * part + 1] = l;
+            if (hh == 0) a.part_ml[2 * part] = m + (kHead - kPromptHead), a.part_ml[2 * part + 1] = large ? -l : l;
         }
     }
 }

@@ -259,11 +259,13 @@ template <class T, int D> __global__ void __launch_bounds__(512, 2) attend_wide_
             }
             if (a.lse && g == 0) a.lse[row_id] = l != 0.0f ? (m - kPromptHead + log2f(l)) * 0.69314718056f : -INFINITY;
         } else {
+            const bool large = unit.peak >= ValueUnit::exponent(__builtin_bit_cast(int, kLargeScale));
+            const float own = ldexpf(1.0f, unit.at - (large ? kLargeUnit : 0));
             const int64_t part = part_row(a, r, h, row) * a.chunks + chunk;
 #pragma unroll
-            for (int v = 0; v < VT; ++v) *reinterpret_cast<f32x4 *>(a.part_o + part * D + 16 * v + 4 * g) = o[v] * ldexpf(1.0f, unit.at);
+            for (int v = 0; v < VT; ++v) *reinterpret_cast<f32x4 *>(a.part_o + part * D + 16 * v + 4 * g) = o[v] * own;
             // (the join takes maxima with the head room of the kernel for few rows)
-            if (g == 0) a.part_ml[2 * part] = m + (kHead - kPromptHead), a.part_ml[2 * part + 1] = l;
+            if (g == 0) a.part_ml[2 * part] = m + (kHead - kPromptHead), a.part_ml[2 * part + 1] = large ? -l : l;
         }
     }
 }

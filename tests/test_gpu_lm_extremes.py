@@ -242,3 +242,18 @@ def test_no_result_is_cut_off_from_what_requires_grad():
             with torch.no_grad():
                 call()
             t.requires_grad_(False)
+
+
+@pytest.mark.parametrize("scale", [2.0 ** 70, 2.0 ** 74, 2.0 ** 100, 2.0 ** 119])
+@pytest.mark.parametrize("dim", [64, 256])
+def test_values_up_to_the_end_of_the_type(dim, scale):
+    # scales alike, and one such page among ordinary ones
+    for requests, most in (([(300, 300), (200, 150)], 300), ([(300, 1), (200, 3)], 3), ([(9001, 40)], 40), ([(40000, 1)], 1)):
+        cache, q, cu, lengths, table = case(requests, 1, dim, 64, torch.bfloat16, 1, q_heads=4)
+        cache[3].mul_(scale / 0.025)  # at most `scale`
+        check_attention(cache, q, cu, lengths, table, (scale, dim, most), max_queries=most)
+        last = [int(table[r, (n - 1) // 64]) for r, (n, _) in enumerate(requests)]
+        small = torch.ones(cache[3].shape[0], 1, device=DEV) * 0.02 / scale
+        small[last] = 1.0
+        cache[3].mul_(small)
+        check_attention(cache, q, cu, lengths, table, (scale, dim, most, "one"), max_queries=most)
