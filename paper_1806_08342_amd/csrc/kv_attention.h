@@ -27,7 +27,7 @@ struct AttendArgs {
     uint16_t *out;
     float *lse;
     float *part_o;  // [requests][heads][part_rows][chunks][dim]
-    float *part_ml; // [requests][heads][part_rows][chunks][2]; l < 0: part_o in units of 2^kLargeUnit
+    float *part_ml; // [requests][heads][part_rows][chunks][2]: reference and sum of a part; sum < 0: part_o in units of 2^kLargeUnit
     int64_t table_width, tokens, window;
     float scale; // times log2(e)
     int32_t q_heads, group, requests;
@@ -39,6 +39,10 @@ struct AttendArgs {
 constexpr float kNothing = -3.0e38f; // running maximum before the first token that is seen
 // probabilities are held as 2^kHead times their value: what binary16 loses below its normal numbers starts that much lower
 constexpr float kHead = 14.0f;
+// Scores (times log2(e)) of this size are 2^-4 apart at least: a head room taken off them would be rounded away, or up to 2^16.
+constexpr float kFarScore = 0x1p20f;
+// what scores are taken against, below their maximum by the head room
+__device__ __forceinline__ float reference_of(float most) { return most - (fabsf(most) < kFarScore ? kHead : 0.0f); }
 // Sums of up to 2^31 probabilities of 2^14 with values of 127 steps stay within binary32 up to scales of 2^72.  Where a page's scale is
 // larger, sums stand in units of 2^48 (parts of a context say so by the sign of l).
 constexpr float kLargeScale = 0x1p72f;

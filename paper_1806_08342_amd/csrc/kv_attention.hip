@@ -200,8 +200,8 @@ template <class T, int D, int U, int NT> __global__ void __launch_bounds__(256, 
                 for (int i = 0; i < S; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) top = fmaxf(top, s[nt][i][e]);
-                const float now = fmaxf(m[nt], max_over_groups(top));
-                shrink[nt] = exp2_fast(m[nt] - now);
+                const float now = fmaxf(m[nt], max_over_groups(top)), against = reference_of(now);
+                shrink[nt] = exp2_fast(reference_of(m[nt]) - against);
                 grew |= now > m[nt];
                 m[nt] = now;
                 float sum = 0.0f;
@@ -209,7 +209,7 @@ template <class T, int D, int U, int NT> __global__ void __launch_bounds__(256, 
                 for (int i = 0; i < S; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float x = exp2_fast(s[nt][i][e] - (now - kHead));
+                        const float x = exp2_fast(s[nt][i][e] - against);
                         sum += x;
                         p[nt][i >> 1][(i & 1) * 4 + e] = (_Float16)x;
                     }
@@ -245,7 +245,7 @@ template <class T, int D, int U, int NT> __global__ void __launch_bounds__(256, 
         // the four waves' parts, joined: two of them, then the other two, in a fixed order
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            l[nt] = sum_over_groups(l[nt]);
+            l[nt] = sum_over_groups(l[nt]), m[nt] = reference_of(m[nt]); // (references from here on)
             if (g == 0) s_m[wave][nt * 16 + c] = m[nt], s_l[wave][nt * 16 + c] = l[nt];
         }
         if (lane == 0) s_large[wave] = large;
@@ -291,7 +291,7 @@ template <class T, int D, int U, int NT> __global__ void __launch_bounds__(256, 
                         const f32x4 x = o[nt][v] * inv * back;
                         *reinterpret_cast<w32x2 *>(out + v * 16 + g * 4) = w32x2{narrow2<T>(x[0], x[1]), narrow2<T>(x[2], x[3])};
                     }
-                    if (a.lse && g == 0) a.lse[row_id[nt]] = l[nt] != 0.0f ? (m[nt] - kHead + log2f(l[nt])) * 0.69314718056f : -INFINITY;
+                    if (a.lse && g == 0) a.lse[row_id[nt]] = l[nt] != 0.0f ? (m[nt] + log2f(l[nt])) * 0.69314718056f : -INFINITY;
                 } else {
                     const int64_t part = part_row(a, r, h, rt + nt * 16 + c) * a.chunks + chunk;
 #pragma unroll
@@ -355,7 +355,7 @@ template <class T, int D, int U, bool SHARED> __global__ void __launch_bounds__(
             for (int d = 0; d < (D + 63) / 64; ++d)
                 if (D % 64 == 0 || d * 64 + lane < D) a.out[id * D + d * 64 + lane] = T::narrow(o[d] * inv * back);
         }
-        if (a.lse && (SHARED ? threadIdx.x == 0 : lane == 0)) a.lse[id] = l != 0.0f ? (top - kHead + log2f(l)) * 0.69314718056f : -INFINITY;
+        if (a.lse && (SHARED ? threadIdx.x == 0 : lane == 0)) a.lse[id] = l != 0.0f ? (top + log2f(l)) * 0.69314718056f : -INFINITY;
         if (SHARED) __syncthreads();
     }
 }

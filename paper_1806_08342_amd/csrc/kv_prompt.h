@@ -118,6 +118,7 @@ template <class T, int D, int WAVES> __global__ void __launch_bounds__(64 * WAVE
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[v][i] = 0.0f;
         ValueUnit unit; // that o stands in
+        bool far = false; // a row's scores are so large that their products have to be rounded before the maximum is taken off
 
         // lane i holds place and scales of the i-th of 64 halves (32 tokens)
         int32_t u_page = 0, u_at = 0;
@@ -239,40 +240,45 @@ template <class T, int D, int WAVES> __global__ void __launch_bounds__(64 * WAVE
                 if (__any(grew) || up != 0) {
                     const float now = fmaxf(m, most), shrink = exp2_fast(m - now), by = ldexpf(shrink, up);
                     m = now, l *= shrink;
+                    far = __any(fabsf(m) >= kFarScore && m > kNothing);
 #pragma unroll
                     for (int v = 0; v < VT; ++v) o[v] *= by;
                 }
                 h16x8 p[4];
-                // probabilities of a tile, times 2^add; returns their sum
-                const auto probabilities = [&](int y, float add) {
-                    const float off = add - m;
+                // probabilities of a tile from the exponents of its scores; returns their sum
+                const auto probabilities = [&](int y, auto exponent) {
                     float sum = 0.0f;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const float e = exp2_fast(fmaf(s[y][i], fk[y], off));
+                        const float e = exp2_fast(exponent(s[y][i]));
                         sum += e;
                         p[2 * y + (i >> 3)][i & 7] = (_Float16)e;
                     }
                     return sum;
                 };
                 const auto value = [&](int v, int k) { return *reinterpret_cast<const h16x8 *>(&s_v[buf][32 * v + c][16 * k + 8 * hh]); };
-                const bool joined = (missing[0] || unit.is_near(vs[0])) && (missing[1] || unit.is_near(vs[1])); // scales are part of p
+                const bool joined = !far && (missing[0] || unit.is_near(vs[0])) && (missing[1] || unit.is_near(vs[1])); // scales are part of p
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
                     const float ratio = joined && !missing[y] ? ldexpf(__builtin_bit_cast(float, vs[y]), -unit.at) : 1.0f;
-                    const float sum = probabilities(y, joined ? __log2f(ratio) + kPromptHead : -INFINITY);
+                    const float off = joined ? __log2f(ratio) + kPromptHead - m : -INFINITY;
+                    const float sum = probabilities(y, [&](float x) { return fmaf(x, fk[y], off); });
                     l = fmaf(sum, __builtin_amdgcn_rcpf(ratio), l); // (takes out of the sum what the scale has brought in)
                 }
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
 #pragma unroll
                     for (int v = 0; v < VT; ++v) o[v] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value(v, k), p[k], o[v], 0, 0, 0);
-                if (!joined) { // nothing so far: each tile's product by itself
+                if (!joined) { // nothing so far: each tile's product by itself, scores as they went into the maximum
                     asm volatile("" : "+v"(l)::"memory"); // (once more from the keys on: scores kept until here would take registers from every unit)
                     scores();
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
-                        l += probabilities(y, kPromptHead);
+                        l += probabilities(y, [&](float x) {
+                            float score = x * fk[y];
+                            asm("" : "+v"(score)); // (rounded: not one operation with the difference)
+                            return score - m + kPromptHead;
+                        });
                         asm volatile("" : "+v"(l)); // (formed here: further down the sum would keep all of them)
                         const float scale = ldexpf(__builtin_bit_cast(float, vs[y]), -unit.at);
 #pragma unroll
@@ -314,8 +320,7 @@ template <class T, int D, int WAVES> __global__ void __launch_bounds__(64 * WAVE
                 for (int i = 0; i < 16; i += 4)
                     *reinterpret_cast<f32x4 *>(a.part_o + part * D + 32 * v + 2 * i + 4 * hh) =
                         f32x4{o[v][i], o[v][i + 1], o[v][i + 2], o[v][i + 3]} * own;
-            // (the join takes maxima with the head room of the kernel for few rows)
-            if (hh == 0) a.part_ml[2 * part] = m + (kHead - kPromptHead), a.part_ml[2 * part + 1] = large ? -l : l;
+            if (hh == 0) a.part_ml[2 * part] = m - kPromptHead, a.part_ml[2 * part + 1] = large ? -l : l;
         }
     }
 }

@@ -81,6 +81,7 @@ template <class T, int D> __global__ void __launch_bounds__(512, 2) attend_wide_
 #pragma unroll
         for (int v = 0; v < VT; ++v) o[v] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         ValueUnit unit; // that o stands in
+        bool far = false; // a row's scores are so large that their products have to be rounded before the maximum is taken off
 
         // lane i holds place and scales of the i-th of 64 halves (32 tokens)
         int32_t u_page = 0, u_at = 0;
@@ -197,40 +198,45 @@ template <class T, int D> __global__ void __launch_bounds__(512, 2) attend_wide_
                 if (__any(most > m + kRoom) || up != 0) {
                     const float now = fmaxf(m, most), shrink = exp2_fast(m - now), by = ldexpf(shrink, up);
                     m = now, l *= shrink;
+                    far = __any(fabsf(m) >= kFarScore && m > kNothing);
 #pragma unroll
                     for (int v = 0; v < VT; ++v) o[v] *= by;
                 }
                 h16x8 p[2];
-                // probabilities of a tile, times 2^add; returns their sum
-                const auto probabilities = [&](int y, float add) {
-                    const float off = add - m;
+                // probabilities of a tile from the exponents of its scores; returns their sum
+                const auto probabilities = [&](int y, auto exponent) {
                     float sum = 0.0f;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const float x = exp2_fast(fmaf(s[2 * y + (i >> 2)][i & 3], fk[y], off));
+                        const float x = exp2_fast(exponent(s[2 * y + (i >> 2)][i & 3]));
                         sum += x;
                         p[y][i] = (_Float16)x;
                     }
                     return sum;
                 };
                 const auto value = [&](int v, int y) { return *reinterpret_cast<const h16x8 *>(&s_v[buf][v_place(16 * v + c, 4 * y + g)]); };
-                const bool joined = (missing[0] || unit.is_near(vs[0])) && (missing[1] || unit.is_near(vs[1])); // scales are part of p
+                const bool joined = !far && (missing[0] || unit.is_near(vs[0])) && (missing[1] || unit.is_near(vs[1])); // scales are part of p
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
                     const float ratio = joined && !missing[y] ? ldexpf(__builtin_bit_cast(float, vs[y]), -unit.at) : 1.0f;
-                    const float sum = probabilities(y, joined ? __log2f(ratio) + kPromptHead : -INFINITY);
+                    const float off = joined ? __log2f(ratio) + kPromptHead - m : -INFINITY;
+                    const float sum = probabilities(y, [&](float x) { return fmaf(x, fk[y], off); });
                     l = fmaf(sum, __builtin_amdgcn_rcpf(ratio), l); // (takes out of the sum what the scale has brought in)
                 }
 #pragma unroll
                 for (int y = 0; y < 2; ++y)
 #pragma unroll
                     for (int v = 0; v < VT; ++v) o[v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(value(v, y), p[y], o[v], 0, 0, 0);
-                if (!joined) { // nothing so far: each tile's product by itself
+                if (!joined) { // nothing so far: each tile's product by itself, scores as they went into the maximum
                     asm volatile("" : "+v"(l)::"memory"); // (once more from the keys on: scores kept until here would take registers from every unit)
                     scores();
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
-                        l += probabilities(y, kPromptHead);
+                        l += probabilities(y, [&](float x) {
+                            float score = x * fk[y];
+                            asm("" : "+v"(score)); // (rounded: not one operation with the difference)
+                            return score - m + kPromptHead;
+                        });
                         asm volatile("" : "+v"(l)); // (formed here: further down the sum would keep all of them)
                         const float scale = ldexpf(__builtin_bit_cast(float, vs[y]), -unit.at);
 #pragma unroll
@@ -264,8 +270,7 @@ template <class T, int D> __global__ void __launch_bounds__(512, 2) attend_wide_
             const int64_t part = part_row(a, r, h, row) * a.chunks + chunk;
 #pragma unroll
             for (int v = 0; v < VT; ++v) *reinterpret_cast<f32x4 *>(a.part_o + part * D + 16 * v + 4 * g) = o[v] * own;
-            // (the join takes maxima with the head room of the kernel for few rows)
-            if (g == 0) a.part_ml[2 * part] = m + (kHead - kPromptHead), a.part_ml[2 * part + 1] = large ? -l : l;
+            if (g == 0) a.part_ml[2 * part] = m - kPromptHead, a.part_ml[2 * part + 1] = large ? -l : l;
         }
     }
 }

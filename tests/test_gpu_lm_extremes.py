@@ -257,3 +257,55 @@ def test_values_up_to_the_end_of_the_type(dim, scale):
         small[last] = 1.0
         cache[3].mul_(small)
         check_attention(cache, q, cu, lengths, table, (scale, dim, most, "one"), max_queries=most)
+
+
+# --------------------------------------------------------------------------- prompts: queries of all kinds, windows, every head size
+
+@pytest.mark.parametrize("dim", [64, 96, 128, 192, 256])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_queries_that_are_large_small_or_no_numbers_in_prompts(dim, dtype):
+    cache, q, cu, lengths, table = case([(300, 300), (200, 70), (90, 90)], 2, dim, 32, dtype, dim, q_heads=4)
+    top = 1e30 if dtype is torch.bfloat16 else 60.0
+    q[250] = (q[250].float() * top).to(dtype)
+    q[251] = (q[251].float() / top).to(dtype)
+    q[252] = 0.0
+    q[253, 1, 5], q[254, 2, 7], q[310, 0, 0] = float("nan"), float("inf"), float("-inf")
+    out = qnn.kv_attention(cache, q, cu, lengths, table, max_queries=300)
+    of = [t.cpu() for t in (cu, lengths, table)]
+    bad = torch.zeros(q.shape[:2], dtype=torch.bool)
+    bad[253, 1] = bad[254, 2] = bad[310, 0] = True
+    assert not torch.isfinite(out.cpu()[bad]).any() and torch.isfinite(out.cpu()[~bad]).all()
+    clean = q.clone()
+    clean[bad.to(DEV)] = 1.0
+    want, _, spread = attend(cache, clean, *of)
+    allowed = attention_allows(cache, clean, want, spread, *of)
+    allowed[250] += 4e-4 * spread[250] + 1e-6  # scores of hundreds in binary32; of 1e30: the largest takes all
+    assert_close(torch.where(bad.to(DEV)[..., None], 0, out), torch.where(bad[..., None], 0.0, want), allowed, (dim, dtype))
+
+
+@pytest.mark.parametrize("window", [1, 31, 64, 100])
+@pytest.mark.parametrize("dim,block", [(96, 32), (96, 64), (192, 96), (192, 128)])
+def test_windows_of_the_other_head_sizes(dim, block, window):
+    args = case([(700, 1), (65, 4), (300, 300), (3, 3), (0, 0), (128, 9), (129, 70)], 2, dim, block, torch.float16, window, q_heads=6)
+    check_attention(*args, (window, dim), window=window, max_queries=300)
+    few = case([(700, 1), (65, 4), (3, 3), (0, 0), (128, 4)], 2, dim, block, torch.float16, window, q_heads=6)
+    check_attention(*few, (window, dim, "few"), window=window, max_queries=4)
+
+
+@pytest.mark.parametrize("size", [2.0 ** 18, 2.0 ** 22, 2.0 ** 25, 2.0 ** 26, 2.0 ** 27, 2.0 ** 28, 2.0 ** 30, 2.0 ** 40, 1e30])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_scores_of_any_size(dim, size):
+    # keys whose scores are whole numbers times the size: the largest takes all, equal ones share, however far up the exponents go
+    g = torch.Generator().manual_seed(dim)
+    for requests, most in (([(300, 300), (200, 70)], 300), ([(300, 1), (200, 3)], 3), ([(5000, 1)], 1), ([(5000, 40)], 40)):
+        cache, q, cu, lengths, table = case(requests, 1, dim, 64, torch.bfloat16, 3, q_heads=2)
+        cache[0][:, :, :, 1:] = 0  # a token's score is its first channel's code
+        cache[0][:, :, :, 0] = torch.randint(-3, 4, cache[0].shape[:3], generator=g).to(torch.int8).to(DEV)
+        cache[1][:] = 1.0
+        q[:, :, 0] = size
+        q[:, 1, 0] *= -1.0
+        out, lse = qnn.kv_attention(cache, q, cu, lengths, table, scale=1.0, max_queries=most, with_lse=True)
+        of = [t.cpu() for t in (cu, lengths, table)]
+        want, want_lse, spread = attend(cache, q, *of, scale=1.0)
+        assert_close(out, want, attention_allows(cache, q, want, spread, *of, scale=1.0), (dim, size, most))
+        assert ((lse.cpu().double() - want_lse).abs() <= 2.0 ** -21 * want_lse.abs() + 1e-4).all()
