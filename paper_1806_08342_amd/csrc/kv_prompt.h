@@ -6,8 +6,8 @@
 // rows the tokens' order in a tile is chosen so that the probabilities are the second product's operand in the lane that
 // computed them: rows of K in LDS have bits 2 and 3 of the token's number exchanged.
 //
-// The running maximum and the unit that the accumulators stand in, a power of two, follow lazily: they are kept while a row's scores stay
-// below 2^kRoom times the reference and pages' value scales within 2^(kRoom - 1) of the unit or so, so that most units of tokens rescale nothing.  A
+// The running maximum and the unit that the accumulators stand in, a value scale, follow lazily: they are kept while a row's scores stay
+// below 2^kRoom times the reference and pages' value scales within 2^(kRoom - 1) of the unit at least, so that most units of tokens rescale nothing.  A
 // page's value scale is then part of the exponent (p * vs / unit), and the sum of p is corrected once per tile.  Where the scales of
 // the two tiles lie further apart, or further from any unit that the accumulators can stand in, probabilities go without them and each tile's
 // product is added by itself, with its scale in binary32: a page says nothing about rows that see only others.
@@ -25,21 +25,25 @@ namespace qnn {
 
 constexpr float kPromptHead = 6.0f, kRoom = 4.0f; // p * vs / unit stays below 2^(6 + 4 + 4) of binary16's 2^16
 
-// The unit 2^at of a wave's accumulators (the same in all lanes, from scales that are).  A page's scale is near it from 2^-3 to just under 2^4 of it.
+// The unit of a wave's accumulators (the same in all lanes, from scales that are): the scale of a page where it can be, so that the probabilities of that
+// page's tokens, 2^6 for a row's only one, are not rounded for their scale's sake.  A page's scale is near it from over 2^-4 to just under 2^4 of it.
 struct ValueUnit {
-    int at = 0, peak = -127; // peak: the largest scale so far
-    // scales are given as their patterns
+    int pattern = 0x3f800000, peak = -127; // of the unit (scales are given as patterns, too); the largest scale's exponent so far
     static __device__ __forceinline__ int exponent(int scale) { return (scale >> 23 & 255) - 127; }
-    __device__ __forceinline__ bool is_near(int scale) const { return (unsigned)(exponent(scale) - at + 3) <= 6u; }
-    // To where the scale is near, as far as accumulators can follow: they are below 2^(10 + 7 + 31) times what the unit lacks of the largest
-    // scale, which is at most 2^79, and in units up to 2^20 rows that see only pages of the smallest scales keep them.  Returns the
-    // exponent of what accumulators are to be multiplied with.
-    __device__ __forceinline__ int move_to(int scale)
+    __device__ __forceinline__ float value() const { return __builtin_bit_cast(float, pattern); }
+    __device__ __forceinline__ float of(int scale) const { return __builtin_bit_cast(float, scale) * __builtin_amdgcn_rcpf(value()); } // a scale in units
+    __device__ __forceinline__ bool is_near(int scale) const { return (unsigned)(exponent(scale) - exponent(pattern) + 3) <= 6u; }
+    // To the scale, as far as accumulators can follow: they are below 2^(10 + 7 + 31) times what the unit lacks of the largest
+    // scale, which is at most 2^79, and in units up to 2^20 rows that see only pages of the smallest scales keep them.  Returns what
+    // accumulators are to be multiplied with.
+    __device__ __forceinline__ float move_to(int scale)
     {
-        const int from = at, e = exponent(scale);
+        const float from = value();
+        const int e = exponent(scale);
         peak = max(peak, e);
-        at = min(max(max(e, peak - 60), -60), max(20, peak - 79));
-        return from - at;
+        const int at = min(max(max(e, peak - 60), -60), max(20, peak - 79));
+        pattern = at == e ? scale : (at + 127) << 23;
+        return from * __builtin_amdgcn_rcpf(value());
     }
 };
 
@@ -236,9 +240,10 @@ template <class T, int D, int WAVES> __global__ void __launch_bounds__(64 * WAVE
                 most = fmaxf(most, other_half(most));
                 grew |= most > m + kRoom;
                 const int vmost = max(vs[0], vs[1]); // (0 where there is no page)
-                const int up = vmost > 0 && !unit.is_near(vmost) ? unit.move_to(vmost) : 0;
-                if (__any(grew) || up != 0) {
-                    const float now = fmaxf(m, most), shrink = exp2_fast(m - now), by = ldexpf(shrink, up);
+                const bool move = vmost > 0 && !unit.is_near(vmost);
+                const float to_unit = move ? unit.move_to(vmost) : 1.0f;
+                if (__any(grew) || move) {
+                    const float now = fmaxf(m, most), shrink = exp2_fast(m - now), by = shrink * to_unit;
                     m = now, l *= shrink;
                     far = __any(fabsf(m) >= kFarScore && m > kNothing);
 #pragma unroll
@@ -260,7 +265,7 @@ template <class T, int D, int WAVES> __global__ void __launch_bounds__(64 * WAVE
                 const bool joined = !far && (missing[0] || unit.is_near(vs[0])) && (missing[1] || unit.is_near(vs[1])); // scales are part of p
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    const float ratio = joined && !missing[y] ? ldexpf(__builtin_bit_cast(float, vs[y]), -unit.at) : 1.0f;
+                    const float ratio = joined && !missing[y] ? unit.of(vs[y]) : 1.0f;
                     const float off = joined ? __log2f(ratio) + kPromptHead - m : -INFINITY;
                     const float sum = probabilities(y, [&](float x) { return fmaf(x, fk[y], off); });
                     l = fmaf(sum, __builtin_amdgcn_rcpf(ratio), l); // (takes out of the sum what the scale has brought in)
@@ -280,7 +285,7 @@ template <class T, int D, int WAVES> __global__ void __launch_bounds__(64 * WAVE
                             return score - m + kPromptHead;
                         });
                         asm volatile("" : "+v"(l)); // (formed here: further down the sum would keep all of them)
-                        const float scale = ldexpf(__builtin_bit_cast(float, vs[y]), -unit.at);
+                        const float scale = unit.of(vs[y]);
 #pragma unroll
                         for (int v = 0; v < VT; ++v) {
                             f32x16 x;
@@ -302,7 +307,7 @@ template <class T, int D, int WAVES> __global__ void __launch_bounds__(64 * WAVE
         l += other_half(l);
         if (wave_row + c >= rows) continue;
         if (chunks == 1) {
-            const float inv = l != 0.0f ? ldexpf(1.0f, unit.at) / l : 0.0f;
+            const float inv = l != 0.0f ? unit.value() / l : 0.0f;
             uint16_t *out = a.out + row_id * D + 4 * hh;
 #pragma unroll
             for (int v = 0; v < VT; ++v)
@@ -312,7 +317,7 @@ template <class T, int D, int WAVES> __global__ void __launch_bounds__(64 * WAVE
             if (a.lse && hh == 0) a.lse[row_id] = l != 0.0f ? (m - kPromptHead + log2f(l)) * 0.69314718056f : -INFINITY;
         } else {
             const bool large = unit.peak >= ValueUnit::exponent(__builtin_bit_cast(int, kLargeScale));
-            const float own = ldexpf(1.0f, unit.at - (large ? kLargeUnit : 0));
+            const float own = ldexpf(unit.value(), large ? -kLargeUnit : 0);
             const int64_t part = part_row(a, r, h, rt + wave * 32 + c) * a.chunks + chunk;
 #pragma unroll
             for (int v = 0; v < VT; ++v)

@@ -194,9 +194,10 @@ template <class T, int D> __global__ void __launch_bounds__(512, 2) attend_wide_
                 }
                 most = max_over_groups(most);
                 const int vmost = max(vs[0], vs[1]); // (0 where there is no page)
-                const int up = vmost > 0 && !unit.is_near(vmost) ? unit.move_to(vmost) : 0;
-                if (__any(most > m + kRoom) || up != 0) {
-                    const float now = fmaxf(m, most), shrink = exp2_fast(m - now), by = ldexpf(shrink, up);
+                const bool move = vmost > 0 && !unit.is_near(vmost);
+                const float to_unit = move ? unit.move_to(vmost) : 1.0f;
+                if (__any(most > m + kRoom) || move) {
+                    const float now = fmaxf(m, most), shrink = exp2_fast(m - now), by = shrink * to_unit;
                     m = now, l *= shrink;
                     far = __any(fabsf(m) >= kFarScore && m > kNothing);
 #pragma unroll
@@ -218,7 +219,7 @@ template <class T, int D> __global__ void __launch_bounds__(512, 2) attend_wide_
                 const bool joined = !far && (missing[0] || unit.is_near(vs[0])) && (missing[1] || unit.is_near(vs[1])); // scales are part of p
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    const float ratio = joined && !missing[y] ? ldexpf(__builtin_bit_cast(float, vs[y]), -unit.at) : 1.0f;
+                    const float ratio = joined && !missing[y] ? unit.of(vs[y]) : 1.0f;
                     const float off = joined ? __log2f(ratio) + kPromptHead - m : -INFINITY;
                     const float sum = probabilities(y, [&](float x) { return fmaf(x, fk[y], off); });
                     l = fmaf(sum, __builtin_amdgcn_rcpf(ratio), l); // (takes out of the sum what the scale has brought in)
@@ -238,7 +239,7 @@ template <class T, int D> __global__ void __launch_bounds__(512, 2) attend_wide_
                             return score - m + kPromptHead;
                         });
                         asm volatile("" : "+v"(l)); // (formed here: further down the sum would keep all of them)
-                        const float scale = ldexpf(__builtin_bit_cast(float, vs[y]), -unit.at);
+                        const float scale = unit.of(vs[y]);
 #pragma unroll
                         for (int v = 0; v < VT; ++v) {
                             const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_f16(value(v, y), p[y], f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
@@ -256,7 +257,7 @@ template <class T, int D> __global__ void __launch_bounds__(512, 2) attend_wide_
         l = sum_over_groups(l);
         if (row >= rows) continue;
         if (chunks == 1) {
-            const float inv = l != 0.0f ? ldexpf(1.0f, unit.at) / l : 0.0f;
+            const float inv = l != 0.0f ? unit.value() / l : 0.0f;
             uint16_t *out = a.out + row_id * D + 4 * g;
 #pragma unroll
             for (int v = 0; v < VT; ++v) {
@@ -266,7 +267,7 @@ template <class T, int D> __global__ void __launch_bounds__(512, 2) attend_wide_
             if (a.lse && g == 0) a.lse[row_id] = l != 0.0f ? (m - kPromptHead + log2f(l)) * 0.69314718056f : -INFINITY;
         } else {
             const bool large = unit.peak >= ValueUnit::exponent(__builtin_bit_cast(int, kLargeScale));
-            const float own = ldexpf(1.0f, unit.at - (large ? kLargeUnit : 0));
+            const float own = ldexpf(unit.value(), large ? -kLargeUnit : 0);
             const int64_t part = part_row(a, r, h, row) * a.chunks + chunk;
 #pragma unroll
             for (int v = 0; v < VT; ++v) *reinterpret_cast<f32x4 *>(a.part_o + part * D + 16 * v + 4 * g) = o[v] * own;
