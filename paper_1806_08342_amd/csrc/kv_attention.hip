@@ -13,8 +13,8 @@
 // that holds them, without LDS or shuffles.  Keys and values come straight from memory into registers: each wave
 // reads tokens of its own, so nothing would be shared through LDS.
 //
-// Bound by reading codes: 4 contexts of 131072 tokens, 40 query heads of 128 over 8: 185 us, 5.8 TB/s; 32 up to 8000, 64 heads over 8: 65 us, where
-// the longest contexts end last; one of 777: 9.5 us, two launches (7 and 2.5) and a chain of loads.
+// Bound by reading codes: 4 contexts of 131072 tokens, 40 query heads of 128 over 8: 190 us, 5.7 TB/s; 32 up to 8000, 64 heads over 8: 67 us, where
+// the longest contexts end last; one of 777: 10 us, two launches (7 and 3) and a chain of loads.
 #include "kv_attention.h"
 #include "kv_prompt.h"
 #include "kv_prompt_wide.h"

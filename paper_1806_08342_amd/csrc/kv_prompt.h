@@ -12,10 +12,11 @@
 // the two tiles lie further apart, or further from any unit that the accumulators can stand in, probabilities go without them and each tile's
 // product is added by itself, with its scale in binary32: a page says nothing about rows that see only others.
 //
-// Bound by the two things that a wave does in turn: products (4 D flops per row and token, at 35 % of the matrix units' cycles) and the
-// softmax between them (an exponential, four more operations and half a conversion per score, 49 % of the vector unit's); two waves on
-// a SIMD seldom overlap them (half a unit apart, or with a higher priority for products, they did not either).  8192 tokens, 32 query
-// heads of 128 over 8: 650 us, 840 TFLOP/s of the half that the mask leaves.  Forms that interleave a unit's products with the next
+// Bound by the two things that a wave does in turn: products (4 D flops per row and token, at 38 % of the matrix units' cycles) and the
+// softmax between them (an exponential, four more operations and half a conversion per score, 51 % of the vector unit's with the work on addresses); two waves on
+// a SIMD seldom overlap them (half a unit apart, or with a higher priority for products, they did not either), and within each of them nearly every product
+// waits for the fragment that is read from LDS right before it.  8192 tokens, 32 query
+// heads of 128 over 8: 630-650 us, 850 TFLOP/s of the half that the mask leaves.  Forms that interleave a unit's products with the next
 // one's softmax in a wave, or let the waves of a SIMD alternate, lost more to registers and scalar work than they gained.
 #pragma once
 

@@ -1,9 +1,9 @@
 // The kernel for many query rows, for large heads: accumulators and queries of 32 rows would leave no registers for two waves on
 // a SIMD (heads of 256: 512 registers, most of them copied to and fro between the register file's halves, 5 us for 64 tokens by 128 rows).  Here a
 // wave has 16 rows, on 16x16x32 tiles: twice the reads from LDS for each product, but eight waves.
-// Five prompts up to 2047, 16 query heads of 256 over 4: 194 us (249 with 32 rows per wave), 455 TFLOP/s.  LDS is read in 31 % of the cycles,
-// the vector unit works in 35 and the matrix units in 20; a wave waits half of its time, for LDS, for results of its own
-// and at the barrier, and registers and LDS have no room for more waves.  (Letting the second wave of each SIMD stage tokens before its products
+// Five prompts up to 2047, 16 query heads of 256 over 4: 182 us (249 with 32 rows per wave), 485 TFLOP/s.  LDS is read in 33 % of the cycles,
+// the vector unit works in 37 and the matrix units in 21; a wave waits for 44 % of its time: nearly every product for the fragment that is read
+// from LDS right before it, with the next one's read behind it, and all waves at the barrier.  (Letting the second wave of each SIMD stage tokens before its products
 // and the first after them changed nothing; uneven ends cost a tenth.)
 #pragma once
 

@@ -206,7 +206,8 @@ template <class T, int MT, int NT, int WAVES, int GS, bool TINY = false> static 
 static int few_tiles(int64_t N) { return N > 16384 ? 2 : 1; }
 
 // waves along K: fewer than four scales in all (no four to load at once); two tiles per wave; as a workgroup of 16 waves has a CU to
-// itself, 16 only where there are no more workgroups than CUs (1 x 12288 x 4096 13.1 us with 16, 9.9 with 8)
+// itself, 16 only where there are no more workgroups than CUs (1 x 12288 x 4096 13.1 us with 16, 9.9 with 8).  (With groups that are not whole 64s
+// 16 waves have too few registers: 21 to 29 are spilled, some of them inside the loop.)
 static int few_form(int64_t N, int64_t groups) { return groups * N < 4 ? 0 : few_tiles(N) == 2 ? 1 : (N + 15) / 16 > 256 ? 2 : 3; }
 
 template <class T, int GS> static void launch_w4(const W4Args &a, hipStream_t s)
@@ -241,10 +242,11 @@ static bool bad_w4_sizes(int64_t M, int64_t N, int64_t K, int64_t group)
 
 // Which kernel, by what each is estimated to take (us):
 // few rows: weights at 4 TB/s and x, read again for every 16 or 32 rows of weights, at 9 TB/s from the L2 (measured / estimated at
-// 16 rows: 4096 x 4096 7.8 / 8.3, 12288 x 4096 19.5 / 20, 28672 x 8192 51 / 58);
-// tens: see w4_parts.hip;  many: for a round of tiles and 128 of K 2 us with groups of whole 128s (200 rows x 28672 x 8192 132 / 133, 1000: 444 /
-// 453), else, for 64 rows, 1.3 with groups of 64s (1000: 570 / 587; 2000 x 12288 x 4096 271 / 255) and 1.65 with smaller ones (333 / 322).  With these
-// groups the kernel for tens takes 1.35 and 1.75 times as long as with whole 128s (2000 x 12288 x 4096 330 / 315 and 416 / 408).
+// 16 rows: 4096 x 4096 7.5 / 8.3, 12288 x 4096 19.5 / 20, 28672 x 8192 51 / 58);
+// tens: see w4_parts.hip;  many: for a round of tiles and 128 of K 2 us with groups of whole 128s (200 rows x 28672 x 8192 135 / 133, 1000: 471 /
+// 453), else, for 64 rows, 1.3 with groups of 64s (1000: 586 / 587; 2000 x 12288 x 4096 271 / 255) and 1.65 with smaller ones (327 / 322).  With these
+// groups the kernel for tens takes 1.35 and 1.75 times as long as with whole 128s (2000 x 12288 x 4096 330 / 315 and 416 / 408); up to 16 rows,
+// where reading the codes takes most of its time (8 x 28672 x 8192 34, 38 and 47 us with groups of 128, 64 and 32), the choice does not look at the group.
 enum class W4Kernel { Few, Tens, Many };
 static W4Kernel w4_kernel(int64_t M, int64_t N, int64_t K, int64_t group)
 {

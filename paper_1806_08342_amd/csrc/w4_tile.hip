@@ -8,7 +8,8 @@
 // x has to fit binary16: a first launch writes it with each row scaled by a power of two, which is exact but for bfloat16 elements below
 // 2^-32 of their row's largest, in the order of expand_nibbles, rows padded with zeros to whole 128s.
 //
-// Bound by the matrix units and the clock they leave: 2000 x 12288 x 4096 with zero-points 195-210 us with the first launch (6-12), 1000
+// Bound by the matrix units (50 % of the cycles) and the vector unit that turns codes into binary16 (49 %), which two waves on a SIMD overlap in part, and by the
+// clock they leave: 2000 x 12288 x 4096 with zero-points 202-216 us with the first launch (6-12), 1000
 // TFLOP/s; the library's product of the same size with 16-bit weights takes 180.  Tiles of 128 x 256 (64 x 256 with groups that are
 // not whole 128s): 768 of them, three rounds of 256 CUs.
 #include "buffer_ops.h"
@@ -229,7 +230,7 @@ template <class T, int MT, int GS, bool ZEROS> __global__ void __launch_bounds__
 template <class T, int GS, bool ZEROS> static void launch_tiles(const W4Args &a, const W4Prepared &p, hipStream_t s)
 {
     // (with groups of 64 and 32 the scales on their way and the sums of 128 rows would not fit the registers of two waves on a SIMD: 2000 x
-    // 12288 x 4096 374 and 606 us, with 64 rows 271 and 333)
+    // 12288 x 4096 with zero-points 374 and 606 us, with 64 rows 280 and 337.  With whole 128s 11 to 15 registers are spilled, outside the loop.)
     constexpr int MT = GS == 1 ? 4 : 2;
     const int m_tiles = (a.M + 32 * MT - 1) / (32 * MT), n_tiles = (a.N + 255) / 256;
     hipLaunchKernelGGL((w4_tile_kernel<T, MT, GS, ZEROS>), dim3((unsigned)(((n_tiles + 7) / 8) * 8 * m_tiles)), dim3(256), 0, s, a, p, m_tiles, n_tiles);
