@@ -16,7 +16,7 @@
 // softmax between them (an exponential, four more operations and half a conversion per score, 51 % of the vector unit's with the work on addresses); two waves on
 // a SIMD seldom overlap them (half a unit apart, or with a higher priority for products, they did not either), and within each of them nearly every product
 // waits for the fragment that is read from LDS right before it.  8192 tokens, 32 query
-// heads of 128 over 8: 630-650 us, 850 TFLOP/s of the half that the mask leaves.  Forms that interleave a unit's products with the next
+// heads of 128 over 8: 611-650 us, 850-900 TFLOP/s of the half that the mask leaves.  Forms that interleave a unit's products with the next
 // one's softmax in a wave, or let the waves of a SIMD alternate, lost more to registers and scalar work than they gained.
 #pragma once
 

@@ -207,6 +207,14 @@ __device__ __forceinline__ GroupUnit enter_group(float s, int z, ScaleUnit &unit
     g.off = h16x2{o, o}, g.mask = none ? 0u : 0x000f000fu;
     return g;
 }
+// What an accumulator stands for, in a row of x that was scaled by 2^-row_exp: the unit's octave goes with the row's, as either alone may
+// lead out of binary32's range.
+struct Result {
+    float mantissa;
+    int octave;
+    __device__ __forceinline__ explicit Result(const ScaleUnit &unit) : mantissa(__builtin_amdgcn_frexp_mantf(unit.at)), octave(__builtin_amdgcn_frexp_expf(unit.at)) {}
+    __device__ __forceinline__ float of(float acc, int row_exp) const { return ldexpf(acc * mantissa, octave + row_exp); }
+};
 // eight weights c - z of a dword, in binary16
 __device__ __forceinline__ h16x8 whole_weights(uint32_t w, const GroupUnit &g, uint32_t bits)
 {

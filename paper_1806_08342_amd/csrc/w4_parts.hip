@@ -130,10 +130,17 @@ template <class T, int MT, int NW, int PARTS, int RING, int GS, bool ZEROS> __gl
     wait_vmcnt<0>(); // (no copy may land on them)
     lds_barrier();
     float *const s_sum = reinterpret_cast<float *>(s_mem);
+    const Result result(unit);
+    using i32x4 = int32_t __attribute__((ext_vector_type(4)));
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s_sum[(part * ROWS + mt * 32 + 8 * (i >> 2) + 4 * hh + (i & 3)) * (BN + 4) + nw * 32 + c] = acc[mt][i] * unit.at;
+        for (int i = 0; i < 16; i += 4) {
+            const int m = mt * 32 + 2 * i + 4 * hh;
+            const i32x4 exp = *reinterpret_cast<const i32x4 *>(p.row_exp + m0 + m); // (of whole tiles)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s_sum[(part * ROWS + m + e) * (BN + 4) + nw * 32 + c] = result.of(acc[mt][i + e], exp[e]);
+        }
     lds_barrier();
     for (int i = tid; i < ROWS * BN; i += 64 * NW * PARTS) {
         const int m = i / BN, n = blockIdx.x * BN + i % BN;
@@ -141,7 +148,7 @@ template <class T, int MT, int NW, int PARTS, int RING, int GS, bool ZEROS> __gl
         float v = 0.0f;
 #pragma unroll
         for (int q = 0; q < PARTS; ++q) v += s_sum[(q * ROWS + m) * (BN + 4) + i % BN];
-        v = ldexpf(v, p.row_exp[m0 + m]) + (a.bias ? T::widen(a.bias[n]) : 0.0f);
+        if (a.bias) v += T::widen(a.bias[n]);
         a.y[(int64_t)(m0 + m) * a.ldy + n] = T::narrow(v);
     }
 }

@@ -9,7 +9,7 @@
 // 2^-32 of their row's largest, in the order of expand_nibbles, rows padded with zeros to whole 128s.
 //
 // Bound by the matrix units (50 % of the cycles) and the vector unit that turns codes into binary16 (49 %), which two waves on a SIMD overlap in part, and by the
-// clock they leave: 2000 x 12288 x 4096 with zero-points 202-216 us with the first launch (6-12), 1000
+// clock they leave: 2000 x 12288 x 4096 with zero-points 199-216 us with the first launch (6-12), 1000
 // TFLOP/s; the library's product of the same size with 16-bit weights takes 180.  Tiles of 128 x 256 (64 x 256 with groups that are
 // not whole 128s): 768 of them, three rounds of 256 CUs.
 #include "buffer_ops.h"
@@ -196,6 +196,7 @@ template <class T, int MT, int GS, bool ZEROS> __global__ void __launch_bounds__
     // outputs through LDS, rows of 64 per wave, 16-byte pieces exchanged as above
     lds_barrier(); // (the buffers' last reads are over)
     uint8_t *const tile = &s_x[0][0] + wave * (BM * 128);
+    const Result result[2] = {Result(unit[0]), Result(unit[1])};
     float bias[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) bias[t] = a.bias ? T::widen(a.bias[n_at[t]]) : 0.0f;
@@ -210,7 +211,7 @@ template <class T, int MT, int GS, bool ZEROS> __global__ void __launch_bounds__
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float v = ldexpf(acc[t][mt][i + e] * unit[t].at, exp[e]) + bias[t];
+                    const float v = result[t].of(acc[t][mt][i + e], exp[e]) + bias[t];
                     *reinterpret_cast<uint16_t *>(tile + (m + e) * 128 + ((4 * t + (c >> 3)) ^ ((m + e) & 7)) * 16 + (c & 7) * 2) = T::narrow(v);
                 }
         }

@@ -309,3 +309,15 @@ def test_scores_of_any_size(dim, size):
         want, want_lse, spread = attend(cache, q, *of, scale=1.0)
         assert_close(out, want, attention_allows(cache, q, want, spread, *of, scale=1.0), (dim, size, most))
         assert ((lse.cpu().double() - want_lse).abs() <= 2.0 ** -21 * want_lse.abs() + 1e-4).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(3, 300, 642), (20, 300, 642), (33, 8300, 514), (201, 17003, 770)])
+def test_rows_and_scales_at_opposite_ends(M, N, K):
+    # small rows with large scales and the other way round: results are ordinary numbers; whole numbers underneath, exact
+    g = torch.Generator().manual_seed(N)
+    x = torch.randint(-8, 9, (M, K), generator=g).to(torch.bfloat16).to(DEV)
+    codes, scales, z = weights(N, K, 64, torch.bfloat16, g)
+    want, _ = w4(x, codes, scales, 64, z)
+    for power in (-118, -60, 60, 118):
+        got = qnn.w4_matmul(x * 2.0 ** power, codes, scales * 2.0 ** -power, 64, z)
+        assert torch.equal(got.cpu(), want.to(torch.bfloat16)), power
