@@ -412,6 +412,68 @@ qnn_status qnn_kv_attention(const qnn_kv_cache *cache, const void *q, int64_t q_
 size_t qnn_kv_attention_workspace_bytes(const qnn_kv_cache *cache, int32_t q_heads, int64_t table_width, int64_t requests,
                                         int64_t tokens, int64_t window, int64_t max_queries);
 
+/* ---------------------------------------------------------------- language models in 8-bit floating point
+ *
+ * Linear layers whose two operands have 8 bits: codes e4m3 (4 exponent bits with a bias of 7, 3 of mantissa, subnormals, no infinities,
+ * 0x7f and 0xff NaN, largest value 448), a uint8 each, and binary32 scales: one per 128 consecutive elements of a row of activations,
+ * scales [ceil(K / 128)][M], and one per 128 x 128 block of weights, scales [ceil(N / 128)][ceil(K / 128)].  A value is code * scale; the last
+ * block of a row or column may be shorter.  Results of 16 or 32 bits: QNN_BF16, QNN_F16 and */
+#define QNN_F32 2
+
+/* Rows as codes and scales: v = x[m][k], or, gated, v = g / (1 + exp(-g)) * u with g = x[m][k] and u = x[m][K + k].  For each block, in binary32:
+ *   s = max(a / 448, 2^-80) with a = max|v| over its FINITE v;  code = e4m3(v / s), to nearest, ties to even
+ * Infinities become +-448 (a block's largest finite value), a NaN a NaN.
+ * x: DEVICE, M x K of `type` (gated: M x 2 K), row pitch ldx elements.  codes: DEVICE [M][ldc], ldc >= K; scales: DEVICE, pitch lds >= M
+ * between blocks (both written).  M up to 2^20 (0 is a no-op), K up to 2^24, fewer than 2^31 blocks. */
+qnn_status qnn_f8_quantize(const void *x, int64_t ldx, int64_t M, int64_t K, int gated, int type, uint8_t *codes, int64_t ldc, float *scales,
+                           int64_t lds, void *stream);
+
+/* Root-mean-square norm of rows, with the addition of a residual before it, as codes and scales:
+ *   h = x, or, with a residual, x + residual rounded to `type`, which is written to `total`
+ *   v = h / sqrt(mean(h^2) + eps) * weight;  codes and scales of v as in qnn_f8_quantize
+ * in binary32 (squares beyond its range included: rows are then taken in units of a power of two).  A row of zeros gives zeros, one with an infinity or
+ * NaN gives what the formula does.  total may be residual, or x, itself; other overlaps are not allowed.
+ * residual, total: DEVICE, pitches ldr and ldt, or both NULL (total is not used without a residual).  weight: DEVICE [K] of `type` or NULL (ones).
+ * y: DEVICE [M][K] of `type`, contiguous: v rounded, or NULL.  eps: in [0, 2^100].  The rest as in qnn_f8_quantize. */
+qnn_status qnn_f8_rmsnorm(const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, float eps, int64_t M, int64_t K,
+                          int type, void *total, int64_t ldt, void *y, uint8_t *codes, int64_t ldc, float *scales, int64_t lds, void *stream);
+
+/* y[m][n] = bias[n] + sum_b x_scales[b][m] * w_scales[n / 128][b] * sum_{k in block b} x[m][k] * w[n][k]
+ * A block's sum comes from the matrix unit: with results of 16 bits on the codes themselves, which aligns the products of 8
+ * consecutive k to the largest and cuts them off 13 bits below it (relative error of a sum of 128 normal products 1.4e-5); with QNN_F32 on the codes as bfloat16, which is
+ * exact, with sums in binary32, at half the rate.  Blocks are joined in binary32 (the product of two scales has to stay within its normal range: below
+ * 2^-126 it loses bits), y is rounded once.  A NaN code gives NaN in its row or column.
+ * x: DEVICE [M][ldx], ldx >= K.  x_scales: DEVICE, pitch ldxs >= M between blocks.  w: DEVICE [N][K], w_scales DEVICE, both contiguous.
+ * bias: DEVICE [N] of `type` or NULL.  y: DEVICE, M x N of `type`, row pitch ldy >= N (written).
+ * Rows at any byte; those that are whole 16-byte pieces at 16-byte aligned addresses run faster.  M up to 2^20 (0 is a no-op), N and K up to 2^24.
+ * workspace: DEVICE scratch, 16-byte aligned, of at least qnn_f8_matmul_workspace_bytes bytes (NULL where that is 0), else QNN_EINVAL. */
+qnn_status qnn_f8_matmul(const uint8_t *x, int64_t ldx, const float *x_scales, int64_t ldxs, const uint8_t *w, const float *w_scales, const void *bias,
+                         int64_t M, int64_t N, int64_t K, int type, void *y, int64_t ldy, void *workspace, size_t workspace_bytes, void *stream);
+size_t qnn_f8_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, int type);
+
+/* Name of the kernel that qnn_f8_matmul selects.  For logging and profiling.  HOST string owned by the library; "" for sizes that are refused. */
+const char *qnn_f8_matmul_plan(int64_t M, int64_t N, int64_t K, int type);
+
+/* A whole layer of experts, for a few tokens.  Token t chooses the top_k largest of its logits (equal ones: the lowest index; -inf and NaN are
+ * never chosen, +inf counts as the largest finite number), with the weights exp(logit) / sum exp, over the chosen ones (renormalize != 0) or over
+ * all logits.  With h_e = silu(gate_e x_t) * (up_e x_t), silu(v) = v / (1 + exp(-v)):
+ *   y[t] = sum over the chosen e of weight_e * (down_e h_e)
+ * A token that chooses nothing gets 0.  Products of x as in qnn_f8_matmul for 16 bits; h is held to 16 significant bits, its products with the codes of
+ * down are exact; everything else is binary32, y is rounded once.  The result does not depend on the order of workgroups.
+ * Reads the weights of the experts chosen, once for every 64 tokens: meant for few of these (for many, group the tokens by expert and call qnn_f8_matmul).
+ * x, x_scales: as above, [T][H].  logits: DEVICE [T][ldl] of logit_type (QNN_BF16, QNN_F16 or QNN_F32), ldl >= E.
+ * up: DEVICE codes [E][2 I][H], the I rows of gate before those of up; up_scales [E][ceil(2 I / 128)][ceil(H / 128)] (a block of rows may
+ * hold rows of both).  down: DEVICE codes [E][H][I], down_scales [E][ceil(H / 128)][ceil(I / 128)].  All contiguous.
+ * y: DEVICE, T x H of `type` (QNN_BF16 or QNN_F16), row pitch ldy >= H (written).  experts: DEVICE int32 [T][top_k], the chosen ones, largest logit
+ * first, -1 where there are fewer; weights: DEVICE float [T][top_k], 0 there; either or both NULL.
+ * T up to 2^20 (0 is a no-op), E up to 1024, top_k up to 32, H a multiple of 16 up to 2^20, I one up to 2^17.
+ * workspace: DEVICE, 16-byte aligned, of at least qnn_f8_moe_workspace_bytes bytes, else QNN_EINVAL. */
+qnn_status qnn_f8_moe(const uint8_t *x, int64_t ldx, const float *x_scales, int64_t ldxs, const void *logits, int64_t ldl, int logit_type,
+                      const uint8_t *up, const float *up_scales, const uint8_t *down, const float *down_scales, int64_t T, int64_t E, int64_t top_k,
+                      int64_t H, int64_t I, int renormalize, int type, void *y, int64_t ldy, int32_t *experts, float *weights, void *workspace,
+                      size_t workspace_bytes, void *stream);
+size_t qnn_f8_moe_workspace_bytes(int64_t T, int64_t E, int64_t top_k, int64_t H, int64_t I);
+
 /* Calibration of the machine for the benchmark (not part of the inference path).
  * qnn_calibrate_mfma: `workgroups` workgroups of 8 waves each issue iters x 4 independent
  *   v_mfma_i32_32x32x32_i8 from registers only (random_operands != 0: a different pseudo-random
@@ -468,6 +530,11 @@ qnn_status qnn_pack_int4(const int8_t *v, size_t n, uint8_t *packed);
  * [ceil(cols / group)][rows]; zeros: HOST int8 of the same shape, or NULL. */
 qnn_status qnn_quantize_weights_grouped(const float *w, size_t rows, size_t cols, size_t group, int type, uint8_t *codes,
                                         uint16_t *scales, int8_t *zeros);
+
+/* Block-wise weight quantizer for qnn_f8_matmul and qnn_f8_moe: for each 128 x 128 block s = max(max|w| / 448, 2^-80), codes e4m3(w / s) in
+ * binary32, to nearest, ties to even.  w: HOST fp32 [rows][cols], finite.  codes: HOST uint8 [rows][cols]; scales: HOST fp32
+ * [ceil(rows / 128)][ceil(cols / 128)]. */
+qnn_status qnn_quantize_weights_blocks(const float *w, size_t rows, size_t cols, uint8_t *codes, float *scales);
 
 #ifdef __cplusplus
 }

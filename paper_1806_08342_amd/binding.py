@@ -27,7 +27,8 @@ EXPORTS = [
     "qnn_qadd_params", "qnn_quantize_weights", "qnn_pack_int4", "qnn_qgemm_workspace_bytes", "qnn_qconv2d_workspace_bytes",
     "qnn_tuning_set", "qnn_calibrate_mfma", "qnn_calibrate_copy", "qnn_qgemm_noalloc", "qnn_quantize_u16", "qnn_dequantize_u16", "qnn_calibrate_rescale",
     "qnn_w4_matmul", "qnn_w4_matmul_workspace_bytes", "qnn_w4_matmul_plan", "qnn_kv_append", "qnn_kv_gather", "qnn_kv_attention", "qnn_kv_attention_workspace_bytes",
-    "qnn_quantize_weights_grouped",
+    "qnn_quantize_weights_grouped", "qnn_f8_quantize", "qnn_f8_rmsnorm", "qnn_f8_matmul", "qnn_f8_matmul_workspace_bytes", "qnn_f8_matmul_plan", "qnn_f8_moe",
+    "qnn_f8_moe_workspace_bytes", "qnn_quantize_weights_blocks",
 ]
 
 
@@ -98,6 +99,11 @@ def load_library():
         "qnn_kv_append": [vp, vp, i64, i64, vp, i64, i64, ci, vp, vp, vp, i64, i64, i64, vp],
         "qnn_kv_gather": [vp, vp, vp, vp, i64, i64, i64, ci, vp, vp, vp],
         "qnn_kv_attention": [vp, vp, i64, i64, i32, ci, vp, vp, vp, i64, i64, i64, f32, i64, i64, vp, vp, vp, sz, vp],
+        "qnn_quantize_weights_blocks": [vp, sz, sz, vp, vp],
+        "qnn_f8_quantize": [vp, i64, i64, i64, ci, ci, vp, i64, vp, i64, vp],
+        "qnn_f8_rmsnorm": [vp, i64, vp, i64, vp, f32, i64, i64, ci, vp, i64, vp, vp, i64, vp, i64, vp],
+        "qnn_f8_matmul": [vp, i64, vp, i64, vp, vp, vp, i64, i64, i64, ci, vp, i64, vp, sz, vp],
+        "qnn_f8_moe": [vp, i64, vp, i64, vp, i64, ci, vp, vp, vp, vp, i64, i64, i64, i64, i64, ci, ci, vp, i64, vp, vp, vp, sz, vp],
     }
     for name, args in sigs.items():
         fn = getattr(lib, name)
@@ -113,6 +119,12 @@ def load_library():
     lib.qnn_w4_matmul_workspace_bytes.argtypes = [i64] * 4
     lib.qnn_kv_attention_workspace_bytes.restype = sz
     lib.qnn_kv_attention_workspace_bytes.argtypes = [vp, i32, i64, i64, i64, i64, i64]
+    lib.qnn_f8_matmul_plan.restype = C.c_char_p
+    lib.qnn_f8_matmul_plan.argtypes = [i64, i64, i64, ci]
+    lib.qnn_f8_matmul_workspace_bytes.restype = sz
+    lib.qnn_f8_matmul_workspace_bytes.argtypes = [i64, i64, i64, ci]
+    lib.qnn_f8_moe_workspace_bytes.restype = sz
+    lib.qnn_f8_moe_workspace_bytes.argtypes = [i64] * 5
     _lib = lib
     return lib
 
@@ -532,3 +544,71 @@ def kv_attention(cache, q, cu, lengths, table, scale=None, window=0, max_queries
     if scale is None:
         scale = q.shape[-1] ** -0.5
     return (_nat or _native()).kv_attention(cache, q, cu, lengths, table, scale, window, max_queries or 0, with_lse, out, workspace)
+
+
+# ------------------------------------------------------------------------------- language models in 8-bit floating point
+
+F32 = 2
+
+
+def _float_code(dtype):
+    torch = _torch()
+    codes = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
+    if dtype not in codes:
+        raise ValueError(f"expected torch.bfloat16, torch.float16 or torch.float32, got {dtype}")
+    return codes[dtype]
+
+
+def quantize_weights_blocks(w):
+    """fp32 [N,K] (numpy, finite) -> what `f8_matmul` takes, on the host: codes float8_e4m3fn [N,K] and float32 scales
+    [ceil(N/128),ceil(K/128)], one per block of 128 x 128: max|w| / 448.  [E,N,K]: the same for each expert of `f8_moe`."""
+    torch = _torch()
+    w = np.ascontiguousarray(w, dtype=np.float32)
+    if w.ndim == 3 and w.shape[0] > 0:
+        each = [quantize_weights_blocks(m) for m in w]
+        return torch.stack([c.view(torch.uint8) for c, _ in each]).view(torch.float8_e4m3fn), torch.stack([s for _, s in each])
+    if w.ndim != 2:
+        raise ValueError(f"expected weights [N, K] or [E, N, K], got shape {w.shape}")
+    n, k = w.shape
+    codes = np.empty((n, k), np.uint8)
+    scales = np.empty((-(-n // 128), -(-k // 128)), np.float32)
+    _check("qnn_quantize_weights_blocks", load_library().qnn_quantize_weights_blocks(w.ctypes.data, n, k, codes.ctypes.data, scales.ctypes.data))
+    return torch.from_numpy(codes).view(torch.float8_e4m3fn), torch.from_numpy(scales)
+
+
+def f8_quantize(x, gated=False, out=None):
+    """Rows of x [M,K] (bfloat16 or float16, rows may be spaced apart) as (codes float8_e4m3fn [M,K], scales float32
+    [ceil(K/128),M]): one scale for 128 consecutive elements, their largest finite one / 448 (2^-80 at least).  gated: x is [M,2K],
+    and silu(x[:,:K]) * x[:,K:] is what is quantized.  out: (codes, scales) to write to, rows may be spaced apart."""
+    return (_nat or _native()).f8_quantize(x, gated, out)
+
+
+def f8_rmsnorm(x, weight=None, eps=1e-6, residual=None, total=None, with_y=False, out=None):
+    """Root-mean-square norm of rows as codes and scales (see `f8_quantize`): h = x, or x + residual rounded to x's type;
+    v = h / sqrt(mean(h^2) + eps) * weight.  Returns (codes, scales), with a residual (codes, scales, h), and with_y one more: v
+    rounded to x's type.  total: where to write h (residual or x themselves will do: in place); out: (codes, scales) to write to."""
+    return (_nat or _native()).f8_rmsnorm(x, weight, eps, residual, total, with_y, out)
+
+
+def f8_matmul(x, x_scales, w, w_scales, bias=None, dtype=None, out=None, workspace=None):
+    """x [M,K] times w [N,K] transposed, both float8_e4m3fn: y[m,n] = bias[n] + sum_k x[m,k] * x_scales[k//128,m] * w[n,k] *
+    w_scales[n//128,k//128].  x's rows may be spaced apart.  dtype: bfloat16 (unless given), float16, or float32, whose sums are exact
+    to binary32 (at half the matrix rate; with 16-bit results a block's sum has a relative error of about 1e-5); the bias is of that type.
+    For inference: tensors that require grad are refused while gradients are recorded."""
+    return (_nat or _native()).f8_matmul(x, x_scales, w, w_scales, bias, BF16 if dtype is None else _float_code(dtype), out, workspace)
+
+
+def f8_matmul_plan(M, N, K, dtype=None):
+    """Name of the kernel that `f8_matmul` runs for these sizes."""
+    return load_library().qnn_f8_matmul_plan(M, N, K, BF16 if dtype is None else _float_code(dtype)).decode()
+
+
+def f8_moe(x, x_scales, logits, up, up_scales, down, down_scales, top_k, renormalize=True, dtype=None, with_choice=False, out=None, workspace=None):
+    """A layer of experts for a few tokens: x [T,H] codes and scales as `f8_quantize` and `f8_rmsnorm` give them, logits [T,E]
+    (float32, bfloat16 or float16), up float8_e4m3fn [E,2*I,H] (gate's rows, then up's) with scales [E,ceil(2I/128),ceil(H/128)], down
+    [E,H,I] with [E,ceil(H/128),ceil(I/128)].  A token goes to its top_k largest logits (ties: the lowest index; never to -inf or NaN),
+    weighed by softmax over these (renormalize) or over all logits: y[t] = sum_e weight * down[e] @ (silu(gate[e] @ x) * (up[e] @ x)).
+    Returns [T,H] of dtype (bfloat16 unless given, or float16), with_choice: (y, experts int32 [T,top_k], weights float32).
+    H and I: multiples of 16.  Reads the chosen experts' weights once for every 64 tokens."""
+    return (_nat or _native()).f8_moe(x, x_scales, logits, up, up_scales, down, down_scales, top_k, renormalize, BF16 if dtype is None else _float_code(dtype),
+                                      with_choice, out, workspace)

@@ -14,6 +14,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <c10/util/Exception.h>
 #include <c10/util/SmallVector.h>
@@ -112,6 +113,7 @@ const char *type_name(at::ScalarType t)
     case at::kFloat: return "a contiguous device tensor of torch.float32";
     case at::kBFloat16: return "a contiguous device tensor of torch.bfloat16";
     case at::kHalf: return "a contiguous device tensor of torch.float16";
+    case at::kFloat8_e4m3fn: return "a contiguous device tensor of torch.float8_e4m3fn";
     default: return "a contiguous device tensor of torch.uint16";
     }
 }
@@ -863,6 +865,196 @@ PyObject *f_kv_attention(Args a) // cache, q, cu, lengths, table, scale, window,
     return with_lse ? pair_of(o.release(), THPVariable_Wrap(std::move(lse))) : o.release();
 }
 
+// ------------------------------------------------------------------------------- language models in 8-bit floating point
+
+// codes [rows][K] and their scales [ceil(K / 128)][rows], rows of either may be spaced apart
+struct F8Rows {
+    uint8_t *codes;
+    float *scales;
+    int64_t ldc, lds;
+};
+int64_t f8_blocks(int64_t n) { return (n + 127) / 128; }
+int64_t f8_pitch(const at::Tensor &t, int64_t width, const char *name) // of a 2-D tensor whose rows are contiguous and do not overlap
+{
+    if (!(t.numel() == 0 || t.size(1) == 1 || t.stride(1) == 1) || (t.size(0) > 1 && t.stride(0) < width)) type_error(name, "contiguous rows that do not overlap");
+    return t.size(0) > 1 ? t.stride(0) : width;
+}
+F8Rows f8_rows(const at::Tensor &c, const at::Tensor &s, const char *codes_name, const char *scales_name)
+{
+    if (!c.is_cuda() || c.scalar_type() != at::kFloat8_e4m3fn || c.dim() != 2) type_error(codes_name, "a 2-D device tensor of torch.float8_e4m3fn");
+    const int64_t M = c.size(0), K = c.size(1);
+    if (!s.is_cuda() || s.scalar_type() != at::kFloat || s.dim() != 2) type_error(scales_name, "a 2-D device tensor of torch.float32");
+    no_grad(c, codes_name), no_grad(s, scales_name);
+    want_shape(s, scales_name, {f8_blocks(K), M});
+    same_device(s, c, scales_name);
+    return {static_cast<uint8_t *>(c.data_ptr()), static_cast<float *>(s.data_ptr()), f8_pitch(c, K, codes_name), f8_pitch(s, M, scales_name)};
+}
+// (codes, scales) as the caller gives them, or new ones
+struct F8Out {
+    Out codes, scales;
+    F8Rows rows;
+};
+F8Out f8_output(PyObject *o, int64_t M, int64_t K, const at::Tensor &like)
+{
+    F8Out out;
+    if (o != Py_None && (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 2)) type_error("out", "a tuple (codes, scales)");
+    out.codes = output(o == Py_None ? o : PyTuple_GET_ITEM(o, 0), {M, K}, at::kFloat8_e4m3fn, like);
+    out.scales = output(o == Py_None ? o : PyTuple_GET_ITEM(o, 1), {f8_blocks(K), M}, at::kFloat, like);
+    out.rows = f8_rows(out.codes.t, out.scales.t, "out", "out scales");
+    same_device(out.codes.t, like, "out");
+    return out;
+}
+// takes what it is given; nothing for a null pointer in the last places
+PyObject *tuple_of(std::initializer_list<PyObject *> items)
+{
+    Py_ssize_t n = 0;
+    for (PyObject *i : items) n += i != nullptr;
+    PyObject *const t = PyTuple_New(n);
+    if (!t) {
+        for (PyObject *i : items) Py_XDECREF(i);
+        throw PythonErrorSet{};
+    }
+    n = 0;
+    for (PyObject *i : items)
+        if (i) PyTuple_SET_ITEM(t, n++, i);
+    return t;
+}
+int truth(PyObject *o)
+{
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw PythonErrorSet{};
+    return v;
+}
+
+PyObject *f_f8_quantize(Args a) // x, gated, out
+{
+    const Halves x = halves(a[0], "x", 2);
+    const c10::DeviceGuard guard(x.t.device());
+    const int gated = truth(a[1]);
+    const int64_t M = x.t.size(0), width = x.t.size(1), K = gated ? width / 2 : width;
+    if (K == 0 || (gated && width % 2 != 0)) type_error("x", gated ? "rows of two halves" : "rows of at least one element");
+    const int64_t ldx = f8_pitch(x.t, width, "x");
+    F8Out out = f8_output(a[2], M, K, x.t);
+    const F8Rows &r = out.rows;
+    call("qnn_f8_quantize", [&](void *s) { return qnn_f8_quantize(x.p, ldx, M, K, gated, x.type, r.codes, r.ldc, r.scales, r.lds, s); });
+    return pair_of(out.codes.release(), out.scales.release());
+}
+
+PyObject *f_f8_rmsnorm(Args a) // x, weight, eps, residual, total, with_y, out
+{
+    const Halves x = halves(a[0], "x", 2);
+    const c10::DeviceGuard guard(x.t.device());
+    const int64_t M = x.t.size(0), K = x.t.size(1);
+    if (K == 0) type_error("x", "rows of at least one element");
+    const int64_t ldx = f8_pitch(x.t, K, "x");
+    const void *const weight = a[1] == Py_None ? nullptr : param(a[1], half_type(x.type), "weight", {K}, x.t);
+    const float eps = real(a[2]);
+    const void *residual = nullptr;
+    int64_t ldr = K, ldt = K;
+    Out total;
+    if (a[3] != Py_None) {
+        const Halves r = halves(a[3], "residual", 2);
+        same_type(r, x.type, "residual"), same_device(r.t, x.t, "residual"), want_shape(r.t, "residual", {M, K});
+        residual = r.p, ldr = f8_pitch(r.t, K, "residual");
+        total = output(a[4], {M, K}, half_type(x.type), x.t);
+        if (total.given) same_type(halves(a[4], "total", 2), x.type, "total"), same_device(total.t, x.t, "total");
+        ldt = f8_pitch(total.t, K, "total");
+    } else if (a[4] != Py_None) {
+        PyErr_SetString(PyExc_ValueError, "total is for x + residual: there is no residual");
+        throw PythonErrorSet{};
+    }
+    const int with_y = truth(a[5]);
+    F8Out out = f8_output(a[6], M, K, x.t);
+    const F8Rows &r = out.rows;
+    at::Tensor y;
+    if (with_y) y = fresh({M, K}, half_type(x.type), x.t);
+    const bool adds = a[3] != Py_None; // (the pointer of a tensor without elements is null)
+    void *const pt = adds ? total.t.data_ptr() : nullptr, *const py = with_y ? y.data_ptr() : nullptr;
+    call("qnn_f8_rmsnorm", [&](void *s) {
+        return qnn_f8_rmsnorm(x.p, ldx, residual, ldr, weight, eps, M, K, x.type, pt, ldt, py, r.codes, r.ldc, r.scales, r.lds, s);
+    });
+    PyObject *const sum = adds ? total.release() : nullptr;
+    return tuple_of({out.codes.release(), out.scales.release(), sum, with_y ? THPVariable_Wrap(std::move(y)) : nullptr});
+}
+
+at::ScalarType float_type(int type) { return type == QNN_F32 ? at::kFloat : half_type(type); }
+void want_float_type(int type, bool wide)
+{
+    if (!bad_type(type) || (wide && type == QNN_F32)) return;
+    PyErr_SetString(PyExc_ValueError, wide ? "dtype must be torch.bfloat16, torch.float16 or torch.float32" : "dtype must be torch.bfloat16 or torch.float16");
+    throw PythonErrorSet{};
+}
+// the caller's [rows][width] tensor of `type` for results, or a new one
+int64_t f8_result(Out &y, int type, const at::Tensor &like)
+{
+    if (y.t.scalar_type() != float_type(type) || !y.t.is_cuda()) type_error("out", "a device tensor of the type of the results");
+    no_grad(y.t, "out");
+    same_device(y.t, like, "out");
+    return f8_pitch(y.t, y.t.size(1), "out");
+}
+
+PyObject *f_f8_matmul(Args a) // x, x_scales, w, w_scales, bias, type, out, workspace
+{
+    const at::Tensor &x = tensor(a[0], "x"), &w = tensor(a[2], "w");
+    const F8Rows r = f8_rows(x, tensor(a[1], "x_scales"), "x", "x_scales");
+    const c10::DeviceGuard guard(x.device());
+    if (w.dim() != 2) type_error("w", "a 2-D device tensor of torch.float8_e4m3fn");
+    const int64_t M = x.size(0), K = x.size(1), N = w.size(0);
+    const int type = i32(a[5]);
+    want_float_type(type, true);
+    const auto *pw = static_cast<const uint8_t *>(param(a[2], at::kFloat8_e4m3fn, "w", {N, K}, x));
+    const auto *ps = static_cast<const float *>(param(a[3], at::kFloat, "w_scales", {f8_blocks(N), f8_blocks(K)}, x));
+    const void *pb = a[4] == Py_None ? nullptr : param(a[4], float_type(type), "bias", {N}, x);
+    Out y = output(a[6], {M, N}, float_type(type), x);
+    const int64_t ldy = f8_result(y, type, x);
+    void *const py = y.t.data_ptr();
+    const Workspace ws = workspace(a[7], x, true, [&] { return qnn_f8_matmul_workspace_bytes(M, N, K, type); });
+    call("qnn_f8_matmul", [&](void *s) { return qnn_f8_matmul(r.codes, r.ldc, r.scales, r.lds, pw, ps, pb, M, N, K, type, py, ldy, ws.p, ws.bytes, s); });
+    return y.release();
+}
+
+PyObject *f_f8_moe(Args a) // x, x_scales, logits, up, up_scales, down, down_scales, top_k, renormalize, type, with_choice, out, workspace
+{
+    const at::Tensor &x = tensor(a[0], "x"), &logits = tensor(a[2], "logits"), &up = tensor(a[3], "up");
+    const F8Rows r = f8_rows(x, tensor(a[1], "x_scales"), "x", "x_scales");
+    const c10::DeviceGuard guard(x.device());
+    const at::ScalarType lt = logits.scalar_type();
+    no_grad(logits, "logits");
+    if (!logits.is_cuda() || logits.dim() != 2 || (lt != at::kFloat && lt != at::kBFloat16 && lt != at::kHalf))
+        type_error("logits", "a 2-D device tensor of torch.float32, torch.bfloat16 or torch.float16");
+    if (up.dim() != 3 || up.size(1) % 2 != 0) type_error("up", "a 3-D device tensor [experts, 2 * inner, hidden] of torch.float8_e4m3fn");
+    const int64_t T = x.size(0), H = x.size(1), E = up.size(0), I = up.size(1) / 2, k = integer(a[7]);
+    want_shape(logits, "logits", {T, E});
+    same_device(logits, x, "logits");
+    const int64_t ldl = f8_pitch(logits, E, "logits");
+    const void *const pl = logits.data_ptr();
+    const int logit_type = lt == at::kFloat ? QNN_F32 : lt == at::kBFloat16 ? QNN_BF16 : QNN_F16;
+    const auto *pu = static_cast<const uint8_t *>(param(a[3], at::kFloat8_e4m3fn, "up", {E, 2 * I, H}, x));
+    const auto *us = static_cast<const float *>(param(a[4], at::kFloat, "up_scales", {E, f8_blocks(2 * I), f8_blocks(H)}, x));
+    const auto *pd = static_cast<const uint8_t *>(param(a[5], at::kFloat8_e4m3fn, "down", {E, H, I}, x));
+    const auto *ds = static_cast<const float *>(param(a[6], at::kFloat, "down_scales", {E, f8_blocks(H), f8_blocks(I)}, x));
+    const int renormalize = truth(a[8]), type = i32(a[9]), with_choice = truth(a[10]);
+    want_float_type(type, false);
+    if (k <= 0 || k > E) {
+        PyErr_SetString(PyExc_ValueError, "top_k must lie between 1 and the number of experts");
+        throw PythonErrorSet{};
+    }
+    Out y = output(a[11], {T, H}, float_type(type), x);
+    const int64_t ldy = f8_result(y, type, x);
+    void *const py = y.t.data_ptr();
+    at::Tensor experts, weights;
+    if (with_choice) experts = fresh({T, k}, at::kInt, x), weights = fresh({T, k}, at::kFloat, x);
+    auto *const pe = with_choice ? static_cast<int32_t *>(experts.data_ptr()) : nullptr;
+    auto *const pw = with_choice ? static_cast<float *>(weights.data_ptr()) : nullptr;
+    const Workspace ws = workspace(a[12], x, true, [&] { return qnn_f8_moe_workspace_bytes(T, E, k, H, I); });
+    call("qnn_f8_moe", [&](void *s) {
+        return qnn_f8_moe(r.codes, r.ldc, r.scales, r.lds, pl, ldl, logit_type, pu, us, pd, ds, T, E, k, H, I, renormalize, type, py, ldy, pe, pw,
+                          ws.p, ws.bytes, s);
+    });
+    if (!with_choice) return y.release();
+    return tuple_of({y.release(), THPVariable_Wrap(std::move(experts)), THPVariable_Wrap(std::move(weights))});
+}
+
 PyObject *f_set_check(Args a)
 {
     Py_INCREF(a[0]);
@@ -900,6 +1092,10 @@ PyMethodDef kMethods[] = {
     QNN_ENTRY("kv_append", f_kv_append, 6),
     QNN_ENTRY("kv_gather", f_kv_gather, 6),
     QNN_ENTRY("kv_attention", f_kv_attention, 11),
+    QNN_ENTRY("f8_quantize", f_f8_quantize, 3),
+    QNN_ENTRY("f8_rmsnorm", f_f8_rmsnorm, 7),
+    QNN_ENTRY("f8_matmul", f_f8_matmul, 8),
+    QNN_ENTRY("f8_moe", f_f8_moe, 13),
     {nullptr, nullptr, 0, nullptr},
 };
 

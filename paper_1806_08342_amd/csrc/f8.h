@@ -1,0 +1,75 @@
+// Operators of language models in 8-bit floating point: what the kernels share.
+//
+// Codes are e4m3 (four exponent bits, three of mantissa, largest value 448, no infinities, 0x7f and 0xff are NaN).  Activations have one
+// binary32 scale per 128 consecutive elements of a row, weights one per block of 128 x 128; a value is code * scale.
+#pragma once
+
+#include "halves.h"
+
+namespace qnn {
+
+constexpr int kF8Block = 128;
+constexpr float kF8Largest = 448.0f, kF8LeastScale = 0x1p-80f;
+
+using i32x8 = int32_t __attribute__((ext_vector_type(8)));
+
+inline int64_t f8_blocks(int64_t n) { return (n + kF8Block - 1) / kF8Block; }
+
+struct F8Args {
+    const uint8_t *x, *w;      // [M][ldx], [N][K]
+    const float *xs, *ws;      // [K / 128][ldxs], [N / 128][K / 128]
+    const void *bias;          // [N] of the output's type, or null
+    void *y;                   // [M][ldy]
+    int64_t ldx, ldxs, ldy;
+    int32_t M, N, K, type;
+};
+
+// outputs of 16 or 32 bits; the type is the same in the whole launch
+__device__ __forceinline__ void store_out(void *y, int64_t at, int type, float v)
+{
+    if (type == QNN_F32) static_cast<float *>(y)[at] = v;
+    else static_cast<uint16_t *>(y)[at] = type == QNN_BF16 ? Bf16::narrow(v) : F16::narrow(v);
+}
+__device__ __forceinline__ float load_out(const void *p, int64_t at, int type)
+{
+    if (type == QNN_F32) return static_cast<const float *>(p)[at];
+    const uint16_t v = static_cast<const uint16_t *>(p)[at];
+    return type == QNN_BF16 ? Bf16::widen(v) : F16::widen(v);
+}
+
+// Products of 16 x 16 outputs over 128 of K.  A lane has 32 bytes of row lane % 16 of either operand, in two pieces of 16; which 32 of the
+// 128 they are does not matter as long as both operands take the same.  Result: column lane % 16 (second operand's row), rows 4 * (lane / 16) + e.
+// NARROW: the matrix unit takes the codes; it aligns the products of 8 consecutive k to the largest and cuts them off 13 bits below it, so that sums of
+// 128 normal products have a relative error of 1.4e-5, which results of 16 bits do not show.
+// Else the codes enter as bfloat16, exactly, at half the rate, and sums are those of binary32 (1e-8).
+template <bool NARROW> __device__ __forceinline__ f32x4 f8_products(const w32x4 (&a)[2], const w32x4 (&b)[2])
+{
+    f32x4 p = {0.0f, 0.0f, 0.0f, 0.0f};
+    if constexpr (NARROW) {
+        const i32x8 u = __builtin_bit_cast(i32x8, a), v = __builtin_bit_cast(i32x8, b);
+        p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(u, v, p, 0, 0, 0, 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w32x4 u, v;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const uint32_t s = a[i >> 1][2 * (i & 1) + j], t = b[i >> 1][2 * (i & 1) + j];
+                u[2 * j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(s, 1.0f, false));
+                u[2 * j + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(s, 1.0f, true));
+                v[2 * j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(t, 1.0f, false));
+                v[2 * j + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(t, 1.0f, true));
+            }
+            p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b16x8, u), __builtin_bit_cast(b16x8, v), p, 0, 0, 0);
+        }
+    }
+    return p;
+}
+
+__device__ __forceinline__ void fma4(f32x4 &acc, const f32x4 p, float s)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] = fmaf(p[e], s, acc[e]);
+}
+
+} // namespace qnn

@@ -1,0 +1,317 @@
+// Rows of 16-bit floats as e4m3 codes with a scale per 128 elements: plain, gated, and behind a root-mean-square norm
+// (qnn_f8_quantize, qnn_f8_rmsnorm).
+//
+//   s = max(max|v| / 448, 2^-80), code = e4m3(v / s): the quotient is the correctly rounded one of binary32.  With r the rounded reciprocal of
+//   s, q = v r and e = v - q s (one fma, exact), q + e r (one more) is that quotient.  (With the bound on s nothing underflows that a code shows.)
+//   An infinity is cut off at the largest finite value's code, a NaN stays one.
+//
+// Bound by memory: each element is read once and written once, the row of a norm stays in registers.  A lane has 8 consecutive
+// elements, sixteen lanes a block of 128.
+#include "f8.h"
+
+namespace qnn {
+
+// over the 16 lanes of a block
+template <class F> __device__ __forceinline__ float over16(float v, F f)
+{
+    const auto turned = [](float u, auto ctrl) {
+        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, u), decltype(ctrl)::value, 0xf, 0xf, true));
+    };
+    v = f(v, turned(v, std::integral_constant<int, 0x128>())); // row_ror:8 and so on
+    v = f(v, turned(v, std::integral_constant<int, 0x124>()));
+    v = f(v, turned(v, std::integral_constant<int, 0x122>()));
+    return f(v, turned(v, std::integral_constant<int, 0x121>()));
+}
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+
+// the codes of a lane's 8 values, and the scale of its block
+__device__ __forceinline__ w32x2 encode8(const float (&v)[8], float &scale)
+{
+    float peak = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) peak = fmaxf(peak, fabsf(v[i])); // (fmaxf passes over NaN)
+    peak = over16(peak, larger);
+    if (peak == INFINITY) {
+        peak = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) peak = fmaxf(peak, fabsf(v[i]) < INFINITY ? fabsf(v[i]) : 0.0f);
+        peak = over16(peak, larger);
+    }
+    scale = fmaxf(peak / kF8Largest, kF8LeastScale);
+    const float r = 1.0f / scale, most = fmaxf(peak, kF8Largest * kF8LeastScale);
+    float q[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float c = __builtin_elementwise_minimum(__builtin_elementwise_maximum(v[i], -most), most); // (a NaN stays)
+        const float t = c * r;
+        q[i] = copysignf(fmaf(fmaf(-t, scale, c), r, t), c); // (that of -0 would be +0)
+    }
+    w32x2 codes;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int low = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * i], q[4 * i + 1], 0, false);
+        codes[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[4 * i + 2], q[4 * i + 3], low, true);
+    }
+    return codes;
+}
+
+// 8 elements from k on, zeros behind the row's end
+template <class T> __device__ __forceinline__ w32x4 load8(const uint16_t *row, int K, int k)
+{
+    return k + 8 <= K ? load_any<w32x4>(row + k) : load_end(reinterpret_cast<const uint8_t *>(row), 2 * K, 2 * k);
+}
+template <class T> __device__ __forceinline__ void widen8(const w32x4 w, float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = T::widen((uint16_t)(w[i >> 1] >> (i & 1) * 16));
+}
+template <class T> __device__ __forceinline__ w32x4 narrow8(const float (&v)[8])
+{
+    return w32x4{narrow2<T>(v[0], v[1]), narrow2<T>(v[2], v[3]), narrow2<T>(v[4], v[5]), narrow2<T>(v[6], v[7])};
+}
+__device__ __forceinline__ void store8(uint16_t *row, int K, int k, const w32x4 v)
+{
+    if (k + 8 <= K) {
+        store_any(row + k, v);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+        if (k + i < K) row[k + i] = (uint16_t)(v[i >> 1] >> (i & 1) * 16);
+}
+__device__ __forceinline__ void store_codes(uint8_t *row, int K, int k, const w32x2 c)
+{
+    if (k + 8 <= K) {
+        store_any(row + k, c);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+        if (k + i < K) row[k + i] = (uint8_t)(c[i >> 2] >> (i & 3) * 8);
+}
+
+// Consecutive rows' scales are consecutive in memory: each XCD takes a stretch of rows of its own, so that its L2 joins them.
+__device__ __forceinline__ uint32_t of_xcd(uint32_t id, uint32_t groups) { return id % 8 * groups + id / 8; }
+
+struct F8RowArgs {
+    const uint16_t *x, *residual, *weight;
+    uint16_t *total, *y;
+    uint8_t *codes;
+    float *scales;
+    int64_t ldx, ldr, ldt, ldc, lds;
+    int32_t M, K;
+    float eps;
+    uint32_t blocks, units, groups; // blocks of a row, of all rows; workgroups (or rows) of an XCD
+};
+
+template <class T, bool GATED> __global__ void __launch_bounds__(256) f8_quantize_kernel(const F8RowArgs a)
+{
+    constexpr int EACH = 4; // blocks of 16 lanes
+    const uint32_t first = of_xcd(blockIdx.x, a.groups) * (16 * EACH) + (threadIdx.x >> 4);
+    const int lane = threadIdx.x & 15;
+    w32x4 in[EACH][GATED ? 2 : 1];
+    uint32_t row[EACH], block[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const uint32_t unit = min(first + 16 * i, a.units - 1);
+        row[i] = unit / a.blocks, block[i] = unit % a.blocks;
+        const uint16_t *const x = a.x + (int64_t)row[i] * a.ldx;
+        const int k = (int)block[i] * kF8Block + lane * 8;
+        in[i][0] = load8<T>(x, a.K, k);
+        if constexpr (GATED) in[i][1] = load8<T>(x + a.K, a.K, k);
+    }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        if (first + 16 * i >= a.units) return;
+        float v[8], scale;
+        widen8<T>(in[i][0], v);
+        if constexpr (GATED) {
+            float up[8];
+            widen8<T>(in[i][1], up);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = v[e] / (1.0f + expf(-v[e])) * up[e];
+        }
+        const w32x2 codes = encode8(v, scale);
+        store_codes(a.codes + (int64_t)row[i] * a.ldc, a.K, (int)block[i] * kF8Block + lane * 8, codes);
+        if (lane == 0) a.scales[(int64_t)block[i] * a.lds + row[i]] = scale;
+    }
+}
+
+// One row per WAVES waves (4 rows per workgroup of single waves).  CHUNKS: pieces of 8 elements that a lane keeps of a row; 0: rows that do not
+// fit the registers are read a second time.
+template <class T, int WAVES, int CHUNKS> __global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) f8_rmsnorm_kernel(const F8RowArgs a)
+{
+    constexpr int ROWS = WAVES == 1 ? 4 : 1, KEPT = CHUNKS ? CHUNKS : 1, LANES = 64 * WAVES;
+    __shared__ float s_part[2][WAVES];
+    const int tid = threadIdx.x % LANES, wave = tid >> 6;
+    const uint32_t row = of_xcd(blockIdx.x, a.groups) * ROWS + threadIdx.x / LANES;
+    if (row >= (uint32_t)a.M) return; // (whole waves, and where waves share a row the whole workgroup)
+    const uint16_t *const x = a.x + row * a.ldx;
+    const uint16_t *const residual = a.residual ? a.residual + row * a.ldr : nullptr;
+    uint16_t *const total = a.total + row * a.ldt;
+    const int turns = CHUNKS ? CHUNKS : (a.K + 8 * LANES - 1) / (8 * LANES);
+    w32x4 h[KEPT], r[KEPT];
+
+    const auto load = [&](int i, int k) {
+        h[i] = load8<T>(x, a.K, k);
+        if (residual) r[i] = load8<T>(residual, a.K, k);
+    };
+    const auto add = [&](int i, int k) {
+        if (!residual) return;
+        float u[8], v[8];
+        widen8<T>(h[i], u), widen8<T>(r[i], v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[e] += v[e];
+        h[i] = narrow8<T>(u);
+        if (k < a.K) store8(total, a.K, k, h[i]);
+    };
+    // over the row
+    int turn = 0;
+    const auto over_row = [&](float v, auto f) {
+        v = over16(v, f);
+        v = f(v, __shfl_xor(v, 16));
+        v = f(v, __shfl_xor(v, 32));
+        if constexpr (WAVES > 1) {
+            turn ^= 1;
+            if ((tid & 63) == 0) s_part[turn][wave] = v;
+            __syncthreads();
+            v = s_part[turn][0];
+#pragma unroll
+            for (int i = 1; i < WAVES; ++i) v = f(v, s_part[turn][i]);
+        }
+        return v;
+    };
+    // f(elements, k) for all pieces of the row as the norm sees it
+    const auto each = [&](auto f) {
+#pragma unroll
+        for (int i = 0; i < (CHUNKS ? CHUNKS : 0); ++i) {
+            float v[8];
+            widen8<T>(h[i], v);
+            f(v, (i * LANES + tid) * 8);
+        }
+        if constexpr (CHUNKS == 0)
+            for (int i = 0; i < turns; ++i) {
+                const int k = (i * LANES + tid) * 8;
+                float v[8];
+                widen8<T>(load8<T>(residual ? total : x, a.K, k), v);
+                f(v, k);
+            }
+    };
+
+    if constexpr (CHUNKS > 0) {
+#pragma unroll
+        for (int i = 0; i < CHUNKS; ++i) load(i, (i * LANES + tid) * 8);
+#pragma unroll
+        for (int i = 0; i < CHUNKS; ++i) add(i, (i * LANES + tid) * 8);
+    } else if (residual) {
+        for (int i = 0; i < turns; ++i) load(0, (i * LANES + tid) * 8), add(0, (i * LANES + tid) * 8);
+    }
+    const auto plus = [](float p, float q) { return p + q; };
+    const float per = 1.0f / (float)a.K;
+    const auto mean_square = [&](float c) {
+        float sum = 0.0f;
+        each([&](float (&v)[8], int) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum = fmaf(v[e] * c, v[e] * c, sum);
+        });
+        return over_row(sum, plus) * per;
+    };
+    float unit = 1.0f, mean = mean_square(1.0f), eps = a.eps;
+    if (!(mean >= 0x1p-90f && mean <= 0x1p100f)) { // squares at the ends of binary32's range: once more in units of 2^e
+        float peak = 0.0f;
+        each([&](float (&v)[8], int) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) peak = fmaxf(peak, fabsf(v[e]));
+        });
+        peak = over_row(peak, larger);
+        if (peak > 0.0f && peak < INFINITY) {
+            unit = ldexpf(1.0f, -max(ilogbf(fmaxf(peak, sqrtf(eps))), -120));
+            mean = mean_square(unit), eps = eps * unit * unit;
+        }
+    }
+    const float by = mean + eps > 0.0f ? 1.0f / sqrtf(mean + eps) : mean + eps == 0.0f ? 0.0f : mean; // (zeros give zeros, NaN a NaN)
+    each([&](float (&v)[8], int k) {
+        if (a.weight) {
+            float g[8];
+            widen8<T>(load8<T>(a.weight, a.K, k), g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = v[e] * unit * by * g[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = v[e] * unit * by;
+        }
+        float scale;
+        const w32x2 codes = encode8(v, scale);
+        if (k >= a.K) return;
+        store_codes(a.codes + row * a.ldc, a.K, k, codes);
+        if (a.y) store8(a.y + (int64_t)row * a.K, a.K, k, narrow8<T>(v));
+        if ((threadIdx.x & 15) == 0) a.scales[(int64_t)(k / kF8Block) * a.lds + row] = scale;
+    });
+}
+
+template <class T, int WAVES, int CHUNKS> static void launch_rmsnorm(F8RowArgs a, hipStream_t s)
+{
+    const uint32_t rows = WAVES == 1 ? 4 : 1, need = (uint32_t)((a.M + rows - 1) / rows);
+    a.groups = (need + 7) / 8;
+    hipLaunchKernelGGL((f8_rmsnorm_kernel<T, WAVES, CHUNKS>), dim3(8 * a.groups), dim3(WAVES == 1 ? 256 : 64 * WAVES), 0, s, a);
+}
+
+template <class T> static void run_rmsnorm(const F8RowArgs &a, hipStream_t s)
+{
+    if (a.K <= 512) launch_rmsnorm<T, 1, 1>(a, s);
+    else if (a.K <= 1024) launch_rmsnorm<T, 1, 2>(a, s);
+    else if (a.K <= 2048) launch_rmsnorm<T, 4, 1>(a, s);
+    else if (a.K <= 4096) launch_rmsnorm<T, 4, 2>(a, s);
+    else if (a.K <= 8192) launch_rmsnorm<T, 4, 4>(a, s);
+    else if (a.K <= 16384) launch_rmsnorm<T, 8, 4>(a, s);
+    else if (a.K <= 32768) launch_rmsnorm<T, 16, 4>(a, s);
+    else launch_rmsnorm<T, 16, 0>(a, s);
+}
+
+} // namespace qnn
+
+using namespace qnn;
+
+extern "C" {
+
+static bool bad_row_sizes(int64_t M, int64_t K) { return M < 0 || K <= 0 || M > (1 << 20) || K > (1 << 24) || M * f8_blocks(K) >= (int64_t)1 << 31; }
+
+qnn_status qnn_f8_quantize(const void *x, int64_t ldx, int64_t M, int64_t K, int gated, int type, uint8_t *codes, int64_t ldc, float *scales,
+                           int64_t lds, void *stream)
+{
+    if (bad_row_sizes(M, K) || bad_half_type(type)) return QNN_EINVAL;
+    if (M == 0) return QNN_OK;
+    if (!x || !codes || !scales || ldx < (gated ? 2 * K : K) || ldc < K || lds < M) return QNN_EINVAL;
+    F8RowArgs a{};
+    a.x = static_cast<const uint16_t *>(x), a.ldx = ldx, a.codes = codes, a.ldc = ldc, a.scales = scales, a.lds = lds;
+    a.M = (int32_t)M, a.K = (int32_t)K, a.blocks = (uint32_t)f8_blocks(K), a.units = (uint32_t)(M * a.blocks);
+    a.groups = ((a.units + 63) / 64 + 7) / 8;
+    const dim3 grid(8 * a.groups), block(256);
+    hipStream_t s = as_stream(stream);
+    if (type == QNN_BF16) {
+        if (gated) hipLaunchKernelGGL((f8_quantize_kernel<Bf16, true>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((f8_quantize_kernel<Bf16, false>), grid, block, 0, s, a);
+    } else {
+        if (gated) hipLaunchKernelGGL((f8_quantize_kernel<F16, true>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((f8_quantize_kernel<F16, false>), grid, block, 0, s, a);
+    }
+    return launch_status(hipGetLastError());
+}
+
+qnn_status qnn_f8_rmsnorm(const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, float eps, int64_t M, int64_t K,
+                          int type, void *total, int64_t ldt, void *y, uint8_t *codes, int64_t ldc, float *scales, int64_t lds, void *stream)
+{
+    if (bad_row_sizes(M, K) || bad_half_type(type) || !(eps >= 0.0f) || !(eps <= 0x1p100f)) return QNN_EINVAL;
+    if (M == 0) return QNN_OK;
+    if (!x || !codes || !scales || ldx < K || ldc < K || lds < M) return QNN_EINVAL;
+    if (residual && (!total || ldr < K || ldt < K)) return QNN_EINVAL;
+    F8RowArgs a{};
+    a.x = static_cast<const uint16_t *>(x), a.ldx = ldx, a.residual = static_cast<const uint16_t *>(residual), a.ldr = ldr;
+    a.weight = static_cast<const uint16_t *>(weight), a.total = static_cast<uint16_t *>(total), a.ldt = ldt, a.y = static_cast<uint16_t *>(y);
+    a.codes = codes, a.ldc = ldc, a.scales = scales, a.lds = lds, a.M = (int32_t)M, a.K = (int32_t)K, a.eps = eps;
+    if (type == QNN_BF16) run_rmsnorm<Bf16>(a, as_stream(stream));
+    else run_rmsnorm<F16>(a, as_stream(stream));
+    return launch_status(hipGetLastError());
+}
+
+} // extern "C"

@@ -46,6 +46,28 @@ template <class V> __device__ __forceinline__ V load_any(const void *p)
 }
 template <class V> __device__ __forceinline__ void store_any(void *p, V v) { __builtin_memcpy(p, &v, sizeof(V)); }
 
+// 16 bytes of a row from byte `at` on where the row ends within them: what lies beyond is zero.  The row's last 16 bytes are
+// loaded and moved down (rows shorter than that go byte by byte).
+__device__ __forceinline__ w32x4 load_end(const uint8_t *row, int bytes, int at)
+{
+    w32x4 v = {0u, 0u, 0u, 0u};
+    const int have = bytes - at;
+    if (have >= 16) return load_any<w32x4>(row + at);
+    if (have <= 0) return v;
+    if (bytes < 16) {
+        for (int b = 0; b < have; ++b) v[b >> 2] |= (uint32_t)row[at + b] << (b & 3) * 8;
+        return v;
+    }
+    const w32x4 last = load_any<w32x4>(row + bytes - 16);
+    const int drop = 16 - have, words = drop >> 2, rest = (drop & 3) * 8;
+    uint32_t u[5] = {last[0], last[1], last[2], last[3], 0u};
+    if (words & 1) u[0] = u[1], u[1] = u[2], u[2] = u[3], u[3] = 0u;
+    if (words & 2) u[0] = u[2], u[1] = u[3], u[2] = 0u, u[3] = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (uint32_t)(((uint64_t)u[i + 1] << 32 | u[i]) >> rest);
+    return v;
+}
+
 // (lanes l, l ^ 16, l ^ 32, l ^ 48 hold the parts of one column)
 __device__ __forceinline__ float max_over_groups(float v)
 {

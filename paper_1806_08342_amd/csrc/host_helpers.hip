@@ -240,4 +240,32 @@ qnn_status qnn_quantize_weights_grouped(const float *w, size_t rows, size_t cols
     return QNN_OK;
 }
 
+static uint8_t e4m3_pattern(float v) // |v| below 464, to nearest even
+{
+    uint32_t u;
+    std::memcpy(&u, &v, 4);
+    const uint32_t sign = u >> 24 & 0x80u, a = u & 0x7fffffffu;
+    if (a < 0x3c800000u) return static_cast<uint8_t>(sign | static_cast<uint32_t>(std::nearbyint(std::fabs(v) * 512.0f))); // below 2^-6: steps of 2^-9
+    return static_cast<uint8_t>(sign | (((a + 0x7ffffu + (a >> 20 & 1u)) >> 20) - (120u << 3)));
+}
+
+qnn_status qnn_quantize_weights_blocks(const float *w, size_t rows, size_t cols, uint8_t *codes, float *scales)
+{
+    if (!w || !codes || !scales || rows == 0 || cols == 0) return QNN_EINVAL;
+    for (size_t i = 0; i < rows * cols; ++i)
+        if (!std::isfinite(w[i])) return QNN_EINVAL;
+    for (size_t n0 = 0; n0 < rows; n0 += 128)
+        for (size_t k0 = 0; k0 < cols; k0 += 128) {
+            const size_t n1 = n0 + 128 < rows ? n0 + 128 : rows, k1 = k0 + 128 < cols ? k0 + 128 : cols;
+            float most = 0.0f;
+            for (size_t n = n0; n < n1; ++n)
+                for (size_t k = k0; k < k1; ++k) most = std::fmax(most, std::fabs(w[n * cols + k]));
+            const float scale = std::fmax(most / 448.0f, 0x1p-80f);
+            scales[n0 / 128 * ((cols + 127) / 128) + k0 / 128] = scale;
+            for (size_t n = n0; n < n1; ++n)
+                for (size_t k = k0; k < k1; ++k) codes[n * cols + k] = e4m3_pattern(w[n * cols + k] / scale);
+        }
+    return QNN_OK;
+}
+
 } // extern "C"

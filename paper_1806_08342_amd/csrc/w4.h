@@ -70,28 +70,6 @@ __device__ __forceinline__ w32x4 pair_order(w32x4 v)
                  __builtin_amdgcn_perm(v[3], v[1], 0x05040100u), __builtin_amdgcn_perm(v[3], v[1], 0x07060302u)};
 }
 
-// 16 bytes of a row from byte `at` on where the row ends within them: what lies beyond is zero.  The row's last 16 bytes are
-// loaded and moved down (rows shorter than that go byte by byte).
-__device__ __forceinline__ w32x4 load_end(const uint8_t *row, int bytes, int at)
-{
-    w32x4 v = {0u, 0u, 0u, 0u};
-    const int have = bytes - at;
-    if (have >= 16) return load_any<w32x4>(row + at);
-    if (have <= 0) return v;
-    if (bytes < 16) {
-        for (int b = 0; b < have; ++b) v[b >> 2] |= (uint32_t)row[at + b] << (b & 3) * 8;
-        return v;
-    }
-    const w32x4 last = load_any<w32x4>(row + bytes - 16);
-    const int drop = 16 - have, words = drop >> 2, rest = (drop & 3) * 8;
-    uint32_t u[5] = {last[0], last[1], last[2], last[3], 0u};
-    if (words & 1) u[0] = u[1], u[1] = u[2], u[2] = u[3], u[3] = 0u;
-    if (words & 2) u[0] = u[2], u[1] = u[3], u[2] = 0u, u[3] = 0u;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = (uint32_t)(((uint64_t)u[i + 1] << 32 | u[i]) >> rest);
-    return v;
-}
-
 // Consecutive dwords of a row of codes.  Where the row does not begin at a multiple of 4 bytes, loads from there take about
 // twice as long (1 x 4100 x 4096 8.3 us, 4104 6.1): the dwords that hold them are loaded instead, one more of them,
 // and shifted into place when they are used.  Every dword that is read holds a byte of the row.

@@ -1,0 +1,115 @@
+"""Operators in 8-bit floating point: what the host checks and computes, without a GPU."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+import f8_reference as ref
+import paper_1806_08342_amd as qnn
+
+EINVAL = 1
+P, NULL = C.c_void_p(4096), C.c_void_p(0)  # never dereferenced
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return qnn.load_library()
+
+
+def caller(fn, fields):
+    return lambda **kw: fn(*[kw.get(k, d) for k, d in fields])
+
+
+def test_bad_rows_are_refused_before_anything_is_launched(lib):
+    f = caller(lib.qnn_f8_quantize, [("x", P), ("ldx", 256), ("M", 4), ("K", 256), ("gated", 0), ("type", 0), ("codes", P), ("ldc", 256), ("scales", P), ("lds", 4), ("s", None)])
+    for bad in (dict(M=-1), dict(K=0), dict(K=-128), dict(M=1 << 21), dict(K=(1 << 24) + 1), dict(type=2), dict(type=-1), dict(x=NULL), dict(codes=NULL), dict(scales=NULL),
+                dict(ldx=255), dict(gated=1, ldx=511), dict(ldc=255), dict(lds=3), dict(M=1 << 20, K=1 << 24, ldx=1 << 24, ldc=1 << 24, lds=1 << 20)):
+        assert f(**bad) == EINVAL, bad
+    assert f(M=0, x=NULL) == 0
+
+
+def test_bad_norms_are_refused_before_anything_is_launched(lib):
+    f = caller(lib.qnn_f8_rmsnorm, [("x", P), ("ldx", 256), ("r", NULL), ("ldr", 256), ("w", P), ("eps", 1e-5), ("M", 4), ("K", 256), ("type", 1), ("total", NULL), ("ldt", 256),
+                                    ("y", NULL), ("codes", P), ("ldc", 256), ("scales", P), ("lds", 4), ("s", None)])
+    for bad in (dict(M=-1), dict(K=0), dict(type=2), dict(x=NULL), dict(codes=NULL), dict(scales=NULL), dict(ldx=255), dict(ldc=1), dict(lds=3), dict(eps=-1e-5),
+                dict(eps=float("nan")), dict(eps=float("inf")), dict(r=P), dict(r=P, total=P, ldr=255), dict(r=P, total=P, ldt=255)):
+        assert f(**bad) == EINVAL, bad
+    assert f(M=0, codes=NULL) == 0
+
+
+def test_bad_products_are_refused_before_anything_is_launched(lib):
+    f = caller(lib.qnn_f8_matmul, [("x", P), ("ldx", 128), ("xs", P), ("ldxs", 4), ("w", P), ("ws", P), ("bias", NULL), ("M", 4), ("N", 8), ("K", 128), ("type", 0), ("y", P), ("ldy", 8),
+                                   ("space", NULL), ("bytes", 0), ("s", None)])
+    for bad in (dict(M=-1), dict(N=0), dict(K=0), dict(M=1 << 21), dict(N=(1 << 24) + 1), dict(K=(1 << 24) + 1), dict(type=3), dict(x=NULL), dict(xs=NULL), dict(w=NULL), dict(ws=NULL),
+                dict(y=NULL), dict(ldx=127), dict(ldxs=3), dict(ldy=7)):
+        assert f(**bad) == EINVAL, bad
+    assert f(M=0, x=NULL, y=NULL) == 0
+    assert qnn.f8_matmul_plan(1, 8, 128) and not qnn.f8_matmul_plan(0, 8, 128) and not qnn.f8_matmul_plan(1, 0, 128)
+    for M, N, K in ((1, 300, 400), (100, 1000, 1000), (1000, 1001, 1027), (300, 300, 20000), (4096, 4096, 4096)):
+        for dtype in (torch.bfloat16, torch.float32):
+            need = lib.qnn_f8_matmul_workspace_bytes(M, N, K, 2 if dtype == torch.float32 else 0)
+            assert qnn.f8_matmul_plan(M, N, K, dtype)
+            if need:
+                sizes = dict(M=M, N=N, K=K, ldx=K, ldxs=M, ldy=N, type=2 if dtype == torch.float32 else 0)
+                for bad in (dict(space=NULL, bytes=need), dict(space=P, bytes=need - 1), dict(space=C.c_void_p(4104), bytes=need)):
+                    assert f(**sizes, **bad) == EINVAL, (M, N, K, bad)
+
+
+def test_bad_layers_of_experts_are_refused_before_anything_is_launched(lib):
+    f = caller(lib.qnn_f8_moe, [("x", P), ("ldx", 128), ("xs", P), ("ldxs", 4), ("logits", P), ("ldl", 8), ("lt", 2), ("up", P), ("ups", P), ("down", P), ("downs", P), ("T", 4), ("E", 8),
+                                ("k", 2), ("H", 128), ("I", 64), ("renorm", 1), ("type", 0), ("y", P), ("ldy", 128), ("experts", NULL), ("weights", NULL), ("space", P), ("bytes", 1 << 30),
+                                ("s", None)])
+    for bad in (dict(T=-1), dict(T=1 << 21), dict(E=0), dict(E=1025, ldl=2000), dict(k=0), dict(k=9), dict(k=33, E=64, ldl=64), dict(H=0), dict(H=120), dict(I=0), dict(I=40), dict(I=1 << 18),
+                dict(type=2), dict(lt=3), dict(lt=-1), dict(ldx=127), dict(ldxs=3), dict(ldl=7), dict(ldy=127), dict(space=NULL), dict(space=C.c_void_p(4100)), dict(bytes=100),
+                *(dict([(n, NULL)]) for n in ("x", "xs", "logits", "up", "ups", "down", "downs", "y"))):
+        assert f(**bad) == EINVAL, bad
+    assert f(T=0, x=NULL, space=NULL, bytes=0) == 0
+    size = lib.qnn_f8_moe_workspace_bytes
+    assert size(1, 8, 2, 128, 64) > 0 and size(64, 8, 2, 128, 64) == size(1000, 8, 2, 128, 64) and size(0, 8, 2, 128, 64) == 0 and size(1, 8, 9, 128, 64) == 0
+    assert f(bytes=size(4, 8, 2, 128, 64) - 1) == EINVAL
+
+
+@pytest.mark.parametrize("shape", [(1, 1), (128, 128), (130, 257), (5, 300)])
+def test_weights_in_blocks(shape):
+    rng = np.random.default_rng(shape[0])
+    w = (rng.standard_normal(shape) * np.exp(rng.standard_normal(shape))).astype(np.float32)
+    codes, scales = qnn.quantize_weights_blocks(w)
+    assert codes.dtype == ref.F8 and codes.shape == shape and scales.shape == (ref.blocks(shape[0]), ref.blocks(shape[1]))
+    for i in range(scales.shape[0]):
+        for j in range(scales.shape[1]):
+            part = torch.from_numpy(w)[128 * i:128 * i + 128, 128 * j:128 * j + 128]
+            s = part.abs().max() / 448.0
+            assert scales[i, j] == s
+            assert torch.equal(codes[128 * i:128 * i + 128, 128 * j:128 * j + 128].view(torch.uint8), (part / s).to(ref.F8).view(torch.uint8))
+
+
+def test_weights_at_the_ends_of_the_range():
+    every = torch.arange(256, dtype=torch.uint8)
+    every = every[(every & 127) != 127].view(ref.F8).float()
+    between = torch.sort(every).values
+    w = torch.cat([every, (between[1:] + between[:-1]) / 2, torch.tensor([448.0])])[None]  # values and ties
+    w = torch.nn.functional.pad(w, (0, -w.shape[1] % 128))
+    w.view(-1, 128)[:, -1] = 448.0
+    codes, scales = qnn.quantize_weights_blocks(w.numpy())
+    assert (scales == 1).all() and torch.equal(codes.float(), w.to(ref.F8).float())
+    codes, scales = qnn.quantize_weights_blocks(np.zeros((3, 200), np.float32))
+    assert (scales == 2.0 ** -80).all() and (codes.view(torch.uint8) == 0).all()
+    stacked, scales = qnn.quantize_weights_blocks(np.ones((2, 130, 140), np.float32))
+    assert stacked.shape == (2, 130, 140) and scales.shape == (2, 2, 2) and (stacked.float() == 448).all()
+    for bad in (w.numpy() * np.nan, w.numpy() * np.inf, np.zeros((0, 4), np.float32)):
+        with pytest.raises(qnn.QnnError):
+            qnn.quantize_weights_blocks(bad)
+    with pytest.raises(ValueError):
+        qnn.quantize_weights_blocks(np.zeros(4, np.float32))
+
+
+def test_tensors_of_the_wrong_kind_are_refused():
+    x, codes, scales = torch.zeros(4, 128, dtype=torch.bfloat16), torch.zeros(4, 128, dtype=ref.F8), torch.zeros(1, 4)
+    for call in (lambda: qnn.f8_quantize(x), lambda: qnn.f8_quantize(None), lambda: qnn.f8_rmsnorm(x), lambda: qnn.f8_rmsnorm(x.float()), lambda: qnn.f8_matmul(codes, scales, codes, scales),
+                 lambda: qnn.f8_matmul(codes.view(torch.uint8), scales, codes, scales), lambda: qnn.f8_moe(codes, scales, scales, codes, scales, codes, scales, 2)):
+        with pytest.raises(TypeError):
+            call()
+    for dtype in (torch.int8, torch.float64):
+        with pytest.raises(ValueError):
+            qnn.f8_matmul(codes, scales, codes, scales, dtype=dtype)
