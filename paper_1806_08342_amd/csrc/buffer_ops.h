@@ -42,6 +42,16 @@ __device__ __forceinline__ buf8 buffer_load8(const uint8_t *base, int bytes, uin
 #endif
 }
 
+__device__ __forceinline__ float buffer_load_float(const float *base, int bytes, uint32_t offset)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(__builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(base), 0, bytes, 0x00020000), (int)offset, 0, 0));
+#else
+    (void)base, (void)bytes, (void)offset;
+    return 0.0f;
+#endif
+}
+
 // 16 bytes per lane to 1024 consecutive bytes of LDS in lane order; `lds` is the same in the whole wave
 __device__ __forceinline__ void buffer_to_lds16(const uint8_t *base, int bytes, uint32_t offset, uint8_t *lds)
 {

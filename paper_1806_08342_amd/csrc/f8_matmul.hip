@@ -3,7 +3,9 @@
 //   y[m][n] = bias[n] + sum_b xs[b][m] ws[n / 128][b] * sum_{k in b} x[m][k] w[n][k]
 //
 // The sum over a block comes from the matrix unit; one multiply-add in binary32 for each output and block joins it to the others.
-#include "f8.h"
+#include "f8_matmul.h"
+
+#include <cstdio>
 
 namespace qnn {
 
@@ -106,6 +108,34 @@ template <int MT, int NT, int WAVES> static void launch_f8_rows(const F8Args &a,
     else hipLaunchKernelGGL((f8_rows_kernel<MT, NT, WAVES, 2, true>), grid, block, 0, s, a);
 }
 
+// By estimated time (us).
+F8Plan f8_plan(int64_t M, int64_t N, int64_t K, int type)
+{
+    F8Plan best{F8Kernel::Rows, 1, 0.0f, false, 0, 0, 0};
+    const float steps = (float)f8_blocks(K);
+    if (M <= 64 || K > (1 << 20)) return best;
+    const bool wide = type == QNN_F32, padded = K % 16 != 0;
+    best.us = 1e30f;
+    const auto consider = [&](F8Kernel kernel, int64_t tile, int64_t per_cu, float one, float full) {
+        const int64_t tiles = ((M + tile - 1) / tile) * ((N + tile - 1) / tile);
+        for (int splits = 1; splits <= 16; ++splits) {
+            if (splits > 1 && (steps / (float)splits < 4.0f || tiles * (splits - 1) >= 256 * per_cu)) break;
+            const int64_t groups = tiles * splits;
+            const float length = ceilf(steps / (float)splits) + 3.0f;
+            const float us = (groups <= 256 ? one : full * (float)((groups + 256 * per_cu - 1) / (256 * per_cu))) * length +
+                             (splits > 1 ? 3.0f + (float)splits * (float)(M * N) * 8.0f / 4e6f : 0.0f);
+            if (us < best.us) best.us = us, best.kernel = kernel, best.splits = splits;
+        }
+    };
+    consider(F8Kernel::Tile128, 128, 2, wide ? 1.2f : 0.9f, wide ? 1.9f : 1.2f);
+    if (!wide) consider(F8Kernel::Tile256, 256, 1, 1.95f, 1.95f);
+    best.padded = padded;
+    const auto rounded = [](int64_t n) { return (size_t)((n + 255) / 256 * 256); };
+    if (padded) best.x_bytes = rounded(M * f8_padded(K)), best.w_bytes = rounded(N * f8_padded(K));
+    best.bytes = best.x_bytes + best.w_bytes + (best.splits > 1 ? rounded(4 * best.splits * M * N) : 0);
+    return best;
+}
+
 } // namespace qnn
 
 using namespace qnn;
@@ -120,20 +150,39 @@ qnn_status qnn_f8_matmul(const uint8_t *x, int64_t ldx, const float *x_scales, i
     if (bad_f8_sizes(M, N, K) || (bad_half_type(type) && type != QNN_F32)) return QNN_EINVAL;
     if (M == 0) return QNN_OK;
     if (!x || !x_scales || !w || !w_scales || !y || ldx < K || ldxs < M || ldy < N) return QNN_EINVAL;
-    const size_t need = qnn_f8_matmul_workspace_bytes(M, N, K, type);
-    if (need > 0 && (!workspace || ((uintptr_t)workspace & 15) != 0 || workspace_bytes < need)) return QNN_EINVAL;
-    const F8Args a{x, w, x_scales, w_scales, bias, y, ldx, ldxs, ldy, (int32_t)M, (int32_t)N, (int32_t)K, type};
-    if (M <= 16) launch_f8_rows<1, 1, 8>(a, as_stream(stream));
-    else launch_f8_rows<4, 2, 4>(a, as_stream(stream));
+    const F8Plan plan = f8_plan(M, N, K, type);
+    if (plan.bytes > 0 && (!workspace || ((uintptr_t)workspace & 15) != 0 || workspace_bytes < plan.bytes)) return QNN_EINVAL;
+    F8Args a{x, w, x_scales, w_scales, bias, y, ldx, ldxs, ldy, (int32_t)M, (int32_t)N, (int32_t)K, type};
+    hipStream_t s = as_stream(stream);
+    const bool pieces = ((uintptr_t)x | (uintptr_t)ldx | (uintptr_t)w | (uintptr_t)K) % 16 == 0 && ldx < (1 << 22);
+    if (plan.kernel != F8Kernel::Rows && (plan.padded || pieces)) {
+        uint8_t *const space = static_cast<uint8_t *>(workspace);
+        if (plan.padded) {
+            launch_f8_pad(a, space, space + plan.x_bytes, s);
+            a.x = space, a.w = space + plan.x_bytes, a.ldx = f8_padded(K);
+        }
+        launch_f8_tiles(a, plan, plan.padded ? f8_padded(K) : K, reinterpret_cast<float *>(space + plan.x_bytes + plan.w_bytes), s);
+    } else if (M <= 16) {
+        launch_f8_rows<1, 1, 8>(a, s);
+    } else {
+        launch_f8_rows<4, 2, 4>(a, s);
+    }
     return launch_status(hipGetLastError());
 }
 
-size_t qnn_f8_matmul_workspace_bytes(int64_t, int64_t, int64_t, int) { return 0; }
+size_t qnn_f8_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, int type)
+{
+    return bad_f8_sizes(M, N, K) || M == 0 || (bad_half_type(type) && type != QNN_F32) ? 0 : f8_plan(M, N, K, type).bytes;
+}
 
 const char *qnn_f8_matmul_plan(int64_t M, int64_t N, int64_t K, int type)
 {
     if (bad_f8_sizes(M, N, K) || M == 0 || (bad_half_type(type) && type != QNN_F32)) return "";
-    return M <= 16 ? "few16x16/8" : "few64x32/4";
+    const F8Plan p = f8_plan(M, N, K, type);
+    static thread_local char name[32];
+    if (p.kernel == F8Kernel::Rows) return M <= 16 ? "rows16x16/8" : "rows64x32/4";
+    std::snprintf(name, sizeof(name), "tile%s/%d", p.kernel == F8Kernel::Tile256 ? "256x256" : "128x128", p.splits);
+    return name;
 }
 
 } // extern "C"

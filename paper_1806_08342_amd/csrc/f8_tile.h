@@ -1,0 +1,253 @@
+// Products of e4m3 rows and weights with block scales, tens of rows and more: tiles of both operands through LDS.
+#pragma once
+
+#include "buffer_ops.h"
+#include "f8.h"
+#include "lds_ring.h"
+
+namespace qnn {
+
+// 32 x 32 outputs over 64 (NARROW) or 16 of K; operands and result as in f8_products, with rows of 32
+__device__ __forceinline__ f32x16 f8_products32(const i32x8 a, const i32x8 b, const f32x16 c)
+{
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);
+}
+__device__ __forceinline__ b16x8 widen_codes(uint32_t low, uint32_t high)
+{
+    return __builtin_bit_cast(b16x8, w32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(low, 1.0f, false)),
+                                           __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(low, 1.0f, true)),
+                                           __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(high, 1.0f, false)),
+                                           __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(high, 1.0f, true))});
+}
+
+struct F8TileArgs {
+    F8Args a;          // x, w: rows of whole 16-byte pieces
+    int64_t ldw;
+    float *parts;      // sums of parts of K: [splits][M][N], or null
+    int32_t m_tiles, n_tiles, splits, band;
+    uint32_t per_xcd;  // workgroups
+};
+
+// Workgroups are dealt to the 8 XCDs in turn.  Each XCD has a stretch of the tiles of its own, in bands of `band` tiles of rows, so that the tiles that
+// it works on at a time share rows and weights in its L2.
+__device__ __forceinline__ bool f8_tile_of(const F8TileArgs &t, int &tm, int &tn, int &part)
+{
+    const uint32_t id = blockIdx.x % 8 * t.per_xcd + blockIdx.x / 8, tiles = (uint32_t)t.m_tiles * t.n_tiles;
+    part = (int)(id / tiles);
+    if (part >= t.splits) return false;
+    const uint32_t at = id % tiles, whole = (uint32_t)t.band * t.n_tiles, group = at / whole, rest = at % whole;
+    const uint32_t high = min((uint32_t)t.band, t.m_tiles - group * t.band);
+    tm = (int)(group * t.band + rest % high), tn = (int)(rest / high);
+    return true;
+}
+
+// BM rows of x by BN rows of weights; WM x WN waves, each with BM / WM by BN / WN of them, in products of 32 x 32 formed transposed (weights are the
+// left operand), so that a lane's outputs are of one row of x and its scale is one register.  K in steps of 128 through LDS,
+// copied there directly, 16-byte pieces of a row exchanged by half its number, so that reads of 16 rows meet the 16 places of the 64 banks.
+// Copies take longer than a step: they are requested two steps ahead, those of weights into a third buffer, those of x, which the waves read
+// into registers as a step begins, into the buffer of that step behind a second barrier.
+template <int BM, int BN, int WM, int WN, bool NARROW, int PER_SIMD> __global__ void __launch_bounds__(64 * WM * WN, PER_SIMD) f8_tile_kernel(const F8TileArgs t)
+{
+    constexpr int WAVES = WM * WN, TJ = BM / WM / 32, TI = BN / WN / 32, X_BYTES = BM * 128, W_BYTES = BN * 128, X_COPIES = BM / 8 / WAVES,
+                  W_COPIES = BN / 8 / WAVES, RING = 2 * X_BYTES + 3 * W_BYTES;
+    static_assert(BN / WN <= 128 && BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0, "a wave's weights lie in one block; whole copies");
+    __shared__ __attribute__((aligned(16))) uint8_t s_ring[RING];
+    uint8_t *const s_w = s_ring + 2 * X_BYTES;
+    const F8Args &a = t.a;
+    int tm, tn, part;
+    if (!f8_tile_of(t, tm, tn, part)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, g = lane >> 5;
+    const int wm = wave % WM, wn = wave / WM, m0 = tm * BM, n0 = tn * BN;
+    const int blocks = (a.K + kF8Block - 1) / kF8Block;
+    const int first = (int)((int64_t)blocks * part / t.splits), last = (int)((int64_t)blocks * (part + 1) / t.splits);
+
+    const uint8_t *const x_tile = a.x + m0 * a.ldx, *const w_tile = a.w + n0 * t.ldw;
+    const int x_bytes = (int)(min(a.M - m0, BM) * a.ldx), w_bytes = (int)(min(a.N - n0, BN) * t.ldw); // rows beyond the last read as zeros
+    // Where a lane's 16 bytes of a block are in the rows that a copy of 8 begins with an even or odd multiple of 8; past the end of this part of K: beyond
+    // the descriptors' sizes (which are below 2^31), where reads give zeros.
+    const int k_end = min(a.K, last * kF8Block);
+    // (Worked out from the lane's number each time: registers are short.)
+    const auto offsets = [&](int b, int row, uint32_t pitch, uint32_t (&at)[2]) {
+        int l = lane;
+        asm volatile("" : "+v"(l));
+        const uint32_t begin = (uint32_t)(row + (l >> 3)) * pitch;
+#pragma unroll
+        for (int odd = 0; odd < 2; ++odd) {
+            const uint32_t k = (uint32_t)(b * kF8Block + ((l & 7) ^ (l >> 4) ^ 4 * odd) * 16);
+            at[odd] = begin + ((int)k < k_end ? k : 0x80000000u);
+        }
+    };
+    const auto copy_x = [&](int b, int buffer) {
+        uint32_t at[2];
+        offsets(b, wave * X_COPIES * 8, (uint32_t)a.ldx, at);
+#pragma unroll
+        for (int i = 0; i < X_COPIES; ++i)
+            buffer_to_lds16(x_tile, x_bytes, at[(wave * X_COPIES + i) & 1] + (uint32_t)(i * 8) * (uint32_t)a.ldx, s_ring + buffer * X_BYTES + (wave * X_COPIES + i) * 1024);
+    };
+    const auto copy_w = [&](int b, int buffer) {
+        uint32_t at[2];
+        offsets(b, wave * W_COPIES * 8, (uint32_t)t.ldw, at);
+#pragma unroll
+        for (int i = 0; i < W_COPIES; ++i)
+            buffer_to_lds16(w_tile, w_bytes, at[(wave * W_COPIES + i) & 1] + (uint32_t)(i * 8) * (uint32_t)t.ldw, s_w + buffer * W_BYTES + (wave * W_COPIES + i) * 1024);
+    };
+    const uint32_t x_at = 4u * (uint32_t)(wm * (BM / WM) + c); // (rows beyond the last: scales of 0)
+    const float *const w_scale = a.ws + (int64_t)min((n0 + wn * (BN / WN)) / kF8Block, (a.N - 1) / kF8Block) * blocks;
+    struct Scales {
+        float x[TJ], w;
+    };
+    const auto load_scales = [&](Scales &s, int b) {
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) s.x[j] = buffer_load_float(a.xs + b * a.ldxs + m0 + 32 * j, 4 * max(min(a.M - m0, BM) - 32 * j, 0), x_at);
+        s.w = w_scale[b];
+    };
+
+    f32x16 acc[TI][TJ];
+#pragma unroll
+    for (int i = 0; i < TI; ++i)
+#pragma unroll
+        for (int j = 0; j < TJ; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+
+    const auto fragment = [&](const uint8_t *rows, int h) { // 32 bytes of row c of 32
+        const w32x4 p = *reinterpret_cast<const w32x4 *>(rows + c * 128 + ((4 * h + 2 * g) ^ (c >> 1 & 7)) * 16);
+        const w32x4 q = *reinterpret_cast<const w32x4 *>(rows + c * 128 + ((4 * h + 2 * g + 1) ^ (c >> 1 & 7)) * 16);
+        return i32x8{(int)p[0], (int)p[1], (int)p[2], (int)p[3], (int)q[0], (int)q[1], (int)q[2], (int)q[3]};
+    };
+    // The tiles of a step one after the other, the multiply-adds of a tile beside the products of the next one, and the pieces of the weights that the
+    // tiles after that need read meanwhile; the last tile's are left for the next step.
+    f32x16 p[2];
+    float late = 0.0f; // the scale of the tile that is left
+#pragma unroll
+    for (int e = 0; e < 16; ++e) p[0][e] = p[1][e] = 0.0f;
+    const auto join = [&](int tile, float by) {
+        const int i = tile / TJ, j = tile % TJ;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = fmaf(p[tile & 1][e], by, acc[i][j][e]);
+    };
+    constexpr int TILES = TI * TJ;
+    static_assert(TILES % 2 == 0 && TI % 2 == 0 && TJ >= 2, "sums and weights in two sets in turn");
+    i32x8 x[TJ][2], w[2][2];
+    const auto x_rows = [&](int buffer) { return s_ring + buffer * X_BYTES + wm * (BM / WM) * 128; };
+    const auto w_rows = [&](int buffer) { return s_w + buffer * W_BYTES + wn * (BN / WN) * 128; };
+    constexpr int SCALES = TJ + 1;
+    Scales now;
+    copy_w(first, 0), copy_x(first, 0);
+    copy_w(first + 1, 1);
+    load_scales(now, first);
+    copy_x(first + 1, 1);
+    wait_vmcnt<W_COPIES + SCALES + X_COPIES>();
+    lds_barrier();
+    copy_w(first + 2, 2);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) w[0][h] = fragment(w_rows(0), h), x[0][h] = fragment(x_rows(0), h);
+    int w_buffer = 0;
+    for (int b = first; b < last; ++b) {
+        const int x_buffer = (b - first) & 1, w_next = w_buffer == 2 ? 0 : w_buffer + 1;
+        float scale[TJ];
+#pragma unroll
+        for (int at = 0; at < TILES; ++at) {
+            const int i = at / TJ, j = at % TJ;
+            if (at == TILES - 1) {
+                // The next step's copies have arrived (those of the one after it, requested after them, may be on their way), and all waves have
+                // this step's weights in registers.
+                wait_vmcnt<W_COPIES + SCALES + X_COPIES>();
+                lds_barrier();
+                copy_w(b + 3, w_buffer);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (i == 0 && j + 1 < TJ) x[j + 1][h] = fragment(x_rows(x_buffer) + (j + 1) * 32 * 128, h);
+                if (j == TJ - 1 && i + 1 < TI) w[(i + 1) & 1][h] = fragment(w_rows(w_buffer) + (i + 1) * 32 * 128, h);
+                if (at == TILES - 1) w[0][h] = fragment(w_rows(w_next), h), x[0][h] = fragment(x_rows(1 - x_buffer), h);
+                if (h == 0)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) p[at & 1][e] = 0.0f;
+                if constexpr (NARROW) {
+                    p[at & 1] = f8_products32(w[i & 1][h], x[j][h], p[at & 1]);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        p[at & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen_codes((uint32_t)w[i & 1][h][2 * q], (uint32_t)w[i & 1][h][2 * q + 1]),
+                                                                            widen_codes((uint32_t)x[j][h][2 * q], (uint32_t)x[j][h][2 * q + 1]), p[at & 1], 0, 0, 0);
+                }
+                if (h == 1) { // (half a tile later than they might be: a wait for the products that they read would hold up all that follows)
+                    if (at == 1)
+#pragma unroll
+                        for (int u = 0; u < TJ; ++u) scale[u] = now.x[u] * now.w;
+                    join((at + TILES - 1) % TILES, at == 0 ? late : scale[(at - 1) % TJ]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (at == TJ - 1) {
+                lds_barrier(); // all waves have this step's x in registers
+                load_scales(now, min(b + 1, last - 1));
+                copy_x(b + 2, x_buffer);
+            }
+        }
+        late = scale[TJ - 1], w_buffer = w_next;
+    }
+    join(TILES - 1, late);
+
+    // Outputs in binary32 through LDS, 32 rows of x by the wave's weights at a time, 16-byte pieces exchanged by the row's number
+    constexpr int WIDE = BN / WN, PIECES = WIDE / 4;
+    static_assert(WAVES * 32 * WIDE * 4 <= RING, "outputs fit the ring");
+    wait_vmcnt<0>();
+    lds_barrier();
+    float *const tile = reinterpret_cast<float *>(s_ring) + wave * 32 * WIDE;
+    constexpr int EACH = 8, LANES = WIDE / EACH, ROWS = 64 / LANES; // outputs of a lane, lanes of a row, rows at a time
+    const int n = n0 + wn * WIDE + lane % LANES * EACH;
+    float bias[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) bias[e] = a.bias && !t.parts && n + e < a.N ? load_out(a.bias, n + e, a.type) : 0.0f;
+#pragma unroll
+    for (int j = 0; j < TJ; ++j) {
+#pragma unroll
+        for (int i = 0; i < TI; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int at = (i * 8 + q * 2 + g) ^ (c & 15);
+                *reinterpret_cast<f32x4 *>(tile + c * WIDE + at * 4) = f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+            }
+        lds_barrier(); // (between waves nothing is exchanged; the compiler keeps the order of writes and reads)
+#pragma unroll
+        for (int r = 0; r < 32 / ROWS; ++r) {
+            const int row = r * ROWS + lane / LANES, m = m0 + wm * (BM / WM) + j * 32 + row;
+            float v[EACH];
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                const f32x4 u = *reinterpret_cast<const f32x4 *>(tile + row * WIDE + ((lane % LANES * 2 + p) ^ (row & 15)) * 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[4 * p + e] = u[e] + bias[4 * p + e];
+            }
+            if (m >= a.M || n >= a.N) continue;
+            if (t.parts) {
+                float *const to = t.parts + ((int64_t)part * a.M + m) * a.N + n;
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    if (n + 4 * p + 4 <= a.N) store_any(to + 4 * p, f32x4{v[4 * p], v[4 * p + 1], v[4 * p + 2], v[4 * p + 3]});
+                    else
+                        for (int e = 0; e < 4; ++e)
+                            if (n + 4 * p + e < a.N) to[4 * p + e] = v[4 * p + e];
+                }
+            } else if (n + EACH <= a.N) {
+                if (a.type == QNN_F32) {
+                    float *const to = static_cast<float *>(a.y) + m * a.ldy + n;
+                    store_any(to, f32x4{v[0], v[1], v[2], v[3]}), store_any(to + 4, f32x4{v[4], v[5], v[6], v[7]});
+                } else {
+                    const w32x4 h = a.type == QNN_BF16 ? w32x4{narrow2<Bf16>(v[0], v[1]), narrow2<Bf16>(v[2], v[3]), narrow2<Bf16>(v[4], v[5]), narrow2<Bf16>(v[6], v[7])}
+                                                       : w32x4{narrow2<F16>(v[0], v[1]), narrow2<F16>(v[2], v[3]), narrow2<F16>(v[4], v[5]), narrow2<F16>(v[6], v[7])};
+                    store_any(static_cast<uint16_t *>(a.y) + m * a.ldy + n, h);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < EACH; ++e)
+                    if (n + e < a.N) store_out(a.y, m * a.ldy + n + e, a.type, v[e]);
+            }
+        }
+        lds_barrier();
+    }
+}
+
+} // namespace qnn
