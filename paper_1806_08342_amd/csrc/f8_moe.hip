@@ -42,56 +42,88 @@ __device__ __forceinline__ uint32_t logit_key(float v)
 }
 __device__ __forceinline__ float key_logit(uint32_t k) { return __builtin_bit_cast(float, k >> 31 ? k & 0x7fffffffu : ~k); }
 
+// largest and smallest over a wave, the same in all lanes
+__device__ __forceinline__ uint32_t wave_most(uint32_t v)
+{
+    const auto turned = [](uint32_t u, auto ctrl) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)u, decltype(ctrl)::value, 0xf, 0xf, true); };
+    v = max(v, turned(v, std::integral_constant<int, 0x128>())); // row_ror:8 and so on: over 16 lanes
+    v = max(v, turned(v, std::integral_constant<int, 0x124>()));
+    v = max(v, turned(v, std::integral_constant<int, 0x122>()));
+    v = max(v, turned(v, std::integral_constant<int, 0x121>()));
+    const auto of = [&](int l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); };
+    return max(max(of(0), of(16)), max(of(32), of(48)));
+}
+__device__ __forceinline__ float wave_sum(float v)
+{
+    const auto turned = [](float u, auto ctrl) {
+        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, u), decltype(ctrl)::value, 0xf, 0xf, true));
+    };
+    v += turned(v, std::integral_constant<int, 0x128>());
+    v += turned(v, std::integral_constant<int, 0x124>());
+    v += turned(v, std::integral_constant<int, 0x122>());
+    v += turned(v, std::integral_constant<int, 0x121>());
+    const auto of = [&](int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), l)); };
+    return (of(0) + of(16)) + (of(32) + of(48));
+}
+
+// A token's choice by a wave: lane j gets the expert at place j (-1 behind the last), and its weight.
+template <int KEYS> __device__ __forceinline__ void choose(const MoeArgs &a, int t, int &expert, float &weight)
+{
+    const int lane = threadIdx.x & 63;
+    uint32_t key[KEYS];
+#pragma unroll
+    for (int i = 0; i < KEYS; ++i) {
+        const int e = i * 64 + lane;
+        const float v = load_out(a.logits, t * a.ldl + min(e, a.E - 1), a.logit_type);
+        key[i] = e < a.E ? logit_key(v) : 0u;
+    }
+    expert = -1;
+    float mine = 0.0f, sum = 0.0f, top = 0.0f; // (mine: exp of the logit at place `lane`, less the largest)
+    for (int j = 0; j < a.k; ++j) {
+        uint32_t here = 0;
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) here = max(here, key[i]);
+        const uint32_t best = wave_most(here);
+        if (best == 0) break;
+        if (j == 0) {
+            top = key_logit(best);
+            if (!a.renormalize)
+#pragma unroll
+                for (int i = 0; i < KEYS; ++i) sum += key[i] ? expf(key_logit(key[i]) - top) : 0.0f;
+        }
+        uint32_t first = 0; // the lowest index of those: the largest complement
+#pragma unroll
+        for (int i = KEYS - 1; i >= 0; --i)
+            if (key[i] == best) first = ~(uint32_t)(i * 64 + lane);
+        const uint64_t who = __ballot(here == best);
+        const int e = (int)~(__popcll(who) == 1 ? (uint32_t)__builtin_amdgcn_readlane((int)first, __ffsll((unsigned long long)who) - 1) : wave_most(first));
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i)
+            if (i * 64 + lane == e) key[i] = 0;
+        if (lane == j) mine = expf(key_logit(best) - top), expert = e;
+    }
+    const float of = wave_sum(a.renormalize ? mine : sum);
+    weight = expert >= 0 ? mine / of : 0.0f;
+}
+
 // One workgroup: a wave per token and turn; then the list.
-__global__ void __launch_bounds__(1024) moe_route_kernel(const MoeArgs a)
+template <int KEYS> __global__ void __launch_bounds__(1024) moe_route_kernel(const MoeArgs a)
 {
     __shared__ uint64_t s_tokens[kMostExperts]; // who chose an expert
-    __shared__ uint16_t s_place[kTokens][kMostChosen];
+    __shared__ int16_t s_place[kTokens][kMostChosen];
     __shared__ int32_t s_sum[2][16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     s_tokens[tid] = 0;
     __syncthreads();
     for (int t = wave; t < a.T; t += 16) {
-        uint32_t key[kMostExperts / 64];
-#pragma unroll
-        for (int i = 0; i < kMostExperts / 64; ++i) {
-            key[i] = 0;
-            if (i * 64 + lane < a.E) key[i] = logit_key(load_out(a.logits, t * a.ldl + i * 64 + lane, a.logit_type));
-        }
-        float top = 0.0f, sum = 0.0f, mine = 0.0f; // (mine: the logit at place `lane`)
-        int mine_at = -1, got = 0;
-        for (int j = 0; j < a.k; ++j) {
-            uint32_t best = 0, at = 0;
-#pragma unroll
-            for (int i = 0; i < kMostExperts / 64; ++i)
-                if (key[i] > best) best = key[i], at = i * 64 + lane;
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) {
-                const uint32_t other = __shfl_xor(best, d), other_at = __shfl_xor(at, d);
-                if (other > best || (other == best && other_at < at)) best = other, at = other_at;
-            }
-            if (best == 0) break;
-#pragma unroll
-            for (int i = 0; i < kMostExperts / 64; ++i)
-                if (j == 0) sum += key[i] ? expf(key_logit(key[i]) - key_logit(best)) : 0.0f;
-            if (j == 0) top = key_logit(best);
-#pragma unroll
-            for (int i = 0; i < kMostExperts / 64; ++i)
-                if (i * 64 + lane == (int)at) key[i] = 0;
-            if (lane == j) mine = expf(key_logit(best) - top), mine_at = (int)at;
-            if (lane == 0) {
-                s_place[t][j] = (uint16_t)at;
-                atomicOr(reinterpret_cast<unsigned long long *>(&s_tokens[at]), 1ull << t);
-            }
-            got = j + 1;
-        }
-        float of = a.renormalize ? mine : sum;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) of += __shfl_xor(of, d);
+        int expert;
+        float weight;
+        choose<KEYS>(a, t, expert, weight);
         if (lane < a.k) {
-            a.weights[t * a.k + lane] = lane < got ? mine / of : 0.0f;
-            if (a.experts) a.experts[t * a.k + lane] = mine_at;
-            if (lane >= got) s_place[t][lane] = 0xffff;
+            s_place[t][lane] = (int16_t)expert;
+            if (expert >= 0) atomicOr(reinterpret_cast<unsigned long long *>(&s_tokens[expert]), 1ull << t);
+            a.weights[t * a.k + lane] = weight;
+            if (a.experts) a.experts[t * a.k + lane] = expert;
         }
     }
     __syncthreads();
@@ -162,7 +194,10 @@ template <int MT> __global__ void __launch_bounds__(256) moe_up_kernel(const Moe
             const w32x4 x[2] = {piece(x_row[mt], k), piece(x_row[mt], k + 64)};
             const float xs = x_scale[mt][b * a.ldxs];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) fma4(acc[mt][u], f8_products<true>(s.w[u], x), xs * s.ws[u]);
+            for (int u = 0; u < 2; ++u) {
+                fma4(acc[mt][u], f8_products<true>(s.w[u], x), xs * s.ws[u]);
+                asm volatile("" : "+v"(acc[mt][u])); // (before the branch: see the other kernel)
+            }
         }
     };
     Step f[DEPTH];
@@ -198,68 +233,96 @@ template <int MT> __global__ void __launch_bounds__(256) moe_up_kernel(const Moe
 
 // Workgroups: 16 columns of y.  The blocks of 128 of all experts chosen are shared out among the waves, a stretch for each; a wave's sums of an
 // expert go to its own part of LDS, weighted, and the waves' parts are added up at the end.
+// Tiles of 8 tokens: the two parts of their h are the 16 columns of one product.  Weights, and h of the first tile, which another XCD may have written,
+// are requested two or three blocks ahead (with h one block ahead 64 tokens x 64 experts x 4096 x 2048 took 197 us).
 template <int MT> __global__ void __launch_bounds__(512) moe_down_kernel(const MoeArgs a)
 {
-    constexpr int WAVES = 8;
-    __shared__ float s_y[WAVES][16 * MT][17];
+    constexpr int WAVES = 8, DEPTH = MT == 8 ? 3 : 4;
+    __shared__ float s_y[WAVES][8 * MT][17];
     const int n0 = blockIdx.x * 16;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
-    for (int i = lane; i < 16 * MT * 17; i += 64) (&s_y[wave][0][0])[i] = 0.0f;
+    for (int i = lane; i < 8 * MT * 17; i += 64) (&s_y[wave][0][0])[i] = 0.0f;
     const int blocks = (a.I + kF8Block - 1) / kF8Block, row_blocks = (a.H + kF8Block - 1) / kF8Block;
     const int units = a.list[0] * blocks;
     const int first = (int)((int64_t)units * wave / WAVES), last = (int)((int64_t)units * (wave + 1) / WAVES);
     const w32x4 zero = {0u, 0u, 0u, 0u};
+    const uint16_t *const part_of_h = c < 8 ? a.h_high : a.h_low;
+    struct Weights {
+        w32x4 w[2];
+        float scale;
+    };
+    struct Inner {
+        w32x4 h[4];
+    };
     for (int u = first; u < last;) {
-        const int j = u / blocks, end = min(last, (j + 1) * blocks);
+        const int j = u / blocks, b0 = u - j * blocks, b1 = min(last - j * blocks, blocks);
         const int e = moe_chosen(a)[j], begin = moe_begins(a)[j], count = moe_begins(a)[j + 1] - begin;
         const uint8_t *const w_row = a.down + ((int64_t)e * a.H + n0 + c) * a.I;
         const float *const w_scale = a.downs + ((int64_t)e * row_blocks + n0 / kF8Block) * blocks;
         f32x4 acc[MT];
-        int64_t h_row[MT];
         int choice[MT];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            choice[mt] = moe_choices(a)[begin + min(mt * 16 + c, count - 1)];
-            h_row[mt] = (int64_t)choice[mt] * a.I, acc[mt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            choice[mt] = moe_choices(a)[begin + min(mt * 8 + (c & 7), count - 1)];
+            acc[mt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
-        for (int b = u - j * blocks; u < end; ++u, ++b) {
-            const int k = b * kF8Block + 16 * g;
-            w32x4 w[2];
-            const float ws = w_scale[b];
+        const auto load = [&](Weights &f, int b) { // (behind the last: that again, unused)
+            const int at = min(b, b1 - 1), k = at * kF8Block + 16 * g;
 #pragma unroll
-            for (int p = 0; p < 2; ++p) w[p] = k + 64 * p < a.I ? load_any<w32x4>(w_row + k + 64 * p) : zero;
-            f32x4 part[MT];
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) part[mt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int p = 0; p < 2; ++p) f.w[p] = k + 64 * p < a.I ? load_any<w32x4>(w_row + k + 64 * p) : zero;
+            f.scale = w_scale[at];
+        };
+        const auto load_inner = [&](Inner &h, int b, int mt) {
+            const uint16_t *const row = part_of_h + (int64_t)choice[mt] * a.I;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                w32x4 wide;
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const uint32_t s = w[i >> 1][2 * (i & 1) + q];
-                    wide[2 * q] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(s, 1.0f, false));
-                    wide[2 * q + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(s, 1.0f, true));
-                }
-                const int at = k + 64 * (i >> 1) + 8 * (i & 1);
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    if (mt * 16 >= count) break;
-                    w32x4 high = zero, low = zero;
-                    if (mt * 16 + c < count && at < a.I) high = load_any<w32x4>(a.h_high + h_row[mt] + at), low = load_any<w32x4>(a.h_low + h_row[mt] + at);
-                    part[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b16x8, wide), __builtin_bit_cast(b16x8, low), part[mt], 0, 0, 0);
-                    part[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b16x8, wide), __builtin_bit_cast(b16x8, high), part[mt], 0, 0, 0);
-                }
+                const int k = min(b, b1 - 1) * kF8Block + 16 * g + 64 * (i >> 1) + 8 * (i & 1);
+                h.h[i] = mt * 8 + (c & 7) < count && k < a.I ? load_any<w32x4>(row + k) : zero;
             }
+        };
+        const auto compute = [&](const Weights &f, const Inner &ahead, int b) {
+            b16x8 wide[4];
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) fma4(acc[mt], part[mt], ws);
+            for (int i = 0; i < 4; ++i) wide[i] = widen_codes(f.w[i >> 1][2 * (i & 1)], f.w[i >> 1][2 * (i & 1) + 1]);
+            Inner h = ahead;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                if (mt * 8 >= count) break;
+                Inner next;
+                if (mt + 1 < MT && (mt + 1) * 8 < count) load_inner(next, b, mt + 1);
+                f32x4 part = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide[i], __builtin_bit_cast(b16x8, h.h[i]), part, 0, 0, 0);
+                fma4(acc[mt], part, f.scale);
+                // (Here, and not behind the branch: the compiler's waits for the products do not reach over it.)
+                asm volatile("" : "+v"(acc[mt]));
+                h = next;
+            }
+        };
+        Weights f[DEPTH];
+        Inner h[DEPTH];
+#pragma unroll
+        for (int d = 0; d < DEPTH - 1; ++d) load_inner(h[d], b0 + d, 0), load(f[d], b0 + d);
+        for (int b = b0; b < b1; b += DEPTH) {
+#pragma unroll
+            for (int d = 0; d < DEPTH; ++d) {
+                if (b + d >= b1) break;
+                load_inner(h[(d + DEPTH - 1) % DEPTH], b + d + DEPTH - 1, 0);
+                load(f[(d + DEPTH - 1) % DEPTH], b + d + DEPTH - 1);
+                compute(f[d], h[d], b + d);
+            }
         }
+        u = j * blocks + b1;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            if (mt * 16 + c >= count) continue;
+            if (mt * 8 >= count) break;
             const float weight = a.weights[choice[mt]];
             const int t = choice[mt] / a.k;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) s_y[wave][t][g * 4 + r] += weight * acc[mt][r];
+            for (int r = 0; r < 4; ++r) {
+                const float v = acc[mt][r] + __shfl_xor(acc[mt][r], 8);
+                if (c < 8 && mt * 8 + c < count) s_y[wave][t][g * 4 + r] += weight * v;
+            }
         }
     }
     __syncthreads();
@@ -289,11 +352,17 @@ static MoeSpace moe_space(int64_t T, int64_t E, int64_t k, int64_t I)
     return m;
 }
 
-template <int MT> static void launch_moe(const MoeArgs &a, hipStream_t s)
+static void launch_moe(const MoeArgs &a, hipStream_t s)
 {
-    hipLaunchKernelGGL(moe_route_kernel, dim3(1), dim3(1024), 0, s, a);
-    hipLaunchKernelGGL(moe_up_kernel<MT>, dim3((unsigned)(a.most * (a.I / 16))), dim3(256), 0, s, a);
-    hipLaunchKernelGGL(moe_down_kernel<MT>, dim3((unsigned)(a.H / 16)), dim3(512), 0, s, a);
+    if (a.E <= 64) hipLaunchKernelGGL(moe_route_kernel<1>, dim3(1), dim3(1024), 0, s, a);
+    else if (a.E <= 256) hipLaunchKernelGGL(moe_route_kernel<4>, dim3(1), dim3(1024), 0, s, a);
+    else hipLaunchKernelGGL(moe_route_kernel<kMostExperts / 64>, dim3(1), dim3(1024), 0, s, a);
+    const dim3 up((unsigned)(a.most * (a.I / 16))), down((unsigned)(a.H / 16));
+    if (a.T <= 16) hipLaunchKernelGGL(moe_up_kernel<1>, up, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(moe_up_kernel<kTokens / 16>, up, dim3(256), 0, s, a);
+    if (a.T <= 8) hipLaunchKernelGGL(moe_down_kernel<1>, down, dim3(512), 0, s, a);
+    else if (a.T <= 16) hipLaunchKernelGGL(moe_down_kernel<2>, down, dim3(512), 0, s, a);
+    else hipLaunchKernelGGL(moe_down_kernel<kTokens / 8>, down, dim3(512), 0, s, a);
 }
 
 } // namespace qnn
@@ -336,8 +405,7 @@ qnn_status qnn_f8_moe(const uint8_t *x, int64_t ldx, const float *x_scales, int6
         a.logit_type = logit_type, a.type = type, a.renormalize = renormalize;
         a.list = reinterpret_cast<int32_t *>(space + m.list), a.h_high = reinterpret_cast<uint16_t *>(space + m.high);
         a.h_low = reinterpret_cast<uint16_t *>(space + m.low), a.most = (int32_t)m.most;
-        if (n <= 16) launch_moe<1>(a, as_stream(stream));
-        else launch_moe<4>(a, as_stream(stream));
+        launch_moe(a, as_stream(stream));
     }
     return launch_status(hipGetLastError());
 }

@@ -12,13 +12,6 @@ __device__ __forceinline__ f32x16 f8_products32(const i32x8 a, const i32x8 b, co
 {
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);
 }
-__device__ __forceinline__ b16x8 widen_codes(uint32_t low, uint32_t high)
-{
-    return __builtin_bit_cast(b16x8, w32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(low, 1.0f, false)),
-                                           __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(low, 1.0f, true)),
-                                           __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(high, 1.0f, false)),
-                                           __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(high, 1.0f, true))});
-}
 
 struct F8TileArgs {
     F8Args a;          // x, w: rows of whole 16-byte pieces
@@ -191,7 +184,7 @@ template <int BM, int BN, int WM, int WN, bool NARROW, int PER_SIMD> __global__ 
     join(TILES - 1, late);
 
     // Outputs in binary32 through LDS, 32 rows of x by the wave's weights at a time, 16-byte pieces exchanged by the row's number
-    constexpr int WIDE = BN / WN, PIECES = WIDE / 4;
+    constexpr int WIDE = BN / WN;
     static_assert(WAVES * 32 * WIDE * 4 <= RING, "outputs fit the ring");
     wait_vmcnt<0>();
     lds_barrier();
