@@ -461,7 +461,7 @@ const char *qnn_f8_matmul_plan(int64_t M, int64_t N, int64_t K, int type);
  * A token that chooses nothing gets 0.  Products of x as in qnn_f8_matmul for 16 bits; h is held to 16 significant bits, its products with the codes of
  * down are exact; everything else is binary32, y is rounded once.  The result does not depend on the order of workgroups.
  * Reads the weights of the experts chosen, once for every 64 tokens: meant for few of these (for many, group the tokens by expert and call qnn_f8_matmul).
- * x, x_scales: as above, [T][H].  logits: DEVICE [T][ldl] of logit_type (QNN_BF16, QNN_F16 or QNN_F32), ldl >= E.
+ * x, x_scales: as above, [T][H], ldx up to 2^24.  logits: DEVICE [T][ldl] of logit_type (QNN_BF16, QNN_F16 or QNN_F32), ldl >= E.
  * up: DEVICE codes [E][2 I][H], the I rows of gate before those of up; up_scales [E][ceil(2 I / 128)][ceil(H / 128)] (a block of rows may
  * hold rows of both).  down: DEVICE codes [E][H][I], down_scales [E][ceil(H / 128)][ceil(I / 128)].  All contiguous.
  * y: DEVICE, T x H of `type` (QNN_BF16 or QNN_F16), row pitch ldy >= H (written).  experts: DEVICE int32 [T][top_k], the chosen ones, largest logit

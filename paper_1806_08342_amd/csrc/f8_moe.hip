@@ -8,6 +8,7 @@
 //
 // h keeps 16 significant bits, as two bfloat16 that are added up: in one it would cost the result as much as its own rounding.  Down's weights enter as
 // bfloat16 beside it, exactly.
+#include "buffer_ops.h"
 #include "f8.h"
 
 namespace qnn {
@@ -25,13 +26,20 @@ struct MoeArgs {
     int64_t ldx, ldxs, ldl, ldy;
     int32_t T, E, k, H, I, logit_type, type, renormalize;
     // workspace
-    int32_t *list;     // number of experts chosen, then each one's number, then where each one's choices begin (one more), then the choices: t * k + place
-    uint16_t *h_high, *h_low; // [choice][I]
-    int32_t most; // experts that can be chosen
+    int32_t *list;     // number of experts chosen, number of stretches; each expert, and where its choices begin (one more); the stretches; the choices: t * k + place
+    uint16_t *h; // [2][choices][padded]: the two parts, each 64 of a row in the order of inner_place
+    int32_t most, choices, padded; // experts that can be chosen; choices; I as a multiple of 64
 };
-__device__ __forceinline__ int32_t *moe_chosen(const MoeArgs &a) { return a.list + 1; }
-__device__ __forceinline__ int32_t *moe_begins(const MoeArgs &a) { return a.list + 1 + a.most; }
-__device__ __forceinline__ int32_t *moe_choices(const MoeArgs &a) { return a.list + 2 + 2 * a.most; }
+__device__ __forceinline__ int32_t *moe_chosen(const MoeArgs &a) { return a.list + 2; }
+__device__ __forceinline__ int32_t *moe_begins(const MoeArgs &a) { return a.list + 2 + a.most; }
+// up to 16 choices of an expert: the expert, where they begin, how many
+constexpr int kStretch = 16;
+__device__ __forceinline__ int32_t *moe_stretches(const MoeArgs &a) { return a.list + 3 + 2 * a.most; }
+__host__ __device__ __forceinline__ int moe_most_stretches(int most, int choices) { return most + choices / kStretch; }
+__device__ __forceinline__ int32_t *moe_choices(const MoeArgs &a) { return moe_stretches(a) + 3 * moe_most_stretches(a.most, a.choices); }
+
+// Where k of a row of h lies: a lane's pieces of 8 for a product of 32 are 16 apart in k, and four lanes' read 64 bytes of a row at once.
+__device__ __forceinline__ int inner_place(int k) { return (k & ~63) | (k & 8) << 2 | (k & 48) >> 1 | (k & 7); }
 
 // larger key: larger logit; 0: never chosen (NaN and -inf)
 __device__ __forceinline__ uint32_t logit_key(float v)
@@ -111,7 +119,7 @@ template <int KEYS> __global__ void __launch_bounds__(1024) moe_route_kernel(con
 {
     __shared__ uint64_t s_tokens[kMostExperts]; // who chose an expert
     __shared__ int16_t s_place[kTokens][kMostChosen];
-    __shared__ int32_t s_sum[2][16];
+    __shared__ int32_t s_sum[3][16], s_begin[kMostExperts];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     s_tokens[tid] = 0;
     __syncthreads();
@@ -130,27 +138,31 @@ template <int KEYS> __global__ void __launch_bounds__(1024) moe_route_kernel(con
     // thread e: how many experts before it were chosen, and how often
     const uint64_t tokens = s_tokens[tid];
     const int count = __popcll(tokens);
-    int before = count > 0, times = count;
+    const int parts = (count + kStretch - 1) / kStretch;
+    int before = count > 0, times = count, stretch = parts;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
-        const int u = __shfl_up(before, d), v = __shfl_up(times, d);
-        if (lane >= d) before += u, times += v;
+        const int u = __shfl_up(before, d), v = __shfl_up(times, d), w = __shfl_up(stretch, d);
+        if (lane >= d) before += u, times += v, stretch += w;
     }
-    if (lane == 63) s_sum[0][wave] = before, s_sum[1][wave] = times;
+    if (lane == 63) s_sum[0][wave] = before, s_sum[1][wave] = times, s_sum[2][wave] = stretch;
     __syncthreads();
-    for (int w = 0; w < wave; ++w) before += s_sum[0][w], times += s_sum[1][w];
+    for (int w = 0; w < wave; ++w) before += s_sum[0][w], times += s_sum[1][w], stretch += s_sum[2][w];
     int32_t *const begins = moe_begins(a);
-    if (tid == 1023) a.list[0] = before, begins[before] = times;
+    if (tid == 1023) a.list[0] = before, a.list[1] = stretch, begins[before] = times;
+    s_begin[tid] = times - count;
     if (count > 0) {
-        int at = times - count;
         moe_chosen(a)[before - 1] = tid;
-        begins[before - 1] = at;
-        for (int t = 0; t < a.T; ++t) {
-            if (!(tokens >> t & 1)) continue;
-            int j = 0;
-            while (s_place[t][j] != tid) ++j;
-            moe_choices(a)[at++] = t * a.k + j;
+        begins[before - 1] = times - count;
+        for (int i = 0; i < parts; ++i) {
+            int32_t *const to = moe_stretches(a) + 3 * (stretch - parts + i);
+            to[0] = tid, to[1] = times - count + i * kStretch, to[2] = min(count - i * kStretch, kStretch);
         }
+    }
+    __syncthreads();
+    for (int i = tid; i < a.T * a.k; i += 1024) { // each choice behind those of the tokens before
+        const int t = i / a.k, e = s_place[t][i - t * a.k];
+        if (e >= 0) moe_choices(a)[s_begin[e] + __popcll(s_tokens[e] & ((1ull << t) - 1))] = i;
     }
 }
 
@@ -163,14 +175,15 @@ template <int MT> __global__ void __launch_bounds__(256) moe_up_kernel(const Moe
     const int e = moe_chosen(a)[j], begin = moe_begins(a)[j], count = moe_begins(a)[j + 1] - begin;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
     const int blocks = (a.H + kF8Block - 1) / kF8Block, two = (2 * a.I + kF8Block - 1) / kF8Block;
-    const uint8_t *const w_row[2] = {a.up + ((int64_t)e * 2 * a.I + i0 + c) * a.H, a.up + ((int64_t)e * 2 * a.I + a.I + i0 + c) * a.H};
+    const uint8_t *const w_rows[2] = {a.up + ((int64_t)e * 2 * a.I + i0) * a.H, a.up + ((int64_t)e * 2 * a.I + a.I + i0) * a.H};
     const float *const w_scale[2] = {a.ups + ((int64_t)e * two + i0 / kF8Block) * blocks, a.ups + ((int64_t)e * two + (a.I + i0) / kF8Block) * blocks};
-    const uint8_t *x_row[MT];
+    const int x_bytes = (int)(a.T * a.ldx); // (below 2^30)
+    uint32_t x_row[MT];
     const float *x_scale[MT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
         const int t = moe_choices(a)[begin + min(mt * 16 + c, count - 1)] / a.k;
-        x_row[mt] = a.x + t * a.ldx, x_scale[mt] = a.xs + t;
+        x_row[mt] = (uint32_t)(t * a.ldx), x_scale[mt] = a.xs + t;
     }
     f32x4 acc[MT][2];
 #pragma unroll
@@ -179,19 +192,22 @@ template <int MT> __global__ void __launch_bounds__(256) moe_up_kernel(const Moe
         w32x4 w[2][2];
         float ws[2];
     };
-    const w32x4 zero = {0u, 0u, 0u, 0u};
-    const auto piece = [&](const uint8_t *row, int k) { return k < a.H ? load_any<w32x4>(row + k) : zero; }; // (H is a multiple of 16)
+    // (H is a multiple of 16; what is behind a row's end lies beyond the buffers)
+    const auto piece = [&](const uint8_t *rows, int bytes, uint32_t row, int k) { return buffer_load16(rows, bytes, k < a.H ? row + (uint32_t)k : 0x80000000u); };
     const auto load = [&](Step &s, int b) {
         const int k = b * kF8Block + 16 * g;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) s.w[u][0] = piece(w_row[u], k), s.w[u][1] = piece(w_row[u], k + 64), s.ws[u] = w_scale[u][b];
+        for (int u = 0; u < 2; ++u) {
+            s.w[u][0] = piece(w_rows[u], 16 * a.H, (uint32_t)(c * a.H), k), s.w[u][1] = piece(w_rows[u], 16 * a.H, (uint32_t)(c * a.H), k + 64);
+            s.ws[u] = w_scale[u][b];
+        }
     };
     const auto compute = [&](const Step &s, int b) {
         const int k = b * kF8Block + 16 * g;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             if (mt * 16 >= count) break;
-            const w32x4 x[2] = {piece(x_row[mt], k), piece(x_row[mt], k + 64)};
+            const w32x4 x[2] = {piece(a.x, x_bytes, x_row[mt], k), piece(a.x, x_bytes, x_row[mt], k + 64)};
             const float xs = x_scale[mt][b * a.ldxs];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
@@ -225,28 +241,31 @@ template <int MT> __global__ void __launch_bounds__(256) moe_up_kernel(const Moe
         for (int w = 0; w < WAVES; ++w) gate += s_acc[w][0][m][n], up += s_acc[w][1][m][n];
         const float h = gate / (1.0f + expf(-gate)) * up;
         const uint16_t high = Bf16::narrow(h);
-        const int64_t at = (int64_t)moe_choices(a)[begin + m] * a.I + i0 + n;
-        a.h_high[at] = high;
-        a.h_low[at] = Bf16::narrow(h - Bf16::widen(high));
+        const int64_t at = (int64_t)moe_choices(a)[begin + m] * a.padded + inner_place(i0 + n);
+        a.h[at] = high;
+        a.h[(int64_t)a.choices * a.padded + at] = Bf16::narrow(h - Bf16::widen(high));
     }
 }
 
-// Workgroups: 16 columns of y.  The blocks of 128 of all experts chosen are shared out among the waves, a stretch for each; a wave's sums of an
-// expert go to its own part of LDS, weighted, and the waves' parts are added up at the end.
-// Tiles of 8 tokens: the two parts of their h are the 16 columns of one product.  Weights, and h of the first tile, which another XCD may have written,
-// are requested two or three blocks ahead (with h one block ahead 64 tokens x 64 experts x 4096 x 2048 took 197 us).
-template <int MT> __global__ void __launch_bounds__(512) moe_down_kernel(const MoeArgs a)
+// Workgroups: 16 columns of y.  The blocks of 128 of all stretches of choices are shared out among the waves; a wave's sums of a stretch
+// go to its own part of LDS, weighted, and the waves' parts are added up at the end.
+// Tiles of 8 tokens: the two parts of their h are the 16 columns of one product.  Weights are requested two or three blocks ahead, h of the first tile one.
+// (An expert's weights are read again for every 16 of its tokens, but from the caches; sums of all 64 take the registers that 16 waves need: 190 us for down
+// with 64 tokens, 64 experts of 4096 x 2048, with eight waves.)
+template <int MT> __global__ void __launch_bounds__(1024, 4) moe_down_kernel(const MoeArgs a)
 {
-    constexpr int WAVES = 8, DEPTH = MT == 8 ? 3 : 4;
-    __shared__ float s_y[WAVES][8 * MT][17];
+    constexpr int WAVES = 16, DEPTH = MT == 1 ? 4 : 3, TURN = MT == 1 ? 4 : 6;
+    extern __shared__ float s_all[]; // [WAVES][T][16]
     const int n0 = blockIdx.x * 16;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
-    for (int i = lane; i < 8 * MT * 17; i += 64) (&s_y[wave][0][0])[i] = 0.0f;
+    float *const s_y = s_all + wave * a.T * 16;
+    for (int i = lane; i < a.T * 16; i += 64) s_y[i] = 0.0f;
     const int blocks = (a.I + kF8Block - 1) / kF8Block, row_blocks = (a.H + kF8Block - 1) / kF8Block;
-    const int units = a.list[0] * blocks;
+    const int units = a.list[1] * blocks;
     const int first = (int)((int64_t)units * wave / WAVES), last = (int)((int64_t)units * (wave + 1) / WAVES);
-    const w32x4 zero = {0u, 0u, 0u, 0u};
-    const uint16_t *const part_of_h = c < 8 ? a.h_high : a.h_low;
+    // (Loads without branches: what is not there lies beyond the buffers, and the compiler counts the loads that are on their way.)
+    const uint8_t *const inner = reinterpret_cast<const uint8_t *>(a.h);
+    const int inner_bytes = 4 * a.choices * a.padded; // (below 2^30)
     struct Weights {
         w32x4 w[2];
         float scale;
@@ -256,72 +275,83 @@ template <int MT> __global__ void __launch_bounds__(512) moe_down_kernel(const M
     };
     for (int u = first; u < last;) {
         const int j = u / blocks, b0 = u - j * blocks, b1 = min(last - j * blocks, blocks);
-        const int e = moe_chosen(a)[j], begin = moe_begins(a)[j], count = moe_begins(a)[j + 1] - begin;
-        const uint8_t *const w_row = a.down + ((int64_t)e * a.H + n0 + c) * a.I;
+        const int32_t *const stretch = moe_stretches(a) + 3 * j;
+        const int e = stretch[0], begin = stretch[1], count = stretch[2];
+        const uint8_t *const w_rows = a.down + ((int64_t)e * a.H + n0) * a.I;
         const float *const w_scale = a.downs + ((int64_t)e * row_blocks + n0 / kF8Block) * blocks;
         f32x4 acc[MT];
         int choice[MT];
+        uint32_t h_row[MT];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             choice[mt] = moe_choices(a)[begin + min(mt * 8 + (c & 7), count - 1)];
+            h_row[mt] = mt * 8 + (c & 7) < count ? 2u * (uint32_t)(((c >> 3) * a.choices + choice[mt]) * a.padded) : 0x80000000u;
             acc[mt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
-        const auto load = [&](Weights &f, int b) { // (behind the last: that again, unused)
-            const int at = min(b, b1 - 1), k = at * kF8Block + 16 * g;
+        // Each workgroup begins at another block: rows lie a power of two apart more often than not, and workgroups that read the same columns of
+        // all rows at one time would keep to a part of the memory's channels.
+        const int many = b1 - b0, turned = (int)(blockIdx.x % (unsigned)many);
+        const auto block_at = [&](int i) { // (behind the last: that again, unused)
+            const int at = min(i, many - 1) + turned;
+            return b0 + (at < many ? at : at - many);
+        };
+        const auto load = [&](Weights &f, int i) {
+            const int at = block_at(i), k = at * kF8Block + 16 * g;
 #pragma unroll
-            for (int p = 0; p < 2; ++p) f.w[p] = k + 64 * p < a.I ? load_any<w32x4>(w_row + k + 64 * p) : zero;
+            for (int p = 0; p < 2; ++p) f.w[p] = buffer_load16(w_rows, 16 * a.I, k + 64 * p < a.I ? (uint32_t)(c * a.I + k + 64 * p) : 0x80000000u);
             f.scale = w_scale[at];
         };
-        const auto load_inner = [&](Inner &h, int b, int mt) {
-            const uint16_t *const row = part_of_h + (int64_t)choice[mt] * a.I;
+        const auto load_inner = [&](Inner &h, int from, int mt) {
+            const int at = block_at(from);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int k = min(b, b1 - 1) * kF8Block + 16 * g + 64 * (i >> 1) + 8 * (i & 1);
-                h.h[i] = mt * 8 + (c & 7) < count && k < a.I ? load_any<w32x4>(row + k) : zero;
+            for (int p = 0; p < 2; ++p) {
+                const int k = at * kF8Block + 16 * g + 64 * p;
+                const uint32_t to = k < a.I ? h_row[mt] + 2u * (uint32_t)(at * kF8Block + 64 * p + 8 * g) : 0x80000000u; // (inner_place(k + 8 * i) is 32 further for i = 1)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) h.h[2 * p + i] = buffer_load16(inner, inner_bytes, to + 64 * i);
             }
         };
         const auto compute = [&](const Weights &f, const Inner &ahead, int b) {
+            Inner second;
+            const bool two = MT > 1 && count > 8;
+            if (two) load_inner(second, b, MT - 1);
             b16x8 wide[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) wide[i] = widen_codes(f.w[i >> 1][2 * (i & 1)], f.w[i >> 1][2 * (i & 1) + 1]);
-            Inner h = ahead;
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                if (mt * 8 >= count) break;
-                Inner next;
-                if (mt + 1 < MT && (mt + 1) * 8 < count) load_inner(next, b, mt + 1);
+            const auto tile = [&](const Inner &h, f32x4 &sum) {
                 f32x4 part = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide[i], __builtin_bit_cast(b16x8, h.h[i]), part, 0, 0, 0);
-                fma4(acc[mt], part, f.scale);
-                // (Here, and not behind the branch: the compiler's waits for the products do not reach over it.)
-                asm volatile("" : "+v"(acc[mt]));
-                h = next;
-            }
+                fma4(sum, part, f.scale);
+                // (Here, and not behind a branch: the compiler's waits for the products do not reach over it.)
+                asm volatile("" : "+v"(sum));
+            };
+            tile(ahead, acc[0]);
+            if (two) tile(second, acc[MT - 1]);
         };
         Weights f[DEPTH];
-        Inner h[DEPTH];
+        Inner h[2];
+        load_inner(h[0], 0, 0);
 #pragma unroll
-        for (int d = 0; d < DEPTH - 1; ++d) load_inner(h[d], b0 + d, 0), load(f[d], b0 + d);
-        for (int b = b0; b < b1; b += DEPTH) {
+        for (int d = 0; d < DEPTH - 1; ++d) load(f[d], d);
+        for (int b = 0; b < many; b += TURN) {
 #pragma unroll
-            for (int d = 0; d < DEPTH; ++d) {
-                if (b + d >= b1) break;
-                load_inner(h[(d + DEPTH - 1) % DEPTH], b + d + DEPTH - 1, 0);
+            for (int d = 0; d < TURN; ++d) {
+                if (b + d >= many) break;
+                load_inner(h[1 - (d & 1)], b + d + 1, 0);
                 load(f[(d + DEPTH - 1) % DEPTH], b + d + DEPTH - 1);
-                compute(f[d], h[d], b + d);
+                compute(f[d % DEPTH], h[d & 1], b + d);
             }
         }
         u = j * blocks + b1;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            if (mt * 8 >= count) break;
             const float weight = a.weights[choice[mt]];
             const int t = choice[mt] / a.k;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const float v = acc[mt][r] + __shfl_xor(acc[mt][r], 8);
-                if (c < 8 && mt * 8 + c < count) s_y[wave][t][g * 4 + r] += weight * v;
+                if (c < 8 && mt * 8 + c < count) s_y[t * 16 + g * 4 + r] += weight * v;
             }
         }
     }
@@ -330,14 +360,14 @@ template <int MT> __global__ void __launch_bounds__(512) moe_down_kernel(const M
         const int t = i / 16, n = i % 16;
         float v = 0.0f;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) v += s_y[w][t][n];
+        for (int w = 0; w < WAVES; ++w) v += s_all[(w * a.T + t) * 16 + n];
         store_out(a.y, t * a.ldy + n0 + n, a.type, v);
     }
 }
 
 struct MoeSpace {
-    size_t list, weights, high, low, bytes;
-    int64_t most;
+    size_t list, weights, inner, bytes;
+    int64_t most, padded;
 };
 static MoeSpace moe_space(int64_t T, int64_t E, int64_t k, int64_t I)
 {
@@ -345,10 +375,10 @@ static MoeSpace moe_space(int64_t T, int64_t E, int64_t k, int64_t I)
     const auto rounded = [](int64_t n) { return (size_t)((n + 255) / 256 * 256); };
     MoeSpace m;
     m.most = most, m.list = 0;
-    m.weights = rounded(4 * (2 + 2 * most + choices));
-    m.high = m.weights + rounded(4 * choices);
-    m.low = m.high + rounded(2 * choices * I);
-    m.bytes = m.low + rounded(2 * choices * I);
+    m.weights = rounded(4 * (3 + 2 * most + 3 * moe_most_stretches((int)most, (int)choices) + choices));
+    m.inner = m.weights + rounded(4 * choices);
+    m.padded = (I + 63) / 64 * 64;
+    m.bytes = m.inner + rounded(4 * choices * m.padded);
     return m;
 }
 
@@ -360,9 +390,9 @@ static void launch_moe(const MoeArgs &a, hipStream_t s)
     const dim3 up((unsigned)(a.most * (a.I / 16))), down((unsigned)(a.H / 16));
     if (a.T <= 16) hipLaunchKernelGGL(moe_up_kernel<1>, up, dim3(256), 0, s, a);
     else hipLaunchKernelGGL(moe_up_kernel<kTokens / 16>, up, dim3(256), 0, s, a);
-    if (a.T <= 8) hipLaunchKernelGGL(moe_down_kernel<1>, down, dim3(512), 0, s, a);
-    else if (a.T <= 16) hipLaunchKernelGGL(moe_down_kernel<2>, down, dim3(512), 0, s, a);
-    else hipLaunchKernelGGL(moe_down_kernel<kTokens / 8>, down, dim3(512), 0, s, a);
+    const size_t lds = 16 * 16 * 4 * (size_t)a.T; // (64 KB at the most)
+    if (a.T <= 8) hipLaunchKernelGGL(moe_down_kernel<1>, down, dim3(1024), lds, s, a);
+    else hipLaunchKernelGGL(moe_down_kernel<2>, down, dim3(1024), lds, s, a);
 }
 
 } // namespace qnn
@@ -388,7 +418,7 @@ qnn_status qnn_f8_moe(const uint8_t *x, int64_t ldx, const float *x_scales, int6
 {
     if (bad_moe_sizes(T, E, top_k, H, I) || bad_half_type(type) || (bad_half_type(logit_type) && logit_type != QNN_F32)) return QNN_EINVAL;
     if (T == 0) return QNN_OK;
-    if (!x || !x_scales || !logits || !up || !up_scales || !down || !down_scales || !y || ldx < H || ldxs < T || ldl < E || ldy < H) return QNN_EINVAL;
+    if (!x || !x_scales || !logits || !up || !up_scales || !down || !down_scales || !y || ldx < H || ldx > (1 << 24) || ldxs < T || ldl < E || ldy < H) return QNN_EINVAL;
     const MoeSpace m = moe_space(T, E, top_k, I);
     if (!workspace || ((uintptr_t)workspace & 15) != 0 || workspace_bytes < m.bytes) return QNN_EINVAL;
     uint8_t *const space = static_cast<uint8_t *>(workspace);
@@ -403,8 +433,8 @@ qnn_status qnn_f8_moe(const uint8_t *x, int64_t ldx, const float *x_scales, int6
         a.ldx = ldx, a.ldxs = ldxs, a.ldl = ldl, a.ldy = ldy;
         a.T = (int32_t)n, a.E = (int32_t)E, a.k = (int32_t)top_k, a.H = (int32_t)H, a.I = (int32_t)I;
         a.logit_type = logit_type, a.type = type, a.renormalize = renormalize;
-        a.list = reinterpret_cast<int32_t *>(space + m.list), a.h_high = reinterpret_cast<uint16_t *>(space + m.high);
-        a.h_low = reinterpret_cast<uint16_t *>(space + m.low), a.most = (int32_t)m.most;
+        a.list = reinterpret_cast<int32_t *>(space + m.list), a.h = reinterpret_cast<uint16_t *>(space + m.inner);
+        a.most = (int32_t)m.most, a.choices = (int32_t)(n * top_k), a.padded = (int32_t)m.padded;
         launch_moe(a, as_stream(stream));
     }
     return launch_status(hipGetLastError());
