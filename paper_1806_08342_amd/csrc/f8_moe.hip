@@ -10,6 +10,7 @@
 // bfloat16 beside it, exactly.
 #include "buffer_ops.h"
 #include "f8.h"
+#include "lds_ring.h"
 
 namespace qnn {
 
@@ -27,8 +28,8 @@ struct MoeArgs {
     int32_t T, E, k, H, I, logit_type, type, renormalize;
     // workspace
     int32_t *list;     // number of experts chosen, number of stretches; each expert, and where its choices begin (one more); the stretches; the choices: t * k + place
-    uint16_t *h; // [2][choices][padded]: the two parts, each 64 of a row in the order of inner_place
-    int32_t most, choices, padded; // experts that can be chosen; choices; I as a multiple of 64
+    uint16_t *h; // [2][choices][I]: the two parts
+    int32_t most, choices; // experts that can be chosen; choices
 };
 __device__ __forceinline__ int32_t *moe_chosen(const MoeArgs &a) { return a.list + 2; }
 __device__ __forceinline__ int32_t *moe_begins(const MoeArgs &a) { return a.list + 2 + a.most; }
@@ -37,9 +38,6 @@ constexpr int kStretch = 16;
 __device__ __forceinline__ int32_t *moe_stretches(const MoeArgs &a) { return a.list + 3 + 2 * a.most; }
 __host__ __device__ __forceinline__ int moe_most_stretches(int most, int choices) { return most + choices / kStretch; }
 __device__ __forceinline__ int32_t *moe_choices(const MoeArgs &a) { return moe_stretches(a) + 3 * moe_most_stretches(a.most, a.choices); }
-
-// Where k of a row of h lies: a lane's pieces of 8 for a product of 32 are 16 apart in k, and four lanes' read 64 bytes of a row at once.
-__device__ __forceinline__ int inner_place(int k) { return (k & ~63) | (k & 8) << 2 | (k & 48) >> 1 | (k & 7); }
 
 // larger key: larger logit; 0: never chosen (NaN and -inf)
 __device__ __forceinline__ uint32_t logit_key(float v)
@@ -241,117 +239,148 @@ template <int MT> __global__ void __launch_bounds__(256) moe_up_kernel(const Moe
         for (int w = 0; w < WAVES; ++w) gate += s_acc[w][0][m][n], up += s_acc[w][1][m][n];
         const float h = gate / (1.0f + expf(-gate)) * up;
         const uint16_t high = Bf16::narrow(h);
-        const int64_t at = (int64_t)moe_choices(a)[begin + m] * a.padded + inner_place(i0 + n);
+        const int64_t at = (int64_t)moe_choices(a)[begin + m] * a.I + i0 + n;
         a.h[at] = high;
-        a.h[(int64_t)a.choices * a.padded + at] = Bf16::narrow(h - Bf16::widen(high));
+        a.h[(int64_t)a.choices * a.I + at] = Bf16::narrow(h - Bf16::widen(high));
     }
+}
+
+__device__ __forceinline__ uint32_t lds_address(const uint8_t *p)
+{
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t *)p;
+}
+// A lane's two pieces of weights, and its four of h in two halves 2048 bytes apart.  (Written out, with their wait: as loads the compiler would have
+// some of them wait for every copy into LDS that is on its way.)
+__device__ __forceinline__ void read_pieces(uint32_t w0, uint32_t w1, uint32_t h0, uint32_t h1, w32x4 (&w)[2], w32x4 (&h)[4])
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("ds_read_b128 %0, %6\n\t"
+                 "ds_read_b128 %1, %7\n\t"
+                 "ds_read_b128 %2, %8\n\t"
+                 "ds_read_b128 %3, %9\n\t"
+                 "ds_read_b128 %4, %8 offset:2048\n\t"
+                 "ds_read_b128 %5, %9 offset:2048\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(w[0]), "=&v"(w[1]), "=&v"(h[0]), "=&v"(h[1]), "=&v"(h[2]), "=&v"(h[3])
+                 : "v"(w0), "v"(w1), "v"(h0), "v"(h1)
+                 : "memory");
+#else
+    (void)w0, (void)w1, (void)h0, (void)h1, (void)w, (void)h;
+#endif
 }
 
 // Workgroups: 16 columns of y.  The blocks of 128 of all stretches of choices are shared out among the waves; a wave's sums of a stretch
 // go to its own part of LDS, weighted, and the waves' parts are added up at the end.
-// Tiles of 8 tokens: the two parts of their h are the 16 columns of one product.  Weights are requested two or three blocks ahead, h of the first tile one.
-// (An expert's weights are read again for every 16 of its tokens, but from the caches; sums of all 64 take the registers that 16 waves need: 190 us for down
-// with 64 tokens, 64 experts of 4096 x 2048, with eight waves.)
-template <int MT> __global__ void __launch_bounds__(1024, 4) moe_down_kernel(const MoeArgs a)
+// Tiles of 8 tokens: the two parts of their h are the 16 rows of one operand.  Weights and h of the first tile are copied into rings in LDS, each
+// wave's own, three blocks and one ahead: as fragments straight into registers, 64 bytes of a row at a time, the texture path took longer over h
+// than the memory over the weights (64 tokens, 64 experts of 4096 x 2048: 93 us for the weights alone, 172 with h).
+template <int TOKENS> __global__ void __launch_bounds__(512, 2) moe_down_kernel(const MoeArgs a)
 {
-    constexpr int WAVES = 16, DEPTH = MT == 1 ? 4 : 3, TURN = MT == 1 ? 4 : 6;
-    extern __shared__ float s_all[]; // [WAVES][T][16]
+    constexpr int WAVES = 8, MT = TOKENS > 8 ? 2 : 1, W_SLOT = 2048, H_SLOT = 4096, RING = 4 * W_SLOT + 2 * H_SLOT;
+    __shared__ __attribute__((aligned(128))) uint8_t s_ring[WAVES][RING];
+    __shared__ float s_y[WAVES][TOKENS][16];
     const int n0 = blockIdx.x * 16;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
-    float *const s_y = s_all + wave * a.T * 16;
-    for (int i = lane; i < a.T * 16; i += 64) s_y[i] = 0.0f;
+    for (int i = lane; i < TOKENS * 16; i += 64) (&s_y[wave][0][0])[i] = 0.0f;
+    uint8_t *const w_ring = s_ring[wave], *const h_ring = w_ring + 4 * W_SLOT;
     const int blocks = (a.I + kF8Block - 1) / kF8Block, row_blocks = (a.H + kF8Block - 1) / kF8Block;
     const int units = a.list[1] * blocks;
     const int first = (int)((int64_t)units * wave / WAVES), last = (int)((int64_t)units * (wave + 1) / WAVES);
-    // (Loads without branches: what is not there lies beyond the buffers, and the compiler counts the loads that are on their way.)
     const uint8_t *const inner = reinterpret_cast<const uint8_t *>(a.h);
-    const int inner_bytes = 4 * a.choices * a.padded; // (below 2^30)
-    struct Weights {
-        w32x4 w[2];
-        float scale;
-    };
-    struct Inner {
-        w32x4 h[4];
-    };
+    const int inner_bytes = 4 * a.choices * a.I; // (up to 2^30)
+    constexpr uint32_t kBeyond = 0x80000000u;    // of either buffer: zeros, without traffic
+    // 16 rows of 128 bytes, 16-byte pieces exchanged by half the row's number, so that reads of 16 rows meet the 16 places of the 64 banks; a
+    // copy's lanes have 8 rows, from `half` * 8 on
+    const auto piece = [&](int half) { return (lane & 7) ^ (lane >> 4) ^ 4 * half; };
+    const uint32_t w_place = lds_address(w_ring) + c * 128 + (g ^ (c >> 1 & 7)) * 16, h_place = lds_address(h_ring) + c * 128 + (2 * g ^ (c >> 1 & 7)) * 16;
     for (int u = first; u < last;) {
-        const int j = u / blocks, b0 = u - j * blocks, b1 = min(last - j * blocks, blocks);
+        const int j = u / blocks, b0 = u - j * blocks, many = min(last - j * blocks, blocks) - b0;
         const int32_t *const stretch = moe_stretches(a) + 3 * j;
         const int e = stretch[0], begin = stretch[1], count = stretch[2];
         const uint8_t *const w_rows = a.down + ((int64_t)e * a.H + n0) * a.I;
         const float *const w_scale = a.downs + ((int64_t)e * row_blocks + n0 / kF8Block) * blocks;
-        f32x4 acc[MT];
-        int choice[MT];
-        uint32_t h_row[MT];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            choice[mt] = moe_choices(a)[begin + min(mt * 8 + (c & 7), count - 1)];
-            h_row[mt] = mt * 8 + (c & 7) < count ? 2u * (uint32_t)(((c >> 3) * a.choices + choice[mt]) * a.padded) : 0x80000000u;
-            acc[mt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        }
         // Each workgroup begins at another block: rows lie a power of two apart more often than not, and workgroups that read the same columns of
         // all rows at one time would keep to a part of the memory's channels.
-        const int many = b1 - b0, turned = (int)(blockIdx.x % (unsigned)many);
-        const auto block_at = [&](int i) { // (behind the last: that again, unused)
-            const int at = min(i, many - 1) + turned;
-            return b0 + (at < many ? at : at - many);
-        };
-        const auto load = [&](Weights &f, int i) {
-            const int at = block_at(i), k = at * kF8Block + 16 * g;
+        const int turned = (int)(blockIdx.x % (unsigned)many);
+        const auto block_at = [&](int i) { return b0 + (i + turned < many ? i + turned : i + turned - many); };
+        const uint32_t copied = 2u * (uint32_t)(moe_choices(a)[begin + min(lane >> 3, count - 1)] * a.I) | (lane >> 3 < count ? 0u : kBeyond);
+        const uint32_t second = 2u * (uint32_t)(((c >> 3) * a.choices + moe_choices(a)[begin + min(8 + (c & 7), count - 1)]) * a.I) | (8 + (c & 7) < count ? 0u : kBeyond);
+        // (Without branches, so that the compiler's count of what is on its way holds: behind the last block nothing is below the end.)
+        const auto end_of = [&](int i) { return a.I & ((i - many) >> 31); };
+        const auto load = [&](float &scale, int i) {
+            const int b = block_at(min(i, many - 1)), end = end_of(i);
 #pragma unroll
-            for (int p = 0; p < 2; ++p) f.w[p] = buffer_load16(w_rows, 16 * a.I, k + 64 * p < a.I ? (uint32_t)(c * a.I + k + 64 * p) : 0x80000000u);
-            f.scale = w_scale[at];
-        };
-        const auto load_inner = [&](Inner &h, int from, int mt) {
-            const int at = block_at(from);
-#pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                const int k = at * kF8Block + 16 * g + 64 * p;
-                const uint32_t to = k < a.I ? h_row[mt] + 2u * (uint32_t)(at * kF8Block + 64 * p + 8 * g) : 0x80000000u; // (inner_place(k + 8 * i) is 32 further for i = 1)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) h.h[2 * p + i] = buffer_load16(inner, inner_bytes, to + 64 * i);
+            for (int half = 0; half < 2; ++half) {
+                const int k = b * kF8Block + 16 * piece(half);
+                buffer_to_lds16(w_rows, 16 * a.I, (uint32_t)((8 * half + (lane >> 3)) * a.I + k) | (k < end ? 0u : kBeyond), w_ring + (i & 3) * W_SLOT + half * 1024);
             }
+            scale = w_scale[b];
         };
-        const auto compute = [&](const Weights &f, const Inner &ahead, int b) {
-            Inner second;
-            const bool two = MT > 1 && count > 8;
-            if (two) load_inner(second, b, MT - 1);
+        const auto load_inner = [&](int i) {
+            const int b = block_at(min(i, many - 1)), end = end_of(i);
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    const int k = b * kF8Block + 64 * p + 8 * piece(part);
+                    buffer_to_lds16(inner, inner_bytes, (copied + 2u * (uint32_t)(part * a.choices * a.I + k)) | (k < end ? 0u : kBeyond),
+                                    h_ring + (i & 1) * H_SLOT + p * 2048 + part * 1024);
+                }
+        };
+        f32x4 acc[MT];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) acc[mt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        const auto compute = [&](int i, float scale) {
+            w32x4 w[2], v[4];
+            const uint32_t w_at = w_place + (i & 3) * W_SLOT, h_at = h_place + (i & 1) * H_SLOT;
+            read_pieces(w_at, w_at ^ 64, h_at, h_at ^ 16, w, v);
             b16x8 wide[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) wide[i] = widen_codes(f.w[i >> 1][2 * (i & 1)], f.w[i >> 1][2 * (i & 1) + 1]);
-            const auto tile = [&](const Inner &h, f32x4 &sum) {
+            for (int p = 0; p < 2; ++p) wide[2 * p] = widen_codes(w[p][0], w[p][1]), wide[2 * p + 1] = widen_codes(w[p][2], w[p][3]);
+            const auto join = [&](const w32x4 (&v)[4], f32x4 &sum) {
                 f32x4 part = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide[i], __builtin_bit_cast(b16x8, h.h[i]), part, 0, 0, 0);
-                fma4(sum, part, f.scale);
+                for (int q = 0; q < 4; ++q) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide[q], __builtin_bit_cast(b16x8, v[q]), part, 0, 0, 0);
+                fma4(sum, part, scale);
                 // (Here, and not behind a branch: the compiler's waits for the products do not reach over it.)
                 asm volatile("" : "+v"(sum));
             };
-            tile(ahead, acc[0]);
-            if (two) tile(second, acc[MT - 1]);
+            join(v, acc[0]);
+            if (MT > 1 && count > 8) {
+                const int b = block_at(i);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int k = b * kF8Block + 64 * (q >> 1) + 16 * g + 8 * (q & 1);
+                    v[q] = buffer_load16(inner, inner_bytes, (second + 2u * (uint32_t)k) | (k < a.I ? 0u : kBeyond));
+                }
+                join(v, acc[MT - 1]);
+            }
         };
-        Weights f[DEPTH];
-        Inner h[2];
-        load_inner(h[0], 0, 0);
+        float scale[4];
+        wait_vmcnt<0>();
+        load_inner(0);
 #pragma unroll
-        for (int d = 0; d < DEPTH - 1; ++d) load(f[d], d);
-        for (int b = 0; b < many; b += TURN) {
+        for (int d = 0; d < 3; ++d) load(scale[d], d);
+        for (int i = 0; i < many; i += 4) {
 #pragma unroll
-            for (int d = 0; d < TURN; ++d) {
-                if (b + d >= many) break;
-                load_inner(h[1 - (d & 1)], b + d + 1, 0);
-                load(f[(d + DEPTH - 1) % DEPTH], b + d + DEPTH - 1);
-                compute(f[d % DEPTH], h[d & 1], b + d);
+            for (int d = 0; d < 4; ++d) {
+                if (i + d >= many) break;
+                load_inner(i + d + 1);
+                load(scale[(d + 3) & 3], i + d + 3);
+                wait_vmcnt<3 + 4 + 3>(); // but the weights of the two blocks ahead and these
+                compute(i + d, scale[d]);
             }
         }
-        u = j * blocks + b1;
+        u = j * blocks + b0 + many;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            const float weight = a.weights[choice[mt]];
-            const int t = choice[mt] / a.k;
+            const int choice = moe_choices(a)[begin + min(mt * 8 + (c & 7), count - 1)];
+            const float weight = a.weights[choice];
+            const int t = choice / a.k;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const float v = acc[mt][r] + __shfl_xor(acc[mt][r], 8);
-                if (c < 8 && mt * 8 + c < count) s_y[t * 16 + g * 4 + r] += weight * v;
+                if (c < 8 && mt * 8 + c < count) s_y[wave][t][g * 4 + r] += weight * v;
             }
         }
     }
@@ -360,14 +389,14 @@ template <int MT> __global__ void __launch_bounds__(1024, 4) moe_down_kernel(con
         const int t = i / 16, n = i % 16;
         float v = 0.0f;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) v += s_all[(w * a.T + t) * 16 + n];
+        for (int w = 0; w < WAVES; ++w) v += s_y[w][t][n];
         store_out(a.y, t * a.ldy + n0 + n, a.type, v);
     }
 }
 
 struct MoeSpace {
     size_t list, weights, inner, bytes;
-    int64_t most, padded;
+    int64_t most;
 };
 static MoeSpace moe_space(int64_t T, int64_t E, int64_t k, int64_t I)
 {
@@ -377,8 +406,7 @@ static MoeSpace moe_space(int64_t T, int64_t E, int64_t k, int64_t I)
     m.most = most, m.list = 0;
     m.weights = rounded(4 * (3 + 2 * most + 3 * moe_most_stretches((int)most, (int)choices) + choices));
     m.inner = m.weights + rounded(4 * choices);
-    m.padded = (I + 63) / 64 * 64;
-    m.bytes = m.inner + rounded(4 * choices * m.padded);
+    m.bytes = m.inner + rounded(4 * choices * I);
     return m;
 }
 
@@ -390,9 +418,8 @@ static void launch_moe(const MoeArgs &a, hipStream_t s)
     const dim3 up((unsigned)(a.most * (a.I / 16))), down((unsigned)(a.H / 16));
     if (a.T <= 16) hipLaunchKernelGGL(moe_up_kernel<1>, up, dim3(256), 0, s, a);
     else hipLaunchKernelGGL(moe_up_kernel<kTokens / 16>, up, dim3(256), 0, s, a);
-    const size_t lds = 16 * 16 * 4 * (size_t)a.T; // (64 KB at the most)
-    if (a.T <= 8) hipLaunchKernelGGL(moe_down_kernel<1>, down, dim3(1024), lds, s, a);
-    else hipLaunchKernelGGL(moe_down_kernel<2>, down, dim3(1024), lds, s, a);
+    if (a.T <= 8) hipLaunchKernelGGL(moe_down_kernel<8>, down, dim3(512), 0, s, a);
+    else hipLaunchKernelGGL(moe_down_kernel<kTokens>, down, dim3(512), 0, s, a);
 }
 
 } // namespace qnn
@@ -434,7 +461,7 @@ qnn_status qnn_f8_moe(const uint8_t *x, int64_t ldx, const float *x_scales, int6
         a.T = (int32_t)n, a.E = (int32_t)E, a.k = (int32_t)top_k, a.H = (int32_t)H, a.I = (int32_t)I;
         a.logit_type = logit_type, a.type = type, a.renormalize = renormalize;
         a.list = reinterpret_cast<int32_t *>(space + m.list), a.h = reinterpret_cast<uint16_t *>(space + m.inner);
-        a.most = (int32_t)m.most, a.choices = (int32_t)(n * top_k), a.padded = (int32_t)m.padded;
+        a.most = (int32_t)m.most, a.choices = (int32_t)(n * top_k);
         launch_moe(a, as_stream(stream));
     }
     return launch_status(hipGetLastError());
