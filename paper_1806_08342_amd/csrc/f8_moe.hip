@@ -84,7 +84,8 @@ template <int KEYS> __device__ __forceinline__ void choose(const MoeArgs &a, int
         key[i] = e < a.E ? logit_key(v) : 0u;
     }
     expert = -1;
-    float mine = 0.0f, sum = 0.0f, top = 0.0f; // (mine: exp of the logit at place `lane`, less the largest)
+    float sum = 0.0f, top = 0.0f;
+    uint32_t mine = 0; // the key at place `lane`
     for (int j = 0; j < a.k; ++j) {
         uint32_t here = 0;
 #pragma unroll
@@ -106,10 +107,11 @@ template <int KEYS> __device__ __forceinline__ void choose(const MoeArgs &a, int
 #pragma unroll
         for (int i = 0; i < KEYS; ++i)
             if (i * 64 + lane == e) key[i] = 0;
-        if (lane == j) mine = expf(key_logit(best) - top), expert = e;
+        if (lane == j) mine = best, expert = e;
     }
-    const float of = wave_sum(a.renormalize ? mine : sum);
-    weight = expert >= 0 ? mine / of : 0.0f;
+    const float part = expert >= 0 ? expf(key_logit(mine) - top) : 0.0f;
+    const float of = wave_sum(a.renormalize ? part : sum);
+    weight = expert >= 0 ? part / of : 0.0f;
 }
 
 // One workgroup: a wave per token and turn; then the list.
@@ -164,13 +166,83 @@ template <int KEYS> __global__ void __launch_bounds__(1024) moe_route_kernel(con
     }
 }
 
+// Up to 64 choices of up to 8 tokens, listed by every workgroup for itself (experts in the order in which they are first chosen): the choices of
+// expert j, as bits.  The first workgroup writes the lists for what follows.  One launch less: a token's layer 42 -> 37 us.
+constexpr int kFewTokens = 8, kFewChoices = 64;
+template <int KEYS> __device__ __forceinline__ uint64_t moe_route_few(const MoeArgs &a, int j, int &expert)
+{
+    __shared__ int16_t s_expert[kFewChoices];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (threadIdx.x < kFewChoices) s_expert[threadIdx.x] = -1;
+    __syncthreads();
+    for (int t = wave; t < a.T; t += 4) {
+        int e;
+        float weight;
+        choose<KEYS>(a, t, e, weight);
+        if (lane < a.k) {
+            s_expert[t * a.k + lane] = (int16_t)e;
+            if (blockIdx.x == 0) {
+                a.weights[t * a.k + lane] = weight;
+                if (a.experts) a.experts[t * a.k + lane] = e;
+            }
+        }
+    }
+    __syncthreads();
+    const int e = s_expert[lane];
+    uint64_t same = __ballot(e >= 0); // the choices of the same expert
+#pragma unroll
+    for (int bit = 0; bit < 10; ++bit) {
+        const uint64_t set = __ballot(e >> bit & 1);
+        same &= e >> bit & 1 ? set : ~set;
+    }
+    const uint64_t below = (1ull << lane) - 1;
+    const bool first = e >= 0 && (same & below) == 0;
+    const uint64_t firsts = __ballot(first);
+    const int at = __popcll(firsts & below);
+    if (blockIdx.x == 0 && wave == 0) {
+        int before = 0; // choices of the experts before
+        for (uint64_t rest = firsts; rest; rest &= rest - 1) {
+            const int l = __ffsll((unsigned long long)rest) - 1;
+            const uint64_t theirs = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(same >> 32), l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)same, l);
+            if (theirs >> lane & 1) moe_choices(a)[before + __popcll(theirs & below)] = lane;
+            const int count = __popcll(theirs);
+            if (lane < (count + kStretch - 1) / kStretch) {
+                // (of an expert chosen by 8 tokens there is one stretch)
+                int32_t *const to = moe_stretches(a) + 3 * __builtin_amdgcn_readlane(at, l);
+                to[0] = __builtin_amdgcn_readlane(e, l), to[1] = before, to[2] = count;
+            }
+            before += count;
+        }
+        if (lane == 0) a.list[0] = a.list[1] = __popcll(firsts);
+    }
+    const uint64_t who = __ballot(first && at == j);
+    if (who == 0) return 0;
+    const int l = __ffsll((unsigned long long)who) - 1;
+    expert = __builtin_amdgcn_readlane(e, l);
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(same >> 32), l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)same, l);
+}
+
 // Workgroups: an expert by 16 columns of h; four waves share H and join their sums in LDS.
-template <int MT> __global__ void __launch_bounds__(256) moe_up_kernel(const MoeArgs a)
+// KEYS: 0: the lists are there; else the workgroup chooses by itself, from so many times 64 logits.
+template <int MT, int KEYS> __global__ void __launch_bounds__(256) moe_up_kernel(const MoeArgs a)
 {
     constexpr int WAVES = 4, DEPTH = 2;
+    __shared__ int32_t s_choice[KEYS ? kFewTokens : 1];
     const int columns = a.I / 16, j = blockIdx.x / columns, i0 = blockIdx.x % columns * 16;
-    if (j >= a.list[0]) return;
-    const int e = moe_chosen(a)[j], begin = moe_begins(a)[j], count = moe_begins(a)[j + 1] - begin;
+    int e, count;
+    const int32_t *choices = s_choice;
+    if constexpr (KEYS == 0) {
+        if (j >= a.list[0]) return;
+        e = moe_chosen(a)[j];
+        const int begin = moe_begins(a)[j];
+        count = moe_begins(a)[j + 1] - begin, choices = moe_choices(a) + begin;
+    } else {
+        const uint64_t mine = moe_route_few<KEYS>(a, j, e);
+        if (mine == 0) return;
+        count = __popcll(mine);
+        if (threadIdx.x < 64 && (mine >> threadIdx.x & 1)) s_choice[__popcll(mine & ((1ull << threadIdx.x) - 1))] = threadIdx.x;
+        __syncthreads();
+    }
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
     const int blocks = (a.H + kF8Block - 1) / kF8Block, two = (2 * a.I + kF8Block - 1) / kF8Block;
     const uint8_t *const w_rows[2] = {a.up + ((int64_t)e * 2 * a.I + i0) * a.H, a.up + ((int64_t)e * 2 * a.I + a.I + i0) * a.H};
@@ -180,7 +252,7 @@ template <int MT> __global__ void __launch_bounds__(256) moe_up_kernel(const Moe
     const float *x_scale[MT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-        const int t = moe_choices(a)[begin + min(mt * 16 + c, count - 1)] / a.k;
+        const int t = choices[min(mt * 16 + c, count - 1)] / a.k;
         x_row[mt] = (uint32_t)(t * a.ldx), x_scale[mt] = a.xs + t;
     }
     f32x4 acc[MT][2];
@@ -239,7 +311,7 @@ template <int MT> __global__ void __launch_bounds__(256) moe_up_kernel(const Moe
         for (int w = 0; w < WAVES; ++w) gate += s_acc[w][0][m][n], up += s_acc[w][1][m][n];
         const float h = gate / (1.0f + expf(-gate)) * up;
         const uint16_t high = Bf16::narrow(h);
-        const int64_t at = (int64_t)moe_choices(a)[begin + m] * a.I + i0 + n;
+        const int64_t at = (int64_t)choices[m] * a.I + i0 + n;
         a.h[at] = high;
         a.h[(int64_t)a.choices * a.I + at] = Bf16::narrow(h - Bf16::widen(high));
     }
@@ -412,12 +484,17 @@ static MoeSpace moe_space(int64_t T, int64_t E, int64_t k, int64_t I)
 
 static void launch_moe(const MoeArgs &a, hipStream_t s)
 {
-    if (a.E <= 64) hipLaunchKernelGGL(moe_route_kernel<1>, dim3(1), dim3(1024), 0, s, a);
-    else if (a.E <= 256) hipLaunchKernelGGL(moe_route_kernel<4>, dim3(1), dim3(1024), 0, s, a);
-    else hipLaunchKernelGGL(moe_route_kernel<kMostExperts / 64>, dim3(1), dim3(1024), 0, s, a);
     const dim3 up((unsigned)(a.most * (a.I / 16))), down((unsigned)(a.H / 16));
-    if (a.T <= 16) hipLaunchKernelGGL(moe_up_kernel<1>, up, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(moe_up_kernel<kTokens / 16>, up, dim3(256), 0, s, a);
+    if (a.T <= kFewTokens && a.choices <= kFewChoices && a.E <= 256) {
+        if (a.E <= 64) hipLaunchKernelGGL((moe_up_kernel<1, 1>), up, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((moe_up_kernel<1, 4>), up, dim3(256), 0, s, a);
+    } else {
+        if (a.E <= 64) hipLaunchKernelGGL(moe_route_kernel<1>, dim3(1), dim3(1024), 0, s, a);
+        else if (a.E <= 256) hipLaunchKernelGGL(moe_route_kernel<4>, dim3(1), dim3(1024), 0, s, a);
+        else hipLaunchKernelGGL(moe_route_kernel<kMostExperts / 64>, dim3(1), dim3(1024), 0, s, a);
+        if (a.T <= 16) hipLaunchKernelGGL((moe_up_kernel<1, 0>), up, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((moe_up_kernel<kTokens / 16, 0>), up, dim3(256), 0, s, a);
+    }
     if (a.T <= 8) hipLaunchKernelGGL(moe_down_kernel<8>, down, dim3(512), 0, s, a);
     else hipLaunchKernelGGL(moe_down_kernel<kTokens>, down, dim3(512), 0, s, a);
 }
