@@ -1,0 +1,112 @@
+// Products of e4m3 rows and weights with block scales, few rows: both operands straight into registers.
+#pragma once
+
+#include "f8.h"
+
+namespace qnn {
+
+// 16 bytes of a row, zeros behind its end
+__device__ __forceinline__ w32x4 f8_load16(const uint8_t *row, int K, int k) { return k + 16 <= K ? load_any<w32x4>(row + k) : load_end(row, K, k); }
+
+// One wave takes 16 * NT rows of the weights and 16 * MT rows of x, the waves of a workgroup share K in turns of 128 and join their
+// sums in LDS in their order.  The product is formed transposed (weights are the left operand): a lane has one row of x and four consecutive
+// outputs.  The operands of the next DEPTH - 1 blocks are on their way while a wave works on one.
+template <int MT, int NT, int WAVES, int DEPTH, bool NARROW> __global__ void __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : 2) f8_rows_kernel(const F8Args a)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
+    const int n0 = blockIdx.x * 16 * NT, m0 = blockIdx.y * 16 * MT;
+    const int whole = a.K / kF8Block, blocks = (a.K + kF8Block - 1) / kF8Block;
+    f32x4 acc[MT][NT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const uint8_t *w_row[NT], *x_row[MT];
+    const float *x_scale[MT], *const w_scale = a.ws + (int64_t)(n0 / kF8Block) * blocks;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) w_row[nt] = a.w + (int64_t)min(n0 + nt * 16 + c, a.N - 1) * a.K;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        const int m = min(m0 + mt * 16 + c, a.M - 1); // (rows beyond the ends are the last one again, and dropped)
+        x_row[mt] = a.x + m * a.ldx, x_scale[mt] = a.xs + m;
+    }
+    struct Step {
+        w32x4 w[NT][2], x[MT][2];
+        float xs[MT], ws;
+    };
+    const auto load = [&](Step &s, int b) {
+        const int k = b * kF8Block + 16 * g;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) s.w[nt][0] = load_any<w32x4>(w_row[nt] + k), s.w[nt][1] = load_any<w32x4>(w_row[nt] + k + 64);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            s.x[mt][0] = load_any<w32x4>(x_row[mt] + k), s.x[mt][1] = load_any<w32x4>(x_row[mt] + k + 64);
+            s.xs[mt] = x_scale[mt][b * a.ldxs];
+        }
+        s.ws = w_scale[b];
+    };
+    const auto compute = [&](const Step &s) {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                fma4(acc[mt][nt], f8_products<NARROW>(s.w[nt], s.x[mt]), s.xs[mt] * s.ws);
+                asm volatile("" : "+v"(acc[mt][nt])); // (here, and not behind a branch, which the compiler's waits for the products do not reach over)
+            }
+    };
+    const int mine = wave < whole ? (whole - wave + WAVES - 1) / WAVES : 0;
+    // Each workgroup begins at another place of K: rows lie a power of two apart more often than not, and workgroups that
+    // read the same columns of all rows at one time would keep to a part of the memory's channels.
+    const int turned = mine > 0 ? (int)(blockIdx.x % (unsigned)mine) : 0;
+    const auto block_at = [&](int i) { // (behind the last: that again, unused)
+        const int at = min(i, mine - 1) + turned;
+        return wave + WAVES * (at < mine ? at : at - mine);
+    };
+    Step f[DEPTH];
+    if (mine > 0) {
+#pragma unroll
+        for (int d = 0; d < DEPTH - 1; ++d) load(f[d], block_at(d));
+    }
+    if (whole < blocks && wave == whole % WAVES) { // the last, shorter block
+        Step &s = f[DEPTH - 1];
+        const int k = whole * kF8Block + 16 * g;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) s.w[nt][0] = f8_load16(w_row[nt], a.K, k), s.w[nt][1] = f8_load16(w_row[nt], a.K, k + 64);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            s.x[mt][0] = f8_load16(x_row[mt], a.K, k), s.x[mt][1] = f8_load16(x_row[mt], a.K, k + 64);
+            s.xs[mt] = x_scale[mt][whole * a.ldxs];
+        }
+        s.ws = w_scale[whole];
+        compute(s);
+    }
+    int i = 0;
+    for (; i + DEPTH <= mine; i += DEPTH) {
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            load(f[(d + DEPTH - 1) % DEPTH], block_at(i + d + DEPTH - 1));
+            compute(f[d]);
+        }
+    }
+#pragma unroll
+    for (int d = 0; d < DEPTH - 1; ++d)
+        if (i + d < mine) compute(f[d]);
+
+    __shared__ float s_acc[WAVES][16 * MT][16 * NT + 4];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) *reinterpret_cast<f32x4 *>(&s_acc[wave][mt * 16 + c][nt * 16 + g * 4]) = acc[mt][nt];
+    __syncthreads();
+    for (int j = threadIdx.x; j < 16 * MT * 16 * NT; j += 64 * WAVES) {
+        const int m = j / (16 * NT), n = j % (16 * NT);
+        if (m0 + m >= a.M || n0 + n >= a.N) continue;
+        float v = s_acc[0][m][n];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) v += s_acc[w][m][n];
+        if (a.bias) v += load_out(a.bias, n0 + n, a.type);
+        store_out(a.y, (m0 + m) * a.ldy + n0 + n, a.type, v);
+    }
+}
+
+} // namespace qnn

@@ -15,7 +15,6 @@ __device__ __forceinline__ f32x16 f8_products32(const i32x8 a, const i32x8 b, co
 
 struct F8TileArgs {
     F8Args a;          // x, w: rows of whole 16-byte pieces
-    int64_t ldw;
     float *parts;      // sums of parts of K: [splits][M][N], or null
     int32_t m_tiles, n_tiles, splits, band;
     uint32_t per_xcd;  // workgroups
@@ -37,32 +36,33 @@ __device__ __forceinline__ bool f8_tile_of(const F8TileArgs &t, int &tm, int &tn
 // BM rows of x by BN rows of weights; WM x WN waves, each with BM / WM by BN / WN of them, in products of 32 x 32 formed transposed (weights are the
 // left operand), so that a lane's outputs are of one row of x and its scale is one register.  K in steps of 128 through LDS,
 // copied there directly, 16-byte pieces of a row exchanged by half its number, so that reads of 16 rows meet the 16 places of the 64 banks.
-// Copies take longer than a step: they are requested two steps ahead, those of weights into a third buffer, those of x, which the waves read
-// into registers as a step begins, into the buffer of that step behind a second barrier.
-template <int BM, int BN, int WM, int WN, bool NARROW, int PER_SIMD> __global__ void __launch_bounds__(64 * WM * WN, PER_SIMD) f8_tile_kernel(const F8TileArgs t)
+// Copies take longer than a step: those of weights are requested WB - 1 steps ahead, into WB buffers, those of x, which the waves read into
+// registers as a step begins, nearly XB, into XB buffers behind a second barrier, and scales SETS (waits are in the order of requests: one step ahead
+// they are also waits for copies that are needed later; but tiles of 256 x 256 have no registers for two sets).
+template <int BM, int BN, int WM, int WN, int XB, int WB, int SETS, bool NARROW, int PER_SIMD> __global__ void __launch_bounds__(64 * WM * WN, PER_SIMD) f8_tile_kernel(const F8TileArgs t)
 {
     constexpr int WAVES = WM * WN, TJ = BM / WM / 32, TI = BN / WN / 32, X_BYTES = BM * 128, W_BYTES = BN * 128, X_COPIES = BM / 8 / WAVES,
-                  W_COPIES = BN / 8 / WAVES, RING = 2 * X_BYTES + 3 * W_BYTES;
+                  W_COPIES = BN / 8 / WAVES, RING = XB * X_BYTES + WB * W_BYTES;
     static_assert(BN / WN <= 128 && BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0, "a wave's weights lie in one block; whole copies");
     __shared__ __attribute__((aligned(16))) uint8_t s_ring[RING];
-    uint8_t *const s_w = s_ring + 2 * X_BYTES;
+    uint8_t *const s_w = s_ring + XB * X_BYTES;
     const F8Args &a = t.a;
     int tm, tn, part;
     if (!f8_tile_of(t, tm, tn, part)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, g = lane >> 5;
     const int wm = wave % WM, wn = wave / WM, m0 = tm * BM, n0 = tn * BN;
     const int blocks = (a.K + kF8Block - 1) / kF8Block;
-    const int first = (int)((int64_t)blocks * part / t.splits), last = (int)((int64_t)blocks * (part + 1) / t.splits);
+    const int first = blocks * part / t.splits, last = blocks * (part + 1) / t.splits; // (up to 2^17 blocks, few parts)
 
-    const uint8_t *const x_tile = a.x + m0 * a.ldx, *const w_tile = a.w + n0 * t.ldw;
-    const int x_bytes = (int)(min(a.M - m0, BM) * a.ldx), w_bytes = (int)(min(a.N - n0, BN) * t.ldw); // rows beyond the last read as zeros
+    const uint8_t *const x_tile = a.x + m0 * a.ldx, *const w_tile = a.w + (int64_t)n0 * a.K;
+    const int x_bytes = (int)(min(a.M - m0, BM) * a.ldx), w_bytes = (int)(min(a.N - n0, BN) * a.K); // rows beyond the last read as zeros
     // Where a lane's 16 bytes of a block are in the rows that a copy of 8 begins with an even or odd multiple of 8; past the end of this part of K: beyond
     // the descriptors' sizes (which are below 2^31), where reads give zeros.
     const int k_end = min(a.K, last * kF8Block);
-    // (Worked out from the lane's number each time: registers are short.)
+    // (Worked out from the lane's number each time where registers are short.)
     const auto offsets = [&](int b, int row, uint32_t pitch, uint32_t (&at)[2]) {
         int l = lane;
-        asm volatile("" : "+v"(l));
+        if constexpr (SETS == 1) asm volatile("" : "+v"(l));
         const uint32_t begin = (uint32_t)(row + (l >> 3)) * pitch;
 #pragma unroll
         for (int odd = 0; odd < 2; ++odd) {
@@ -79,10 +79,10 @@ template <int BM, int BN, int WM, int WN, bool NARROW, int PER_SIMD> __global__ 
     };
     const auto copy_w = [&](int b, int buffer) {
         uint32_t at[2];
-        offsets(b, wave * W_COPIES * 8, (uint32_t)t.ldw, at);
+        offsets(b, wave * W_COPIES * 8, (uint32_t)a.K, at);
 #pragma unroll
         for (int i = 0; i < W_COPIES; ++i)
-            buffer_to_lds16(w_tile, w_bytes, at[(wave * W_COPIES + i) & 1] + (uint32_t)(i * 8) * (uint32_t)t.ldw, s_w + buffer * W_BYTES + (wave * W_COPIES + i) * 1024);
+            buffer_to_lds16(w_tile, w_bytes, at[(wave * W_COPIES + i) & 1] + (uint32_t)(i * 8) * (uint32_t)a.K, s_w + buffer * W_BYTES + (wave * W_COPIES + i) * 1024);
     };
     const uint32_t x_at = 4u * (uint32_t)(wm * (BM / WM) + c); // (rows beyond the last: scales of 0)
     const float *const w_scale = a.ws + (int64_t)min((n0 + wn * (BN / WN)) / kF8Block, (a.N - 1) / kF8Block) * blocks;
@@ -124,36 +124,44 @@ template <int BM, int BN, int WM, int WN, bool NARROW, int PER_SIMD> __global__ 
     i32x8 x[TJ][2], w[2][2];
     const auto x_rows = [&](int buffer) { return s_ring + buffer * X_BYTES + wm * (BM / WM) * 128; };
     const auto w_rows = [&](int buffer) { return s_w + buffer * W_BYTES + wn * (BN / WN) * 128; };
-    constexpr int SCALES = TJ + 1;
-    Scales now;
-    copy_w(first, 0), copy_x(first, 0);
-    copy_w(first + 1, 1);
-    load_scales(now, first);
-    copy_x(first + 1, 1);
-    wait_vmcnt<W_COPIES + SCALES + X_COPIES>();
-    lds_barrier();
-    copy_w(first + 2, 2);
+    constexpr int STEP = TJ + 1 + X_COPIES + W_COPIES; // requests of a step: behind its first tiles scales and x, before its last tile weights
+    // What is requested after the next step's x, and after its weights, when they are waited for:
+    constexpr int ALLOWED = (XB - 1) * STEP < (WB - 1) * STEP - W_COPIES ? (XB - 1) * STEP : (WB - 1) * STEP - W_COPIES;
+    static_assert(XB >= 2 && XB <= SETS + 1 && WB > XB, "the requests before the first step are those of a step from its second last on");
+    Scales scales[SETS];
+    const auto follow = [](int buffer, int many) { return buffer + 1 == many ? 0 : buffer + 1; };
+#pragma unroll
+    for (int v = -WB; v < 0; ++v) { // as the steps before the first would
+        if (v >= -SETS) load_scales(scales[v & (SETS - 1)], min(first + v + SETS, last - 1));
+        if (v >= -XB) copy_x(first + v + XB, v + XB);
+        if (v == -1) {
+            wait_vmcnt<ALLOWED>();
+            lds_barrier();
+        }
+        copy_w(first + v + WB, v + WB);
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) w[0][h] = fragment(w_rows(0), h), x[0][h] = fragment(x_rows(0), h);
-    int w_buffer = 0;
-    for (int b = first; b < last; ++b) {
-        const int x_buffer = (b - first) & 1, w_next = w_buffer == 2 ? 0 : w_buffer + 1;
+    int w_buffer = 0, x_buffer = 0;
+    const auto step = [&](int b, auto odd) {
+        Scales &now = scales[decltype(odd)::value];
+        const int w_next = follow(w_buffer, WB), x_next = follow(x_buffer, XB);
         float scale[TJ];
 #pragma unroll
         for (int at = 0; at < TILES; ++at) {
             const int i = at / TJ, j = at % TJ;
             if (at == TILES - 1) {
-                // The next step's copies have arrived (those of the one after it, requested after them, may be on their way), and all waves have
-                // this step's weights in registers.
-                wait_vmcnt<W_COPIES + SCALES + X_COPIES>();
+                // The next step's copies have arrived (those requested after them may be on their way), and all waves have this step's weights in
+                // registers.
+                wait_vmcnt<ALLOWED>();
                 lds_barrier();
-                copy_w(b + 3, w_buffer);
+                copy_w(b + WB, w_buffer);
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 if (i == 0 && j + 1 < TJ) x[j + 1][h] = fragment(x_rows(x_buffer) + (j + 1) * 32 * 128, h);
                 if (j == TJ - 1 && i + 1 < TI) w[(i + 1) & 1][h] = fragment(w_rows(w_buffer) + (i + 1) * 32 * 128, h);
-                if (at == TILES - 1) w[0][h] = fragment(w_rows(w_next), h), x[0][h] = fragment(x_rows(1 - x_buffer), h);
+                if (at == TILES - 1) w[0][h] = fragment(w_rows(w_next), h), x[0][h] = fragment(x_rows(x_next), h);
                 if (h == 0)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) p[at & 1][e] = 0.0f;
@@ -175,11 +183,16 @@ template <int BM, int BN, int WM, int WN, bool NARROW, int PER_SIMD> __global__ 
             }
             if (at == TJ - 1) {
                 lds_barrier(); // all waves have this step's x in registers
-                load_scales(now, min(b + 1, last - 1));
-                copy_x(b + 2, x_buffer);
+                load_scales(now, min(b + SETS, last - 1));
+                copy_x(b + XB, x_buffer);
             }
         }
-        late = scale[TJ - 1], w_buffer = w_next;
+        late = scale[TJ - 1], w_buffer = w_next, x_buffer = x_next;
+    };
+    for (int b = first; b < last; b += SETS) {
+        step(b, std::integral_constant<int, 0>());
+        if constexpr (SETS == 2)
+            if (b + 1 < last) step(b + 1, std::integral_constant<int, 1>());
     }
     join(TILES - 1, late);
 

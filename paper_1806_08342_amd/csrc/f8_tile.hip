@@ -38,21 +38,21 @@ __global__ void __launch_bounds__(256) f8_pad_kernel(const F8Args a, uint8_t *x,
     for (int i = threadIdx.x; i < pieces; i += 256) *reinterpret_cast<w32x4 *>(to + i * 16) = load_end(from, a.K, i * 16);
 }
 
-template <int BM, int BN, int WM, int WN, bool NARROW, int PER_SIMD> static void launch_tiles(const F8Args &a, int splits, int64_t ldw, float *parts, hipStream_t s)
+template <int BM, int BN, int WM, int WN, int SETS, bool NARROW> static void launch_tiles(const F8Args &a, int splits, float *parts, hipStream_t s)
 {
     F8TileArgs t{};
-    t.a = a, t.ldw = ldw, t.parts = splits > 1 ? parts : nullptr, t.splits = splits;
+    t.a = a, t.parts = splits > 1 ? parts : nullptr, t.splits = splits;
     t.m_tiles = (a.M + BM - 1) / BM, t.n_tiles = (a.N + BN - 1) / BN;
     t.band = 8;
     t.per_xcd = (uint32_t)(((int64_t)t.m_tiles * t.n_tiles * splits + 7) / 8);
-    hipLaunchKernelGGL((f8_tile_kernel<BM, BN, WM, WN, NARROW, PER_SIMD>), dim3(8 * t.per_xcd), dim3(64 * WM * WN), 0, s, t);
+    hipLaunchKernelGGL((f8_tile_kernel<BM, BN, WM, WN, 2, 3, SETS, NARROW, 2>), dim3(8 * t.per_xcd), dim3(64 * WM * WN), 0, s, t);
 }
 
-void launch_f8_tiles(const F8Args &a, const F8Plan &plan, int64_t ldw, float *parts, hipStream_t s)
+void launch_f8_tiles(const F8Args &a, const F8Plan &plan, float *parts, hipStream_t s)
 {
-    if (a.type == QNN_F32) launch_tiles<128, 128, 2, 2, false, 2>(a, plan.splits, ldw, parts, s);
-    else if (plan.kernel == F8Kernel::Tile256) launch_tiles<256, 256, 4, 2, true, 2>(a, plan.splits, ldw, parts, s);
-    else launch_tiles<128, 128, 2, 2, true, 2>(a, plan.splits, ldw, parts, s);
+    if (a.type == QNN_F32) launch_tiles<128, 128, 2, 2, 1, false>(a, plan.splits, parts, s);
+    else if (plan.kernel == F8Kernel::Tile256) launch_tiles<256, 256, 4, 2, 1, true>(a, plan.splits, parts, s);
+    else launch_tiles<128, 128, 2, 2, 2, true>(a, plan.splits, parts, s);
     if (plan.splits > 1) {
         const int64_t n = (int64_t)a.M * a.N;
         hipLaunchKernelGGL(f8_sum_kernel, dim3((unsigned)((n + 1023) / 1024)), dim3(256), 0, s, a, parts, plan.splits);
