@@ -55,9 +55,14 @@ __device__ __forceinline__ w32x2 encode8(const float (&v)[8], float &scale)
     return codes;
 }
 
-// 8 elements from k on, zeros behind the row's end
-template <class T> __device__ __forceinline__ w32x4 load8(const uint16_t *row, int K, int k)
+// 8 elements from k on, zeros behind the row's end.  WHOLE: K is a multiple of 8, and no branch is needed.
+template <bool WHOLE> __device__ __forceinline__ w32x4 load8(const uint16_t *row, int K, int k)
 {
+    if constexpr (WHOLE) {
+        const w32x4 v = load_any<w32x4>(row + min(k, K - 8));
+        const uint32_t there = k < K ? ~0u : 0u;
+        return v & w32x4{there, there, there, there};
+    }
     return k + 8 <= K ? load_any<w32x4>(row + k) : load_end(reinterpret_cast<const uint8_t *>(row), 2 * K, 2 * k);
 }
 template <class T> __device__ __forceinline__ void widen8(const w32x4 w, float (&v)[8])
@@ -69,9 +74,9 @@ template <class T> __device__ __forceinline__ w32x4 narrow8(const float (&v)[8])
 {
     return w32x4{narrow2<T>(v[0], v[1]), narrow2<T>(v[2], v[3]), narrow2<T>(v[4], v[5]), narrow2<T>(v[6], v[7])};
 }
-__device__ __forceinline__ void store8(uint16_t *row, int K, int k, const w32x4 v)
+template <bool WHOLE> __device__ __forceinline__ void store8(uint16_t *row, int K, int k, const w32x4 v) // k < K
 {
-    if (k + 8 <= K) {
+    if (WHOLE || k + 8 <= K) {
         store_any(row + k, v);
         return;
     }
@@ -79,9 +84,9 @@ __device__ __forceinline__ void store8(uint16_t *row, int K, int k, const w32x4 
     for (int i = 0; i < 7; ++i)
         if (k + i < K) row[k + i] = (uint16_t)(v[i >> 1] >> (i & 1) * 16);
 }
-__device__ __forceinline__ void store_codes(uint8_t *row, int K, int k, const w32x2 c)
+template <bool WHOLE> __device__ __forceinline__ void store_codes(uint8_t *row, int K, int k, const w32x2 c) // k < K
 {
-    if (k + 8 <= K) {
+    if (WHOLE || k + 8 <= K) {
         store_any(row + k, c);
         return;
     }
@@ -102,9 +107,10 @@ struct F8RowArgs {
     int32_t M, K;
     float eps;
     uint32_t blocks, units, groups; // blocks of a row, of all rows; workgroups (or rows) of an XCD
+    uint32_t magic, shift;          // of the division by blocks
 };
 
-template <class T, bool GATED> __global__ void __launch_bounds__(256) f8_quantize_kernel(const F8RowArgs a)
+template <class T, bool GATED, bool WHOLE> __global__ void __launch_bounds__(256) f8_quantize_kernel(const F8RowArgs a)
 {
     constexpr int EACH = 4; // blocks of 16 lanes
     const uint32_t first = of_xcd(blockIdx.x, a.groups) * (16 * EACH) + (threadIdx.x >> 4);
@@ -114,11 +120,11 @@ template <class T, bool GATED> __global__ void __launch_bounds__(256) f8_quantiz
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
         const uint32_t unit = min(first + 16 * i, a.units - 1);
-        row[i] = unit / a.blocks, block[i] = unit % a.blocks;
+        row[i] = a.magic ? __umulhi(unit, a.magic) >> a.shift : unit, block[i] = unit - row[i] * a.blocks;
         const uint16_t *const x = a.x + (int64_t)row[i] * a.ldx;
         const int k = (int)block[i] * kF8Block + lane * 8;
-        in[i][0] = load8<T>(x, a.K, k);
-        if constexpr (GATED) in[i][1] = load8<T>(x + a.K, a.K, k);
+        in[i][0] = load8<WHOLE>(x, a.K, k);
+        if constexpr (GATED) in[i][1] = load8<WHOLE>(x + a.K, a.K, k);
     }
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
@@ -132,29 +138,30 @@ template <class T, bool GATED> __global__ void __launch_bounds__(256) f8_quantiz
             for (int e = 0; e < 8; ++e) v[e] = v[e] / (1.0f + expf(-v[e])) * up[e];
         }
         const w32x2 codes = encode8(v, scale);
-        store_codes(a.codes + (int64_t)row[i] * a.ldc, a.K, (int)block[i] * kF8Block + lane * 8, codes);
+        const int k = (int)block[i] * kF8Block + lane * 8;
+        if (k < a.K) store_codes<WHOLE>(a.codes + (int64_t)row[i] * a.ldc, a.K, k, codes);
         if (lane == 0) a.scales[(int64_t)block[i] * a.lds + row[i]] = scale;
     }
 }
 
-// One row per WAVES waves (4 rows per workgroup of single waves).  CHUNKS: pieces of 8 elements that a lane keeps of a row; 0: rows that do not
-// fit the registers are read a second time.
-template <class T, int WAVES, int CHUNKS> __global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) f8_rmsnorm_kernel(const F8RowArgs a)
+// One row per workgroup of up to 16 waves (4 rows per workgroup where one wave does).  CHUNKS: pieces of 8 elements that a lane keeps of a row; 0: rows
+// that do not fit the registers are read a second time.
+template <class T, int CHUNKS, bool SINGLE, bool WHOLE> __global__ void __launch_bounds__(SINGLE ? 256 : 1024) f8_rmsnorm_kernel(const F8RowArgs a)
 {
-    constexpr int ROWS = WAVES == 1 ? 4 : 1, KEPT = CHUNKS ? CHUNKS : 1, LANES = 64 * WAVES;
-    __shared__ float s_part[2][WAVES];
-    const int tid = threadIdx.x % LANES, wave = tid >> 6;
-    const uint32_t row = of_xcd(blockIdx.x, a.groups) * ROWS + threadIdx.x / LANES;
+    constexpr int ROWS = SINGLE ? 4 : 1, KEPT = CHUNKS ? CHUNKS : 1;
+    __shared__ float s_part[2][16];
+    const int lanes = SINGLE ? 64 : blockDim.x, tid = SINGLE ? threadIdx.x & 63 : threadIdx.x, waves = lanes >> 6;
+    const uint32_t row = of_xcd(blockIdx.x, a.groups) * ROWS + (SINGLE ? threadIdx.x >> 6 : 0);
     if (row >= (uint32_t)a.M) return; // (whole waves, and where waves share a row the whole workgroup)
     const uint16_t *const x = a.x + row * a.ldx;
     const uint16_t *const residual = a.residual ? a.residual + row * a.ldr : nullptr;
     uint16_t *const total = a.total + row * a.ldt;
-    const int turns = CHUNKS ? CHUNKS : (a.K + 8 * LANES - 1) / (8 * LANES);
+    const int turns = CHUNKS ? CHUNKS : (a.K + 8 * lanes - 1) / (8 * lanes);
     w32x4 h[KEPT], r[KEPT];
 
     const auto load = [&](int i, int k) {
-        h[i] = load8<T>(x, a.K, k);
-        if (residual) r[i] = load8<T>(residual, a.K, k);
+        h[i] = load8<WHOLE>(x, a.K, k);
+        if (residual) r[i] = load8<WHOLE>(residual, a.K, k);
     };
     const auto add = [&](int i, int k) {
         if (!residual) return;
@@ -163,7 +170,7 @@ template <class T, int WAVES, int CHUNKS> __global__ void __launch_bounds__(WAVE
 #pragma unroll
         for (int e = 0; e < 8; ++e) u[e] += v[e];
         h[i] = narrow8<T>(u);
-        if (k < a.K) store8(total, a.K, k, h[i]);
+        if (k < a.K) store8<WHOLE>(total, a.K, k, h[i]);
     };
     // over the row
     int turn = 0;
@@ -171,13 +178,12 @@ template <class T, int WAVES, int CHUNKS> __global__ void __launch_bounds__(WAVE
         v = over16(v, f);
         v = f(v, __shfl_xor(v, 16));
         v = f(v, __shfl_xor(v, 32));
-        if constexpr (WAVES > 1) {
+        if constexpr (!SINGLE) {
             turn ^= 1;
-            if ((tid & 63) == 0) s_part[turn][wave] = v;
+            if ((tid & 63) == 0) s_part[turn][tid >> 6] = v;
             __syncthreads();
             v = s_part[turn][0];
-#pragma unroll
-            for (int i = 1; i < WAVES; ++i) v = f(v, s_part[turn][i]);
+            for (int i = 1; i < waves; ++i) v = f(v, s_part[turn][i]);
         }
         return v;
     };
@@ -187,24 +193,24 @@ template <class T, int WAVES, int CHUNKS> __global__ void __launch_bounds__(WAVE
         for (int i = 0; i < (CHUNKS ? CHUNKS : 0); ++i) {
             float v[8];
             widen8<T>(h[i], v);
-            f(v, (i * LANES + tid) * 8);
+            f(v, (i * lanes + tid) * 8);
         }
         if constexpr (CHUNKS == 0)
             for (int i = 0; i < turns; ++i) {
-                const int k = (i * LANES + tid) * 8;
+                const int k = (i * lanes + tid) * 8;
                 float v[8];
-                widen8<T>(load8<T>(residual ? total : x, a.K, k), v);
+                widen8<T>(load8<WHOLE>(residual ? total : x, a.K, k), v);
                 f(v, k);
             }
     };
 
     if constexpr (CHUNKS > 0) {
 #pragma unroll
-        for (int i = 0; i < CHUNKS; ++i) load(i, (i * LANES + tid) * 8);
+        for (int i = 0; i < CHUNKS; ++i) load(i, (i * lanes + tid) * 8);
 #pragma unroll
-        for (int i = 0; i < CHUNKS; ++i) add(i, (i * LANES + tid) * 8);
+        for (int i = 0; i < CHUNKS; ++i) add(i, (i * lanes + tid) * 8);
     } else if (residual) {
-        for (int i = 0; i < turns; ++i) load(0, (i * LANES + tid) * 8), add(0, (i * LANES + tid) * 8);
+        for (int i = 0; i < turns; ++i) load(0, (i * lanes + tid) * 8), add(0, (i * lanes + tid) * 8);
     }
     const auto plus = [](float p, float q) { return p + q; };
     const float per = 1.0f / (float)a.K;
@@ -233,7 +239,7 @@ template <class T, int WAVES, int CHUNKS> __global__ void __launch_bounds__(WAVE
     each([&](float (&v)[8], int k) {
         if (a.weight) {
             float g[8];
-            widen8<T>(load8<T>(a.weight, a.K, k), g);
+            widen8<T>(load8<WHOLE>(a.weight, a.K, k), g);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = v[e] * unit * by * g[e];
         } else {
@@ -243,29 +249,37 @@ template <class T, int WAVES, int CHUNKS> __global__ void __launch_bounds__(WAVE
         float scale;
         const w32x2 codes = encode8(v, scale);
         if (k >= a.K) return;
-        store_codes(a.codes + row * a.ldc, a.K, k, codes);
-        if (a.y) store8(a.y + (int64_t)row * a.K, a.K, k, narrow8<T>(v));
+        store_codes<WHOLE>(a.codes + row * a.ldc, a.K, k, codes);
+        if (a.y) store8<WHOLE>(a.y + (int64_t)row * a.K, a.K, k, narrow8<T>(v));
         if ((threadIdx.x & 15) == 0) a.scales[(int64_t)(k / kF8Block) * a.lds + row] = scale;
     });
 }
 
-template <class T, int WAVES, int CHUNKS> static void launch_rmsnorm(F8RowArgs a, hipStream_t s)
+template <class T, int CHUNKS, bool SINGLE = false> static void launch_rmsnorm(F8RowArgs a, hipStream_t s)
 {
-    const uint32_t rows = WAVES == 1 ? 4 : 1, need = (uint32_t)((a.M + rows - 1) / rows);
+    const uint32_t rows = SINGLE ? 4 : 1, need = (uint32_t)((a.M + rows - 1) / rows);
     a.groups = (need + 7) / 8;
-    hipLaunchKernelGGL((f8_rmsnorm_kernel<T, WAVES, CHUNKS>), dim3(8 * a.groups), dim3(WAVES == 1 ? 256 : 64 * WAVES), 0, s, a);
+    const int each = 512 * (CHUNKS ? CHUNKS : 4), waves = SINGLE ? 4 : CHUNKS ? (a.K + each - 1) / each : 16;
+    if (a.K % 8 == 0) hipLaunchKernelGGL((f8_rmsnorm_kernel<T, CHUNKS, SINGLE, true>), dim3(8 * a.groups), dim3(64 * waves), 0, s, a);
+    else hipLaunchKernelGGL((f8_rmsnorm_kernel<T, CHUNKS, SINGLE, false>), dim3(8 * a.groups), dim3(64 * waves), 0, s, a);
 }
 
+// Few rows: as many waves as they can use, up to 16.  Many: fewer with more each, for fewer waits on the others.
 template <class T> static void run_rmsnorm(const F8RowArgs &a, hipStream_t s)
 {
-    if (a.K <= 512) launch_rmsnorm<T, 1, 1>(a, s);
-    else if (a.K <= 1024) launch_rmsnorm<T, 1, 2>(a, s);
-    else if (a.K <= 2048) launch_rmsnorm<T, 4, 1>(a, s);
-    else if (a.K <= 4096) launch_rmsnorm<T, 4, 2>(a, s);
-    else if (a.K <= 8192) launch_rmsnorm<T, 4, 4>(a, s);
-    else if (a.K <= 16384) launch_rmsnorm<T, 8, 4>(a, s);
-    else if (a.K <= 32768) launch_rmsnorm<T, 16, 4>(a, s);
-    else launch_rmsnorm<T, 16, 0>(a, s);
+    const bool few = a.M <= 512;
+    if (a.K <= 512) launch_rmsnorm<T, 1, true>(a, s);
+    else if (few && a.K <= 8192) launch_rmsnorm<T, 1>(a, s);
+    else if (a.K <= 1024) launch_rmsnorm<T, 2, true>(a, s);
+    else if (a.K <= (few ? 16384 : 6144)) launch_rmsnorm<T, 2>(a, s);
+    else if (a.K <= 32768) launch_rmsnorm<T, 4>(a, s);
+    else launch_rmsnorm<T, 0>(a, s);
+}
+
+template <class T, bool GATED> static void launch_quantize(const F8RowArgs &a, hipStream_t s)
+{
+    if (a.K % 8 == 0) hipLaunchKernelGGL((f8_quantize_kernel<T, GATED, true>), dim3(8 * a.groups), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((f8_quantize_kernel<T, GATED, false>), dim3(8 * a.groups), dim3(256), 0, s, a);
 }
 
 } // namespace qnn
@@ -286,15 +300,10 @@ qnn_status qnn_f8_quantize(const void *x, int64_t ldx, int64_t M, int64_t K, int
     a.x = static_cast<const uint16_t *>(x), a.ldx = ldx, a.codes = codes, a.ldc = ldc, a.scales = scales, a.lds = lds;
     a.M = (int32_t)M, a.K = (int32_t)K, a.blocks = (uint32_t)f8_blocks(K), a.units = (uint32_t)(M * a.blocks);
     a.groups = ((a.units + 63) / 64 + 7) / 8;
-    const dim3 grid(8 * a.groups), block(256);
+    fast_division(a.blocks, a.magic, a.shift);
     hipStream_t s = as_stream(stream);
-    if (type == QNN_BF16) {
-        if (gated) hipLaunchKernelGGL((f8_quantize_kernel<Bf16, true>), grid, block, 0, s, a);
-        else hipLaunchKernelGGL((f8_quantize_kernel<Bf16, false>), grid, block, 0, s, a);
-    } else {
-        if (gated) hipLaunchKernelGGL((f8_quantize_kernel<F16, true>), grid, block, 0, s, a);
-        else hipLaunchKernelGGL((f8_quantize_kernel<F16, false>), grid, block, 0, s, a);
-    }
+    if (type == QNN_BF16) gated ? launch_quantize<Bf16, true>(a, s) : launch_quantize<Bf16, false>(a, s);
+    else gated ? launch_quantize<F16, true>(a, s) : launch_quantize<F16, false>(a, s);
     return launch_status(hipGetLastError());
 }
 
