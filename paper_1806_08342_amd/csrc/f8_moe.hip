@@ -30,6 +30,8 @@ struct MoeArgs {
     int32_t *list;     // number of experts chosen, number of stretches; each expert, and where its choices begin (one more); the stretches; the choices: t * k + place
     uint16_t *h; // [2][choices][I]: the two parts
     int32_t most, choices; // experts that can be chosen; choices
+    float *sums;           // of parts of the blocks, [parts][T][H], or null
+    int32_t parts;
 };
 __device__ __forceinline__ int32_t *moe_chosen(const MoeArgs &a) { return a.list + 2; }
 __device__ __forceinline__ int32_t *moe_begins(const MoeArgs &a) { return a.list + 2 + a.most; }
@@ -351,13 +353,14 @@ template <int TOKENS> __global__ void __launch_bounds__(512, 2) moe_down_kernel(
     constexpr int WAVES = 8, MT = TOKENS > 8 ? 2 : 1, W_SLOT = 2048, H_SLOT = 4096, RING = 4 * W_SLOT + 2 * H_SLOT;
     __shared__ __attribute__((aligned(128))) uint8_t s_ring[WAVES][RING];
     __shared__ float s_y[WAVES][TOKENS][16];
-    const int n0 = blockIdx.x * 16;
+    const int n0 = blockIdx.x * 16, part = blockIdx.y;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
     for (int i = lane; i < TOKENS * 16; i += 64) (&s_y[wave][0][0])[i] = 0.0f;
     uint8_t *const w_ring = s_ring[wave], *const h_ring = w_ring + 4 * W_SLOT;
     const int blocks = (a.I + kF8Block - 1) / kF8Block, row_blocks = (a.H + kF8Block - 1) / kF8Block;
     const int units = a.list[1] * blocks;
-    const int first = (int)((int64_t)units * wave / WAVES), last = (int)((int64_t)units * (wave + 1) / WAVES);
+    const int sharing = WAVES * a.parts, mine = part * WAVES + wave;
+    const int first = (int)((int64_t)units * mine / sharing), last = (int)((int64_t)units * (mine + 1) / sharing);
     const uint8_t *const inner = reinterpret_cast<const uint8_t *>(a.h);
     const int inner_bytes = 4 * a.choices * a.I; // (up to 2^30)
     constexpr uint32_t kBeyond = 0x80000000u;    // of either buffer: zeros, without traffic
@@ -462,15 +465,27 @@ template <int TOKENS> __global__ void __launch_bounds__(512, 2) moe_down_kernel(
         float v = 0.0f;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) v += s_y[w][t][n];
-        store_out(a.y, t * a.ldy + n0 + n, a.type, v);
+        if (a.sums) a.sums[((int64_t)part * a.T + t) * a.H + n0 + n] = v;
+        else store_out(a.y, t * a.ldy + n0 + n, a.type, v);
     }
 }
 
+// y = the parts' sums in their order
+__global__ void __launch_bounds__(256) moe_sum_kernel(const MoeArgs a)
+{
+    const int n = blockIdx.x * 256 + threadIdx.x, t = blockIdx.y;
+    if (n >= a.H) return;
+    float v = 0.0f;
+    for (int p = 0; p < a.parts; ++p) v += a.sums[((int64_t)p * a.T + t) * a.H + n];
+    store_out(a.y, t * a.ldy + n, a.type, v);
+}
+
 struct MoeSpace {
-    size_t list, weights, inner, bytes;
+    size_t list, weights, inner, sums, bytes;
     int64_t most;
+    int parts;
 };
-static MoeSpace moe_space(int64_t T, int64_t E, int64_t k, int64_t I)
+static MoeSpace moe_space(int64_t T, int64_t E, int64_t k, int64_t H, int64_t I)
 {
     const int64_t tokens = T < kTokens ? T : kTokens, choices = tokens * k, most = choices < E ? choices : E;
     const auto rounded = [](int64_t n) { return (size_t)((n + 255) / 256 * 256); };
@@ -478,13 +493,20 @@ static MoeSpace moe_space(int64_t T, int64_t E, int64_t k, int64_t I)
     m.most = most, m.list = 0;
     m.weights = rounded(4 * (3 + 2 * most + 3 * moe_most_stretches((int)most, (int)choices) + choices));
     m.inner = m.weights + rounded(4 * choices);
-    m.bytes = m.inner + rounded(4 * choices * I);
+    m.sums = m.inner + rounded(4 * choices * I);
+    // A workgroup of down has 48 KB on its way, 20 KB/us; where 16 columns each are too few of them for the memory, the blocks are divided too, for a launch
+    // more (4 us).
+    const int64_t groups = H / 16, parts = groups >= 256 ? 1 : (256 + groups - 1) / groups;
+    m.parts = (int)(parts < 8 ? parts : 8);
+    const float us = (float)most * (float)H * (float)I / ((float)groups * 20e3f);
+    if (us * (1.0f - 1.0f / (float)m.parts) < 4.0f) m.parts = 1;
+    m.bytes = m.sums + (m.parts > 1 ? rounded(4 * m.parts * tokens * H) : 0);
     return m;
 }
 
 static void launch_moe(const MoeArgs &a, hipStream_t s)
 {
-    const dim3 up((unsigned)(a.most * (a.I / 16))), down((unsigned)(a.H / 16));
+    const dim3 up((unsigned)(a.most * (a.I / 16))), down((unsigned)(a.H / 16), (unsigned)a.parts);
     if (a.T <= kFewTokens && a.choices <= kFewChoices && a.E <= 256) {
         if (a.E <= 64) hipLaunchKernelGGL((moe_up_kernel<1, 1>), up, dim3(256), 0, s, a);
         else hipLaunchKernelGGL((moe_up_kernel<1, 4>), up, dim3(256), 0, s, a);
@@ -497,6 +519,7 @@ static void launch_moe(const MoeArgs &a, hipStream_t s)
     }
     if (a.T <= 8) hipLaunchKernelGGL(moe_down_kernel<8>, down, dim3(512), 0, s, a);
     else hipLaunchKernelGGL(moe_down_kernel<kTokens>, down, dim3(512), 0, s, a);
+    if (a.sums) hipLaunchKernelGGL(moe_sum_kernel, dim3((unsigned)((a.H + 255) / 256), (unsigned)a.T), dim3(256), 0, s, a);
 }
 
 } // namespace qnn
@@ -513,7 +536,7 @@ static bool bad_moe_sizes(int64_t T, int64_t E, int64_t k, int64_t H, int64_t I)
 
 size_t qnn_f8_moe_workspace_bytes(int64_t T, int64_t E, int64_t top_k, int64_t H, int64_t I)
 {
-    return bad_moe_sizes(T, E, top_k, H, I) || T == 0 ? 0 : moe_space(T, E, top_k, I).bytes;
+    return bad_moe_sizes(T, E, top_k, H, I) || T == 0 ? 0 : moe_space(T, E, top_k, H, I).bytes;
 }
 
 qnn_status qnn_f8_moe(const uint8_t *x, int64_t ldx, const float *x_scales, int64_t ldxs, const void *logits, int64_t ldl, int logit_type, const uint8_t *up,
@@ -523,7 +546,7 @@ qnn_status qnn_f8_moe(const uint8_t *x, int64_t ldx, const float *x_scales, int6
     if (bad_moe_sizes(T, E, top_k, H, I) || bad_half_type(type) || (bad_half_type(logit_type) && logit_type != QNN_F32)) return QNN_EINVAL;
     if (T == 0) return QNN_OK;
     if (!x || !x_scales || !logits || !up || !up_scales || !down || !down_scales || !y || ldx < H || ldx > (1 << 24) || ldxs < T || ldl < E || ldy < H) return QNN_EINVAL;
-    const MoeSpace m = moe_space(T, E, top_k, I);
+    const MoeSpace m = moe_space(T, E, top_k, H, I);
     if (!workspace || ((uintptr_t)workspace & 15) != 0 || workspace_bytes < m.bytes) return QNN_EINVAL;
     uint8_t *const space = static_cast<uint8_t *>(workspace);
     for (int64_t t = 0; t < T; t += kTokens) {
@@ -539,6 +562,7 @@ qnn_status qnn_f8_moe(const uint8_t *x, int64_t ldx, const float *x_scales, int6
         a.logit_type = logit_type, a.type = type, a.renormalize = renormalize;
         a.list = reinterpret_cast<int32_t *>(space + m.list), a.h = reinterpret_cast<uint16_t *>(space + m.inner);
         a.most = (int32_t)m.most, a.choices = (int32_t)(n * top_k);
+        a.parts = m.parts, a.sums = m.parts > 1 ? reinterpret_cast<float *>(space + m.sums) : nullptr;
         launch_moe(a, as_stream(stream));
     }
     return launch_status(hipGetLastError());
