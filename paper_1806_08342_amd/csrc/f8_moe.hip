@@ -35,8 +35,8 @@ struct MoeArgs {
 };
 __device__ __forceinline__ int32_t *moe_chosen(const MoeArgs &a) { return a.list + 2; }
 __device__ __forceinline__ int32_t *moe_begins(const MoeArgs &a) { return a.list + 2 + a.most; }
-// up to 16 choices of an expert: the expert, where they begin, how many
-constexpr int kStretch = 16;
+// up to 8 choices of an expert: the expert, where they begin, how many
+constexpr int kStretch = 8;
 __device__ __forceinline__ int32_t *moe_stretches(const MoeArgs &a) { return a.list + 3 + 2 * a.most; }
 __host__ __device__ __forceinline__ int moe_most_stretches(int most, int choices) { return most + choices / kStretch; }
 __device__ __forceinline__ int32_t *moe_choices(const MoeArgs &a) { return moe_stretches(a) + 3 * moe_most_stretches(a.most, a.choices); }
@@ -345,12 +345,12 @@ __device__ __forceinline__ void read_pieces(uint32_t w0, uint32_t w1, uint32_t h
 
 // Workgroups: 16 columns of y.  The blocks of 128 of all stretches of choices are shared out among the waves; a wave's sums of a stretch
 // go to its own part of LDS, weighted, and the waves' parts are added up at the end.
-// Tiles of 8 tokens: the two parts of their h are the 16 rows of one operand.  Weights and h of the first tile are copied into rings in LDS, each
-// wave's own, three blocks and one ahead: as fragments straight into registers, 64 bytes of a row at a time, the texture path took longer over h
+// The two parts of the h of up to 8 choices are the 16 rows of one operand (an expert's weights are read again, from the caches, for more).  Weights and h
+// are copied into rings in LDS, each wave's own, three blocks and one ahead: as fragments straight into registers, 64 bytes of a row at a time, the texture path took longer over h
 // than the memory over the weights (64 tokens, 64 experts of 4096 x 2048: 93 us for the weights alone, 172 with h).
 template <int TOKENS> __global__ void __launch_bounds__(512, 2) moe_down_kernel(const MoeArgs a)
 {
-    constexpr int WAVES = 8, MT = TOKENS > 8 ? 2 : 1, W_SLOT = 2048, H_SLOT = 4096, RING = 4 * W_SLOT + 2 * H_SLOT;
+    constexpr int WAVES = 8, W_SLOT = 2048, H_SLOT = 4096, RING = 4 * W_SLOT + 2 * H_SLOT;
     __shared__ __attribute__((aligned(128))) uint8_t s_ring[WAVES][RING];
     __shared__ float s_y[WAVES][TOKENS][16];
     const int n0 = blockIdx.x * 16, part = blockIdx.y;
@@ -379,7 +379,6 @@ template <int TOKENS> __global__ void __launch_bounds__(512, 2) moe_down_kernel(
         const int turned = (int)(blockIdx.x % (unsigned)many);
         const auto block_at = [&](int i) { return b0 + (i + turned < many ? i + turned : i + turned - many); };
         const uint32_t copied = 2u * (uint32_t)(moe_choices(a)[begin + min(lane >> 3, count - 1)] * a.I) | (lane >> 3 < count ? 0u : kBeyond);
-        const uint32_t second = 2u * (uint32_t)(((c >> 3) * a.choices + moe_choices(a)[begin + min(8 + (c & 7), count - 1)]) * a.I) | (8 + (c & 7) < count ? 0u : kBeyond);
         // (Without branches, so that the compiler's count of what is on its way holds: behind the last block nothing is below the end.)
         const auto end_of = [&](int i) { return a.I & ((i - many) >> 31); };
         const auto load = [&](float &scale, int i) {
@@ -402,9 +401,7 @@ template <int TOKENS> __global__ void __launch_bounds__(512, 2) moe_down_kernel(
                                     h_ring + (i & 1) * H_SLOT + p * 2048 + part * 1024);
                 }
         };
-        f32x4 acc[MT];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) acc[mt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
         const auto compute = [&](int i, float scale) {
             w32x4 w[2], v[4];
             const uint32_t w_at = w_place + (i & 3) * W_SLOT, h_at = h_place + (i & 1) * H_SLOT;
@@ -412,24 +409,11 @@ template <int TOKENS> __global__ void __launch_bounds__(512, 2) moe_down_kernel(
             b16x8 wide[4];
 #pragma unroll
             for (int p = 0; p < 2; ++p) wide[2 * p] = widen_codes(w[p][0], w[p][1]), wide[2 * p + 1] = widen_codes(w[p][2], w[p][3]);
-            const auto join = [&](const w32x4 (&v)[4], f32x4 &sum) {
-                f32x4 part = {0.0f, 0.0f, 0.0f, 0.0f};
+            f32x4 part = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int q = 0; q < 4; ++q) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide[q], __builtin_bit_cast(b16x8, v[q]), part, 0, 0, 0);
-                fma4(sum, part, scale);
-                // (Here, and not behind a branch: the compiler's waits for the products do not reach over it.)
-                asm volatile("" : "+v"(sum));
-            };
-            join(v, acc[0]);
-            if (MT > 1 && count > 8) {
-                const int b = block_at(i);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int k = b * kF8Block + 64 * (q >> 1) + 16 * g + 8 * (q & 1);
-                    v[q] = buffer_load16(inner, inner_bytes, (second + 2u * (uint32_t)k) | (k < a.I ? 0u : kBeyond));
-                }
-                join(v, acc[MT - 1]);
-            }
+            for (int q = 0; q < 4; ++q) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide[q], __builtin_bit_cast(b16x8, v[q]), part, 0, 0, 0);
+            fma4(acc, part, scale);
+            asm volatile("" : "+v"(acc)); // (here, and not behind a branch, which the compiler's waits for the products do not reach over)
         };
         float scale[4];
         wait_vmcnt<0>();
@@ -447,16 +431,13 @@ template <int TOKENS> __global__ void __launch_bounds__(512, 2) moe_down_kernel(
             }
         }
         u = j * blocks + b0 + many;
+        const int choice = moe_choices(a)[begin + min(c & 7, count - 1)];
+        const float weight = a.weights[choice];
+        const int t = choice / a.k;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            const int choice = moe_choices(a)[begin + min(mt * 8 + (c & 7), count - 1)];
-            const float weight = a.weights[choice];
-            const int t = choice / a.k;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float v = acc[mt][r] + __shfl_xor(acc[mt][r], 8);
-                if (c < 8 && mt * 8 + c < count) s_y[wave][t][g * 4 + r] += weight * v;
-            }
+        for (int r = 0; r < 4; ++r) {
+            const float v = acc[r] + __shfl_xor(acc[r], 8);
+            if (c < 8 && c < count) s_y[wave][t][g * 4 + r] += weight * v;
         }
     }
     __syncthreads();
