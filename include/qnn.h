@@ -424,7 +424,7 @@ size_t qnn_kv_attention_workspace_bytes(const qnn_kv_cache *cache, int32_t q_hea
  *   s = max(a / 448, 2^-80) with a = max|v| over its FINITE v;  code = e4m3(v / s), to nearest, ties to even
  * Infinities become +-448 (a block's largest finite value), a NaN a NaN.
  * x: DEVICE, M x K of `type` (gated: M x 2 K), row pitch ldx elements.  codes: DEVICE [M][ldc], ldc >= K; scales: DEVICE, pitch lds >= M
- * between blocks (both written).  M up to 2^20 (0 is a no-op), K up to 2^24, fewer than 2^31 blocks. */
+ * between blocks (both written).  M up to 2^20 (0 is a no-op), K up to 2^24, fewer than 2^30 blocks. */
 qnn_status qnn_f8_quantize(const void *x, int64_t ldx, int64_t M, int64_t K, int gated, int type, uint8_t *codes, int64_t ldc, float *scales,
                            int64_t lds, void *stream);
 
@@ -463,7 +463,8 @@ const char *qnn_f8_matmul_plan(int64_t M, int64_t N, int64_t K, int type);
  * Reads the weights of the experts chosen, once for every 64 tokens: meant for few of these (for many, group the tokens by expert and call qnn_f8_matmul).
  * x, x_scales: as above, [T][H], ldx up to 2^24.  logits: DEVICE [T][ldl] of logit_type (QNN_BF16, QNN_F16 or QNN_F32), ldl >= E.
  * up: DEVICE codes [E][2 I][H], the I rows of gate before those of up; up_scales [E][ceil(2 I / 128)][ceil(H / 128)] (a block of rows may
- * hold rows of both).  down: DEVICE codes [E][H][I], down_scales [E][ceil(H / 128)][ceil(I / 128)].  All contiguous.
+ * hold rows of both).  down: DEVICE codes [E][H][I], down_scales [E][ceil(H / 128)][ceil(I / 128)].  All contiguous, up and
+ * down 16-byte aligned.
  * y: DEVICE, T x H of `type` (QNN_BF16 or QNN_F16), row pitch ldy >= H (written).  experts: DEVICE int32 [T][top_k], the chosen ones, largest logit
  * first, -1 where there are fewer; weights: DEVICE float [T][top_k], 0 there; either or both NULL.
  * T up to 2^20 (0 is a no-op), E up to 1024, top_k up to 32, H a multiple of 16 up to 2^20, I one up to 2^17.

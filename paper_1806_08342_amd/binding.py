@@ -595,7 +595,7 @@ def f8_matmul(x, x_scales, w, w_scales, bias=None, dtype=None, out=None, workspa
     w_scales[n//128,k//128].  x's rows may be spaced apart.  dtype: bfloat16 (unless given), float16, or float32, whose sums are exact
     to binary32 (at half the matrix rate; with 16-bit results a block's sum has a relative error of about 1e-5); the bias is of that type.
     For inference: tensors that require grad are refused while gradients are recorded."""
-    return (_nat or _native()).f8_matmul(x, x_scales, w, w_scales, bias, BF16 if dtype is None else _float_code(dtype), out, workspace)
+    return (_nat or _native()).f8_matmul(x, x_scales, w, w_scales, bias, dtype, out, workspace)
 
 
 def f8_matmul_plan(M, N, K, dtype=None):
@@ -610,5 +610,4 @@ def f8_moe(x, x_scales, logits, up, up_scales, down, down_scales, top_k, renorma
     weighed by softmax over these (renormalize) or over all logits: y[t] = sum_e weight * down[e] @ (silu(gate[e] @ x) * (up[e] @ x)).
     Returns [T,H] of dtype (bfloat16 unless given, or float16), with_choice: (y, experts int32 [T,top_k], weights float32).
     H and I: multiples of 16.  Reads the chosen experts' weights once for every 64 tokens."""
-    return (_nat or _native()).f8_moe(x, x_scales, logits, up, up_scales, down, down_scales, top_k, renormalize, BF16 if dtype is None else _float_code(dtype),
-                                      with_choice, out, workspace)
+    return (_nat or _native()).f8_moe(x, x_scales, logits, up, up_scales, down, down_scales, top_k, renormalize, dtype, with_choice, out, workspace)

@@ -18,6 +18,7 @@
 #include <c10/hip/HIPStream.h>
 #include <c10/util/Exception.h>
 #include <c10/util/SmallVector.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <ATen/core/grad_mode.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -978,9 +979,13 @@ PyObject *f_f8_rmsnorm(Args a) // x, weight, eps, residual, total, with_y, out
 }
 
 at::ScalarType float_type(int type) { return type == QNN_F32 ? at::kFloat : half_type(type); }
-void want_float_type(int type, bool wide)
+int float_type_of(PyObject *dtype, bool wide) // None: bfloat16
 {
-    if (!bad_type(type) || (wide && type == QNN_F32)) return;
+    if (dtype == Py_None) return QNN_BF16;
+    const at::ScalarType t = THPDtype_Check(dtype) ? reinterpret_cast<THPDtype *>(dtype)->scalar_type : at::kByte;
+    if (t == at::kBFloat16) return QNN_BF16;
+    if (t == at::kHalf) return QNN_F16;
+    if (t == at::kFloat && wide) return QNN_F32;
     PyErr_SetString(PyExc_ValueError, wide ? "dtype must be torch.bfloat16, torch.float16 or torch.float32" : "dtype must be torch.bfloat16 or torch.float16");
     throw PythonErrorSet{};
 }
@@ -993,27 +998,32 @@ int64_t f8_result(Out &y, int type, const at::Tensor &like)
     return f8_pitch(y.t, y.t.size(1), "out");
 }
 
-PyObject *f_f8_matmul(Args a) // x, x_scales, w, w_scales, bias, type, out, workspace
+template <class Query> Workspace f8_workspace(PyObject *o, const at::Tensor &like, Query query)
 {
+    if (o != Py_None) same_device(tensor(o, "workspace"), like, "workspace");
+    return workspace(o, like, true, query);
+}
+
+PyObject *f_f8_matmul(Args a) // x, x_scales, w, w_scales, bias, dtype, out, workspace
+{
+    const int type = float_type_of(a[5], true);
     const at::Tensor &x = tensor(a[0], "x"), &w = tensor(a[2], "w");
     const F8Rows r = f8_rows(x, tensor(a[1], "x_scales"), "x", "x_scales");
     const c10::DeviceGuard guard(x.device());
     if (w.dim() != 2) type_error("w", "a 2-D device tensor of torch.float8_e4m3fn");
     const int64_t M = x.size(0), K = x.size(1), N = w.size(0);
-    const int type = i32(a[5]);
-    want_float_type(type, true);
     const auto *pw = static_cast<const uint8_t *>(param(a[2], at::kFloat8_e4m3fn, "w", {N, K}, x));
     const auto *ps = static_cast<const float *>(param(a[3], at::kFloat, "w_scales", {f8_blocks(N), f8_blocks(K)}, x));
     const void *pb = a[4] == Py_None ? nullptr : param(a[4], float_type(type), "bias", {N}, x);
     Out y = output(a[6], {M, N}, float_type(type), x);
     const int64_t ldy = f8_result(y, type, x);
     void *const py = y.t.data_ptr();
-    const Workspace ws = workspace(a[7], x, true, [&] { return qnn_f8_matmul_workspace_bytes(M, N, K, type); });
+    const Workspace ws = f8_workspace(a[7], x, [&] { return qnn_f8_matmul_workspace_bytes(M, N, K, type); });
     call("qnn_f8_matmul", [&](void *s) { return qnn_f8_matmul(r.codes, r.ldc, r.scales, r.lds, pw, ps, pb, M, N, K, type, py, ldy, ws.p, ws.bytes, s); });
     return y.release();
 }
 
-PyObject *f_f8_moe(Args a) // x, x_scales, logits, up, up_scales, down, down_scales, top_k, renormalize, type, with_choice, out, workspace
+PyObject *f_f8_moe(Args a) // x, x_scales, logits, up, up_scales, down, down_scales, top_k, renormalize, dtype, with_choice, out, workspace
 {
     const at::Tensor &x = tensor(a[0], "x"), &logits = tensor(a[2], "logits"), &up = tensor(a[3], "up");
     const F8Rows r = f8_rows(x, tensor(a[1], "x_scales"), "x", "x_scales");
@@ -1033,8 +1043,7 @@ PyObject *f_f8_moe(Args a) // x, x_scales, logits, up, up_scales, down, down_sca
     const auto *us = static_cast<const float *>(param(a[4], at::kFloat, "up_scales", {E, f8_blocks(2 * I), f8_blocks(H)}, x));
     const auto *pd = static_cast<const uint8_t *>(param(a[5], at::kFloat8_e4m3fn, "down", {E, H, I}, x));
     const auto *ds = static_cast<const float *>(param(a[6], at::kFloat, "down_scales", {E, f8_blocks(H), f8_blocks(I)}, x));
-    const int renormalize = truth(a[8]), type = i32(a[9]), with_choice = truth(a[10]);
-    want_float_type(type, false);
+    const int renormalize = truth(a[8]), type = float_type_of(a[9], false), with_choice = truth(a[10]);
     if (k <= 0 || k > E) {
         PyErr_SetString(PyExc_ValueError, "top_k must lie between 1 and the number of experts");
         throw PythonErrorSet{};
@@ -1046,7 +1055,7 @@ PyObject *f_f8_moe(Args a) // x, x_scales, logits, up, up_scales, down, down_sca
     if (with_choice) experts = fresh({T, k}, at::kInt, x), weights = fresh({T, k}, at::kFloat, x);
     auto *const pe = with_choice ? static_cast<int32_t *>(experts.data_ptr()) : nullptr;
     auto *const pw = with_choice ? static_cast<float *>(weights.data_ptr()) : nullptr;
-    const Workspace ws = workspace(a[12], x, true, [&] { return qnn_f8_moe_workspace_bytes(T, E, k, H, I); });
+    const Workspace ws = f8_workspace(a[12], x, [&] { return qnn_f8_moe_workspace_bytes(T, E, k, H, I); });
     call("qnn_f8_moe", [&](void *s) {
         return qnn_f8_moe(r.codes, r.ldc, r.scales, r.lds, pl, ldl, logit_type, pu, us, pd, ds, T, E, k, H, I, renormalize, type, py, ldy, pe, pw,
                           ws.p, ws.bytes, s);

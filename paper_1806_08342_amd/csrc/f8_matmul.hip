@@ -43,7 +43,7 @@ F8Plan f8_plan(int64_t M, int64_t N, int64_t K, int type)
     const bool wide = type == QNN_F32;
     const int64_t turns = (M + 63) / 64, tiles_of_16 = M < 64 ? (M + 15) / 16 : 4;
     best.us = (float)turns * (weights * (0.17f + (float)tiles_of_16 * (wide_rows(M, N) ? 0.061f : 0.13f)) * (wide ? 1.3f : 1.0f)) + 3.5f;
-    if (K > (1 << 20) || M * N >= (int64_t)1 << 40) return best;
+    if (K > (1 << 20) || M * N >= (int64_t)1 << 37) return best; // (beyond the tiles' offsets, and 2^32 threads)
     const bool padded = K % 16 != 0; // (loads from rows at any byte take twice as long)
     const float before = padded ? 3.0f + (weights + (float)M * (float)K * 1e-6f) * 0.45f : 0.0f;
     const float us64 = 4.4f + before + (float)((turns * ((N + 63) / 64) + 255) / 256) * steps * 0.475f;

@@ -315,7 +315,7 @@ template <int MT, int KEYS> __global__ void __launch_bounds__(256) moe_up_kernel
         const uint16_t high = Bf16::narrow(h);
         const int64_t at = (int64_t)choices[m] * a.I + i0 + n;
         a.h[at] = high;
-        a.h[(int64_t)a.choices * a.I + at] = Bf16::narrow(h - Bf16::widen(high));
+        a.h[(int64_t)a.choices * a.I + at] = fabsf(h) < INFINITY ? Bf16::narrow(h - Bf16::widen(high)) : 0; // (of an infinity the first part is all)
     }
 }
 
@@ -527,6 +527,7 @@ qnn_status qnn_f8_moe(const uint8_t *x, int64_t ldx, const float *x_scales, int6
     if (bad_moe_sizes(T, E, top_k, H, I) || bad_half_type(type) || (bad_half_type(logit_type) && logit_type != QNN_F32)) return QNN_EINVAL;
     if (T == 0) return QNN_OK;
     if (!x || !x_scales || !logits || !up || !up_scales || !down || !down_scales || !y || ldx < H || ldx > (1 << 24) || ldxs < T || ldl < E || ldy < H) return QNN_EINVAL;
+    if (((uintptr_t)up | (uintptr_t)down) % 16 != 0) return QNN_EINVAL;
     const MoeSpace m = moe_space(T, E, top_k, H, I);
     if (!workspace || ((uintptr_t)workspace & 15) != 0 || workspace_bytes < m.bytes) return QNN_EINVAL;
     uint8_t *const space = static_cast<uint8_t *>(workspace);

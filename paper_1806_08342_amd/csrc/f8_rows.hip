@@ -288,7 +288,7 @@ using namespace qnn;
 
 extern "C" {
 
-static bool bad_row_sizes(int64_t M, int64_t K) { return M < 0 || K <= 0 || M > (1 << 20) || K > (1 << 24) || M * f8_blocks(K) >= (int64_t)1 << 31; }
+static bool bad_row_sizes(int64_t M, int64_t K) { return M < 0 || K <= 0 || M > (1 << 20) || K > (1 << 24) || M * f8_blocks(K) >= (int64_t)1 << 30; }
 
 qnn_status qnn_f8_quantize(const void *x, int64_t ldx, int64_t M, int64_t K, int gated, int type, uint8_t *codes, int64_t ldc, float *scales,
                            int64_t lds, void *stream)

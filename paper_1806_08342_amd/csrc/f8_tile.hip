@@ -30,12 +30,12 @@ __global__ void __launch_bounds__(256) f8_sum_kernel(const F8Args a, const float
 }
 
 // rows of x and then of w as rows of whole 16-byte pieces, zeros behind their ends
-__global__ void __launch_bounds__(256) f8_pad_kernel(const F8Args a, uint8_t *x, uint8_t *w, int pieces)
+__global__ void __launch_bounds__(128) f8_pad_kernel(const F8Args a, uint8_t *x, uint8_t *w, int pieces)
 {
     const int row = blockIdx.x;
     const uint8_t *const from = row < a.M ? a.x + row * a.ldx : a.w + (int64_t)(row - a.M) * a.K;
     uint8_t *const to = row < a.M ? x + (int64_t)row * pieces * 16 : w + (int64_t)(row - a.M) * pieces * 16;
-    for (int i = threadIdx.x; i < pieces; i += 256) *reinterpret_cast<w32x4 *>(to + i * 16) = load_end(from, a.K, i * 16);
+    for (int i = threadIdx.x; i < pieces; i += 128) *reinterpret_cast<w32x4 *>(to + i * 16) = load_end(from, a.K, i * 16);
 }
 
 template <int BM, int BN, int WM, int WN, int SETS, bool NARROW> static void launch_tiles(const F8Args &a, int splits, float *parts, hipStream_t s)
@@ -61,7 +61,8 @@ void launch_f8_tiles(const F8Args &a, const F8Plan &plan, float *parts, hipStrea
 
 void launch_f8_pad(const F8Args &a, uint8_t *x, uint8_t *w, hipStream_t s)
 {
-    hipLaunchKernelGGL(f8_pad_kernel, dim3((unsigned)(a.M + a.N)), dim3(256), 0, s, a, x, w, (int)(f8_padded(a.K) / 16));
+    hipLaunchKernelGGL(f8_pad_kernel, dim3((unsigned)(a.M + a.N)), dim3(128), 0, s, a, x, w, // (128 lanes: fewer than 2^32 threads)
+                       (int)(f8_padded(a.K) / 16));
 }
 
 } // namespace qnn

@@ -61,7 +61,7 @@ def test_bad_layers_of_experts_are_refused_before_anything_is_launched(lib):
                                 ("k", 2), ("H", 128), ("I", 64), ("renorm", 1), ("type", 0), ("y", P), ("ldy", 128), ("experts", NULL), ("weights", NULL), ("space", P), ("bytes", 1 << 30),
                                 ("s", None)])
     for bad in (dict(T=-1), dict(T=1 << 21), dict(E=0), dict(E=1025, ldl=2000), dict(k=0), dict(k=9), dict(k=33, E=64, ldl=64), dict(H=0), dict(H=120), dict(I=0), dict(I=40), dict(I=1 << 18),
-                dict(type=2), dict(lt=3), dict(lt=-1), dict(ldx=127), dict(ldxs=3), dict(ldl=7), dict(ldy=127), dict(space=NULL), dict(space=C.c_void_p(4100)), dict(bytes=100),
+                dict(type=2), dict(lt=3), dict(lt=-1), dict(ldx=127), dict(ldxs=3), dict(ldl=7), dict(ldy=127), dict(space=NULL), dict(space=C.c_void_p(4100)), dict(bytes=100), dict(up=C.c_void_p(4104)), dict(down=C.c_void_p(4097)), dict(ldx=(1 << 24) + 1),
                 *(dict([(n, NULL)]) for n in ("x", "xs", "logits", "up", "ups", "down", "downs", "y"))):
         assert f(**bad) == EINVAL, bad
     assert f(T=0, x=NULL, space=NULL, bytes=0) == 0
