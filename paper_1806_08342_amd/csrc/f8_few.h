@@ -34,18 +34,29 @@ template <int MT, int NT, int WAVES, int DEPTH, bool NARROW> __global__ void __l
         w32x4 w[NT][2], x[MT][2];
         float xs[MT], ws;
     };
+    uint32_t w_first[NT], x_first[MT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) w_first[nt] = 64 * half_first((uint32_t)(uintptr_t)w_row[nt], c);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) x_first[mt] = 64 * half_first((uint32_t)(uintptr_t)x_row[mt], c);
     const auto load = [&](Step &s, int b) {
         const int k = b * kF8Block + 16 * g;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) s.w[nt][0] = load_any<w32x4>(w_row[nt] + k), s.w[nt][1] = load_any<w32x4>(w_row[nt] + k + 64);
+        for (int nt = 0; nt < NT; ++nt) s.w[nt][0] = load_any<w32x4>(w_row[nt] + (k + w_first[nt])), s.w[nt][1] = load_any<w32x4>(w_row[nt] + (k + (w_first[nt] ^ 64)));
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            s.x[mt][0] = load_any<w32x4>(x_row[mt] + k), s.x[mt][1] = load_any<w32x4>(x_row[mt] + k + 64);
+            s.x[mt][0] = load_any<w32x4>(x_row[mt] + (k + x_first[mt])), s.x[mt][1] = load_any<w32x4>(x_row[mt] + (k + (x_first[mt] ^ 64)));
             s.xs[mt] = x_scale[mt][b * a.ldxs];
         }
         s.ws = w_scale[b];
     };
-    const auto compute = [&](const Step &s) {
+    const auto compute = [&](const Step &t) {
+        Step s;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) in_order(t.w[nt], w_first[nt], s.w[nt]);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) in_order(t.x[mt], x_first[mt], s.x[mt]), s.xs[mt] = t.xs[mt];
+        s.ws = t.ws;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -71,10 +82,10 @@ template <int MT, int NT, int WAVES, int DEPTH, bool NARROW> __global__ void __l
         Step &s = f[DEPTH - 1];
         const int k = whole * kF8Block + 16 * g;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) s.w[nt][0] = f8_load16(w_row[nt], a.K, k), s.w[nt][1] = f8_load16(w_row[nt], a.K, k + 64);
+        for (int nt = 0; nt < NT; ++nt) s.w[nt][0] = f8_load16(w_row[nt], a.K, k + (int)w_first[nt]), s.w[nt][1] = f8_load16(w_row[nt], a.K, k + (int)(w_first[nt] ^ 64));
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            s.x[mt][0] = f8_load16(x_row[mt], a.K, k), s.x[mt][1] = f8_load16(x_row[mt], a.K, k + 64);
+            s.x[mt][0] = f8_load16(x_row[mt], a.K, k + (int)x_first[mt]), s.x[mt][1] = f8_load16(x_row[mt], a.K, k + (int)(x_first[mt] ^ 64));
             s.xs[mt] = x_scale[mt][whole * a.ldxs];
         }
         s.ws = w_scale[whole];

@@ -2,8 +2,9 @@
 //
 //   y[t] = sum_e weight[t][e] * down[e] (silu(gate[e] x[t]) * (up[e] x[t]))
 //
-// Bound by reading the weights of the experts that some token chose, each once.  Three launches for up to 64 tokens: the choice, as a list of the experts
-// chosen with their tokens; gate and up, whose product h of each choice goes to the workspace; down, which gathers a token's experts.  No atomics on
+// Bound by reading the weights of the experts that some token chose, each once.  Three launches for up to 64 tokens: the choice;
+// gate and up, whose product h of each choice goes to the workspace, and beside them the list of the experts chosen with their tokens; down, which gathers
+// a token's experts.  No atomics on
 // memory: an output is the sum of its experts in the order of their numbers and of parts of K, whatever the order of workgroups.
 //
 // h keeps 16 significant bits, as two bfloat16 that are added up: in one it would cost the result as much as its own rounding.  Down's weights enter as
@@ -27,19 +28,26 @@ struct MoeArgs {
     int64_t ldx, ldxs, ldl, ldy;
     int32_t T, E, k, H, I, logit_type, type, renormalize;
     // workspace
-    int32_t *list;     // number of experts chosen, number of stretches; each expert, and where its choices begin (one more); the stretches; the choices: t * k + place
+    int32_t *chosen;   // [T][k]: a choice's expert, or -1
+    uint64_t *bits;    // [T][words]: the experts that a token chose
+    uint8_t *places;   // [T][E]: where among its choices, of those
+    int32_t *list;     // how many stretches there are, then the stretches: heads (expert, how many), their choices (t * k + place) and their weights
     uint16_t *h; // [2][choices][I]: the two parts
     int32_t most, choices; // experts that can be chosen; choices
     float *sums;           // of parts of the blocks, [parts][T][H], or null
     int32_t parts;
 };
-__device__ __forceinline__ int32_t *moe_chosen(const MoeArgs &a) { return a.list + 2; }
-__device__ __forceinline__ int32_t *moe_begins(const MoeArgs &a) { return a.list + 2 + a.most; }
-// up to 8 choices of an expert: the expert, where they begin, how many
+// A stretch is up to 8 choices of one expert.
 constexpr int kStretch = 8;
-__device__ __forceinline__ int32_t *moe_stretches(const MoeArgs &a) { return a.list + 3 + 2 * a.most; }
 __host__ __device__ __forceinline__ int moe_most_stretches(int most, int choices) { return most + choices / kStretch; }
-__device__ __forceinline__ int32_t *moe_choices(const MoeArgs &a) { return moe_stretches(a) + 3 * moe_most_stretches(a.most, a.choices); }
+struct MoeHead {
+    int32_t expert, count;
+};
+__device__ __forceinline__ MoeHead *moe_heads(const MoeArgs &a) { return reinterpret_cast<MoeHead *>(a.list + 2); }
+__device__ __forceinline__ int32_t *moe_choices(const MoeArgs &a) { return a.list + 2 + 2 * moe_most_stretches(a.most, a.choices); }
+__device__ __forceinline__ float *moe_shares(const MoeArgs &a) { return reinterpret_cast<float *>(a.list + 2 + 10 * moe_most_stretches(a.most, a.choices)); }
+
+__host__ __device__ __forceinline__ int moe_words(int E) { return (E + 63) / 64; }
 
 // larger key: larger logit; 0: never chosen (NaN and -inf)
 __device__ __forceinline__ uint32_t logit_key(float v)
@@ -116,56 +124,93 @@ template <int KEYS> __device__ __forceinline__ void choose(const MoeArgs &a, int
     weight = expert >= 0 ? part / of : 0.0f;
 }
 
-// One workgroup: a wave per token and turn; then the list.
-template <int KEYS> __global__ void __launch_bounds__(1024) moe_route_kernel(const MoeArgs a)
+// One wave per token.  (One workgroup for all of them, which made the lists too, took 7 us for 63 tokens and 4 experts, 14 for 64 of which each chose 8.)
+template <int KEYS> __global__ void __launch_bounds__(64) moe_choose_kernel(const MoeArgs a)
 {
-    __shared__ uint64_t s_tokens[kMostExperts]; // who chose an expert
-    __shared__ int16_t s_place[kTokens][kMostChosen];
-    __shared__ int32_t s_sum[3][16], s_begin[kMostExperts];
+    const int t = blockIdx.x, lane = threadIdx.x;
+    int expert;
+    float weight;
+    choose<KEYS>(a, t, expert, weight);
+    if (lane < a.k) {
+        a.chosen[t * a.k + lane] = expert;
+        a.weights[t * a.k + lane] = weight;
+        if (a.experts) a.experts[t * a.k + lane] = expert;
+        if (expert >= 0) a.places[t * a.E + expert] = (uint8_t)lane;
+    }
+    // (all k of a wave's lanes, one after the other, into the word that lane w has)
+    uint64_t word = 0;
+    for (int j = 0; j < a.k; ++j) {
+        const int e = __builtin_amdgcn_readlane(expert, j);
+        if (e >= 0 && e / 64 == lane) word |= 1ull << (e & 63);
+    }
+    if (lane < moe_words(a.E)) a.bits[t * moe_words(a.E) + lane] = word;
+}
+
+// The stretches of all choices, experts in their order and an expert's tokens in theirs: by one workgroup of 256.
+constexpr int kListBytes = kMostExperts * (8 + 4) + 16;
+__device__ __forceinline__ void moe_list(const MoeArgs &a, uint8_t *shared)
+{
+    uint64_t *const s_tokens = reinterpret_cast<uint64_t *>(shared);             // who chose an expert
+    int32_t *const s_at = reinterpret_cast<int32_t *>(shared + kMostExperts * 8); // an expert's first stretch
+    int32_t *const s_sum = s_at + kMostExperts;
+    constexpr int EACH = kMostExperts / 256;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    s_tokens[tid] = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) s_tokens[tid + 256 * i] = 0;
     __syncthreads();
-    for (int t = wave; t < a.T; t += 16) {
-        int expert;
-        float weight;
-        choose<KEYS>(a, t, expert, weight);
-        if (lane < a.k) {
-            s_place[t][lane] = (int16_t)expert;
-            if (expert >= 0) atomicOr(reinterpret_cast<unsigned long long *>(&s_tokens[expert]), 1ull << t);
-            a.weights[t * a.k + lane] = weight;
-            if (a.experts) a.experts[t * a.k + lane] = expert;
-        }
+    for (int i = tid; i < a.choices; i += 256) {
+        const int e = a.chosen[i];
+        if (e >= 0) atomicOr(reinterpret_cast<unsigned long long *>(&s_tokens[e]), 1ull << i / a.k);
     }
     __syncthreads();
-    // thread e: how many experts before it were chosen, and how often
-    const uint64_t tokens = s_tokens[tid];
-    const int count = __popcll(tokens);
-    const int parts = (count + kStretch - 1) / kStretch;
-    int before = count > 0, times = count, stretch = parts;
+    int parts[EACH], before = 0; // (of the experts before this thread's, then)
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) parts[i] = (__popcll(s_tokens[EACH * tid + i]) + kStretch - 1) / kStretch, before += parts[i];
+    const int own = before;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
-        const int u = __shfl_up(before, d), v = __shfl_up(times, d), w = __shfl_up(stretch, d);
-        if (lane >= d) before += u, times += v, stretch += w;
+        const int u = __shfl_up(before, d);
+        if (lane >= d) before += u;
     }
-    if (lane == 63) s_sum[0][wave] = before, s_sum[1][wave] = times, s_sum[2][wave] = stretch;
+    if (lane == 63) s_sum[wave] = before;
     __syncthreads();
-    for (int w = 0; w < wave; ++w) before += s_sum[0][w], times += s_sum[1][w], stretch += s_sum[2][w];
-    int32_t *const begins = moe_begins(a);
-    if (tid == 1023) a.list[0] = before, a.list[1] = stretch, begins[before] = times;
-    s_begin[tid] = times - count;
-    if (count > 0) {
-        moe_chosen(a)[before - 1] = tid;
-        begins[before - 1] = times - count;
-        for (int i = 0; i < parts; ++i) {
-            int32_t *const to = moe_stretches(a) + 3 * (stretch - parts + i);
-            to[0] = tid, to[1] = times - count + i * kStretch, to[2] = min(count - i * kStretch, kStretch);
-        }
+    for (int w = 0; w < wave; ++w) before += s_sum[w];
+    if (tid == 255) a.list[0] = before;
+    before -= own;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int e = EACH * tid + i, count = __popcll(s_tokens[e]);
+        s_at[e] = before;
+        for (int j = 0; j < parts[i]; ++j) moe_heads(a)[before + j] = MoeHead{e, min(count - j * kStretch, kStretch)};
+        before += parts[i];
     }
     __syncthreads();
-    for (int i = tid; i < a.T * a.k; i += 1024) { // each choice behind those of the tokens before
-        const int t = i / a.k, e = s_place[t][i - t * a.k];
-        if (e >= 0) moe_choices(a)[s_begin[e] + __popcll(s_tokens[e] & ((1ull << t) - 1))] = i;
+    for (int i = tid; i < a.choices; i += 256) {
+        const int e = a.chosen[i];
+        if (e < 0) continue;
+        const int at = s_at[e] * kStretch + __popcll(s_tokens[e] & ((1ull << i / a.k) - 1));
+        moe_choices(a)[at] = i, moe_shares(a)[at] = a.weights[i];
     }
+}
+
+constexpr int kSums = 20; // 16 sums of up, and what is between them
+// Choices of the expert that group j of the workgroups has, in the order of their tokens, and how many (0: none).  Where there are
+// no more experts than choices that is expert j, else the one of choice j, if none before chose it.
+// (Found in the list of all choices, with two barriers more, 64 tokens that choose 8 of 64 experts took 75 us for what is 67 so.)
+__device__ __forceinline__ int moe_choices_of(const MoeArgs &a, int j, int &expert, int32_t *s_choice)
+{
+    const int lane = threadIdx.x & 63, t = min(lane, a.T - 1), e = a.E <= a.choices ? j : a.chosen[j];
+    if (e < 0) return 0;
+    const uint64_t word = a.bits[t * moe_words(a.E) + e / 64];
+    const int choice = t * a.k + a.places[t * a.E + e];
+    const bool own = lane < a.T && (word >> (e & 63) & 1);
+    const uint64_t who = __ballot(own);
+    if (who == 0) return 0;
+    if (a.E > a.choices && __builtin_amdgcn_readlane(choice, __ffsll((unsigned long long)who) - 1) != j) return 0;
+    if (threadIdx.x < 64 && own) s_choice[kSums * __popcll(who & ((1ull << lane) - 1))] = choice;
+    __syncthreads();
+    expert = __builtin_amdgcn_readfirstlane(e);
+    return __popcll(who);
 }
 
 // Up to 64 choices of up to 8 tokens, listed by every workgroup for itself (experts in the order in which they are first chosen): the choices of
@@ -174,6 +219,7 @@ constexpr int kFewTokens = 8, kFewChoices = 64;
 template <int KEYS> __device__ __forceinline__ uint64_t moe_route_few(const MoeArgs &a, int j, int &expert)
 {
     __shared__ int16_t s_expert[kFewChoices];
+    __shared__ float s_share[kFewChoices];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (threadIdx.x < kFewChoices) s_expert[threadIdx.x] = -1;
     __syncthreads();
@@ -182,7 +228,7 @@ template <int KEYS> __device__ __forceinline__ uint64_t moe_route_few(const MoeA
         float weight;
         choose<KEYS>(a, t, e, weight);
         if (lane < a.k) {
-            s_expert[t * a.k + lane] = (int16_t)e;
+            s_expert[t * a.k + lane] = (int16_t)e, s_share[t * a.k + lane] = weight;
             if (blockIdx.x == 0) {
                 a.weights[t * a.k + lane] = weight;
                 if (a.experts) a.experts[t * a.k + lane] = e;
@@ -202,20 +248,13 @@ template <int KEYS> __device__ __forceinline__ uint64_t moe_route_few(const MoeA
     const uint64_t firsts = __ballot(first);
     const int at = __popcll(firsts & below);
     if (blockIdx.x == 0 && wave == 0) {
-        int before = 0; // choices of the experts before
-        for (uint64_t rest = firsts; rest; rest &= rest - 1) {
-            const int l = __ffsll((unsigned long long)rest) - 1;
-            const uint64_t theirs = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(same >> 32), l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)same, l);
-            if (theirs >> lane & 1) moe_choices(a)[before + __popcll(theirs & below)] = lane;
-            const int count = __popcll(theirs);
-            if (lane < (count + kStretch - 1) / kStretch) {
-                // (of an expert chosen by 8 tokens there is one stretch)
-                int32_t *const to = moe_stretches(a) + 3 * __builtin_amdgcn_readlane(at, l);
-                to[0] = __builtin_amdgcn_readlane(e, l), to[1] = before, to[2] = count;
-            }
-            before += count;
+        const int stretch = __shfl(at, same ? __ffsll((unsigned long long)same) - 1 : 0); // (of an expert chosen by up to 8 tokens there is one)
+        if (e >= 0) {
+            const int to = stretch * kStretch + __popcll(same & below);
+            moe_choices(a)[to] = lane, moe_shares(a)[to] = s_share[lane];
         }
-        if (lane == 0) a.list[0] = a.list[1] = __popcll(firsts);
+        if (first) moe_heads(a)[at] = MoeHead{e, (int)__popcll(same)};
+        if (lane == 0) a.list[0] = __popcll(firsts);
     }
     const uint64_t who = __ballot(first && at == j);
     if (who == 0) return 0;
@@ -225,24 +264,27 @@ template <int KEYS> __device__ __forceinline__ uint64_t moe_route_few(const MoeA
 }
 
 // Workgroups: an expert by 16 columns of h; four waves share H and join their sums in LDS.
-// KEYS: 0: the lists are there; else the workgroup chooses by itself, from so many times 64 logits.
+// KEYS: 0: the choices are there, and the last workgroup lists them for what follows; else each workgroup chooses by itself, from so many times
+// 64 logits.
 template <int MT, int KEYS> __global__ void __launch_bounds__(256) moe_up_kernel(const MoeArgs a)
 {
-    constexpr int WAVES = 4, DEPTH = 2;
-    __shared__ int32_t s_choice[KEYS ? kFewTokens : 1];
+    constexpr int WAVES = 4, DEPTH = 2, SUMS = WAVES * 2 * 16 * MT * kSums * 4;
+    __shared__ __attribute__((aligned(16))) uint8_t shared[KEYS == 0 && SUMS < kListBytes ? kListBytes : SUMS];
+    int32_t *const choices = reinterpret_cast<int32_t *>(shared) + 16; // each behind 16 sums (in 40 KB, of which a CU holds four)
     const int columns = a.I / 16, j = blockIdx.x / columns, i0 = blockIdx.x % columns * 16;
     int e, count;
-    const int32_t *choices = s_choice;
     if constexpr (KEYS == 0) {
-        if (j >= a.list[0]) return;
-        e = moe_chosen(a)[j];
-        const int begin = moe_begins(a)[j];
-        count = moe_begins(a)[j + 1] - begin, choices = moe_choices(a) + begin;
+        if (j == a.most) {
+            moe_list(a, shared);
+            return;
+        }
+        count = moe_choices_of(a, j, e, choices);
+        if (count == 0) return;
     } else {
         const uint64_t mine = moe_route_few<KEYS>(a, j, e);
         if (mine == 0) return;
         count = __popcll(mine);
-        if (threadIdx.x < 64 && (mine >> threadIdx.x & 1)) s_choice[__popcll(mine & ((1ull << threadIdx.x) - 1))] = threadIdx.x;
+        if (threadIdx.x < 64 && (mine >> threadIdx.x & 1)) choices[kSums * __popcll(mine & ((1ull << threadIdx.x) - 1))] = threadIdx.x;
         __syncthreads();
     }
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
@@ -254,7 +296,7 @@ template <int MT, int KEYS> __global__ void __launch_bounds__(256) moe_up_kernel
     const float *x_scale[MT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-        const int t = choices[min(mt * 16 + c, count - 1)] / a.k;
+        const int t = choices[kSums * min(mt * 16 + c, count - 1)] / a.k;
         x_row[mt] = (uint32_t)(t * a.ldx), x_scale[mt] = a.xs + t;
     }
     f32x4 acc[MT][2];
@@ -266,24 +308,35 @@ template <int MT, int KEYS> __global__ void __launch_bounds__(256) moe_up_kernel
     };
     // (H is a multiple of 16; what is behind a row's end lies beyond the buffers)
     const auto piece = [&](const uint8_t *rows, int bytes, uint32_t row, int k) { return buffer_load16(rows, bytes, k < a.H ? row + (uint32_t)k : 0x80000000u); };
+    uint32_t w_first[2], x_first[MT]; // (with many tokens the exchange costs as much as it saves: 16 tokens, 8 experts of 4096 x 4096 91.9 us without, 94.3 with)
+#pragma unroll
+    for (int u = 0; u < 2; ++u) w_first[u] = KEYS == 0 ? 0 : half_first((uint32_t)(uintptr_t)w_rows[u] + (uint32_t)(c * a.H), c);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) x_first[mt] = KEYS == 0 ? 0 : half_first((uint32_t)(uintptr_t)a.x + x_row[mt], c);
     const auto load = [&](Step &s, int b) {
         const int k = b * kF8Block + 16 * g;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            s.w[u][0] = piece(w_rows[u], 16 * a.H, (uint32_t)(c * a.H), k), s.w[u][1] = piece(w_rows[u], 16 * a.H, (uint32_t)(c * a.H), k + 64);
+            s.w[u][0] = piece(w_rows[u], 16 * a.H, (uint32_t)(c * a.H), k + 64 * (int)w_first[u]);
+            s.w[u][1] = piece(w_rows[u], 16 * a.H, (uint32_t)(c * a.H), k + 64 * (int)(w_first[u] ^ 1));
             s.ws[u] = w_scale[u][b];
         }
     };
     const auto compute = [&](const Step &s, int b) {
         const int k = b * kF8Block + 16 * g;
+        w32x4 w[2][2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) in_order(s.w[u], w_first[u], w[u]);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             if (mt * 16 >= count) break;
-            const w32x4 x[2] = {piece(a.x, x_bytes, x_row[mt], k), piece(a.x, x_bytes, x_row[mt], k + 64)};
+            const w32x4 loaded[2] = {piece(a.x, x_bytes, x_row[mt], k + 64 * (int)x_first[mt]), piece(a.x, x_bytes, x_row[mt], k + 64 * (int)(x_first[mt] ^ 1))};
+            w32x4 x[2];
+            in_order(loaded, x_first[mt], x);
             const float xs = x_scale[mt][b * a.ldxs];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                fma4(acc[mt][u], f8_products<true>(s.w[u], x), xs * s.ws[u]);
+                fma4(acc[mt][u], f8_products<true>(w[u], x), xs * s.ws[u]);
                 asm volatile("" : "+v"(acc[mt][u])); // (before the branch: see the other kernel)
             }
         }
@@ -300,7 +353,7 @@ template <int MT, int KEYS> __global__ void __launch_bounds__(256) moe_up_kernel
         load(f[0], b);
         compute(f[0], b);
     }
-    __shared__ float s_acc[WAVES][2][16 * MT][20];
+    float(*const s_acc)[2][16 * MT][kSums] = reinterpret_cast<float(*)[2][16 * MT][kSums]>(shared);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -313,12 +366,21 @@ template <int MT, int KEYS> __global__ void __launch_bounds__(256) moe_up_kernel
         for (int w = 0; w < WAVES; ++w) gate += s_acc[w][0][m][n], up += s_acc[w][1][m][n];
         const float h = gate / (1.0f + expf(-gate)) * up;
         const uint16_t high = Bf16::narrow(h);
-        const int64_t at = (int64_t)choices[m] * a.I + i0 + n;
+        const int64_t at = (int64_t)choices[kSums * m] * a.I + i0 + n;
         a.h[at] = high;
         a.h[(int64_t)a.choices * a.I + at] = fabsf(h) < INFINITY ? Bf16::narrow(h - Bf16::widen(high)) : 0; // (of an infinity the first part is all)
     }
 }
 
+// A value at an address that is the same in the whole wave, which nothing writes while the kernel runs, over the scalar cache.
+__device__ __forceinline__ float scalar_load(const float *p)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    return *(const __attribute__((address_space(4))) float *)(uintptr_t)p;
+#else
+    return *p;
+#endif
+}
 __device__ __forceinline__ uint32_t lds_address(const uint8_t *p)
 {
     return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t *)p;
@@ -358,53 +420,88 @@ template <int TOKENS> __global__ void __launch_bounds__(512, 2) moe_down_kernel(
     for (int i = lane; i < TOKENS * 16; i += 64) (&s_y[wave][0][0])[i] = 0.0f;
     uint8_t *const w_ring = s_ring[wave], *const h_ring = w_ring + 4 * W_SLOT;
     const int blocks = (a.I + kF8Block - 1) / kF8Block, row_blocks = (a.H + kF8Block - 1) / kF8Block;
-    const int units = a.list[1] * blocks;
+    const int stretches = a.list[0], units = stretches * blocks;
     const int sharing = WAVES * a.parts, mine = part * WAVES + wave;
-    const int first = (int)((int64_t)units * mine / sharing), last = (int)((int64_t)units * (mine + 1) / sharing);
+    const int first = units * mine / sharing, last = units * (mine + 1) / sharing; // (below 1280 stretches of 1024 blocks by 128)
     const uint8_t *const inner = reinterpret_cast<const uint8_t *>(a.h);
     const int inner_bytes = 4 * a.choices * a.I; // (up to 2^30)
     constexpr uint32_t kBeyond = 0x80000000u;    // of either buffer: zeros, without traffic
     // 16 rows of 128 bytes, 16-byte pieces exchanged by half the row's number, so that reads of 16 rows meet the 16 places of the 64 banks; a
     // copy's lanes have 8 rows, from `half` * 8 on
     const auto piece = [&](int half) { return (lane & 7) ^ (lane >> 4) ^ 4 * half; };
+    // A lane's place among 16 rows of weights and in a row of h, and whether that is there in the last block
+    const int tail = a.I - (blocks - 1) * kF8Block;
+    const uint32_t w_lane[2] = {(uint32_t)((lane >> 3) * a.I + 16 * piece(0)), (uint32_t)((8 + (lane >> 3)) * a.I + 16 * piece(1))};
+    const bool w_there[2] = {16 * piece(0) < tail, 16 * piece(1) < tail};
+    const bool h_there[2][2] = {{8 * piece(0) < tail, 8 * piece(1) < tail}, {64 + 8 * piece(0) < tail, 64 + 8 * piece(1) < tail}};
     const uint32_t w_place = lds_address(w_ring) + c * 128 + (g ^ (c >> 1 & 7)) * 16, h_place = lds_address(h_ring) + c * 128 + (2 * g ^ (c >> 1 & 7)) * 16;
-    for (int u = first; u < last;) {
-        const int j = u / blocks, b0 = u - j * blocks, many = min(last - j * blocks, blocks) - b0;
-        const int32_t *const stretch = moe_stretches(a) + 3 * j;
-        const int e = stretch[0], begin = stretch[1], count = stretch[2];
-        const uint8_t *const w_rows = a.down + ((int64_t)e * a.H + n0) * a.I;
-        const float *const w_scale = a.downs + ((int64_t)e * row_blocks + n0 / kF8Block) * blocks;
-        // Each workgroup begins at another block: rows lie a power of two apart more often than not, and workgroups that read the same columns of
-        // all rows at one time would keep to a part of the memory's channels.
-        const int turned = (int)(blockIdx.x % (unsigned)many);
-        const auto block_at = [&](int i) { return b0 + (i + turned < many ? i + turned : i + turned - many); };
-        const uint32_t copied = 2u * (uint32_t)(moe_choices(a)[begin + min(lane >> 3, count - 1)] * a.I) | (lane >> 3 < count ? 0u : kBeyond);
-        // (Without branches, so that the compiler's count of what is on its way holds: behind the last block nothing is below the end.)
-        const auto end_of = [&](int i) { return a.I & ((i - many) >> 31); };
-        const auto load = [&](float &scale, int i) {
-            const int b = block_at(min(i, many - 1)), end = end_of(i);
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int k = b * kF8Block + 16 * piece(half);
-                buffer_to_lds16(w_rows, 16 * a.I, (uint32_t)((8 * half + (lane >> 3)) * a.I + k) | (k < end ? 0u : kBeyond), w_ring + (i & 3) * W_SLOT + half * 1024);
-            }
-            scale = w_scale[b];
+    // Each workgroup begins a stretch at another block: rows lie a power of two apart more often than not, and workgroups that read the same columns
+    // of all rows at one time would keep to a part of the memory's channels.
+    const int turn = (int)(blockIdx.x % (unsigned)blocks);
+    // Up to 8 stretches at a time, whose lists lie in the lanes: lane l has choice l & 7 of stretch l >> 3.  What is on its way runs on from one
+    // stretch into the next (before, with each stretch by itself: 64 tokens, 64 experts of 4096 x 2048 132 us).
+    for (int from = first; from < last;) {
+        const int j0 = from / blocks, to = min(last, (j0 + 8) * blocks), many = to - from;
+        const int mine_j = min(j0 + (lane >> 3), stretches - 1);
+        const MoeHead head = moe_heads(a)[mine_j];
+        const int listed = moe_choices(a)[mine_j * kStretch + (lane & 7)]; // (anything behind the last)
+        const float share = moe_shares(a)[mine_j * kStretch + (lane & 7)];
+        const bool there = (lane & 7) < head.count;
+        const int choice = there ? listed : 0, token = choice / a.k;
+        const uint32_t copied = 2u * (uint32_t)(choice * a.I) | (there ? 0u : kBeyond);
+        struct Cursor { // a place among these blocks
+            int j, i, n, b0, turned; // stretch, block within what there is of it here, how many those are, the first, where it begins
         };
-        const auto load_inner = [&](int i) {
-            const int b = block_at(min(i, many - 1)), end = end_of(i);
+        const auto enter = [&](Cursor &at, int j) {
+            const int begin = (j0 + j) * blocks, low = max(from, begin), high = min(to, begin + blocks);
+            at.j = j, at.i = 0, at.n = high - low, at.b0 = low - begin, at.turned = turn < at.n ? turn : 0;
+        };
+        const auto advance = [&](Cursor &at) { // to another stretch? (behind the last block: n is 0 or less, and stays so)
+            if (++at.i < at.n || at.n <= 0) return false;
+            enter(at, at.j + 1);
+            return true;
+        };
+        const auto block_of = [&](const Cursor &at) { return at.b0 + (at.i + at.turned < at.n ? at.i + at.turned : at.i + at.turned - at.n); };
+        Cursor here, next, ahead;
+        enter(here, 0), enter(next, 0), enter(ahead, 0);
+        const uint8_t *w_rows;
+        const float *scales;
+        const auto enter_weights = [&](int j) { w_rows = a.down + ((int64_t)__builtin_amdgcn_readlane(head.expert, 8 * min(j, 7)) * a.H + n0) * a.I; };
+        const auto enter_scales = [&](int j) {
+            scales = a.downs + ((int64_t)__builtin_amdgcn_readlane(head.expert, 8 * min(j, 7)) * row_blocks + n0 / kF8Block) * blocks;
+        };
+        enter_weights(0), enter_scales(0);
+        uint32_t row[2];
+        const auto enter_rows = [&](int j) {
+            const uint32_t first = (uint32_t)__shfl((int)copied, 8 * min(j, 7) + (lane >> 3));
+            row[0] = first + 16 * piece(0), row[1] = first + 2 * a.choices * a.I + 16 * piece(1);
+        };
+        enter_rows(0);
+        // (Without branches, so that the compiler's count of what is on its way holds: behind the last block the buffers have no bytes.)
+        const auto load = [&](Cursor &at, int slot) {
+            const int b = at.n > 0 ? block_of(at) : 0;
+            const bool inside = b < blocks - 1;
+            const int bytes = at.n > 0 ? 16 * a.I - b * kF8Block : 0;
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+                buffer_to_lds16(w_rows + b * kF8Block, bytes, inside || w_there[half] ? w_lane[half] : kBeyond, w_ring + slot * W_SLOT + half * 1024);
+            if (advance(at)) enter_weights(at.j);
+        };
+        const auto load_inner = [&](Cursor &at, int slot) {
+            const int b = at.n > 0 ? block_of(at) : 0;
+            const bool inside = b < blocks - 1;
+            const int before = 2 * b * kF8Block, bytes = at.n > 0 ? inner_bytes - before : 0;
 #pragma unroll
             for (int p = 0; p < 2; ++p)
 #pragma unroll
-                for (int part = 0; part < 2; ++part) {
-                    const int k = b * kF8Block + 64 * p + 8 * piece(part);
-                    buffer_to_lds16(inner, inner_bytes, (copied + 2u * (uint32_t)(part * a.choices * a.I + k)) | (k < end ? 0u : kBeyond),
-                                    h_ring + (i & 1) * H_SLOT + p * 2048 + part * 1024);
-                }
+                for (int part = 0; part < 2; ++part)
+                    buffer_to_lds16(inner + before + 128 * p, bytes, inside || h_there[p][part] ? row[part] : kBeyond, h_ring + slot * H_SLOT + p * 2048 + part * 1024);
+            if (advance(at)) enter_rows(at.j);
         };
         f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-        const auto compute = [&](int i, float scale) {
+        const auto compute = [&](int slot, float scale) {
             w32x4 w[2], v[4];
-            const uint32_t w_at = w_place + (i & 3) * W_SLOT, h_at = h_place + (i & 1) * H_SLOT;
+            const uint32_t w_at = w_place + slot * W_SLOT, h_at = h_place + (slot & 1) * H_SLOT;
             read_pieces(w_at, w_at ^ 64, h_at, h_at ^ 16, w, v);
             b16x8 wide[4];
 #pragma unroll
@@ -415,30 +512,32 @@ template <int TOKENS> __global__ void __launch_bounds__(512, 2) moe_down_kernel(
             fma4(acc, part, scale);
             asm volatile("" : "+v"(acc)); // (here, and not behind a branch, which the compiler's waits for the products do not reach over)
         };
-        float scale[4];
-        wait_vmcnt<0>();
-        load_inner(0);
+        const auto finish = [&]() { // a stretch's sums, weighted, to their tokens
+            const int l = 8 * here.j + (c & 7), t = __shfl(token, l);
+            const float weight = __shfl(share, l);
+            const int count = __builtin_amdgcn_readlane(head.count, 8 * here.j);
 #pragma unroll
-        for (int d = 0; d < 3; ++d) load(scale[d], d);
-        for (int i = 0; i < many; i += 4) {
-#pragma unroll
-            for (int d = 0; d < 4; ++d) {
-                if (i + d >= many) break;
-                load_inner(i + d + 1);
-                load(scale[(d + 3) & 3], i + d + 3);
-                wait_vmcnt<3 + 4 + 3>(); // but the weights of the two blocks ahead and these
-                compute(i + d, scale[d]);
+            for (int r = 0; r < 4; ++r) {
+                const float v = acc[r] + __shfl_xor(acc[r], 8);
+                if (c < 8 && c < count) s_y[wave][t][g * 4 + r] += weight * v;
             }
+            acc = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        };
+        wait_vmcnt<0>();
+        load_inner(next, 0);
+#pragma unroll 1
+        for (int i = 0; i < 3; ++i) load(ahead, i);
+#pragma unroll 1
+        for (int i = 0; i < many; ++i) { // (not unrolled: the first passes over longer code would cost a small layer 1.5 us)
+            const float scale = scalar_load(scales + block_of(here));
+            load_inner(next, (i + 1) & 1);
+            load(ahead, (i + 3) & 3);
+            wait_vmcnt<2 + 4 + 2>(); // but the weights of the two blocks ahead and these
+            compute(i & 3, scale);
+            if (here.i + 1 == here.n) finish();
+            if (advance(here)) enter_scales(here.j);
         }
-        u = j * blocks + b0 + many;
-        const int choice = moe_choices(a)[begin + min(c & 7, count - 1)];
-        const float weight = a.weights[choice];
-        const int t = choice / a.k;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const float v = acc[r] + __shfl_xor(acc[r], 8);
-            if (c < 8 && c < count) s_y[wave][t][g * 4 + r] += weight * v;
-        }
+        from = to;
     }
     __syncthreads();
     for (int i = threadIdx.x; i < a.T * 16; i += 64 * WAVES) {
@@ -452,18 +551,22 @@ template <int TOKENS> __global__ void __launch_bounds__(512, 2) moe_down_kernel(
 }
 
 // y = the parts' sums in their order
+constexpr int kMostParts = 16;
 __global__ void __launch_bounds__(256) moe_sum_kernel(const MoeArgs a)
 {
     const int n = blockIdx.x * 256 + threadIdx.x, t = blockIdx.y;
     if (n >= a.H) return;
+    float u[kMostParts]; // (all on their way at once: one after the other 8 took 4.8 us)
+#pragma unroll
+    for (int p = 0; p < kMostParts; ++p) u[p] = a.sums[((int64_t)min(p, a.parts - 1) * a.T + t) * a.H + n];
     float v = 0.0f;
-    for (int p = 0; p < a.parts; ++p) v += a.sums[((int64_t)p * a.T + t) * a.H + n];
+#pragma unroll
+    for (int p = 0; p < kMostParts; ++p) v += p < a.parts ? u[p] : 0.0f;
     store_out(a.y, t * a.ldy + n, a.type, v);
 }
 
 struct MoeSpace {
-    size_t list, weights, inner, sums, bytes;
-    int64_t most;
+    size_t chosen, bits, places, list, weights, inner, sums, bytes;
     int parts;
 };
 static MoeSpace moe_space(int64_t T, int64_t E, int64_t k, int64_t H, int64_t I)
@@ -471,32 +574,36 @@ static MoeSpace moe_space(int64_t T, int64_t E, int64_t k, int64_t H, int64_t I)
     const int64_t tokens = T < kTokens ? T : kTokens, choices = tokens * k, most = choices < E ? choices : E;
     const auto rounded = [](int64_t n) { return (size_t)((n + 255) / 256 * 256); };
     MoeSpace m;
-    m.most = most, m.list = 0;
-    m.weights = rounded(4 * (3 + 2 * most + 3 * moe_most_stretches((int)most, (int)choices) + choices));
+    m.chosen = 0;
+    m.bits = rounded(4 * choices);
+    m.places = m.bits + rounded(8 * tokens * moe_words((int)E));
+    m.list = m.places + rounded(tokens * E);
+    m.weights = m.list + rounded(4 * (2 + (2 + 2 * kStretch) * moe_most_stretches((int)most, (int)choices)));
     m.inner = m.weights + rounded(4 * choices);
     m.sums = m.inner + rounded(4 * choices * I);
-    // A workgroup of down has 48 KB on its way, 20 KB/us; where 16 columns each are too few of them for the memory, the blocks are divided too, for a launch
-    // more (4 us).
-    const int64_t groups = H / 16, parts = groups >= 256 ? 1 : (256 + groups - 1) / groups;
-    m.parts = (int)(parts < 8 ? parts : 8);
-    const float us = (float)most * (float)H * (float)I / ((float)groups * 20e3f);
-    if (us * (1.0f - 1.0f / (float)m.parts) < 4.0f) m.parts = 1;
+    // Where 16 columns each are too few workgroups of down for the CUs, the blocks are divided too, for a launch more (5 us): a block takes a wave 0.75 us
+    // (41 tokens, 4 experts of 320 x 864, of which each token takes all: 20 workgroups 19 us).
+    const int64_t groups = H / 16, parts = groups >= 256 ? 1 : 256 / groups;
+    const float us = (float)(most + choices / 16) * (float)((I + kF8Block - 1) / kF8Block) * (0.75f / 8);
+    m.parts = (int)(parts < kMostParts ? parts : kMostParts);
+    if (us * (1.0f - 1.0f / (float)m.parts) < 5.0f) m.parts = 1;
     m.bytes = m.sums + (m.parts > 1 ? rounded(4 * m.parts * tokens * H) : 0);
     return m;
 }
 
 static void launch_moe(const MoeArgs &a, hipStream_t s)
 {
-    const dim3 up((unsigned)(a.most * (a.I / 16))), down((unsigned)(a.H / 16), (unsigned)a.parts);
+    const dim3 up((unsigned)(a.most * (a.I / 16))), up_and_list((unsigned)(a.most * (a.I / 16) + 1)), down((unsigned)(a.H / 16), (unsigned)a.parts);
     if (a.T <= kFewTokens && a.choices <= kFewChoices && a.E <= 256) {
         if (a.E <= 64) hipLaunchKernelGGL((moe_up_kernel<1, 1>), up, dim3(256), 0, s, a);
         else hipLaunchKernelGGL((moe_up_kernel<1, 4>), up, dim3(256), 0, s, a);
     } else {
-        if (a.E <= 64) hipLaunchKernelGGL(moe_route_kernel<1>, dim3(1), dim3(1024), 0, s, a);
-        else if (a.E <= 256) hipLaunchKernelGGL(moe_route_kernel<4>, dim3(1), dim3(1024), 0, s, a);
-        else hipLaunchKernelGGL(moe_route_kernel<kMostExperts / 64>, dim3(1), dim3(1024), 0, s, a);
-        if (a.T <= 16) hipLaunchKernelGGL((moe_up_kernel<1, 0>), up, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((moe_up_kernel<kTokens / 16, 0>), up, dim3(256), 0, s, a);
+        const dim3 tokens((unsigned)a.T);
+        if (a.E <= 64) hipLaunchKernelGGL(moe_choose_kernel<1>, tokens, dim3(64), 0, s, a);
+        else if (a.E <= 256) hipLaunchKernelGGL(moe_choose_kernel<4>, tokens, dim3(64), 0, s, a);
+        else hipLaunchKernelGGL(moe_choose_kernel<kMostExperts / 64>, tokens, dim3(64), 0, s, a);
+        if (a.T <= 16) hipLaunchKernelGGL((moe_up_kernel<1, 0>), up_and_list, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((moe_up_kernel<kTokens / 16, 0>), up_and_list, dim3(256), 0, s, a);
     }
     if (a.T <= 8) hipLaunchKernelGGL(moe_down_kernel<8>, down, dim3(512), 0, s, a);
     else hipLaunchKernelGGL(moe_down_kernel<kTokens>, down, dim3(512), 0, s, a);
@@ -542,8 +649,9 @@ qnn_status qnn_f8_moe(const uint8_t *x, int64_t ldx, const float *x_scales, int6
         a.ldx = ldx, a.ldxs = ldxs, a.ldl = ldl, a.ldy = ldy;
         a.T = (int32_t)n, a.E = (int32_t)E, a.k = (int32_t)top_k, a.H = (int32_t)H, a.I = (int32_t)I;
         a.logit_type = logit_type, a.type = type, a.renormalize = renormalize;
+        a.chosen = reinterpret_cast<int32_t *>(space + m.chosen), a.bits = reinterpret_cast<uint64_t *>(space + m.bits), a.places = space + m.places;
         a.list = reinterpret_cast<int32_t *>(space + m.list), a.h = reinterpret_cast<uint16_t *>(space + m.inner);
-        a.most = (int32_t)m.most, a.choices = (int32_t)(n * top_k);
+        a.choices = (int32_t)(n * top_k), a.most = a.choices < a.E ? a.choices : a.E;
         a.parts = m.parts, a.sums = m.parts > 1 ? reinterpret_cast<float *>(space + m.sums) : nullptr;
         launch_moe(a, as_stream(stream));
     }
