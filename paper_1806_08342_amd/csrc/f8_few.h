@@ -8,6 +8,13 @@ namespace qnn {
 // 16 bytes of a row, zeros behind its end
 __device__ __forceinline__ w32x4 f8_load16(const uint8_t *row, int K, int k) { return k + 16 <= K ? load_any<w32x4>(row + k) : load_end(row, K, k); }
 
+// the same of a row of whole pieces, without a branch
+__device__ __forceinline__ w32x4 f8_load_piece(const uint8_t *row, int K, int k)
+{
+    const uint32_t there = k < K ? ~0u : 0u;
+    return load_any<w32x4>(row + min(k, K - 16)) & w32x4{there, there, there, there};
+}
+
 // One wave takes 16 * NT rows of the weights and 16 * MT rows of x, the waves of a workgroup share K in turns of 128 and join their
 // sums in LDS in their order.  The product is formed transposed (weights are the left operand): a lane has one row of x and four consecutive
 // outputs.  The operands of the next DEPTH - 1 blocks are on their way while a wave works on one.
@@ -34,11 +41,13 @@ template <int MT, int NT, int WAVES, int DEPTH, bool NARROW> __global__ void __l
         w32x4 w[NT][2], x[MT][2];
         float xs[MT], ws;
     };
+    // (with 64 x 64 rows in binary32 the vector instructions are what bounds it: 1021 x 1001 x 1027 15.3 us with the exchange, 13.9 without)
+    constexpr uint32_t HALF = NARROW || MT * NT < 16 ? 64 : 0;
     uint32_t w_first[NT], x_first[MT];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) w_first[nt] = 64 * half_first((uint32_t)(uintptr_t)w_row[nt], c);
+    for (int nt = 0; nt < NT; ++nt) w_first[nt] = HALF * half_first((uint32_t)(uintptr_t)w_row[nt], c);
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) x_first[mt] = 64 * half_first((uint32_t)(uintptr_t)x_row[mt], c);
+    for (int mt = 0; mt < MT; ++mt) x_first[mt] = HALF * half_first((uint32_t)(uintptr_t)x_row[mt], c);
     const auto load = [&](Step &s, int b) {
         const int k = b * kF8Block + 16 * g;
 #pragma unroll
@@ -81,13 +90,17 @@ template <int MT, int NT, int WAVES, int DEPTH, bool NARROW> __global__ void __l
     if (whole < blocks && wave == whole % WAVES) { // the last, shorter block
         Step &s = f[DEPTH - 1];
         const int k = whole * kF8Block + 16 * g;
+        const auto load_last = [&](auto load) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) s.w[nt][0] = f8_load16(w_row[nt], a.K, k + (int)w_first[nt]), s.w[nt][1] = f8_load16(w_row[nt], a.K, k + (int)(w_first[nt] ^ 64));
+            for (int nt = 0; nt < NT; ++nt) s.w[nt][0] = load(w_row[nt], a.K, k + (int)w_first[nt]), s.w[nt][1] = load(w_row[nt], a.K, k + (int)(w_first[nt] ^ 64));
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            s.x[mt][0] = f8_load16(x_row[mt], a.K, k + (int)x_first[mt]), s.x[mt][1] = f8_load16(x_row[mt], a.K, k + (int)(x_first[mt] ^ 64));
-            s.xs[mt] = x_scale[mt][whole * a.ldxs];
-        }
+            for (int mt = 0; mt < MT; ++mt) s.x[mt][0] = load(x_row[mt], a.K, k + (int)x_first[mt]), s.x[mt][1] = load(x_row[mt], a.K, k + (int)(x_first[mt] ^ 64));
+        };
+        // (one load waits for the other where branches lie between: 1021 x 1001 x 1027, whose copies have whole pieces, 14.1 us with f8_load16, 13.5 so)
+        if (a.K % 16 == 0) load_last([](const uint8_t *row, int K, int at) { return f8_load_piece(row, K, at); });
+        else load_last([](const uint8_t *row, int K, int at) { return f8_load16(row, K, at); });
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) s.xs[mt] = x_scale[mt][whole * a.ldxs];
         s.ws = w_scale[whole];
         compute(s);
     }

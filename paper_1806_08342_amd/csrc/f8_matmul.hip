@@ -17,8 +17,8 @@ template <int MT, int NT, int WAVES, int DEPTH> static void launch_rows(const F8
     else hipLaunchKernelGGL((f8_rows_kernel<MT, NT, WAVES, DEPTH, true>), grid, block, 0, s, a);
 }
 
-// 32 rows of weights per wave halve what x costs, where workgroups for all CUs are left: 16 x 28672 x 8192 54 us against 58, 64 rows 96 against 141; but
-// one row 47 against 42, and 16 x 4096 x 4096 9.4 against 7.2.
+// 32 rows of weights per wave halve what x costs, where workgroups for all CUs are left: 24 x 28672 x 8192 51.5 us, 64 rows 74 (with 16: 55 and 104); but
+// 8 rows 45 against 47, and 16 x 4096 x 4096 6.0 against 7.2.
 static bool wide_rows(int64_t M, int64_t N) { return M > 8 && N >= 8192; }
 
 static void launch_f8_rows(const F8Args &a, hipStream_t s)
@@ -30,37 +30,49 @@ static void launch_f8_rows(const F8Args &a, hipStream_t s)
     else wide ? launch_rows<4, 2, 4, 3>(a, s) : launch_rows<4, 1, 8, 2>(a, s);
 }
 
-// By estimated time (us):
-// rows: a launch, weights at 5.9 TB/s, and x from the L2 for every 16 rows of it and 16 or 32 of weights (measured / estimated: 16 x 4096 x 4096
-// 7.2 / 8.5, 64 rows 15.1 / 15.0; 16 x 28672 x 8192 54 / 58, 64 rows 96 / 101; 32 x 12288 x 4096 18.6 / 18.1);
-// 64 rows by 64 of weights per workgroup, whose 8 waves share K: 0.475 for a block of 128 on 256 CUs (1021 x 1001 x 1024 8.2 / 8.2, x 512 6.3 / 6.3);
-// tiles: a CU does a step of 128 with a tile of 128 x 128 in 0.58 us, with binary32 results 0.9, of 256 x 256 in 1.93, or as fast as the weights come
-// (24 x 28672 x 8192 52.5 / 52, 300 x 4096 x 4096 in two parts 16.6 and its sum / 17.6, 1000 x 12288 x 4096 67.5 / 59, 8192 x 8192 x 8192 495 / 499).
+// By estimated time (us), of a launch and what follows.  Measured / estimated, with bfloat16 results and weights that no cache holds:
+// rows: 256 workgroups at a time, each a step of 128 in 0.045 and 0.0025 for each row (1 x 28672 x 8192 41.9 / 42, 32 x 4096 x 4096 7.0 / 7.8,
+// 64 rows 10.1 / 10.4, 1000 rows 121 / 121), or wide by the weights' bytes (24 x 28672 x 8192 51.5 / 52, 64 x 12288 x 4096 21.6 / 20.3) while one turn
+// takes all rows, then 512 at a time, 0.4 for a step (300 x 12288 x 4096 56 / 57).  Loads from rows at any byte but a word's first
+// take two to four times as long (1 x 4096 x 4095 10.1 / 10.3, 64 rows 30.6 / 30.8, but x 4092 10.9), so that a copy with whole pieces comes first where that
+// is less: 2.2, and 0.365 for a megabyte (64 x 4096 x 4095 20.7 with it).
+// 64 rows by 64 of weights per workgroup, whose 8 waves share K: 0.4 for a step on 256 CUs (1000 x 1024 x 1024 7.0 / 7.0, 500 x 2048 x 9216 32.3 / 32.6);
+// tiles: a CU does a step of 128 with a tile of 128 x 128 in 0.62 us, with binary32 results 0.97, of 256 x 256 in 1.85, or as fast as the weights come
+// (64 x 28672 x 8192 59 / 55, 300 x 4096 x 4096 in two parts 21.6 / 21, 1000 x 12288 x 4096 68.9 / 64.5 and 61.2 / 64.2, 8192 x 8192 x 8192 495 / 479).
 F8Plan f8_plan(int64_t M, int64_t N, int64_t K, int type)
 {
     F8Plan best{F8Kernel::Rows, 1, 1e30f, false, 0, 0, 0};
     const float steps = (float)f8_blocks(K), weights = (float)N * (float)K * 1e-6f, outputs = (float)M * (float)N * 1e-6f; // (MB, if bytes)
-    const bool wide = type == QNN_F32;
-    const int64_t turns = (M + 63) / 64, tiles_of_16 = M < 64 ? (M + 15) / 16 : 4;
-    best.us = (float)turns * (weights * (0.17f + (float)tiles_of_16 * (wide_rows(M, N) ? 0.061f : 0.13f)) * (wide ? 1.3f : 1.0f)) + 3.5f;
+    const bool wide = type == QNN_F32, parts = K % 16 != 0, odd = K % 4 != 0;
+    const int64_t turns = (M + 63) / 64;
+    const float rows = M < 64 ? (float)M : 64.0f; // of a turn
+    const auto rounds = [](int64_t groups, int64_t at_once) { return (float)((groups + at_once - 1) / at_once); };
+    const auto rows_us = [&](bool any_byte) {
+        if (!wide_rows(M, N)) return 3.0f + rounds(turns * ((N + 15) / 16), 256) * (0.8f + steps * (any_byte ? 0.19f + 0.0102f * rows : 0.045f + 0.0025f * rows));
+        const float wider = wide && M > 48 ? 1.5f : 1.0f;
+        if (any_byte) return 10.0f + (float)turns * weights * (0.32f + 0.0096f * rows) * wider;
+        if (turns == 1) return 6.0f + weights * (0.142f + 0.00224f * rows) * wider;
+        return 3.0f + rounds(turns * ((N + 31) / 32), 512) * (0.8f + steps * 0.4f * wider);
+    };
+    best.us = rows_us(odd);
     if (K > (1 << 20) || M * N >= (int64_t)1 << 37) return best; // (beyond the tiles' offsets, and 2^32 threads)
-    const bool padded = K % 16 != 0; // (loads from rows at any byte take twice as long)
-    const float before = padded ? 3.0f + (weights + (float)M * (float)K * 1e-6f) * 0.45f : 0.0f;
-    const float us64 = 4.4f + before + (float)((turns * ((N + 63) / 64) + 255) / 256) * steps * 0.475f;
-    if (M > 64 && us64 < best.us) best.us = us64, best.kernel = F8Kernel::Rows64, best.padded = padded;
+    const float before = parts ? 2.2f + (weights + (float)M * (float)K * 1e-6f) * 0.365f : 0.0f;
+    if (odd && before + rows_us(false) < best.us - 1.0f) best.us = before + rows_us(false), best.padded = true;
+    const float us64 = 3.0f + (odd ? before : 0.0f) + rounds(turns * ((N + 63) / 64), 256) * (0.8f + steps * (wide ? 0.51f : 0.4f));
+    if (M > 64 && us64 < best.us) best.us = us64, best.kernel = F8Kernel::Rows64, best.padded = odd;
     const auto consider = [&](F8Kernel kernel, int64_t tile, float step) {
         const int64_t tiles = ((M + tile - 1) / tile) * ((N + tile - 1) / tile);
         for (int splits = 1; splits <= 16; ++splits) {
             if (splits > 1 && (steps < 4.0f * (float)splits || tiles * (splits - 1) >= 512)) break;
             const float turn = (float)((tiles * splits + 255) / 256);
             float us = turn * ceilf(steps / (float)splits) * step;
-            if (us < weights * 0.2f) us = weights * 0.2f;
+            if (us < weights * (wide ? 0.25f : 0.215f)) us = weights * (wide ? 0.25f : 0.215f);
             us += 5.0f + before + (splits > 1 ? 4.0f + (float)splits * outputs * 1.6f : 0.0f);
-            if (us < best.us) best.us = us, best.kernel = kernel, best.splits = splits, best.padded = padded;
+            if (us < best.us) best.us = us, best.kernel = kernel, best.splits = splits, best.padded = parts;
         }
     };
-    consider(F8Kernel::Tile128, 128, wide ? 0.9f : 0.58f);
-    if (!wide) consider(F8Kernel::Tile256, 256, 1.93f);
+    consider(F8Kernel::Tile128, 128, wide ? 0.97f : 0.62f);
+    if (!wide) consider(F8Kernel::Tile256, 256, 1.85f);
     const auto rounded = [](int64_t n) { return (size_t)((n + 255) / 256 * 256); };
     if (best.padded) best.x_bytes = rounded(M * f8_padded(K)), best.w_bytes = rounded(N * f8_padded(K));
     best.bytes = best.x_bytes + best.w_bytes + (best.splits > 1 ? rounded(4 * best.splits * M * N) : 0);
