@@ -10,11 +10,16 @@
 
 namespace qnn {
 
-template <int MT, int NT, int WAVES, int DEPTH> static void launch_rows(const F8Args &a, hipStream_t s)
+// Rows that begin with a word each.  (Those that do not: one step ahead, and 16 rows of weights; 32 would not fit the registers.)
+static bool words(const F8Args &a) { return ((uintptr_t)a.x | (uintptr_t)a.ldx | (uintptr_t)a.w | (uintptr_t)a.K) % 4 == 0; }
+
+template <int MT, int NT, int WAVES, int DEPTH, bool ANY = false> static void launch_rows(const F8Args &a, hipStream_t s)
 {
     const dim3 grid((unsigned)((a.N + 16 * NT - 1) / (16 * NT)), (unsigned)((a.M + 16 * MT - 1) / (16 * MT))), block(64 * WAVES);
-    if (a.type == QNN_F32) hipLaunchKernelGGL((f8_rows_kernel<MT, NT, WAVES, DEPTH, false>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((f8_rows_kernel<MT, NT, WAVES, DEPTH, true>), grid, block, 0, s, a);
+    if constexpr (!ANY && NT != 2)
+        if (!words(a)) return launch_rows<MT, NT, WAVES, 2, true>(a, s);
+    if (a.type == QNN_F32) hipLaunchKernelGGL((f8_rows_kernel<MT, NT, WAVES, DEPTH, false, ANY>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((f8_rows_kernel<MT, NT, WAVES, DEPTH, true, ANY>), grid, block, 0, s, a);
 }
 
 // 32 rows of weights per wave halve what x costs, where workgroups for all CUs are left: 24 x 28672 x 8192 51.5 us, 64 rows 74 (with 16: 55 and 104); but
@@ -23,7 +28,7 @@ static bool wide_rows(int64_t M, int64_t N) { return M > 8 && N >= 8192; }
 
 static void launch_f8_rows(const F8Args &a, hipStream_t s)
 {
-    const bool wide = wide_rows(a.M, a.N);
+    const bool wide = wide_rows(a.M, a.N) && words(a);
     if (a.M <= 16) wide ? launch_rows<1, 2, 4, 3>(a, s) : launch_rows<1, 1, 8, 3>(a, s);
     else if (a.M <= 32) wide ? launch_rows<2, 2, 4, 3>(a, s) : launch_rows<2, 1, 8, 2>(a, s);
     else if (a.M <= 48) wide ? launch_rows<3, 2, 4, 3>(a, s) : launch_rows<3, 1, 8, 2>(a, s);
@@ -33,9 +38,9 @@ static void launch_f8_rows(const F8Args &a, hipStream_t s)
 // By estimated time (us), of a launch and what follows.  Measured / estimated, with bfloat16 results and weights that no cache holds:
 // rows: 256 workgroups at a time, each a step of 128 in 0.045 and 0.0025 for each row (1 x 28672 x 8192 41.9 / 42, 32 x 4096 x 4096 7.0 / 7.8,
 // 64 rows 10.1 / 10.4, 1000 rows 121 / 121), or wide by the weights' bytes (24 x 28672 x 8192 51.5 / 52, 64 x 12288 x 4096 21.6 / 20.3) while one turn
-// takes all rows, then 512 at a time, 0.4 for a step (300 x 12288 x 4096 56 / 57).  Loads from rows at any byte but a word's first
-// take two to four times as long (1 x 4096 x 4095 10.1 / 10.3, 64 rows 30.6 / 30.8, but x 4092 10.9), so that a copy with whole pieces comes first where that
-// is less: 2.2, and 0.365 for a megabyte (64 x 4096 x 4095 20.7 with it).
+// takes all rows, then 512 at a time, 0.4 for a step (300 x 12288 x 4096 56 / 57).  Rows that begin within a
+// word take 0.1 and 0.0065 (1 x 4096 x 4095 6.6 / 7.2, 64 rows 20.0 / 20.3), so that a copy with whole pieces comes first where that is less: 3, and 0.365 for
+// a megabyte (64 x 4096 x 4095 19.3 / 20).
 // 64 rows by 64 of weights per workgroup, whose 8 waves share K: 0.4 for a step on 256 CUs (1000 x 1024 x 1024 7.0 / 7.0, 500 x 2048 x 9216 32.3 / 32.6);
 // tiles: a CU does a step of 128 with a tile of 128 x 128 in 0.62 us, with binary32 results 0.97, of 256 x 256 in 1.85, or as fast as the weights come
 // (64 x 28672 x 8192 59 / 55, 300 x 4096 x 4096 in two parts 21.6 / 21, 1000 x 12288 x 4096 68.9 / 64.5 and 61.2 / 64.2, 8192 x 8192 x 8192 495 / 479).
@@ -48,16 +53,15 @@ F8Plan f8_plan(int64_t M, int64_t N, int64_t K, int type)
     const float rows = M < 64 ? (float)M : 64.0f; // of a turn
     const auto rounds = [](int64_t groups, int64_t at_once) { return (float)((groups + at_once - 1) / at_once); };
     const auto rows_us = [&](bool any_byte) {
-        if (!wide_rows(M, N)) return 3.0f + rounds(turns * ((N + 15) / 16), 256) * (0.8f + steps * (any_byte ? 0.19f + 0.0102f * rows : 0.045f + 0.0025f * rows));
+        if (any_byte || !wide_rows(M, N)) return 3.0f + rounds(turns * ((N + 15) / 16), 256) * (0.8f + steps * (any_byte ? 0.1f + 0.0065f * rows : 0.045f + 0.0025f * rows));
         const float wider = wide && M > 48 ? 1.5f : 1.0f;
-        if (any_byte) return 10.0f + (float)turns * weights * (0.32f + 0.0096f * rows) * wider;
         if (turns == 1) return 6.0f + weights * (0.142f + 0.00224f * rows) * wider;
         return 3.0f + rounds(turns * ((N + 31) / 32), 512) * (0.8f + steps * 0.4f * wider);
     };
     best.us = rows_us(odd);
     if (K > (1 << 20) || M * N >= (int64_t)1 << 37) return best; // (beyond the tiles' offsets, and 2^32 threads)
-    const float before = parts ? 2.2f + (weights + (float)M * (float)K * 1e-6f) * 0.365f : 0.0f;
-    if (odd && before + rows_us(false) < best.us - 1.0f) best.us = before + rows_us(false), best.padded = true;
+    const float before = parts ? 3.0f + (weights + (float)M * (float)K * 1e-6f) * 0.365f : 0.0f;
+    if (odd && before + rows_us(false) < best.us) best.us = before + rows_us(false), best.padded = true;
     const float us64 = 3.0f + (odd ? before : 0.0f) + rounds(turns * ((N + 63) / 64), 256) * (0.8f + steps * (wide ? 0.51f : 0.4f));
     if (M > 64 && us64 < best.us) best.us = us64, best.kernel = F8Kernel::Rows64, best.padded = odd;
     const auto consider = [&](F8Kernel kernel, int64_t tile, float step) {
@@ -119,7 +123,7 @@ const char *qnn_f8_matmul_plan(int64_t M, int64_t N, int64_t K, int type)
     if (bad_f8_sizes(M, N, K) || M == 0 || (bad_half_type(type) && type != QNN_F32)) return "";
     const F8Plan p = f8_plan(M, N, K, type);
     static thread_local char name[32];
-    if (p.kernel == F8Kernel::Rows) std::snprintf(name, sizeof(name), "rows%dx%s", M < 64 ? (int)((M + 15) / 16 * 16) : 64, wide_rows(M, N) ? "32" : "16");
+    if (p.kernel == F8Kernel::Rows) std::snprintf(name, sizeof(name), "rows%dx%s", M < 64 ? (int)((M + 15) / 16 * 16) : 64, wide_rows(M, N) && (p.padded || K % 4 == 0) ? "32" : "16");
     else if (p.kernel == F8Kernel::Rows64) return "rows64x64";
     else std::snprintf(name, sizeof(name), "tile%s/%d", p.kernel == F8Kernel::Tile256 ? "256x256" : "128x128", p.splits);
     return name;

@@ -59,7 +59,8 @@ def check(x, xs, w, ws, bias, y, most_rows=20, most_columns=200, what=""):
     (1, 4096, 1024, BF16, "rows16x16"), (16, 1000, 2000, F32, "rows16x16"), (9, 9000, 512, BF16, "rows16x32"), (32, 500, 1040, F16, "rows32x16"), (20, 8200, 528, F32, "rows32x32"),
     (33, 600, 4096, BF16, "rows48x16"), (40, 600, 2047, F16, "rows48x16"), (48, 10000, 640, BF16, "rows48x32"), (64, 900, 2048, BF16, "rows64x16"), (50, 8192, 300, F32, "rows64x32"),
     (900, 1000, 512, BF16, "rows64x64"), (1021, 999, 1111, F32, "rows64x64"), (291, 1280, 692, F32, "rows64x64"), (130, 12000, 2048, BF16, "tile128x128/1"), (1000, 12288, 1040, F32, "tile128x128/1"),
-    (300, 4096, 4096, BF16, "tile128x128/2"), (3970, 4090, 2047, BF16, "tile256x256/1"), (4096, 8192, 2048, F16, "tile256x256/1")])
+    (1, 4100, 4095, BF16, "rows16x16"), (24, 2050, 1030, F16, "rows32x16"),
+    (64, 1000, 1021, F32, "rows64x16"), (8, 600, 2049, F32, "rows16x16"), (300, 4096, 4096, BF16, "tile128x128/2"), (3970, 4090, 2047, BF16, "tile256x256/1"), (4096, 8192, 2048, F16, "tile256x256/1")])
 def test_each_kernel(M, N, K, dtype, plan):
     assert qnn.f8_matmul_plan(M, N, K, dtype) == plan
     x, xs, w, ws, b = operands(M, N, K)
