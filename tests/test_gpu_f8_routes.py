@@ -209,3 +209,61 @@ def test_infinite_products_between_the_experts_matrices():
     y = qnn.f8_moe(*(c[n] for n in NAMES), 2)
     keep = [0, 2, 3, 5]
     assert torch.equal(y[keep], clean[keep]) and not torch.isfinite(y[[1, 4]]).any()
+
+
+@pytest.mark.parametrize("M,N,K,dtype", [(300, 4096, 4096, BF16), (1000, 1003, 1111, F32), (3970, 1030, 2047, BF16)])
+def test_products_with_workspaces_on_two_streams_and_in_two_graphs_at_once(M, N, K, dtype):
+    # parts of K and padded copies lie in memory of each call's, or graph's, own
+    assert qnn.load_library().qnn_f8_matmul_workspace_bytes(M, N, K, 2 if dtype == F32 else 0) > 0
+    args = [operands(M, N, K, seed)[:4] for seed in (1, 2)]
+    want = [qnn.f8_matmul(*a, dtype=dtype) for a in args]
+    torch.cuda.synchronize()
+    streams, graphs, results = [torch.cuda.Stream() for _ in args], [], []
+    got = [[], []]
+    for _ in range(6):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(qnn.f8_matmul(*args[i], dtype=dtype))
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, w) for ys, w in zip(got, want) for y in ys)
+    for a in args:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            results.append(qnn.f8_matmul(*a, dtype=dtype))
+    for _ in range(4):
+        for y in results:
+            y.zero_()
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(y, w) for y, w in zip(results, want))
+
+
+def test_a_workspace_of_the_callers_and_results_in_place_of_others():
+    M, N, K = 300, 4096, 4096
+    x, xs, w, ws, _ = operands(M, N, K)
+    want = qnn.f8_matmul(x, xs, w, ws)
+    space = torch.full((qnn.load_library().qnn_f8_matmul_workspace_bytes(M, N, K, 0) + 256,), 0xff, dtype=torch.uint8, device=DEV)
+    out = torch.full((M, N), math.nan, dtype=BF16, device=DEV)
+    assert qnn.f8_matmul(x, xs, w, ws, out=out, workspace=space[:-256]) is out and torch.equal(out, want) and (space[-256:] == 0xff).all()
+    with pytest.raises(Exception):
+        qnn.f8_matmul(x, xs, w, ws, workspace=space[:1024])
+    c = filled(20, 8, 144, 96)
+    want = qnn.f8_moe(*(c[n] for n in NAMES), 3)
+    space = torch.full((qnn.load_library().qnn_f8_moe_workspace_bytes(20, 8, 3, 144, 96) + 256,), 0xff, dtype=torch.uint8, device=DEV)
+    assert torch.equal(qnn.f8_moe(*(c[n] for n in NAMES), 3, workspace=space[:-256]), want) and (space[-256:] == 0xff).all()
+    with pytest.raises(Exception):
+        qnn.f8_moe(*(c[n] for n in NAMES), 3, workspace=space[:256])
+
+
+def test_tensors_that_require_grad_are_refused():
+    x, xs, w, ws, b = operands(4, 128, 128)
+    rows = torch.randn(4, 128, device=DEV, dtype=BF16, requires_grad=True)
+    scales = xs.clone().requires_grad_()
+    for call in (lambda: qnn.f8_quantize(rows), lambda: qnn.f8_rmsnorm(rows), lambda: qnn.f8_rmsnorm(rows.detach(), residual=rows), lambda: qnn.f8_matmul(x, scales, w, ws)):
+        with pytest.raises(Exception):
+            call()
+        with torch.no_grad():
+            call()
