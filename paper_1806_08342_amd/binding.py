@@ -579,7 +579,8 @@ def quantize_weights_blocks(w):
 def f8_quantize(x, gated=False, out=None):
     """Rows of x [M,K] (bfloat16 or float16, rows may be spaced apart) as (codes float8_e4m3fn [M,K], scales float32
     [ceil(K/128),M]): one scale for 128 consecutive elements, their largest finite one / 448 (2^-80 at least).  gated: x is [M,2K],
-    and silu(x[:,:K]) * x[:,K:] is what is quantized.  out: (codes, scales) to write to, rows may be spaced apart."""
+    and silu(x[:,:K]) * x[:,K:] is what is quantized.  out: (codes, scales) to write to, rows may be spaced apart; new ones are two
+    tensors in one piece of memory, which stays while either lives."""
     return (_nat or _native()).f8_quantize(x, gated, out)
 
 

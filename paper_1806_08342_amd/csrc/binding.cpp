@@ -898,9 +898,22 @@ struct F8Out {
 F8Out f8_output(PyObject *o, int64_t M, int64_t K, const at::Tensor &like)
 {
     F8Out out;
-    if (o != Py_None && (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 2)) type_error("out", "a tuple (codes, scales)");
-    out.codes = output(o == Py_None ? o : PyTuple_GET_ITEM(o, 0), {M, K}, at::kFloat8_e4m3fn, like);
-    out.scales = output(o == Py_None ? o : PyTuple_GET_ITEM(o, 1), {f8_blocks(K), M}, at::kFloat, like);
+    if (o == Py_None) { // new ones in one piece of memory: they are used together, and a second request costs 0.4 us of the host's 4.7
+        const int64_t bytes = (M * K + 255) / 256 * 256, blocks = f8_blocks(K);
+        const at::Tensor both = fresh({bytes + 4 * blocks * M}, at::kByte, like);
+        const auto part = [&](at::ScalarType type, int64_t offset, at::IntArrayRef shape) {
+            at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(both.storage()), c10::DispatchKeySet(c10::DispatchKey::CUDA), c10::scalarTypeToTypeMeta(type));
+            t.unsafeGetTensorImpl()->set_storage_offset(offset);
+            t.unsafeGetTensorImpl()->set_sizes_contiguous(shape);
+            return t;
+        };
+        out.codes.t = part(at::kFloat8_e4m3fn, 0, {M, K}), out.scales.t = part(at::kFloat, bytes / 4, {blocks, M});
+        out.rows = {static_cast<uint8_t *>(out.codes.t.data_ptr()), static_cast<float *>(out.scales.t.data_ptr()), K, M};
+        return out;
+    }
+    if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 2) type_error("out", "a tuple (codes, scales)");
+    out.codes = output(PyTuple_GET_ITEM(o, 0), {M, K}, at::kFloat8_e4m3fn, like);
+    out.scales = output(PyTuple_GET_ITEM(o, 1), {f8_blocks(K), M}, at::kFloat, like);
     out.rows = f8_rows(out.codes.t, out.scales.t, "out", "out scales");
     same_device(out.codes.t, like, "out");
     return out;

@@ -171,3 +171,22 @@ def test_captured_and_replayed_with_other_rows():
         torch.cuda.synchronize()
         for got, want in zip(a + b, qnn.f8_rmsnorm(x, residual=r) + qnn.f8_quantize(x, True)):
             assert torch.equal(got.view(torch.uint8), want.view(torch.uint8))
+
+
+@pytest.mark.parametrize("M, K", [(1, 1), (3, 130), (257, 1000)])
+def test_new_codes_and_scales_are_tensors_of_their_own(M, K):
+    x = torch.randn(M, K, device=DEV).to(torch.bfloat16)
+    codes, scales = qnn.f8_quantize(x)
+    assert codes.is_contiguous() and scales.is_contiguous() and not codes.requires_grad and scales.data_ptr() % 256 == 0
+    kept, copy = scales.clone(), codes.view(torch.uint8).clone()
+    codes.view(torch.uint8).fill_(0x7f)
+    assert torch.equal(scales, kept)
+    scales.fill_(2.0)
+    assert (codes.view(torch.uint8) == 0x7f).all()
+    again, _ = qnn.f8_quantize(x)
+    del codes, scales
+    torch.empty(1 << 20, device=DEV).fill_(1.0)
+    assert torch.equal(again.view(torch.uint8), copy)
+    with torch.inference_mode():
+        codes, scales = qnn.f8_quantize(x)
+        assert torch.equal(codes.view(torch.uint8), copy) and torch.equal(scales, kept)
