@@ -6,7 +6,7 @@
 //   An infinity is cut off at the largest finite value's code, a NaN stays one.
 //
 // Bound by memory: each element is read once and written once, the row of a norm stays in registers.  A lane has 8 consecutive
-// elements, sixteen lanes a block of 128.  16384 x 8192 with a residual 175 us (5.4 TB/s; a copy has 5.1), 9001 x 4100 to codes 23 us;
+// elements, sixteen lanes a block of 128.  16384 x 8192 with a residual 175 us (5.4 TB/s; a copy has 5.1), 9001 x 4100 to codes 24 us, gated 43;
 // one row of 4096 3.1 us, a launch and one chain of loads.
 #include "f8.h"
 
@@ -111,38 +111,38 @@ struct F8RowArgs {
     uint32_t magic, shift;          // of the division by blocks
 };
 
+// v / (1 + exp(-v)) by a reciprocal (off by 2^-23), but where that would leave the normal numbers: 9001 x 4100 gated 43 us, with divisions 49
+__device__ __forceinline__ float silu(float v)
+{
+    const float q = 1.0f + expf(-v);
+    return q < 0x1p100f ? v * __builtin_amdgcn_rcpf(q) : v / q;
+}
+
+// 16 lanes per block; kSlab blocks of the grid's first dimension.  (Several blocks after each other, their loads ahead, took longer at all sizes:
+// with four 24 x 14336 gated 4.9 us for 2.6, 4096 x 4096 13.1 for 9.8, 9001 x 4100 24.2 for 24.3.)
+constexpr uint32_t kSlab = 1u << 24;
 template <class T, bool GATED, bool WHOLE> __global__ void __launch_bounds__(256) f8_quantize_kernel(const F8RowArgs a)
 {
-    constexpr int EACH = 4; // blocks of 16 lanes
-    const uint32_t first = of_xcd(blockIdx.x, a.groups) * (16 * EACH) + (threadIdx.x >> 4);
+    const uint32_t unit = blockIdx.y * kSlab + of_xcd(blockIdx.x, a.groups) * 16 + (threadIdx.x >> 4);
+    if (unit >= a.units) return; // (whole blocks)
     const int lane = threadIdx.x & 15;
-    w32x4 in[EACH][GATED ? 2 : 1];
-    uint32_t row[EACH], block[EACH];
+    const uint32_t row = a.magic ? __umulhi(unit, a.magic) >> a.shift : unit, block = unit - row * a.blocks;
+    const uint16_t *const x = a.x + (int64_t)row * a.ldx;
+    const int k = (int)block * kF8Block + lane * 8;
+    float v[8], scale;
+    const w32x4 in = load8<WHOLE>(x, a.K, k);
+    if constexpr (GATED) {
+        const w32x4 in_up = load8<WHOLE>(x + a.K, a.K, k);
+        float up[8];
+        widen8<T>(in, v), widen8<T>(in_up, up);
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        const uint32_t unit = min(first + 16 * i, a.units - 1);
-        row[i] = a.magic ? __umulhi(unit, a.magic) >> a.shift : unit, block[i] = unit - row[i] * a.blocks;
-        const uint16_t *const x = a.x + (int64_t)row[i] * a.ldx;
-        const int k = (int)block[i] * kF8Block + lane * 8;
-        in[i][0] = load8<WHOLE>(x, a.K, k);
-        if constexpr (GATED) in[i][1] = load8<WHOLE>(x + a.K, a.K, k);
+        for (int e = 0; e < 8; ++e) v[e] = silu(v[e]) * up[e];
+    } else {
+        widen8<T>(in, v);
     }
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        if (first + 16 * i >= a.units) return;
-        float v[8], scale;
-        widen8<T>(in[i][0], v);
-        if constexpr (GATED) {
-            float up[8];
-            widen8<T>(in[i][1], up);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = v[e] / (1.0f + expf(-v[e])) * up[e];
-        }
-        const w32x2 codes = encode8(v, scale);
-        const int k = (int)block[i] * kF8Block + lane * 8;
-        if (k < a.K) store_codes<WHOLE>(a.codes + (int64_t)row[i] * a.ldc, a.K, k, codes);
-        if (lane == 0) a.scales[(int64_t)block[i] * a.lds + row[i]] = scale;
-    }
+    const w32x2 codes = encode8(v, scale);
+    if (k < a.K) store_codes<WHOLE>(a.codes + (int64_t)row * a.ldc, a.K, k, codes);
+    if (lane == 0) a.scales[(int64_t)block * a.lds + row] = scale;
 }
 
 // One row per workgroup of up to 16 waves (4 rows per workgroup where one wave does).  CHUNKS: pieces of 8 elements that a lane keeps of a row; 0: rows
@@ -278,10 +278,12 @@ template <class T> static void run_rmsnorm(const F8RowArgs &a, hipStream_t s)
     else launch_rmsnorm<T, 0>(a, s);
 }
 
-template <class T, bool GATED> static void launch_quantize(const F8RowArgs &a, hipStream_t s)
+template <class T, bool GATED> static void launch_quantize(F8RowArgs a, hipStream_t s)
 {
-    if (a.K % 8 == 0) hipLaunchKernelGGL((f8_quantize_kernel<T, GATED, true>), dim3(8 * a.groups), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((f8_quantize_kernel<T, GATED, false>), dim3(8 * a.groups), dim3(256), 0, s, a);
+    a.groups = ((a.units < kSlab ? a.units : kSlab) + 127) / 128;
+    const dim3 grid(8 * a.groups, (a.units + kSlab - 1) / kSlab);
+    if (a.K % 8 == 0) hipLaunchKernelGGL((f8_quantize_kernel<T, GATED, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((f8_quantize_kernel<T, GATED, false>), grid, dim3(256), 0, s, a);
 }
 
 } // namespace qnn
@@ -301,7 +303,6 @@ qnn_status qnn_f8_quantize(const void *x, int64_t ldx, int64_t M, int64_t K, int
     F8RowArgs a{};
     a.x = static_cast<const uint16_t *>(x), a.ldx = ldx, a.codes = codes, a.ldc = ldc, a.scales = scales, a.lds = lds;
     a.M = (int32_t)M, a.K = (int32_t)K, a.blocks = (uint32_t)f8_blocks(K), a.units = (uint32_t)(M * a.blocks);
-    a.groups = ((a.units + 63) / 64 + 7) / 8;
     fast_division(a.blocks, a.magic, a.shift);
     hipStream_t s = as_stream(stream);
     if (type == QNN_BF16) gated ? launch_quantize<Bf16, true>(a, s) : launch_quantize<Bf16, false>(a, s);
