@@ -56,7 +56,9 @@ __device__ __forceinline__ w32x2 encode8(const float (&v)[8], float &scale)
     return codes;
 }
 
-// 8 elements from k on, zeros behind the row's end.  WHOLE: K is a multiple of 8, and no branch is needed.
+// 8 elements from k on, zeros behind the row's end, in two steps: loads of several, which no branch holds up, and then, where the row ends within or before
+// them, what was loaded before its end moved down (777 x 5003 with a residual 11.4 us in one step with a branch, 11.0 so, 20 x 5003 4.4 and 4.1).  WHOLE: K is a
+// multiple of 8, and the first step is all.
 template <bool WHOLE> __device__ __forceinline__ w32x4 load8(const uint16_t *row, int K, int k)
 {
     if constexpr (WHOLE) {
@@ -64,7 +66,19 @@ template <bool WHOLE> __device__ __forceinline__ w32x4 load8(const uint16_t *row
         const uint32_t there = k < K ? ~0u : 0u;
         return v & w32x4{there, there, there, there};
     }
-    return k + 8 <= K ? load_any<w32x4>(row + k) : load_end(reinterpret_cast<const uint8_t *>(row), 2 * K, 2 * k);
+    return K >= 8 ? load_any<w32x4>(row + min(k, K - 8)) : load_end(reinterpret_cast<const uint8_t *>(row), 2 * K, 2 * k);
+}
+template <bool WHOLE> __device__ __forceinline__ void settle8(w32x4 &v, int K, int k)
+{
+    if (WHOLE || K < 8 || k + 8 <= K) return;
+    const int drop = min(k + 8 - K, 8);
+    uint32_t u[5] = {v[0], v[1], v[2], v[3], 0u};
+    if (drop & 2) u[0] = u[1], u[1] = u[2], u[2] = u[3], u[3] = 0u;
+    if (drop & 4) u[0] = u[2], u[1] = u[3], u[2] = 0u, u[3] = 0u;
+    if (drop & 8) u[0] = u[1] = u[2] = u[3] = 0u;
+    const uint32_t by = 2 * (drop & 1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_alignbyte(u[i + 1], u[i], by);
 }
 template <class T> __device__ __forceinline__ void widen8(const w32x4 w, float (&v)[8])
 {
@@ -130,14 +144,16 @@ template <class T, bool GATED, bool WHOLE> __global__ void __launch_bounds__(256
     const uint16_t *const x = a.x + (int64_t)row * a.ldx;
     const int k = (int)block * kF8Block + lane * 8;
     float v[8], scale;
-    const w32x4 in = load8<WHOLE>(x, a.K, k);
+    w32x4 in = load8<WHOLE>(x, a.K, k);
     if constexpr (GATED) {
-        const w32x4 in_up = load8<WHOLE>(x + a.K, a.K, k);
+        w32x4 in_up = load8<WHOLE>(x + a.K, a.K, k);
+        settle8<WHOLE>(in, a.K, k), settle8<WHOLE>(in_up, a.K, k);
         float up[8];
         widen8<T>(in, v), widen8<T>(in_up, up);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = silu(v[e]) * up[e];
     } else {
+        settle8<WHOLE>(in, a.K, k);
         widen8<T>(in, v);
     }
     const w32x2 codes = encode8(v, scale);
@@ -165,7 +181,9 @@ template <class T, int CHUNKS, bool SINGLE, bool WHOLE> __global__ void __launch
         if (residual) r[i] = load8<WHOLE>(residual, a.K, k);
     };
     const auto add = [&](int i, int k) {
+        settle8<WHOLE>(h[i], a.K, k);
         if (!residual) return;
+        settle8<WHOLE>(r[i], a.K, k);
         float u[8], v[8];
         widen8<T>(h[i], u), widen8<T>(r[i], v);
 #pragma unroll
@@ -200,7 +218,9 @@ template <class T, int CHUNKS, bool SINGLE, bool WHOLE> __global__ void __launch
             for (int i = 0; i < turns; ++i) {
                 const int k = (i * lanes + tid) * 8;
                 float v[8];
-                widen8<T>(load8<WHOLE>(residual ? total : x, a.K, k), v);
+                w32x4 in = load8<WHOLE>(residual ? total : x, a.K, k);
+                settle8<WHOLE>(in, a.K, k);
+                widen8<T>(in, v);
                 f(v, k);
             }
     };
@@ -240,7 +260,9 @@ template <class T, int CHUNKS, bool SINGLE, bool WHOLE> __global__ void __launch
     each([&](float (&v)[8], int k) {
         if (a.weight) {
             float g[8];
-            widen8<T>(load8<WHOLE>(a.weight, a.K, k), g);
+            w32x4 weight = load8<WHOLE>(a.weight, a.K, k);
+            settle8<WHOLE>(weight, a.K, k);
+            widen8<T>(weight, g);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = v[e] * unit * by * g[e];
         } else {
@@ -266,12 +288,13 @@ template <class T, int CHUNKS, bool SINGLE = false> static void launch_rmsnorm(F
 }
 
 // Few rows: as many waves as they can use, up to 16.  Many: fewer with more each, for fewer waits on the others (between the two nothing jumps: 512 x
-// 5000 4.2 us with a wave for every 512 elements, 516 rows 4.4 with one for 1024; 512 x 8192 6.1, 516 rows 6.7 with one for 2048).
+// 5000 4.2 us with a wave for every 512 elements, 516 rows 4.4 with one for 1024; 512 x 8192 6.1, 516 rows 6.7 with one for 2048).  With a residual, whose
+// stores lie between the loads and the sum, more rows are few: 2048 x 4096 13.1 and 15.3, 2048 x 8192 27.0 and 29.7, but 777 x 5003 11.8 and 11.4.
 template <class T> static void run_rmsnorm(const F8RowArgs &a, hipStream_t s)
 {
     const bool few = a.M <= 512;
     if (a.K <= 512) launch_rmsnorm<T, 1, true>(a, s);
-    else if (few && a.K <= 8192) launch_rmsnorm<T, 1>(a, s);
+    else if ((few || (a.residual && a.K % 8 == 0 && a.M <= 4096)) && a.K <= 8192) launch_rmsnorm<T, 1>(a, s);
     else if (a.K <= 1024) launch_rmsnorm<T, 2, true>(a, s);
     else if (a.K <= (few ? 16384 : 6144)) launch_rmsnorm<T, 2>(a, s);
     else if (a.K <= 32768) launch_rmsnorm<T, 4>(a, s);
