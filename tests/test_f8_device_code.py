@@ -103,3 +103,23 @@ def test_no_read_is_on_its_way_at_a_barrier_of_the_tiles(objects):  # noqa: F811
         assert at_barrier and not any(at_barrier.values()), (symbol, at_barrier)
         seen += 1
     assert seen >= 3
+
+
+def test_copies_are_counted_as_the_waits_for_them_assume(objects):  # noqa: F811
+    # moe_down_kernel waits until all but the newest eight copies have arrived: six of a pass over its loop and two of the one before
+    seen = 0
+    for symbol, code in kernels(objects, "moe_down_kernel"):
+        texts = [text for _, text, _ in code]
+        waits = [i for i, t in enumerate(texts) if re.fullmatch(r"s_waitcnt vmcnt\(8\)", t)]
+        assert len(waits) == 1, symbol
+        first_product = next(i for i, t in enumerate(texts) if t.startswith("v_mfma"))
+        assert waits[0] < first_product
+        base = code[0][0]
+        # the loop: from what a later branch goes back to, before the wait, to the last such branch
+        backs = [(base + to, i) for i, (_, t, to) in enumerate(code) if i > waits[0] and t.startswith(("s_cbranch", "s_branch")) and to is not None and base + to < code[waits[0]][0]]
+        index = {at: i for i, (at, _, _) in enumerate(code)}
+        begin, end = max((index[to], i) for to, i in backs)
+        memory = [t for t in texts[begin:end] if t.startswith(("global_", "buffer_", "flat_", "scratch_"))]
+        assert len(memory) == 6 and all(t.startswith("buffer_load_dwordx4") and t.endswith(" lds") for t in memory), (symbol, memory)
+        seen += 1
+    assert seen >= 2
