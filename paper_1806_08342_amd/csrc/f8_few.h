@@ -22,7 +22,7 @@ __device__ __forceinline__ w32x4 f8_load_piece(const uint8_t *row, int K, int k)
 // 1 x 4096 x 4096: 4.7 us call behind call, a launch and a chain of loads.
 // ANY: rows that begin within a word.  A lane has 32 bytes in a row then, loads the nine words that they lie in and moves them down: loads at any byte
 // took longer (1 x 4096 x 4095 10.1 us, so 6.6; 16 rows 15 and 9, 64 rows 30 and 20).
-template <int MT, int NT, int WAVES, int DEPTH, bool NARROW, bool ANY> __global__ void __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : 2) f8_rows_kernel(const F8Args a)
+template <int MT, int NT, int WAVES, int DEPTH, bool NARROW, bool ANY> __global__ void __launch_bounds__(64 * WAVES, 2) f8_rows_kernel(const F8Args a)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
     const int n0 = blockIdx.x * 16 * NT, m0 = blockIdx.y * 16 * MT;

@@ -264,10 +264,10 @@ template <int KEYS> __device__ __forceinline__ uint64_t moe_route_few(const MoeA
 }
 
 // Workgroups: an expert by 16 columns of h; four waves share H and join their sums in LDS.
-// Bound by the memory where H is long (64 tokens, 64 experts of 4096 x 2048 203 us, 5.3 TB/s; of 1024 x 2048 70 us, 3.8: a wave has two blocks).
-// KEYS: 0: the choices are there, and the last workgroup lists them for what follows; else each workgroup chooses by itself, from so many times
+// Bound by the memory where H is long (64 tokens, 64 experts of 4096 x 2048 201 us, 5.3 TB/s; of 1024 x 2048 62 us, 4.3: a wave has two blocks).
+// MORE: for experts of more than 16 MT tokens.  KEYS: 0: the choices are there, and the last workgroup lists them for what follows; else each workgroup chooses by itself, from so many times
 // 64 logits.
-template <int MT, int KEYS> __global__ void __launch_bounds__(256) moe_up_kernel(const MoeArgs a)
+template <int MT, int KEYS, bool MORE = false> __global__ void __launch_bounds__(256) moe_up_kernel(const MoeArgs a)
 {
     constexpr int WAVES = 4, DEPTH = 2, SUMS = WAVES * 2 * 16 * MT * kSums * 4;
     __shared__ __attribute__((aligned(16))) uint8_t shared[KEYS == 0 && SUMS < kListBytes ? kListBytes : SUMS];
@@ -293,83 +293,86 @@ template <int MT, int KEYS> __global__ void __launch_bounds__(256) moe_up_kernel
     const uint8_t *const w_rows[2] = {a.up + ((int64_t)e * 2 * a.I + i0) * a.H, a.up + ((int64_t)e * 2 * a.I + a.I + i0) * a.H};
     const float *const w_scale[2] = {a.ups + ((int64_t)e * two + i0 / kF8Block) * blocks, a.ups + ((int64_t)e * two + (a.I + i0) / kF8Block) * blocks};
     const int x_bytes = (int)(a.T * a.ldx); // (below 2^30)
-    uint32_t x_row[MT];
-    const float *x_scale[MT];
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        const int t = choices[kSums * min(mt * 16 + c, count - 1)] / a.k;
-        x_row[mt] = (uint32_t)(t * a.ldx), x_scale[mt] = a.xs + t;
-    }
-    f32x4 acc[MT][2];
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) acc[mt][0] = acc[mt][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    struct Step {
-        w32x4 w[2][2];
-        float ws[2];
-    };
-    // (H is a multiple of 16; what is behind a row's end lies beyond the buffers)
-    const auto piece = [&](const uint8_t *rows, int bytes, uint32_t row, int k) { return buffer_load16(rows, bytes, k < a.H ? row + (uint32_t)k : 0x80000000u); };
-    uint32_t w_first[2], x_first[MT]; // (with many tokens the exchange costs as much as it saves: 16 tokens, 8 experts of 4096 x 4096 91.9 us without, 94.3 with)
-#pragma unroll
-    for (int u = 0; u < 2; ++u) w_first[u] = KEYS == 0 ? 0 : half_first((uint32_t)(uintptr_t)w_rows[u] + (uint32_t)(c * a.H), c);
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) x_first[mt] = KEYS == 0 ? 0 : half_first((uint32_t)(uintptr_t)a.x + x_row[mt], c);
-    const auto load = [&](Step &s, int b) {
-        const int k = b * kF8Block + 16 * g;
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            s.w[u][0] = piece(w_rows[u], 16 * a.H, (uint32_t)(c * a.H), k + 64 * (int)w_first[u]);
-            s.w[u][1] = piece(w_rows[u], 16 * a.H, (uint32_t)(c * a.H), k + 64 * (int)(w_first[u] ^ 1));
-            s.ws[u] = w_scale[u][b];
-        }
-    };
-    const auto compute = [&](const Step &s, int b) {
-        const int k = b * kF8Block + 16 * g;
-        w32x4 w[2][2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) in_order(s.w[u], w_first[u], w[u]);
+    for (int from = 0; from < (MORE ? count : 1); from += 16 * MT) { // (an expert's weights again, from the caches, for more)
+        if (from > 0) __syncthreads();
+        uint32_t x_row[MT];
+        const float *x_scale[MT];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            if (mt * 16 >= count) break;
-            const w32x4 loaded[2] = {piece(a.x, x_bytes, x_row[mt], k + 64 * (int)x_first[mt]), piece(a.x, x_bytes, x_row[mt], k + 64 * (int)(x_first[mt] ^ 1))};
-            w32x4 x[2];
-            in_order(loaded, x_first[mt], x);
-            const float xs = x_scale[mt][b * a.ldxs];
+            const int t = choices[kSums * min(from + mt * 16 + c, count - 1)] / a.k;
+            x_row[mt] = (uint32_t)(t * a.ldx), x_scale[mt] = a.xs + t;
+        }
+        f32x4 acc[MT][2];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) acc[mt][0] = acc[mt][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        struct Step {
+            w32x4 w[2][2];
+            float ws[2];
+        };
+        // (H is a multiple of 16; what is behind a row's end lies beyond the buffers)
+        const auto piece = [&](const uint8_t *rows, int bytes, uint32_t row, int k) { return buffer_load16(rows, bytes, k < a.H ? row + (uint32_t)k : 0x80000000u); };
+        uint32_t w_first[2], x_first[MT]; // (with many tokens the exchange costs as much as it saves: 16 tokens, 8 experts of 4096 x 4096 91.9 us without, 94.3 with)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) w_first[u] = KEYS == 0 ? 0 : half_first((uint32_t)(uintptr_t)w_rows[u] + (uint32_t)(c * a.H), c);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) x_first[mt] = KEYS == 0 ? 0 : half_first((uint32_t)(uintptr_t)a.x + x_row[mt], c);
+        const auto load = [&](Step &s, int b) {
+            const int k = b * kF8Block + 16 * g;
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                fma4(acc[mt][u], f8_products<true>(w[u], x), xs * s.ws[u]);
-                asm volatile("" : "+v"(acc[mt][u])); // (before the branch: see the other kernel)
+                s.w[u][0] = piece(w_rows[u], 16 * a.H, (uint32_t)(c * a.H), k + 64 * (int)w_first[u]);
+                s.w[u][1] = piece(w_rows[u], 16 * a.H, (uint32_t)(c * a.H), k + 64 * (int)(w_first[u] ^ 1));
+                s.ws[u] = w_scale[u][b];
             }
+        };
+        const auto compute = [&](const Step &s, int b) {
+            const int k = b * kF8Block + 16 * g;
+            w32x4 w[2][2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) in_order(s.w[u], w_first[u], w[u]);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                if (from + mt * 16 >= count) break;
+                const w32x4 loaded[2] = {piece(a.x, x_bytes, x_row[mt], k + 64 * (int)x_first[mt]), piece(a.x, x_bytes, x_row[mt], k + 64 * (int)(x_first[mt] ^ 1))};
+                w32x4 x[2];
+                in_order(loaded, x_first[mt], x);
+                const float xs = x_scale[mt][b * a.ldxs];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    fma4(acc[mt][u], f8_products<true>(w[u], x), xs * s.ws[u]);
+                    asm volatile("" : "+v"(acc[mt][u])); // (before the branch: see the other kernel)
+                }
+            }
+        };
+        Step f[DEPTH];
+        int b = wave;
+        for (; b + (DEPTH - 1) * WAVES < blocks; b += DEPTH * WAVES) {
+#pragma unroll
+            for (int d = 0; d < DEPTH; ++d) load(f[d], b + d * WAVES);
+#pragma unroll
+            for (int d = 0; d < DEPTH; ++d) compute(f[d], b + d * WAVES);
         }
-    };
-    Step f[DEPTH];
-    int b = wave;
-    for (; b + (DEPTH - 1) * WAVES < blocks; b += DEPTH * WAVES) {
+        for (; b < blocks; b += WAVES) {
+            load(f[0], b);
+            compute(f[0], b);
+        }
+        float(*const s_acc)[2][16 * MT][kSums] = reinterpret_cast<float(*)[2][16 * MT][kSums]>(shared);
 #pragma unroll
-        for (int d = 0; d < DEPTH; ++d) load(f[d], b + d * WAVES);
+        for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int d = 0; d < DEPTH; ++d) compute(f[d], b + d * WAVES);
-    }
-    for (; b < blocks; b += WAVES) {
-        load(f[0], b);
-        compute(f[0], b);
-    }
-    float(*const s_acc)[2][16 * MT][kSums] = reinterpret_cast<float(*)[2][16 * MT][kSums]>(shared);
+            for (int u = 0; u < 2; ++u) *reinterpret_cast<f32x4 *>(&s_acc[wave][u][mt * 16 + c][g * 4]) = acc[mt][u];
+        __syncthreads();
+        for (int i = threadIdx.x; i < min(count - from, 16 * MT) * 16; i += 64 * WAVES) {
+            const int m = i / 16, n = i % 16;
+            float gate = 0.0f, up = 0.0f;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) *reinterpret_cast<f32x4 *>(&s_acc[wave][u][mt * 16 + c][g * 4]) = acc[mt][u];
-    __syncthreads();
-    for (int i = threadIdx.x; i < min(count, 16 * MT) * 16; i += 64 * WAVES) {
-        const int m = i / 16, n = i % 16;
-        float gate = 0.0f, up = 0.0f;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) gate += s_acc[w][0][m][n], up += s_acc[w][1][m][n];
-        const float h = gate / (1.0f + expf(-gate)) * up;
-        const uint16_t high = Bf16::narrow(h);
-        const int64_t at = (int64_t)choices[kSums * m] * a.I + i0 + n;
-        a.h[at] = high;
-        a.h[(int64_t)a.choices * a.I + at] = fabsf(h) < INFINITY ? Bf16::narrow(h - Bf16::widen(high)) : 0; // (of an infinity the first part is all)
+            for (int w = 0; w < WAVES; ++w) gate += s_acc[w][0][m][n], up += s_acc[w][1][m][n];
+            const float h = gate / (1.0f + expf(-gate)) * up;
+            const uint16_t high = Bf16::narrow(h);
+            const int64_t at = (int64_t)choices[kSums * (from + m)] * a.I + i0 + n;
+            a.h[at] = high;
+            a.h[(int64_t)a.choices * a.I + at] = fabsf(h) < INFINITY ? Bf16::narrow(h - Bf16::widen(high)) : 0; // (of an infinity the first part is all)
+        }
     }
 }
 
@@ -605,6 +608,10 @@ static void launch_moe(const MoeArgs &a, hipStream_t s)
         else if (a.E <= 256) hipLaunchKernelGGL(moe_choose_kernel<4>, tokens, dim3(64), 0, s, a);
         else hipLaunchKernelGGL(moe_choose_kernel<kMostExperts / 64>, tokens, dim3(64), 0, s, a);
         if (a.T <= 16) hipLaunchKernelGGL((moe_up_kernel<1, 0>), up_and_list, dim3(256), 0, s, a);
+        // With 16 tokens at a time a CU holds more workgroups than the four with 64 at a time, which counts where there are more of them, but weights are read again
+        // for experts of more: 64 tokens that choose 8 of 64 experts of 1024 x 2048 113 us and 119, 40 that choose 4 of 64 of 1024 x 1024 55 and 58; but 64
+        // that choose 2 of 16 of 2048 x 1024 39 and 38, of 8 of 4096 x 4096 147 and 133.
+        else if (a.choices <= 8 * a.most && a.most * (a.I / 16) > 1024) hipLaunchKernelGGL((moe_up_kernel<1, 0, true>), up_and_list, dim3(256), 0, s, a);
         else hipLaunchKernelGGL((moe_up_kernel<kTokens / 16, 0>), up_and_list, dim3(256), 0, s, a);
     }
     if (a.T <= 8) hipLaunchKernelGGL(moe_down_kernel<8>, down, dim3(512), 0, s, a);

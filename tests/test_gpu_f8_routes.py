@@ -267,3 +267,13 @@ def test_tensors_that_require_grad_are_refused():
             call()
         with torch.no_grad():
             call()
+
+
+@pytest.mark.parametrize("T,E,k,H,I", [(64, 40, 2, 64, 480), (17, 128, 3, 144, 336), (50, 33, 8, 272, 512)])
+def test_many_experts_some_of_many_tokens(T, E, k, H, I):
+    # 16 tokens of an expert at a time, and up to all of them in one
+    c = filled(T, E, H, I)
+    check_moe(c, k)
+    c["logits"][:, E - 2] = 50.0
+    c["logits"][: T // 2 + 1, 1] = 49.0
+    check_moe(c, k, dtype=F16)
