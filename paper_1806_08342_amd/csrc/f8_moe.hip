@@ -12,6 +12,8 @@
 #include "f8.h"
 #include "lds_ring.h"
 
+#include <algorithm>
+
 namespace qnn {
 
 constexpr int kTokens = 64;    // of one set of launches
@@ -555,24 +557,158 @@ template <int TOKENS> __global__ void __launch_bounds__(512, 2) moe_down_kernel(
     }
 }
 
+// The same for more tokens: workgroups of 128 columns of y, 16 for each wave, which share the h of a stretch, two blocks at a time behind one barrier, in
+// three slots; the weights' rings hold as much.  (With each wave's own copies of h, as above, the L2 delivers more of them than of weights: 64 tokens,
+// 64 experts of 4096 x 2048 125 us, so 99, 5.4 TB/s of weights; 8 experts of 4096 x 4096 67 and 56.)
+template <int TOKENS> __global__ void __launch_bounds__(512, 2) moe_down_wide_kernel(const MoeArgs a)
+{
+    constexpr int WAVES = 8, W_SLOT = 4096, H_SLOT = 8192, SLOTS = 3;
+    __shared__ __attribute__((aligned(128))) uint8_t s_w[WAVES][SLOTS * W_SLOT], s_h[SLOTS * H_SLOT];
+    __shared__ float s_y[WAVES][TOKENS][16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
+    const int n0 = blockIdx.x * 128 + wave * 16, part = blockIdx.y;
+    const bool mine = n0 < a.H; // (a wave behind the last column copies its share of h all the same)
+    for (int i = lane; i < TOKENS * 16; i += 64) (&s_y[wave][0][0])[i] = 0.0f;
+    const int blocks = (a.I + kF8Block - 1) / kF8Block, pairs = (blocks + 1) / 2, row_blocks = (a.H + kF8Block - 1) / kF8Block;
+    const int stretches = a.list[0], units = stretches * pairs;
+    const int first = units * part / a.parts, last = units * (part + 1) / a.parts;
+    const uint8_t *const inner = reinterpret_cast<const uint8_t *>(a.h);
+    const int inner_bytes = 4 * a.choices * a.I;
+    constexpr uint32_t kBeyond = 0x80000000u;
+    const auto piece = [&](int half) { return (lane & 7) ^ (lane >> 4) ^ 4 * half; };
+    const int tail = a.I - (blocks - 1) * kF8Block;
+    const uint32_t w_lane[2] = {(uint32_t)((lane >> 3) * a.I + 16 * piece(0)), (uint32_t)((8 + (lane >> 3)) * a.I + 16 * piece(1))};
+    const bool w_there[2] = {16 * piece(0) < tail, 16 * piece(1) < tail};
+    // of two blocks' h a wave copies a block's half rows of one part
+    const int own_block = wave >> 2, own_half = wave >> 1 & 1, own_part = wave & 1, own_piece = (lane & 7) ^ (lane >> 4) ^ 4 * own_part;
+    const bool own_there = 64 * own_half + 8 * own_piece < tail;
+    uint8_t *const own_slot = s_h + own_block * 4096 + own_half * 2048 + own_part * 1024;
+    const uint32_t w_place = lds_address(s_w[wave]) + c * 128 + (g ^ (c >> 1 & 7)) * 16, h_place = lds_address(s_h) + c * 128 + (2 * g ^ (c >> 1 & 7)) * 16;
+    const int turn = (int)(blockIdx.x % (unsigned)pairs);
+    for (int from = first; from < last;) {
+        const int j0 = from / pairs, to = min(last, (j0 + 8) * pairs), many = to - from;
+        const int mine_j = min(j0 + (lane >> 3), stretches - 1);
+        const MoeHead head = moe_heads(a)[mine_j];
+        const int listed = moe_choices(a)[mine_j * kStretch + (lane & 7)];
+        const float share = moe_shares(a)[mine_j * kStretch + (lane & 7)];
+        const bool there = (lane & 7) < head.count;
+        const int choice = there ? listed : 0, token = choice / a.k;
+        const uint32_t copied = 2u * (uint32_t)(choice * a.I) | (there ? 0u : kBeyond);
+        struct Cursor { // a place among these pairs of blocks
+            int j, i, n, u0, turned;
+        };
+        const auto enter = [&](Cursor &at, int j) {
+            const int begin = (j0 + j) * pairs, low = max(from, begin), high = min(to, begin + pairs);
+            at.j = j, at.i = 0, at.n = high - low, at.u0 = low - begin, at.turned = turn < at.n ? turn : 0;
+        };
+        const auto advance = [&](Cursor &at) {
+            if (++at.i < at.n || at.n <= 0) return false;
+            enter(at, at.j + 1);
+            return true;
+        };
+        const auto block_of = [&](const Cursor &at) { return 2 * (at.u0 + (at.i + at.turned < at.n ? at.i + at.turned : at.i + at.turned - at.n)); };
+        Cursor here, ahead;
+        enter(here, 0), enter(ahead, 0);
+        const uint8_t *w_rows;
+        const float *scales;
+        uint32_t row;
+        const auto enter_ahead = [&](int j) {
+            w_rows = a.down + ((int64_t)__builtin_amdgcn_readlane(head.expert, 8 * min(j, 7)) * a.H + (mine ? n0 : 0)) * a.I;
+            row = (uint32_t)__shfl((int)copied, 8 * min(j, 7) + (lane >> 3)) + (uint32_t)(own_part * 2 * a.choices * a.I) + 16 * own_piece;
+        };
+        const auto enter_scales = [&](int j) { scales = a.downs + ((int64_t)__builtin_amdgcn_readlane(head.expert, 8 * min(j, 7)) * row_blocks + blockIdx.x) * blocks; };
+        enter_ahead(0), enter_scales(0);
+        const auto load = [&](int slot) {
+            const int b0 = ahead.n > 0 ? block_of(ahead) : blocks;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const int b = b0 + q, bytes = b < blocks && mine ? 16 * a.I - b * kF8Block : 0;
+                const bool inside = b < blocks - 1;
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+                    buffer_to_lds16(w_rows + b * kF8Block, bytes, inside || w_there[half] ? w_lane[half] : kBeyond, s_w[wave] + slot * W_SLOT + q * 2048 + half * 1024);
+            }
+            const int b = b0 + own_block, before = 2 * b * kF8Block, bytes = b < blocks ? inner_bytes - before : 0;
+            buffer_to_lds16(inner + before + 128 * own_half, bytes, b < blocks - 1 || own_there ? row : kBeyond, own_slot + slot * H_SLOT);
+            if (advance(ahead)) enter_ahead(ahead.j);
+        };
+        f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+        const auto compute = [&](int slot, int q, float scale) {
+            w32x4 w[2], v[4];
+            const uint32_t w_at = w_place + slot * W_SLOT + q * 2048, h_at = h_place + slot * H_SLOT + q * 4096;
+            read_pieces(w_at, w_at ^ 64, h_at, h_at ^ 16, w, v);
+            b16x8 wide[4];
+#pragma unroll
+            for (int p = 0; p < 2; ++p) wide[2 * p] = widen_codes(w[p][0], w[p][1]), wide[2 * p + 1] = widen_codes(w[p][2], w[p][3]);
+            f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide[i], __builtin_bit_cast(b16x8, v[i]), sum, 0, 0, 0);
+            fma4(acc, sum, scale);
+            asm volatile("" : "+v"(acc)); // (here, and not behind a branch, which the compiler's waits for the products do not reach over)
+        };
+        const auto finish = [&]() {
+            const int l = 8 * here.j + (c & 7), t = __shfl(token, l);
+            const float weight = __shfl(share, l);
+            const int count = __builtin_amdgcn_readlane(head.count, 8 * here.j);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float v = acc[r] + __shfl_xor(acc[r], 8);
+                if (c < 8 && c < count) s_y[wave][t][g * 4 + r] += weight * v;
+            }
+            acc = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        };
+        wait_vmcnt<0>();
+        lds_barrier(); // (all waves are through with the stretches before, and nothing is on its way into the slots)
+        load(0), load(1);
+        int slot = 0;
+#pragma unroll 1
+        for (int i = 0; i < many; ++i) {
+            const int b = block_of(here);
+            const float scale = scalar_load(scales + b), second = b + 1 < blocks ? scalar_load(scales + b + 1) : 0.0f;
+            wait_vmcnt<5>(); // but the next pair's copies
+            lds_barrier();   // all waves' copies are here, and what the pair before was in is free
+            load(slot == 0 ? 2 : slot - 1);
+            compute(slot, 0, scale), compute(slot, 1, second);
+            if (here.i + 1 == here.n) finish();
+            if (advance(here)) enter_scales(here.j);
+            slot = slot == 2 ? 0 : slot + 1;
+        }
+        from = to;
+    }
+    __syncthreads();
+    for (int i = lane; mine && i < a.T * 16; i += 64) {
+        const int t = i / 16, n = i % 16;
+        const float v = s_y[wave][t][n];
+        if (a.sums) a.sums[((int64_t)part * a.T + t) * a.H + n0 + n] = v;
+        else store_out(a.y, t * a.ldy + n0 + n, a.type, v);
+    }
+}
+
 // y = the parts' sums in their order
-constexpr int kMostParts = 16;
+constexpr int kMostParts = 32;
 __global__ void __launch_bounds__(256) moe_sum_kernel(const MoeArgs a)
 {
     const int n = blockIdx.x * 256 + threadIdx.x, t = blockIdx.y;
     if (n >= a.H) return;
-    float u[kMostParts]; // (all on their way at once: one after the other 8 took 4.8 us)
-#pragma unroll
-    for (int p = 0; p < kMostParts; ++p) u[p] = a.sums[((int64_t)min(p, a.parts - 1) * a.T + t) * a.H + n];
     float v = 0.0f;
+    const auto add = [&](int begin, auto many) { // (all on their way at once: one after the other 8 took 4.8 us)
+        constexpr int MANY = decltype(many)::value;
+        float u[MANY];
 #pragma unroll
-    for (int p = 0; p < kMostParts; ++p) v += p < a.parts ? u[p] : 0.0f;
+        for (int p = 0; p < MANY; ++p) u[p] = a.sums[((int64_t)min(begin + p, a.parts - 1) * a.T + t) * a.H + n];
+#pragma unroll
+        for (int p = 0; p < MANY; ++p) v += begin + p < a.parts ? u[p] : 0.0f;
+    };
+    if (a.parts <= 4) add(0, std::integral_constant<int, 4>());
+    else
+        for (int begin = 0; begin < a.parts; begin += 16) add(begin, std::integral_constant<int, 16>());
     store_out(a.y, t * a.ldy + n, a.type, v);
 }
 
 struct MoeSpace {
     size_t chosen, bits, places, list, weights, inner, sums, bytes;
     int parts;
+    bool wide; // down by 128 columns
 };
 static MoeSpace moe_space(int64_t T, int64_t E, int64_t k, int64_t H, int64_t I)
 {
@@ -592,11 +728,19 @@ static MoeSpace moe_space(int64_t T, int64_t E, int64_t k, int64_t H, int64_t I)
     const float us = (float)(most + choices / 16) * (float)((I + kF8Block - 1) / kF8Block) * (0.75f / 8);
     m.parts = (int)(parts < kMostParts ? parts : kMostParts);
     if (us * (1.0f - 1.0f / (float)m.parts) < 5.0f) m.parts = 1;
+    // By 128 columns (a launch more always, and a barrier for two blocks) where there are many tokens' h and weights to read: 64 tokens that choose 6 of 64 experts
+    // of 4096 x 2048 306 us for the layer, by 16 columns 323, 48 that choose 2 of 4 of 4096 x 4096 83 and 88; but 16 that choose 2 of 8 of those 94 and
+    // 90, 64 that choose 2 of 16 of 2048 x 1024 40 and 38.
+    m.wide = tokens > 16 && H >= 1024 && (most + choices / 16) * H * I >= 100000000;
+    if (m.wide) {
+        const int64_t groups = (H + 127) / 128;
+        m.parts = (int)(groups >= 256 ? 1 : std::min<int64_t>(kMostParts, 256 / groups));
+    }
     m.bytes = m.sums + (m.parts > 1 ? rounded(4 * m.parts * tokens * H) : 0);
     return m;
 }
 
-static void launch_moe(const MoeArgs &a, hipStream_t s)
+static void launch_moe(const MoeArgs &a, bool wide, hipStream_t s)
 {
     const dim3 up((unsigned)(a.most * (a.I / 16))), up_and_list((unsigned)(a.most * (a.I / 16) + 1)), down((unsigned)(a.H / 16), (unsigned)a.parts);
     if (a.T <= kFewTokens && a.choices <= kFewChoices && a.E <= 256) {
@@ -614,7 +758,8 @@ static void launch_moe(const MoeArgs &a, hipStream_t s)
         else if (a.choices <= 8 * a.most && a.most * (a.I / 16) > 1024) hipLaunchKernelGGL((moe_up_kernel<1, 0, true>), up_and_list, dim3(256), 0, s, a);
         else hipLaunchKernelGGL((moe_up_kernel<kTokens / 16, 0>), up_and_list, dim3(256), 0, s, a);
     }
-    if (a.T <= 8) hipLaunchKernelGGL(moe_down_kernel<8>, down, dim3(512), 0, s, a);
+    if (wide) hipLaunchKernelGGL(moe_down_wide_kernel<kTokens>, dim3((unsigned)((a.H + 127) / 128), (unsigned)a.parts), dim3(512), 0, s, a);
+    else if (a.T <= 8) hipLaunchKernelGGL(moe_down_kernel<8>, down, dim3(512), 0, s, a);
     else hipLaunchKernelGGL(moe_down_kernel<kTokens>, down, dim3(512), 0, s, a);
     if (a.sums) hipLaunchKernelGGL(moe_sum_kernel, dim3((unsigned)((a.H + 255) / 256), (unsigned)a.T), dim3(256), 0, s, a);
 }
@@ -662,7 +807,7 @@ qnn_status qnn_f8_moe(const uint8_t *x, int64_t ldx, const float *x_scales, int6
         a.list = reinterpret_cast<int32_t *>(space + m.list), a.h = reinterpret_cast<uint16_t *>(space + m.inner);
         a.choices = (int32_t)(n * top_k), a.most = a.choices < a.E ? a.choices : a.E;
         a.parts = m.parts, a.sums = m.parts > 1 ? reinterpret_cast<float *>(space + m.sums) : nullptr;
-        launch_moe(a, as_stream(stream));
+        launch_moe(a, m.wide, as_stream(stream));
     }
     return launch_status(hipGetLastError());
 }

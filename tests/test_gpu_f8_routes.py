@@ -277,3 +277,22 @@ def test_many_experts_some_of_many_tokens(T, E, k, H, I):
     c["logits"][:, E - 2] = 50.0
     c["logits"][: T // 2 + 1, 1] = 49.0
     check_moe(c, k, dtype=F16)
+
+
+@pytest.mark.parametrize("T,E,k,H,I", [(17, 3, 3, 4112, 4112), (40, 2, 2, 3600, 4112), (70, 2, 2, 4096, 3696)])
+def test_large_experts_for_many_tokens(T, E, k, H, I):
+    # 128 columns of the second product for a workgroup, the last of them not whole, odd numbers of blocks, parts that begin within an expert
+    c = filled(T, E, H, I)
+    c["logits"][3] = -math.inf
+    c["logits"][5, 1] = -math.inf
+    check_moe(c, k)
+    a = [c[n] for n in NAMES]
+    want = qnn.f8_moe(*a, k)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = qnn.f8_moe(*a, k)
+    for _ in range(3):
+        y.fill_(math.nan)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want)
