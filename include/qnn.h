@@ -445,7 +445,8 @@ qnn_status qnn_f8_rmsnorm(const void *x, int64_t ldx, const void *residual, int6
  * 2^-126 it loses bits), y is rounded once.  A NaN code gives NaN in its row or column.
  * x: DEVICE [M][ldx], ldx >= K.  x_scales: DEVICE, pitch ldxs >= M between blocks.  w: DEVICE [N][K], w_scales DEVICE, both contiguous.
  * bias: DEVICE [N] of `type` or NULL.  y: DEVICE, M x N of `type`, row pitch ldy >= N (written).
- * Rows at any byte; those that are whole 16-byte pieces at 16-byte aligned addresses run faster.  M up to 2^20 (0 is a no-op), N and K up to 2^24.
+ * Rows at any byte; those that are whole 16-byte pieces at 16-byte aligned addresses run faster (others may be copied into the workspace first, which
+ * is as large as both operands then).  M up to 2^20 (0 is a no-op), N and K up to 2^24.
  * workspace: DEVICE scratch, 16-byte aligned, of at least qnn_f8_matmul_workspace_bytes bytes (NULL where that is 0), else QNN_EINVAL. */
 qnn_status qnn_f8_matmul(const uint8_t *x, int64_t ldx, const float *x_scales, int64_t ldxs, const uint8_t *w, const float *w_scales, const void *bias,
                          int64_t M, int64_t N, int64_t K, int type, void *y, int64_t ldy, void *workspace, size_t workspace_bytes, void *stream);
