@@ -7,7 +7,7 @@
 //
 // Bound by memory: each element is read once and written once, the row of a norm stays in registers.  A lane has 8 consecutive
 // elements, sixteen lanes a block of 128.  16384 x 8192 with a residual 175 us (5.4 TB/s; a copy has 5.1), 9001 x 4100 to codes 23 us, gated 43;
-// one row of 4096 3.1 us, a launch and one chain of loads.
+// one row of 4096 2.9 us in a graph, a launch and one chain of loads.
 #include "f8.h"
 
 namespace qnn {
