@@ -274,21 +274,16 @@ template <class T, int CHUNKS, bool SINGLE, bool WHOLE> __global__ void __launch
         for (int e = 0; e < 8; ++e) u[e] = a.weight ? v[e] * g[e] : v[e];
         bool infinite;
         w32x2 codes = encode8(u, scale, infinite);
-        const bool exact = regular && !infinite && scale >= 0x1p-60f && scale <= 0x1p60f && scale * by >= kF8LeastScale;
-        if (!exact) {
+        const bool exact = regular && !infinite && scale >= 0x1p-60f && scale <= 0x1p60f && scale * by >= kF8LeastScale && scale * by <= 0x1p118f;
+        if (!exact || a.y) { // (a product too small for binary32 has the code of zero, but its result is not that)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) u[e] = a.weight ? v[e] * unit * by * g[e] : v[e] * unit * by;
-            codes = encode8(u, scale, infinite);
+            for (int e = 0; e < 8; ++e) v[e] = a.weight ? v[e] * unit * by * g[e] : v[e] * unit * by;
         }
-        const float rest = exact ? by : 1.0f;
-        scale *= rest;
+        if (exact) scale *= by;
+        else codes = encode8(v, scale, infinite);
         if (k >= a.K) return;
         store_codes<WHOLE>(a.codes + row * a.ldc, a.K, k, codes);
-        if (a.y) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) u[e] *= rest;
-            store8<WHOLE>(a.y + (int64_t)row * a.K, a.K, k, narrow8<T>(u));
-        }
+        if (a.y) store8<WHOLE>(a.y + (int64_t)row * a.K, a.K, k, narrow8<T>(v));
         if ((threadIdx.x & 15) == 0) a.scales[(int64_t)(k / kF8Block) * a.lds + row] = scale;
     });
 }

@@ -190,3 +190,24 @@ def test_new_codes_and_scales_are_tensors_of_their_own(M, K):
     with torch.inference_mode():
         codes, scales = qnn.f8_quantize(x)
         assert torch.equal(codes.view(torch.uint8), copy) and torch.equal(scales, kept)
+
+
+@pytest.mark.parametrize("size, weight", [(1e10, 1e30), (1e-10, 1e-30), (1.0, 3e37), (1e15, 1e-38), (1e-17, 1e38), (1e17, 1e20), (3e-3, 1e-22)])
+@pytest.mark.parametrize("K", [200, 5003])
+def test_norm_with_weights_at_the_ends_of_the_range(size, weight, K):
+    # products of elements and weights that leave binary32 although what the norm makes of them does not, and scales near their bound
+    g = torch.Generator().manual_seed(K)
+    x, w = (torch.randn(3, K, generator=g) * size).to(torch.bfloat16), ((0.5 + torch.rand(K, generator=g)) * weight).to(torch.bfloat16)
+    w[K // 2:] = 1.0
+    codes, scales, y = qnn.f8_rmsnorm(x.to(DEV), w.to(DEV), 0.0, with_y=True)
+    v = x.double()
+    v = v / v.square().mean(1, keepdim=True).sqrt() * w.double()
+    # v is held in binary32: what passes its largest number, 2^128 (1 - 2^-24), is infinite there (1.5e38 times a normal number over 2.3 is), which is
+    # cut off at the largest finite one of its block
+    passes = v.abs() > torch.finfo(torch.float32).max
+    finite = torch.nn.functional.pad(torch.where(passes, 0.0, v.abs()), (0, -K % 128)).view(3, -1, 128)
+    most = finite.amax(2, keepdim=True).expand(finite.shape).reshape(3, -1)[:, :K]
+    ref.assert_codes(codes, scales, torch.where(passes, most * v.sign(), v), 2.0 ** -20)
+    # (a result is rounded to bfloat16 once, behind roundings in binary32; below its normal numbers to the last of their steps)
+    ref.assert_close(torch.where(passes, 0.0, y.cpu().double()), torch.where(passes, 0.0, v), v.abs() * (ref.half_ulp(torch.bfloat16) + 2.0 ** -20) + 2.0 ** -133)
+    assert (y.cpu()[passes].abs() == math.inf).all()
