@@ -262,25 +262,30 @@ template <class T, int CHUNKS, bool SINGLE, bool WHOLE> __global__ void __launch
     // The codes do not depend on what a row is divided by: they are taken from its products with the weights, which are exact, so that only the scale and the
     // quotient are rounded, and the scale is multiplied afterwards.  (Of rows of 4096 bfloat16 33 % have a code that is another one than that
     // of 64 bits, where the products lie exactly between two; from v 42 %.)  Not so where the products, the factor or the scale come near the ends of the range.
-    const bool regular = unit == 1.0f && by >= 0x1p-60f && by <= 0x1p60f;
+    // Where v itself is asked for, codes are v's too: both ways in one took 777 x 5003 from 8.4 us to 8.9.
+    const bool regular = !a.y && unit == 1.0f && by >= 0x1p-60f && by <= 0x1p60f;
     each([&](float (&v)[8], int k) {
-        float g[8], u[8], scale;
+        float g[8], scale;
         if (a.weight) {
             w32x4 weight = load8<WHOLE>(a.weight, a.K, k);
             settle8<WHOLE>(weight, a.K, k);
             widen8<T>(weight, g);
         }
+        w32x2 codes;
+        bool infinite, exact = false;
+        if (regular) {
+            float u[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) u[e] = a.weight ? v[e] * g[e] : v[e];
-        bool infinite;
-        w32x2 codes = encode8(u, scale, infinite);
-        const bool exact = regular && !infinite && scale >= 0x1p-60f && scale <= 0x1p60f && scale * by >= kF8LeastScale && scale * by <= 0x1p118f;
-        if (!exact || a.y) { // (a product too small for binary32 has the code of zero, but its result is not that)
+            for (int e = 0; e < 8; ++e) u[e] = a.weight ? v[e] * g[e] : v[e];
+            codes = encode8(u, scale, infinite);
+            exact = !infinite && scale >= 0x1p-60f && scale <= 0x1p60f && scale * by >= kF8LeastScale && scale * by <= 0x1p118f;
+            scale *= by;
+        }
+        if (!exact) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = a.weight ? v[e] * unit * by * g[e] : v[e] * unit * by;
+            codes = encode8(v, scale, infinite);
         }
-        if (exact) scale *= by;
-        else codes = encode8(v, scale, infinite);
         if (k >= a.K) return;
         store_codes<WHOLE>(a.codes + row * a.ldc, a.K, k, codes);
         if (a.y) store8<WHOLE>(a.y + (int64_t)row * a.K, a.K, k, narrow8<T>(v));

@@ -207,7 +207,8 @@ def test_norm_with_weights_at_the_ends_of_the_range(size, weight, K):
     passes = v.abs() > torch.finfo(torch.float32).max
     finite = torch.nn.functional.pad(torch.where(passes, 0.0, v.abs()), (0, -K % 128)).view(3, -1, 128)
     most = finite.amax(2, keepdim=True).expand(finite.shape).reshape(3, -1)[:, :K]
-    ref.assert_codes(codes, scales, torch.where(passes, most * v.sign(), v), 2.0 ** -20)
+    for c, s in ((codes, scales), qnn.f8_rmsnorm(x.to(DEV), w.to(DEV), 0.0)):  # (without y codes come from the products with the weights)
+        ref.assert_codes(c, s, torch.where(passes, most * v.sign(), v), 2.0 ** -20)
     # (a result is rounded to bfloat16 once, behind roundings in binary32; below its normal numbers to the last of their steps)
     ref.assert_close(torch.where(passes, 0.0, y.cpu().double()), torch.where(passes, 0.0, v), v.abs() * (ref.half_ulp(torch.bfloat16) + 2.0 ** -20) + 2.0 ** -133)
     assert (y.cpu()[passes].abs() == math.inf).all()
