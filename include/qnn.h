@@ -459,8 +459,9 @@ const char *qnn_f8_matmul_plan(int64_t M, int64_t N, int64_t K, int type);
  * never chosen, +inf counts as the largest finite number), with the weights exp(logit) / sum exp, over the chosen ones (renormalize != 0) or over
  * all logits.  With h_e = silu(gate_e x_t) * (up_e x_t), silu(v) = v / (1 + exp(-v)):
  *   y[t] = sum over the chosen e of weight_e * (down_e h_e)
- * A token that chooses nothing gets 0.  Products of x as in qnn_f8_matmul for 16 bits; h is held to 16 significant bits, its products with the codes of
- * down are exact; everything else is binary32, y is rounded once.  The result does not depend on the order of workgroups.
+ * A token that chooses nothing gets 0.  Products of x as in qnn_f8_matmul for 16 bits; h is held to 16 significant bits, up to binary32's largest, its products with the codes of
+ * down are exact (a block's sum of them, before the scale, has to stay within binary32); everything else is binary32, y is rounded once.  The result does not depend on the
+ * order of workgroups.
  * Reads the weights of the experts chosen, once for every 64 tokens: meant for few of these (for many, group the tokens by expert and call qnn_f8_matmul).
  * x, x_scales: as above, [T][H], ldx up to 2^24.  logits: DEVICE [T][ldl] of logit_type (QNN_BF16, QNN_F16 or QNN_F32), ldl >= E.
  * up: DEVICE codes [E][2 I][H], the I rows of gate before those of up; up_scales [E][ceil(2 I / 128)][ceil(H / 128)] (a block of rows may

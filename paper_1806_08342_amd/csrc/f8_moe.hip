@@ -265,6 +265,21 @@ template <int KEYS> __device__ __forceinline__ uint64_t moe_route_few(const MoeA
     return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(same >> 32), l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)same, l);
 }
 
+// h as two bfloat16 that are added up, its first 16 significant bits at least: the nearest, and what is left, rounded.  Finite numbers from
+// 2^128 (1 - 2^-9) on, whose nearest is infinite, are the largest bfloat16 and what is left cut off (rounded, the two could add up to 2^128).  Of an infinity or a NaN the first
+// part is all.
+__device__ __forceinline__ void two_parts(float h, uint16_t &first, uint16_t &second)
+{
+    uint16_t high = Bf16::narrow(h), low = 0;
+    if (fabsf(h) < INFINITY) {
+        const bool past = (high & 0x7fff) == 0x7f80;
+        high = (uint16_t)(high - past);
+        const float rest = h - Bf16::widen(high);
+        low = past ? (uint16_t)(__builtin_bit_cast(uint32_t, rest) >> 16) : Bf16::narrow(rest);
+    }
+    first = high, second = low;
+}
+
 // Workgroups: an expert by 16 columns of h; four waves share H and join their sums in LDS.
 // Bound by the memory where H is long (64 tokens, 64 experts of 4096 x 2048 201 us, 5.3 TB/s; of 1024 x 2048 62 us, 4.3: a wave has two blocks).
 // MORE: for experts of more than 16 MT tokens.  KEYS: 0: the choices are there, and the last workgroup lists them for what follows; else each workgroup chooses by itself, from so many times
@@ -370,10 +385,8 @@ template <int MT, int KEYS, bool MORE = false> __global__ void __launch_bounds__
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) gate += s_acc[w][0][m][n], up += s_acc[w][1][m][n];
             const float h = gate / (1.0f + expf(-gate)) * up;
-            const uint16_t high = Bf16::narrow(h);
             const int64_t at = (int64_t)choices[kSums * (from + m)] * a.I + i0 + n;
-            a.h[at] = high;
-            a.h[(int64_t)a.choices * a.I + at] = fabsf(h) < INFINITY ? Bf16::narrow(h - Bf16::widen(high)) : 0; // (of an infinity the first part is all)
+            two_parts(h, a.h[at], a.h[(int64_t)a.choices * a.I + at]);
         }
     }
 }

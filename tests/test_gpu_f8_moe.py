@@ -167,3 +167,32 @@ def test_as_dense_layers_of_the_chosen_experts():
         h, hs = qnn.f8_quantize(both, gated=True)
         dense = qnn.f8_matmul(h, hs, a[5][e], a[6][e])
         assert (dense.float() - y[0][t:t + 1].float()).norm() < 0.06 * y[0][t:t + 1].float().norm()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T,E,k", [(3, 5, 1), (8, 70, 2), (12, 10, 2), (40, 6, 1), (64, 150, 4)])
+def test_inner_values_up_to_the_end_of_binary32(T, E, k, dtype):
+    # Gates of 2^64 (silu is exactly that) times ups of around 2^64.  bfloat16, whose two parts hold an inner value, rounds to infinity from 2^128 (1 - 2^-9) on:
+    # that number, the one before it, one behind, binary32's largest, and one far from all of them.
+    H = I = 128
+    ups = [2.0 ** 64 * v for v in (1 - 2.0 ** -9, 1 - 2.0 ** -9 - 2.0 ** -24, 1 - 2.0 ** -10, 1 - 2.0 ** -24, 0.71875)]
+    g = torch.Generator().manual_seed(T)
+    sign = torch.where(torch.arange(I) % 3 == 1, -1.0, 1.0)
+    one = torch.arange(E) % len(ups)
+    c = layer(T, E, H, I)
+    x, up, down = torch.randn(T, H, generator=g), torch.zeros(E, 2 * I, H), torch.zeros(E, H, I)
+    x[:, 0], up[:, :I, 0], up[:, I:, 0] = 1.0, 1.0, sign
+    n = torch.arange(H)
+    down[:, n, n] = torch.where(n % 2 == 0, 1.0, 0.5)  # (whose sums with inner values stay within binary32)
+    down[:, n[n % 2 == 1], (n[n % 2 == 1] + 5) % I] = -0.25
+    c.update(x=x.to(ref.F8), xs=torch.ones(1, T), up=up.to(ref.F8), down=down.to(ref.F8), downs=torch.full((E, 1, 1), 2.0 ** -120))
+    c["ups"] = torch.stack([torch.full((E,), 2.0 ** 64), torch.tensor(ups)[one]], 1)[:, :, None].contiguous()
+    chosen = torch.arange(T) * 7 % E
+    c["logits"] = torch.where(torch.arange(E)[None] == chosen[:, None], 0.5, -math.inf)
+    y = qnn.f8_moe(*on_gpu(c), k, dtype=dtype)
+    h = 2.0 ** 64 * torch.tensor(ups).double()[one[chosen]][:, None] * sign.double()
+    w = down[0].double() * 2.0 ** -120
+    want, size = h @ w.t(), h.abs() @ w.abs().t()
+    # two parts of 8 bits, of which the second may be cut off rather than rounded, and a few roundings of binary32
+    off = size * (2.0 ** -16 + 8 * 2.0 ** -24)
+    ref.assert_close(y, want, off + (want.abs() + off) * ref.half_ulp(dtype), (T, E, k))
