@@ -212,3 +212,24 @@ def test_norm_with_weights_at_the_ends_of_the_range(size, weight, K):
     # (a result is rounded to bfloat16 once, behind roundings in binary32; below its normal numbers to the last of their steps)
     ref.assert_close(torch.where(passes, 0.0, y.cpu().double()), torch.where(passes, 0.0, v), v.abs() * (ref.half_ulp(torch.bfloat16) + 2.0 ** -20) + 2.0 ** -133)
     assert (y.cpu()[passes].abs() == math.inf).all()
+
+
+# Rows that a wave has alone with two pieces per lane, rows of four and of two waves with two and four pieces, whole pieces and not: forms that many
+# rows, or lengths past 8192, take.
+@pytest.mark.parametrize("dtype", KINDS)
+@pytest.mark.parametrize("residual,weighted", [(False, True), (True, False), (True, True)])
+@pytest.mark.parametrize("M,K", [(600, 1000), (600, 1001), (600, 4096), (600, 5001), (600, 7001), (600, 12288), (4100, 1000), (4100, 2048), (3, 16384), (2, 16001), (2, 20001), (3, 32768)])
+def test_norm_of_many_and_of_long_rows(M, K, residual, weighted, dtype):
+    g = torch.Generator().manual_seed(M + K)
+    x, r = rows(g, M, K, dtype, 0.7), rows(g, M, K, dtype, 0.7) if residual else None
+    w = (0.5 + torch.rand(K, generator=g)).to(dtype) if weighted else None
+    h, v = norm(x, r, w, 1e-5)
+    x, r, w = (None if t is None else t.to(DEV) for t in (x, r, w))
+    for with_y in (False, True):
+        got = qnn.f8_rmsnorm(x, w, 1e-5, residual=r, with_y=with_y)
+        assert len(got) == 2 + residual + with_y
+        ref.assert_codes(got[0], got[1], v, NORM, (M, K, with_y))
+        if residual:
+            assert torch.equal(got[2].cpu(), h)
+        if with_y:
+            ref.assert_close(got[-1], v, v.abs() * (ref.half_ulp(dtype) + 2 * NORM) + torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps, (M, K))
