@@ -296,3 +296,17 @@ def test_large_experts_for_many_tokens(T, E, k, H, I):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("M,N,K,dtype,plan", [
+    (257, 1000, 4096, F16, "tile128x128/8"), (257, 1000, 4111, BF16, "tile128x128/7"), (1500, 2986, 6144, BF16, "tile256x256/3"), (1500, 2986, 6147, F16, "tile256x256/3"),
+    (129, 9000, 6147, BF16, "tile256x256/7"), (130, 2051, 6144, F32, "tile128x128/7"), (129, 2047, 4111, F32, "tile128x128/7"), (257, 4099, 4096, F32, "tile128x128/2")])
+def test_tiles_in_parts(M, N, K, dtype, plan):
+    # with K of whole pieces, and of others, whose copies lie in the workspace before the parts' sums
+    assert qnn.f8_matmul_plan(M, N, K, dtype) == plan
+    x, xs, w, ws, b = operands(M, N, K)
+    space = torch.full((qnn.load_library().qnn_f8_matmul_workspace_bytes(M, N, K, {BF16: 0, F16: 1, F32: 2}[dtype]) + 256,), 0xff, dtype=torch.uint8, device=DEV)
+    for bias in (None, b.to(dtype)):
+        y = qnn.f8_matmul(x, xs, w, ws, bias=bias, dtype=dtype, workspace=space[:-256])
+        check(x, xs, w, ws, bias, y, what=plan)
+        assert (space[-256:] == 0xff).all()
