@@ -433,6 +433,8 @@ qnn_status qnn_f8_quantize(const void *x, int64_t ldx, int64_t M, int64_t K, int
  *   v = h / sqrt(mean(h^2) + eps) * weight;  codes and scales of v as in qnn_f8_quantize
  * in binary32 (squares beyond its range included: rows are then taken in units of a power of two).  A row of zeros gives zeros, one with an infinity or
  * NaN gives what the formula does.  total may be residual, or x, itself; other overlaps are not allowed.
+ * Without y the codes are mostly those of h * weight, which is exact in binary32, and the scale is theirs times the row's factor; with y they are those of the v that y is
+ * rounded from.  Both are v's to binary32's accuracy, but the last bits of a scale, and codes of quotients next to the middle of two, may differ.
  * residual, total: DEVICE, pitches ldr and ldt, or both NULL (total is not used without a residual).  weight: DEVICE [K] of `type` or NULL (ones).
  * y: DEVICE [M][K] of `type`, contiguous: v rounded, or NULL.  eps: in [0, 2^100].  The rest as in qnn_f8_quantize. */
 qnn_status qnn_f8_rmsnorm(const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, float eps, int64_t M, int64_t K,

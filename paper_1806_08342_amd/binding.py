@@ -587,7 +587,8 @@ def f8_quantize(x, gated=False, out=None):
 def f8_rmsnorm(x, weight=None, eps=1e-6, residual=None, total=None, with_y=False, out=None):
     """Root-mean-square norm of rows as codes and scales (see `f8_quantize`): h = x, or x + residual rounded to x's type;
     v = h / sqrt(mean(h^2) + eps) * weight.  Returns (codes, scales), with a residual (codes, scales, h), and with_y one more: v
-    rounded to x's type.  total: where to write h (residual or x themselves will do: in place); out: (codes, scales) to write to."""
+    rounded to x's type (codes may then differ from those without where a quotient lies next to the middle of two, and scales in their
+    last bits).  total: where to write h (residual or x themselves will do: in place); out: (codes, scales) to write to."""
     return (_nat or _native()).f8_rmsnorm(x, weight, eps, residual, total, with_y, out)
 
 
