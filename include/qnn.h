@@ -447,14 +447,17 @@ qnn_status qnn_f8_rmsnorm(const void *x, int64_t ldx, const void *residual, int6
  * 2^-126 it loses bits), y is rounded once.  A NaN code gives NaN in its row or column.
  * x: DEVICE [M][ldx], ldx >= K.  x_scales: DEVICE, pitch ldxs >= M between blocks.  w: DEVICE [N][K], w_scales DEVICE, both contiguous.
  * bias: DEVICE [N] of `type` or NULL.  y: DEVICE, M x N of `type`, row pitch ldy >= N (written).
- * Rows at any byte; those that are whole 16-byte pieces at 16-byte aligned addresses run faster (others may be copied into the workspace first, which
- * is as large as both operands then).  M up to 2^20 (0 is a no-op), N and K up to 2^24.
+ * Rows at any byte; those that are whole 16-byte pieces at 16-byte aligned addresses run faster.  Where K is no multiple of 16 both operands may be copied into the
+ * workspace first, which has room for them then.  Where it is one, nothing is copied: rows at other addresses (x with such a pitch, x or w that begins so) take a slower kernel where
+ * qnn_f8_matmul_plan names tiles, 1.3 to 3.4 times as long at 300 to 8192 rows where they begin with a word each and 2 to 7 where not (8192 x 8192 x 8192 1620 and 3110 us
+ * for 491): copy such an x before the call.  M up to 2^20 (0 is a no-op), N and K up to 2^24.
  * workspace: DEVICE scratch, 16-byte aligned, of at least qnn_f8_matmul_workspace_bytes bytes (NULL where that is 0), else QNN_EINVAL. */
 qnn_status qnn_f8_matmul(const uint8_t *x, int64_t ldx, const float *x_scales, int64_t ldxs, const uint8_t *w, const float *w_scales, const void *bias,
                          int64_t M, int64_t N, int64_t K, int type, void *y, int64_t ldy, void *workspace, size_t workspace_bytes, void *stream);
 size_t qnn_f8_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, int type);
 
-/* Name of the kernel that qnn_f8_matmul selects.  For logging and profiling.  HOST string owned by the library; "" for sizes that are refused. */
+/* Name of the kernel that qnn_f8_matmul selects, for x and w that begin at 16-byte aligned addresses, x with such a pitch (others, where K is a multiple of 16: "rows64x64"
+ * for any "tile...").  For logging and profiling.  HOST string owned by the library; "" for sizes that are refused. */
 const char *qnn_f8_matmul_plan(int64_t M, int64_t N, int64_t K, int type);
 
 /* A whole layer of experts, for a few tokens.  Token t chooses the top_k largest of its logits (equal ones: the lowest index; -inf and NaN are

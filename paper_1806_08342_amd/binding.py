@@ -594,14 +594,15 @@ def f8_rmsnorm(x, weight=None, eps=1e-6, residual=None, total=None, with_y=False
 
 def f8_matmul(x, x_scales, w, w_scales, bias=None, dtype=None, out=None, workspace=None):
     """x [M,K] times w [N,K] transposed, both float8_e4m3fn: y[m,n] = bias[n] + sum_k x[m,k] * x_scales[k//128,m] * w[n,k] *
-    w_scales[n//128,k//128].  x's rows may be spaced apart.  dtype: bfloat16 (unless given), float16, or float32, whose sums are exact
+    w_scales[n//128,k//128].  x's rows may be spaced apart; where K is a multiple of 16 and x's pitch or address is not, many rows take several
+    times as long (a copy of it first is faster).  dtype: bfloat16 (unless given), float16, or float32, whose sums are exact
     to binary32 (at half the matrix rate; with 16-bit results a block's sum has a relative error of about 1e-5); the bias is of that type.
     For inference: tensors that require grad are refused while gradients are recorded."""
     return (_nat or _native()).f8_matmul(x, x_scales, w, w_scales, bias, dtype, out, workspace)
 
 
 def f8_matmul_plan(M, N, K, dtype=None):
-    """Name of the kernel that `f8_matmul` runs for these sizes."""
+    """Name of the kernel that `f8_matmul` runs for these sizes (x and its pitch at multiples of 16 bytes)."""
     return load_library().qnn_f8_matmul_plan(M, N, K, BF16 if dtype is None else _float_code(dtype)).decode()
 
 

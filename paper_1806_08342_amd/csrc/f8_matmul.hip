@@ -10,7 +10,8 @@
 
 namespace qnn {
 
-// Rows that begin with a word each.  (Those that do not: one step ahead, and 16 rows of weights; 32 would not fit the registers.)
+// Rows that begin with a word each.  (Those that do not: one step ahead, and 16 rows of weights; 32 would not fit the registers.  64 by 64, which is
+// what is left where that or tiles were planned for rows that begin with a word, spills 43 registers, with binary32 results 53.)
 static bool words(const F8Args &a) { return ((uintptr_t)a.x | (uintptr_t)a.ldx | (uintptr_t)a.w | (uintptr_t)a.K) % 4 == 0; }
 
 template <int MT, int NT, int WAVES, int DEPTH, bool ANY = false> static void launch_rows(const F8Args &a, hipStream_t s)
@@ -36,14 +37,14 @@ static void launch_f8_rows(const F8Args &a, hipStream_t s)
 }
 
 // By estimated time (us), of a launch and what follows.  Measured / estimated, with bfloat16 results and weights that no cache holds:
-// rows: 256 workgroups at a time, each a step of 128 in 0.045 and 0.0025 for each row (1 x 28672 x 8192 41.9 / 42, 32 x 4096 x 4096 7.0 / 7.8,
-// 64 rows 10.1 / 10.4, 1000 rows 121 / 121), or wide by the weights' bytes (24 x 28672 x 8192 51.5 / 52, 64 x 12288 x 4096 21.6 / 20.3) while one turn
+// rows: 256 workgroups at a time, each a step of 128 in 0.045 and 0.0025 for each row (32 x 4096 x 4096 7.0 / 7.8,
+// 64 rows 10.1 / 10.4, 1000 rows 121 / 121; without a bound by the weights' bytes: 1 x 28672 x 8192 51 / 29.9, 8 rows 50 / 37.7, where the others' are higher still), or wide by the weights' bytes (24 x 28672 x 8192 51.5 / 52, 64 x 12288 x 4096 21.6 / 20.3) while one turn
 // takes all rows, then 512 at a time, 0.4 for a step (300 x 12288 x 4096 56 / 57).  Rows that begin within a
 // word take 0.1 and 0.0065 (1 x 4096 x 4095 6.6 / 7.2, 64 rows 20.0 / 20.3), so that a copy with whole pieces comes first where that is less: 3, and 0.365 for
 // a megabyte (64 x 4096 x 4095 19.3 / 20).
 // 64 rows by 64 of weights per workgroup, whose 8 waves share K: 0.4 for a step on 256 CUs (1000 x 1024 x 1024 7.0 / 7.0, 500 x 2048 x 9216 32.3 / 32.6);
 // tiles: a CU does a step of 128 with a tile of 128 x 128 in 0.62 us, with binary32 results 0.97, of 256 x 256 in 1.85, or as fast as the weights come
-// (64 x 28672 x 8192 59 / 55, 300 x 4096 x 4096 in two parts 21.6 / 21, 1000 x 12288 x 4096 68.9 / 64.5 and 61.2 / 64.2, 8192 x 8192 x 8192 495 / 479).
+// (64 x 28672 x 8192 59 / 55, 300 x 4096 x 4096 in two parts 21.6 / 22.9, 1000 x 12288 x 4096 68.9 / 64.5 and 61.2 / 64.2, 8192 x 8192 x 8192 495 / 479).
 F8Plan f8_plan(int64_t M, int64_t N, int64_t K, int type)
 {
     F8Plan best{F8Kernel::Rows, 1, 1e30f, false, 0, 0, 0};
@@ -106,6 +107,8 @@ qnn_status qnn_f8_matmul(const uint8_t *x, int64_t ldx, const float *x_scales, i
         launch_f8_pad(a, space, space + plan.x_bytes, s);
         a.x = space, a.w = space + plan.x_bytes, a.ldx = a.K = (int32_t)f8_padded(K);
     }
+    // (What is planned does not depend on addresses and pitches, and tiles need whole pieces: others, where K has them, go by 64 rows at a time.  4096 x
+    // 4096 x 4096 67 us in tiles, 227 from rows that begin with a word, 460 from rows that do not.)
     const bool pieces = ((uintptr_t)a.x | (uintptr_t)a.ldx | (uintptr_t)a.w | (uintptr_t)a.K) % 16 == 0 && a.ldx < (1 << 22);
     if ((plan.kernel == F8Kernel::Tile128 || plan.kernel == F8Kernel::Tile256) && pieces) launch_f8_tiles(a, plan, reinterpret_cast<float *>(space + plan.x_bytes + plan.w_bytes), s);
     else if (plan.kernel == F8Kernel::Rows) launch_f8_rows(a, s);
