@@ -441,7 +441,7 @@ template <int TOKENS> __global__ void __launch_bounds__(512, 2) moe_down_kernel(
     const int blocks = (a.I + kF8Block - 1) / kF8Block, row_blocks = (a.H + kF8Block - 1) / kF8Block;
     const int stretches = a.list[0], units = stretches * blocks;
     const int sharing = WAVES * a.parts, mine = part * WAVES + wave;
-    const int first = units * mine / sharing, last = units * (mine + 1) / sharing; // (below 1280 stretches of 1024 blocks by 128)
+    const int first = units * mine / sharing, last = units * (mine + 1) / sharing; // (up to 1280 stretches of 1024 blocks, by 256)
     const uint8_t *const inner = reinterpret_cast<const uint8_t *>(a.h);
     const int inner_bytes = 4 * a.choices * a.I; // (up to 2^30)
     constexpr uint32_t kBeyond = 0x80000000u;    // of either buffer: zeros, without traffic

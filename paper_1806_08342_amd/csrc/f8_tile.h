@@ -55,7 +55,7 @@ template <int BM, int BN, int WM, int WN, int XB, int WB, int SETS, bool NARROW,
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, g = lane >> 5;
     const int wm = wave % WM, wn = wave / WM, m0 = tm * BM, n0 = tn * BN;
     const int blocks = (a.K + kF8Block - 1) / kF8Block;
-    const int first = blocks * part / t.splits, last = blocks * (part + 1) / t.splits; // (up to 2^17 blocks, few parts)
+    const int first = blocks * part / t.splits, last = blocks * (part + 1) / t.splits; // (up to 2^13 blocks by 16)
 
     const uint8_t *const x_tile = a.x + m0 * a.ldx, *const w_tile = a.w + (int64_t)n0 * a.K;
     const int x_bytes = (int)(min(a.M - m0, BM) * a.ldx), w_bytes = (int)(min(a.N - n0, BN) * a.K); // rows beyond the last read as zeros
